@@ -362,6 +362,74 @@ size_t xconv_relu_mask_bytes(long long n);
 xconv_status xconv_relu_fwd(int dtype, const void *X_dev, void *Y_dev, void *mask_dev, long long n, void *stream);
 xconv_status xconv_relu_bwd(int dtype, const void *dY_dev, const void *mask_dev, void *dX_dev, long long n, void *stream);
 
+/* ---- layer normalisation over channels ---------------------------------------------
+ * The normalisation between the convolutions of a network, over the C channels of every position:
+ *
+ *   forward   mean = (1/C) sum_c X[o,c,i];  var = (1/C) sum_c (X[o,c,i] - mean)^2;  rstd = 1/sqrt(var + eps)
+ *             Y[o,c,i] = (X[o,c,i] - mean) rstd gamma[c] + beta[c]
+ *   backward  g = dY gamma;  xh = (X - mean) rstd
+ *             dX = rstd (g - (1/C) sum_c g - xh (1/C) sum_c (g xh))
+ *             dgamma[c] = sum_{o,i} dY xh;  dbeta[c] = sum_{o,i} dY
+ *
+ * X, Y, dY, dX are [outer, C, inner] of `dtype`: planes (outer images, inner positions) or, with inner == 1, rows
+ * (channels-last activations).  gamma, beta, dgamma, dbeta are [C] of `w_dtype` (XCONV_F32 or `dtype`); gamma_dev NULL
+ * means ones, beta_dev NULL zeros.  mean_dev, rstd_dev: [outer * inner] floats, written by the forward pass (NULL: not
+ * wanted), read by the backward pass.  dX_dev, dgamma_dev, dbeta_dev NULL: not wanted.  Sums are fp32, the variance of
+ * the centred values, each output rounded once (nearest even) and overwritten; deterministic.  Y_dev may be X_dev, dX_dev may be dY_dev or X_dev.  Pointers aligned to the element
+ * size.  ws_dev (4-byte aligned): xconv_layernorm_workspace_bytes() bytes, for the backward pass with dgamma or dbeta;
+ * else it may be NULL.  outer == 0 is a no-op of the forward pass and gives zero dgamma and dbeta.
+ * XCONV_EINVAL: null desc or pointer, C or inner < 1, outer < 0, bad enum, eps negative or not finite;
+ * XCONV_EUNSUPPORTED: C above 2^24, inner above 2^30, outer * inner above 2^40. */
+typedef struct xconv_norm_desc {
+    int64_t outer, inner;
+    int32_t C, dtype, w_dtype;
+    float eps;
+} xconv_norm_desc;
+size_t xconv_layernorm_workspace_bytes(const xconv_norm_desc *desc);
+xconv_status xconv_layernorm_fwd(const xconv_norm_desc *desc, const void *X_dev, const void *gamma_dev, const void *beta_dev, void *Y_dev,
+                                 float *mean_dev, float *rstd_dev, void *stream);
+xconv_status xconv_layernorm_bwd(const xconv_norm_desc *desc, const void *dY_dev, const void *X_dev, const float *mean_dev, const float *rstd_dev,
+                                 const void *gamma_dev, void *dX_dev, void *dgamma_dev, void *dbeta_dev, void *ws_dev, size_t ws_bytes, void *stream);
+
+/* ---- orthogonalised weight updates ---------------------------------------------------
+ * What a weight gradient (of xconv_dw_estimate, say) can be used for: `steps` Newton-Schulz products bring the singular
+ * values of a matrix near one.  A convolution's weights [C_out, C_in, kH, kW] count as [C_out, C_in*kH*kW].
+ *
+ *   orth(G)   X_0 = G / max(|G|_F, eps), transposed when rows > cols;  A = X X^T;  X <- a X + (b A + c A A) X;  O = X_steps
+ *             (transposed back)
+ *   muon      M <- M + (1 - momentum)(G - M);  U = G + momentum (M - G) (nesterov != 0) or M
+ *             W <- (1 - lr weight_decay) W - lr sqrt(max(1, rows/cols)) orth(U)
+ *
+ * One call takes `count` matrices of any shapes; each launch covers all of them.  G_dev: [rows, cols] of g_dtype;
+ * out_dev: O, or the weights W (updated in place), of out_dtype; M_dev: [rows, cols] floats, updated in place (not used by
+ * xconv_orth).  Row-major, aligned to the element size; outputs of one call do not overlap anything else it is given.
+ * Products run on the 16-bit matrix cores with every float as the sum of two fp16 numbers (22 bits; three products, fp32
+ * sums): results are as far from 64 bits as those of fp32 products.  O and W are rounded once.  A zero matrix gives
+ * zeros; a matrix with an infinity or a NaN gives NaN (its momentum keeps the value).  Deterministic.
+ * ws_dev: xconv_orth_workspace_bytes() bytes, 256-byte aligned.
+ * XCONV_EINVAL: a null pointer, count < 0, rows or cols < 1, bad enum, steps < 0, eps, lr, momentum, weight_decay or a
+ * coefficient not finite, eps < 0; XCONV_EUNSUPPORTED: min(rows, cols) above 32768, an extent above 2^24, rows * cols above
+ * 2^31, steps above 64, and coefficients with which a singular value s that starts in [0, 1] passes 3.5 before the last step
+ * or |a + b s^2 + c s^4| passes 12 (the fp16 numbers could overflow).  count == 0 is a no-op. */
+typedef struct xconv_orth_item {
+    int32_t rows, cols;
+    const void *G_dev;
+    void *out_dev;
+    float *M_dev;
+} xconv_orth_item;
+typedef struct xconv_orth_args {
+    int32_t g_dtype, out_dtype, steps;
+    float a, b, c, eps;
+} xconv_orth_args;
+typedef struct xconv_muon_args {
+    float lr, momentum, weight_decay;
+    int32_t nesterov;
+} xconv_muon_args;
+size_t xconv_orth_workspace_bytes(const xconv_orth_item *items, int count, const xconv_orth_args *args);   /* reads rows and cols; 0: not valid */
+xconv_status xconv_orth(const xconv_orth_item *items, int count, const xconv_orth_args *args, void *ws_dev, size_t ws_bytes, void *stream);
+xconv_status xconv_muon_step(const xconv_orth_item *items, int count, const xconv_orth_args *args, const xconv_muon_args *muon, void *ws_dev,
+                             size_t ws_bytes, void *stream);
+
 /* Reference measurement for the roofline figures (not part of the method): enqueues a loop of `iters` x 4
  * independent 32x32 matrix instructions per wave (32x32x16 for the 16-bit types, 32x32x2 for fp32) on every
  * SIMD of the device, with operands of random bits, and stores the number of floating-point operations of

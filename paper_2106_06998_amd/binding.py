@@ -35,6 +35,25 @@ class xconv3d_desc(ctypes.Structure):
                 ("pad_d", ctypes.c_int32)]
 
 
+class xconv_norm_desc(ctypes.Structure):
+    _fields_ = [("outer", ctypes.c_int64), ("inner", ctypes.c_int64), ("C", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("w_dtype", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+class xconv_orth_item(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("cols", ctypes.c_int32), ("G_dev", ctypes.c_void_p), ("out_dev", ctypes.c_void_p),
+                ("M_dev", ctypes.c_void_p)]
+
+
+class xconv_orth_args(ctypes.Structure):
+    _fields_ = [("g_dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32), ("steps", ctypes.c_int32), ("a", ctypes.c_float),
+                ("b", ctypes.c_float), ("c", ctypes.c_float), ("eps", ctypes.c_float)]
+
+
+class xconv_muon_args(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_float), ("momentum", ctypes.c_float), ("weight_decay", ctypes.c_float), ("nesterov", ctypes.c_int32)]
+
+
 class XConvError(RuntimeError):
     def __init__(self, status, where):
         self.status = status
@@ -136,6 +155,20 @@ def lib():
         L.xconv_pixel_indep_probe_fwd.argtypes = [P, vp, vp, vp, sz, vp]
         L.xconv_pixel_indep_dw_estimate.restype = i32
         L.xconv_pixel_indep_dw_estimate.argtypes = [P, vp, vp, vp, vp, sz, vp]
+        PN, PI = ctypes.POINTER(xconv_norm_desc), ctypes.POINTER(xconv_orth_item)
+        PA, PM = ctypes.POINTER(xconv_orth_args), ctypes.POINTER(xconv_muon_args)
+        L.xconv_layernorm_workspace_bytes.restype = sz
+        L.xconv_layernorm_workspace_bytes.argtypes = [PN]
+        L.xconv_layernorm_fwd.restype = i32
+        L.xconv_layernorm_fwd.argtypes = [PN, vp, vp, vp, vp, vp, vp, vp]
+        L.xconv_layernorm_bwd.restype = i32
+        L.xconv_layernorm_bwd.argtypes = [PN, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.xconv_orth_workspace_bytes.restype = sz
+        L.xconv_orth_workspace_bytes.argtypes = [PI, i32, PA]
+        L.xconv_orth.restype = i32
+        L.xconv_orth.argtypes = [PI, i32, PA, vp, sz, vp]
+        L.xconv_muon_step.restype = i32
+        L.xconv_muon_step.argtypes = [PI, i32, PA, PM, vp, sz, vp]
         L.xconv_diag_mfma_rate.restype = i32
         L.xconv_diag_mfma_rate.argtypes = [i32, i32, vp, sz, ctypes.POINTER(ctypes.c_double), vp]
         L.xconv_prof_enable.restype = None
@@ -450,3 +483,50 @@ def xconv_relu_bwd(dtype, dY_dev, mask_dev, dX_dev, n, stream=None):
     _check(lib().xconv_relu_bwd(DTYPES[dtype] if isinstance(dtype, str) else dtype, _ptr(dY_dev), _ptr(mask_dev), _ptr(dX_dev), int(n),
                                 _stream(stream)), "xconv_relu_bwd")
 
+
+# ---- layer normalisation over channels ------------------------------------------------
+def make_norm_desc(outer, C, inner=1, dtype="f32", w_dtype=None, eps=1e-5):
+    dt = DTYPES[dtype] if isinstance(dtype, str) else dtype
+    wt = dt if w_dtype is None else DTYPES[w_dtype] if isinstance(w_dtype, str) else w_dtype
+    return xconv_norm_desc(outer, inner, C, dt, wt, eps)
+
+
+def xconv_layernorm_workspace_bytes(desc):
+    return int(lib().xconv_layernorm_workspace_bytes(ctypes.byref(desc)))
+
+
+def xconv_layernorm_fwd(desc, X_dev, gamma_dev, beta_dev, Y_dev, mean_dev=None, rstd_dev=None, stream=None):
+    _check(lib().xconv_layernorm_fwd(ctypes.byref(desc), _ptr(X_dev), _ptr(gamma_dev), _ptr(beta_dev), _ptr(Y_dev), _ptr(mean_dev),
+                                     _ptr(rstd_dev), _stream(stream)), "xconv_layernorm_fwd")
+
+
+def xconv_layernorm_bwd(desc, dY_dev, X_dev, mean_dev, rstd_dev, gamma_dev, dX_dev, dgamma_dev, dbeta_dev, ws_dev, stream=None):
+    _check(lib().xconv_layernorm_bwd(ctypes.byref(desc), _ptr(dY_dev), _ptr(X_dev), _ptr(mean_dev), _ptr(rstd_dev), _ptr(gamma_dev),
+                                     _ptr(dX_dev), _ptr(dgamma_dev), _ptr(dbeta_dev), _ptr(ws_dev), _nbytes(ws_dev), _stream(stream)),
+           "xconv_layernorm_bwd")
+
+
+# ---- orthogonalised weight updates ------------------------------------------------------
+def make_orth_items(matrices):
+    """An array of xconv_orth_item from (rows, cols, G, out, M) tuples of tensors, addresses or None."""
+    def at(t):
+        return None if t is None else t if isinstance(t, int) else t.data_ptr()
+    return (xconv_orth_item * max(1, len(matrices)))(*[xconv_orth_item(r, c, at(g), at(o), at(m)) for r, c, g, o, m in matrices])
+
+
+def make_orth_args(g_dtype="f32", out_dtype="f32", steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7):
+    code = lambda t: DTYPES[t] if isinstance(t, str) else t
+    return xconv_orth_args(code(g_dtype), code(out_dtype), steps, *coefficients, eps)
+
+
+def xconv_orth_workspace_bytes(items, count, args):
+    return int(lib().xconv_orth_workspace_bytes(items, int(count), ctypes.byref(args)))
+
+
+def xconv_orth(items, count, args, ws_dev, stream=None):
+    _check(lib().xconv_orth(items, int(count), ctypes.byref(args), _ptr(ws_dev), _nbytes(ws_dev), _stream(stream)), "xconv_orth")
+
+
+def xconv_muon_step(items, count, args, muon, ws_dev, stream=None):
+    _check(lib().xconv_muon_step(items, int(count), ctypes.byref(args), ctypes.byref(muon), _ptr(ws_dev), _nbytes(ws_dev), _stream(stream)),
+           "xconv_muon_step")

@@ -35,7 +35,9 @@ enum KernelId {
     K_PASS2 = 16,
     K_DIAG = 17,
     K_BIAS = 18,
-    K_COUNT = 19
+    K_NORM = 19,
+    K_ORTH = 20,
+    K_COUNT = 21
 };
 
 // Where the probe output of a voxel goes in Xt.  sd == 0: plain order, pixel `first` of the

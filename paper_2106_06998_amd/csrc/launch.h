@@ -132,6 +132,16 @@ hipError_t launch_side_jobs(const SideJobs &J, hipStream_t st);
 size_t bias_ws_bytes(int C);
 hipError_t launch_bias_grad(int dtype, const void *dY, float *part, void *db, int B, int C, int HW, bool nhwc, hipStream_t st, SideJobs *J = nullptr);
 
+// norm_kernels.hip: layer normalisation over channels; part: norm_ws_bytes(d) bytes, not read when neither dgamma nor dbeta is wanted
+size_t norm_ws_bytes(const xconv_norm_desc *d);
+hipError_t launch_norm_fwd(const xconv_norm_desc *d, const void *X, const void *gamma, const void *beta, void *Y, float *mean, float *rstd, hipStream_t st);
+hipError_t launch_norm_bwd(const xconv_norm_desc *d, const void *dY, const void *X, const float *mean, const float *rstd, const void *gamma, void *dX,
+                           void *dgamma, void *dbeta, float *part, hipStream_t st);
+
+// orth_kernels.hip: orthogonalisation of matrices (muon: of a momentum, with the update of the weights); ws: orth_ws_bytes
+size_t orth_ws_bytes(const xconv_orth_item *items, int count);
+hipError_t launch_orth(const xconv_orth_item *items, int count, const xconv_orth_args *args, const xconv_muon_args *muon, void *ws, hipStream_t st);
+
 // pixel_kernels.hip: Xbar[b, j] = sum_k X[b, k] Zimg[j, k] (forward product of the pixel x channel probes)
 bool pixel_fwd_ok(int dtype, long long K, const void *X);
 size_t pixel_fwd_partial_bytes(int dtype, long long K, int B, int r);

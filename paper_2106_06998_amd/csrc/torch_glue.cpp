@@ -41,6 +41,12 @@ struct Lib {
     decltype(&xconv_relu_mask_bytes) relu_mask_bytes;
     decltype(&xconv_relu_fwd) relu_fwd;
     decltype(&xconv_relu_bwd) relu_bwd;
+    decltype(&xconv_layernorm_workspace_bytes) layernorm_workspace_bytes;
+    decltype(&xconv_layernorm_fwd) layernorm_fwd;
+    decltype(&xconv_layernorm_bwd) layernorm_bwd;
+    decltype(&xconv_orth_workspace_bytes) orth_workspace_bytes;
+    decltype(&xconv_orth) orth;
+    decltype(&xconv_muon_step) muon_step;
     decltype(&xconv_status_string) status_string;
 } L;
 bool g_ready = false;
@@ -357,6 +363,256 @@ PyObject *relu_backward(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     return wrap(dx);
 }
 
+// ---- layer normalisation over channels ----
+bool storage_type(const Tensor &t) { return t.scalar_type() == at::kFloat || t.scalar_type() == at::kBFloat16 || t.scalar_type() == at::kHalf; }
+[[noreturn]] void refuse(const std::string &what) { throw std::runtime_error(what); }
+
+// the memory of x as [outer, C, inner] with the channels at `axis` (1 or the last), and the sizes of its statistics
+struct NormView {
+    Tensor x;
+    xconv_norm_desc d;
+    at::MemoryFormat format;
+    std::vector<int64_t> stats;
+};
+NormView norm_view(const Tensor &x, const Tensor &weight, const Tensor &bias, int64_t axis, double eps)
+{
+    if (!x.is_cuda()) refuse("layer_norm: runs on the GPU only (input on " + x.device().str() + ")");
+    if (!storage_type(x)) refuse(std::string("layer_norm: storage type ") + at::toString(x.scalar_type()) + " is not supported (float32, bfloat16, float16)");
+    const int64_t dim = x.dim();
+    if (axis < 0) axis += dim;
+    if (dim < 1 || (axis != dim - 1 && (axis != 1 || dim < 2))) refuse("layer_norm: the channels are the last axis or axis 1 of the input");
+    NormView v;
+    v.format = at::MemoryFormat::Contiguous;
+    const int64_t C = x.size(axis);
+    if (C < 1 || C > INT32_MAX) refuse("layer_norm: no channels");
+    int wt = -1;
+    for (const Tensor *p : {&weight, &bias}) {
+        if (!p->defined()) continue;
+        if (p->device() != x.device() || p->dim() != 1 || p->size(0) != C) refuse("layer_norm: expected parameters of " + std::to_string(C) + " channels on the input's device");
+        if (!storage_type(*p) || (p->scalar_type() != at::kFloat && p->scalar_type() != x.scalar_type()))
+            refuse("layer_norm: parameters are float32 or of the input's type");
+        const int t = dtype_code(p->scalar_type());
+        if (wt >= 0 && wt != t) refuse("layer_norm: weight and bias are of one type");
+        wt = t;
+    }
+    int64_t inner = 1;
+    v.x = x;
+    if (axis == dim - 1) {
+        v.x = x.contiguous();
+    } else if (!x.is_contiguous() && dim == 4 && x.is_contiguous(at::MemoryFormat::ChannelsLast)) {
+        v.format = at::MemoryFormat::ChannelsLast;
+    } else if (!x.is_contiguous() && dim == 5 && x.is_contiguous(at::MemoryFormat::ChannelsLast3d)) {
+        v.format = at::MemoryFormat::ChannelsLast3d;
+    } else {
+        v.x = x.contiguous();
+        for (int64_t i = 2; i < dim; ++i) inner *= x.size(i);
+    }
+    for (int64_t i = 0; i < dim; ++i)
+        if (i != axis) v.stats.push_back(x.size(i));
+    const int64_t n = x.numel();
+    if (inner < 1) inner = 1;        // an empty plane: nothing to do, outer is 0 too
+    v.d = xconv_norm_desc{n / C / inner, inner, (int32_t)C, dtype_code(x.scalar_type()), wt < 0 ? dtype_code(x.scalar_type()) : wt, (float)eps};
+    return v;
+}
+Tensor solid(const Tensor &t) { return t.defined() ? t.contiguous() : t; }
+
+// norm_forward(x, weight or None, bias or None, eps, axis, stream) -> (y, mean, rstd)
+PyObject *norm_forward(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    if (!ready(nargs, 6, "norm_forward")) return nullptr;
+    const Tensor x = tensor_arg(args[0]), weight = tensor_arg(args[1]), bias = tensor_arg(args[2]);
+    const double eps = PyFloat_AsDouble(args[3]);
+    if (eps == -1.0 && PyErr_Occurred()) return nullptr;
+    long long v[2];
+    if (!ints(args, 4, 2, v)) return nullptr;
+    Tensor y, mean, rstd;
+    if (!run([&] {
+            const c10::DeviceGuard guard(x.device());
+            const NormView n = norm_view(x, weight, bias, v[0], eps);
+            const Tensor w = solid(weight), b = solid(bias);
+            y = at::empty(x.sizes(), x.options(), n.format);
+            mean = at::empty(n.stats, x.options().dtype(at::kFloat));
+            rstd = at::empty(n.stats, mean.options());
+            check(L.layernorm_fwd(&n.d, ptr(n.x), ptr(w), ptr(b), ptr(y), mean.data_ptr<float>(), rstd.data_ptr<float>(), reinterpret_cast<void *>(v[1])),
+                  "xconv_layernorm_fwd");
+        }))
+        return nullptr;
+    return Py_BuildValue("NNN", wrap(y), wrap(mean), wrap(rstd));
+}
+
+// norm_backward(dy, x, mean, rstd, weight or None, axis, need_dx, need_dw, need_db, stream) -> (dx, dw, db), None where not asked for
+PyObject *norm_backward(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    if (!ready(nargs, 10, "norm_backward")) return nullptr;
+    const Tensor dy = tensor_arg(args[0]), x = tensor_arg(args[1]), mean = tensor_arg(args[2]), rstd = tensor_arg(args[3]), weight = tensor_arg(args[4]);
+    long long v[5];
+    if (!ints(args, 5, 5, v)) return nullptr;
+    Tensor dx, dw, db;
+    if (!run([&] {
+            const c10::DeviceGuard guard(x.device());
+            NormView n = norm_view(x, weight, Tensor(), v[0], 0.0);
+            if (dy.sizes() != x.sizes() || dy.device() != x.device()) refuse("layer_norm: the gradient has another shape or device than the input");
+            for (const Tensor *t : {&mean, &rstd})
+                if (t->scalar_type() != at::kFloat || t->device() != x.device() || t->numel() != n.d.outer * n.d.inner)
+                    refuse("layer_norm: mean and rstd are those of the forward pass");
+            const Tensor g = (dy.scalar_type() == x.scalar_type() ? dy : dy.to(x.scalar_type())).contiguous(n.format);
+            const Tensor w = solid(weight), mu = mean.contiguous(), rs = rstd.contiguous();
+            const at::TensorOptions po = x.options().dtype(weight.defined() ? weight.scalar_type() : x.scalar_type());
+            if (v[1]) dx = at::empty(x.sizes(), x.options(), n.format);
+            if (v[2]) dw = at::empty({n.d.C}, po);
+            if (v[3]) db = at::empty({n.d.C}, po);
+            Tensor ws;
+            if (v[2] || v[3]) ws = bytes_on(L.layernorm_workspace_bytes(&n.d), x);
+            check(L.layernorm_bwd(&n.d, ptr(g), ptr(n.x), ptr(mu) ? mu.data_ptr<float>() : nullptr, ptr(rs) ? rs.data_ptr<float>() : nullptr, ptr(w), ptr(dx),
+                                  ptr(dw), ptr(db), ptr(ws), ws.defined() ? (size_t)ws.numel() : 0, reinterpret_cast<void *>(v[4])),
+                  "xconv_layernorm_bwd");
+        }))
+        return nullptr;
+    return Py_BuildValue("NNN", wrap(dx), wrap(dw), wrap(db));
+}
+
+// ---- orthogonalised weight updates ----
+bool tensors(PyObject *o, std::vector<Tensor> &out)
+{
+    PyObject *seq = PySequence_Fast(o, "a list of tensors is expected");
+    if (!seq) return false;
+    const Py_ssize_t n = PySequence_Fast_GET_SIZE(seq);
+    out.reserve(n);
+    bool ok = true;
+    for (Py_ssize_t i = 0; i < n && ok; ++i) {
+        PyObject *t = PySequence_Fast_GET_ITEM(seq, i);
+        if (!THPVariable_Check(t)) {
+            PyErr_SetString(PyExc_TypeError, "a list of tensors is expected");
+            ok = false;
+        } else {
+            out.push_back(THPVariable_Unpack(t));
+        }
+    }
+    Py_DECREF(seq);
+    return ok;
+}
+bool floats(PyObject *const *args, int first, int n, double *out)
+{
+    for (int i = 0; i < n; ++i) {
+        out[i] = PyFloat_AsDouble(args[first + i]);
+        if (out[i] == -1.0 && PyErr_Occurred()) return false;
+    }
+    return true;
+}
+void check_matrix(const Tensor &t, const Tensor &first, const char *where)
+{
+    if (!t.is_cuda()) refuse(std::string(where) + ": runs on the GPU only (tensor on " + t.device().str() + ")");
+    if (t.device() != first.device()) refuse(std::string(where) + ": tensors of one call are on one device");
+    if (!storage_type(t)) refuse(std::string(where) + ": storage type " + at::toString(t.scalar_type()) + " is not supported (float32, bfloat16, float16)");
+    if (t.dim() < 2) refuse(std::string(where) + ": matrices, or weights of more axes, are expected");
+    if (t.size(0) > INT32_MAX || (t.size(0) > 0 && t.numel() / t.size(0) > INT32_MAX)) throw Failed{XCONV_EUNSUPPORTED, where};
+}
+// A tensor whose rows (the first axis) lie one after the other with nothing between or over them: the order of the columns may
+// be any, the operators do not depend on it
+bool dense_rows(const Tensor &t)
+{
+    return t.is_contiguous() || (t.is_non_overlapping_and_dense() && t.size(0) > 0 && t.stride(0) == t.numel() / t.size(0));
+}
+struct OrthJob {
+    Tensor g, out, m;
+};
+// one call of the library for all jobs of equal types
+template <class F> void in_groups(const std::vector<OrthJob> &jobs, F &&call)
+{
+    for (int gt = 0; gt < 3; ++gt)
+        for (int ot = 0; ot < 3; ++ot) {
+            std::vector<xconv_orth_item> items;
+            for (const OrthJob &j : jobs)
+                if (j.g.numel() > 0 && dtype_code(j.g.scalar_type()) == gt && dtype_code(j.out.scalar_type()) == ot)
+                    items.push_back({(int32_t)j.g.size(0), (int32_t)(j.g.numel() / j.g.size(0)), ptr(j.g), ptr(j.out), j.m.defined() ? j.m.data_ptr<float>() : nullptr});
+            if (!items.empty()) call(items, gt, ot);
+        }
+}
+Tensor orth_scratch(const std::vector<xconv_orth_item> &items, const xconv_orth_args &a, const Tensor &like)
+{
+    return bytes_on(L.orth_workspace_bytes(items.data(), (int)items.size(), &a), like);    // (0: the call below says why)
+}
+
+// orthogonalize([G ...], steps, a, b, c, eps, stream) -> [O ...]
+PyObject *orthogonalize(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    if (!ready(nargs, 7, "orthogonalize")) return nullptr;
+    std::vector<Tensor> g;
+    long long steps, s;
+    double f[4];
+    if (!tensors(args[0], g) || !ints(args, 1, 1, &steps) || !floats(args, 2, 4, f) || !ints(args, 6, 1, &s)) return nullptr;
+    std::vector<OrthJob> jobs;
+    if (!run([&] {
+            if (g.empty()) return;
+            for (const Tensor &t : g) check_matrix(t, g[0], "orthogonalize");
+            if (steps < 0 || steps > INT32_MAX) throw Failed{XCONV_EINVAL, "xconv_orth"};
+            const c10::DeviceGuard guard(g[0].device());
+            for (const Tensor &t : g) {
+                const Tensor c = dense_rows(t) ? t : t.contiguous();
+                jobs.push_back({c, at::empty_like(c), Tensor()});
+            }
+            in_groups(jobs, [&](const std::vector<xconv_orth_item> &items, int gt, int ot) {
+                const xconv_orth_args a{gt, ot, (int32_t)steps, (float)f[0], (float)f[1], (float)f[2], (float)f[3]};
+                const Tensor ws = orth_scratch(items, a, g[0]);
+                check(L.orth(items.data(), (int)items.size(), &a, ptr(ws), (size_t)ws.numel(), reinterpret_cast<void *>(s)), "xconv_orth");
+            });
+        }))
+        return nullptr;
+    PyObject *out = PyList_New((Py_ssize_t)jobs.size());
+    for (size_t i = 0; out && i < jobs.size(); ++i) PyList_SET_ITEM(out, (Py_ssize_t)i, wrap(jobs[i].out));
+    return out;
+}
+
+// muon_step([W ...], [G ...], [M ...], lr, momentum, weight decay, nesterov, steps, a, b, c, eps, stream); W and M in place
+PyObject *muon_step(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    if (!ready(nargs, 13, "muon_step")) return nullptr;
+    std::vector<Tensor> w, g, m;
+    double h[3], f[4];
+    long long v[2], s;
+    if (!tensors(args[0], w) || !tensors(args[1], g) || !tensors(args[2], m) || !floats(args, 3, 3, h) || !ints(args, 6, 2, v) || !floats(args, 8, 4, f) ||
+        !ints(args, 12, 1, &s))
+        return nullptr;
+    if (!run([&] {
+            if (w.size() != g.size() || w.size() != m.size()) refuse("muon_step: as many gradients and momenta as weights are expected");
+            if (w.empty()) return;
+            if (v[1] < 0 || v[1] > INT32_MAX) throw Failed{XCONV_EINVAL, "xconv_muon_step"};
+            for (size_t i = 0; i < w.size(); ++i) {
+                for (const Tensor *t : {&w[i], &g[i], &m[i]}) check_matrix(*t, w[0], "muon_step");
+                if (g[i].sizes() != w[i].sizes() || m[i].sizes() != w[i].sizes()) refuse("muon_step: a gradient or a momentum has another shape than its weight");
+                if (m[i].scalar_type() != at::kFloat) refuse("muon_step: momenta are float32");
+            }
+            const c10::DeviceGuard guard(w[0].device());
+            std::vector<OrthJob> jobs;
+            for (size_t i = 0; i < w.size(); ++i) {
+                // all three in the weight's order of memory; what is not is copied, and copied back below
+                OrthJob j;
+                j.out = dense_rows(w[i]) ? w[i] : w[i].contiguous();
+                auto in_order = [&](const Tensor &t) {
+                    if (t.strides() == j.out.strides()) return t;
+                    return at::empty_strided(j.out.sizes(), j.out.strides(), t.options()).copy_(t);
+                };
+                j.g = in_order(g[i]);
+                j.m = in_order(m[i]);
+                jobs.push_back(std::move(j));
+            }
+            const xconv_muon_args mu{(float)h[0], (float)h[1], (float)h[2], (int32_t)(v[0] != 0)};
+            in_groups(jobs, [&](const std::vector<xconv_orth_item> &items, int gt, int ot) {
+                const xconv_orth_args a{gt, ot, (int32_t)v[1], (float)f[0], (float)f[1], (float)f[2], (float)f[3]};
+                const Tensor ws = orth_scratch(items, a, w[0]);
+                check(L.muon_step(items.data(), (int)items.size(), &a, &mu, ptr(ws), (size_t)ws.numel(), reinterpret_cast<void *>(s)), "xconv_muon_step");
+            });
+            for (size_t i = 0; i < w.size(); ++i) {
+                if (!jobs[i].out.is_same(w[i])) w[i].copy_(jobs[i].out);
+                else w[i].unsafeGetTensorImpl()->bump_version();
+                if (!jobs[i].m.is_same(m[i])) m[i].copy_(jobs[i].m);
+                else m[i].unsafeGetTensorImpl()->bump_version();
+            }
+        }))
+        return nullptr;
+    Py_RETURN_NONE;
+}
+
 // init(path of the loaded library, error type)
 PyObject *glue_init(PyObject *, PyObject *const *args, Py_ssize_t nargs)
 {
@@ -400,6 +656,12 @@ PyObject *glue_init(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     get(L.relu_mask_bytes, "xconv_relu_mask_bytes");
     get(L.relu_fwd, "xconv_relu_fwd");
     get(L.relu_bwd, "xconv_relu_bwd");
+    get(L.layernorm_workspace_bytes, "xconv_layernorm_workspace_bytes");
+    get(L.layernorm_fwd, "xconv_layernorm_fwd");
+    get(L.layernorm_bwd, "xconv_layernorm_bwd");
+    get(L.orth_workspace_bytes, "xconv_orth_workspace_bytes");
+    get(L.orth, "xconv_orth");
+    get(L.muon_step, "xconv_muon_step");
     get(L.status_string, "xconv_status_string");
     if (missing) {
         PyErr_Format(PyExc_RuntimeError, "%s has no %s", path, missing);
@@ -419,6 +681,10 @@ PyMethodDef g_methods[] = {
     XC_METHOD("backward", layer_backward),
     XC_METHOD("relu_forward", relu_forward),
     XC_METHOD("relu_backward", relu_backward),
+    XC_METHOD("norm_forward", norm_forward),
+    XC_METHOD("norm_backward", norm_backward),
+    XC_METHOD("orthogonalize", orthogonalize),
+    XC_METHOD("muon_step", muon_step),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_torch_glue", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};

@@ -1,6 +1,8 @@
 // C ABI of libxconv: argument validation, scratch layout, kernel sequencing and
 // the optional per-kernel event timing.  Declarations and their contracts are
 // in include/xconv.h.
+#include <algorithm>
+#include <cmath>
 #include <cstdlib>
 #include <cstring>
 #include <mutex>
@@ -1326,6 +1328,125 @@ xconv_status xconv_relu_bwd(int dtype, const void *dY_dev, const void *mask_dev,
     return XCONV_OK;
 }
 
+// ---- layer normalisation over channels ------------------------------------------------
+namespace {
+xconv_status check_norm(const xconv_norm_desc *d)
+{
+    if (!d || d->outer < 0 || d->inner < 1 || d->C < 1) return XCONV_EINVAL;
+    if (d->dtype < XCONV_F32 || d->dtype > XCONV_F16 || (d->w_dtype != XCONV_F32 && d->w_dtype != d->dtype)) return XCONV_EINVAL;
+    if (!(d->eps >= 0.f) || !std::isfinite(d->eps)) return XCONV_EINVAL;
+    if (d->C > (1 << 24) || d->inner > (1LL << 30) || d->outer > (1LL << 40) / d->inner) return XCONV_EUNSUPPORTED;
+    return XCONV_OK;
+}
+inline bool aligned_to(const void *p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+}  // namespace
+
+size_t xconv_layernorm_workspace_bytes(const xconv_norm_desc *desc)
+{
+    return check_norm(desc) == XCONV_OK && desc->outer > 0 ? norm_ws_bytes(desc) : 0;
+}
+
+xconv_status xconv_layernorm_fwd(const xconv_norm_desc *desc, const void *X_dev, const void *gamma_dev, const void *beta_dev, void *Y_dev,
+                                 float *mean_dev, float *rstd_dev, void *stream)
+{
+    const xconv_status s = check_norm(desc);
+    if (s != XCONV_OK) return s;
+    if (desc->outer == 0) return XCONV_OK;
+    if (!X_dev || !Y_dev) return XCONV_EINVAL;
+    const size_t e = elem_bytes(desc->dtype), w = elem_bytes(desc->w_dtype);
+    if (!aligned_to(X_dev, e) || !aligned_to(Y_dev, e) || !aligned_to(gamma_dev, w) || !aligned_to(beta_dev, w) || !aligned_to(mean_dev, 4) ||
+        !aligned_to(rstd_dev, 4))
+        return XCONV_EINVAL;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    XC_LAUNCH(K_NORM, st, launch_norm_fwd(desc, X_dev, gamma_dev, beta_dev, Y_dev, mean_dev, rstd_dev, st));
+    return XCONV_OK;
+}
+
+xconv_status xconv_layernorm_bwd(const xconv_norm_desc *desc, const void *dY_dev, const void *X_dev, const float *mean_dev, const float *rstd_dev,
+                                 const void *gamma_dev, void *dX_dev, void *dgamma_dev, void *dbeta_dev, void *ws_dev, size_t ws_bytes, void *stream)
+{
+    const xconv_status s = check_norm(desc);
+    if (s != XCONV_OK) return s;
+    const bool sums = dgamma_dev || dbeta_dev;
+    if (!sums && (!dX_dev || desc->outer == 0)) return XCONV_OK;
+    const size_t e = elem_bytes(desc->dtype), w = elem_bytes(desc->w_dtype);
+    if (!aligned_to(dY_dev, e) || !aligned_to(X_dev, e) || !aligned_to(dX_dev, e) || !aligned_to(gamma_dev, w) || !aligned_to(dgamma_dev, w) ||
+        !aligned_to(dbeta_dev, w) || !aligned_to(mean_dev, 4) || !aligned_to(rstd_dev, 4) || !aligned_to(ws_dev, 4))
+        return XCONV_EINVAL;
+    if (desc->outer > 0) {
+        if (!dY_dev || !X_dev || !mean_dev || !rstd_dev || (sums && !ws_dev)) return XCONV_EINVAL;
+        if (sums && ws_bytes < norm_ws_bytes(desc)) return XCONV_EWORKSPACE;
+    }
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    XC_LAUNCH(K_NORM, st, launch_norm_bwd(desc, dY_dev, X_dev, mean_dev, rstd_dev, gamma_dev, dX_dev, dgamma_dev, dbeta_dev, static_cast<float *>(ws_dev), st));
+    return XCONV_OK;
+}
+
+// ---- orthogonalised weight updates ------------------------------------------------------
+namespace {
+// pointers: also those of the matrices
+xconv_status check_orth(const xconv_orth_item *items, int count, const xconv_orth_args *a, const xconv_muon_args *mu, bool pointers)
+{
+    if (count < 0 || !a || (count > 0 && !items)) return XCONV_EINVAL;
+    if (a->g_dtype < XCONV_F32 || a->g_dtype > XCONV_F16 || a->out_dtype < XCONV_F32 || a->out_dtype > XCONV_F16 || a->steps < 0) return XCONV_EINVAL;
+    if (!std::isfinite(a->a) || !std::isfinite(a->b) || !std::isfinite(a->c) || !std::isfinite(a->eps) || a->eps < 0.f) return XCONV_EINVAL;
+    if (mu && (!std::isfinite(mu->lr) || !std::isfinite(mu->momentum) || !std::isfinite(mu->weight_decay))) return XCONV_EINVAL;
+    for (int i = 0; i < count; ++i) {
+        const xconv_orth_item &t = items[i];
+        if (t.rows < 1 || t.cols < 1) return XCONV_EINVAL;
+        if (!pointers) continue;
+        if (!t.G_dev || !t.out_dev || (mu && !t.M_dev)) return XCONV_EINVAL;
+        if (!aligned_to(t.G_dev, elem_bytes(a->g_dtype)) || !aligned_to(t.out_dev, elem_bytes(a->out_dtype)) || (mu && !aligned_to(t.M_dev, 4))) return XCONV_EINVAL;
+    }
+    for (int i = 0; i < count; ++i) {
+        const xconv_orth_item &t = items[i];
+        if (t.rows > (1 << 24) || t.cols > (1 << 24) || std::min(t.rows, t.cols) > 32768 || (long long)t.rows * t.cols > (1LL << 31)) return XCONV_EUNSUPPORTED;
+    }
+    if (a->steps > 64) return XCONV_EUNSUPPORTED;
+    // how far the steps take singular values from [0, 1]: the fp16 numbers hold entries below 16 of X, X X^T and the polynomial
+    double top = 1.0;
+    for (int k = 0; k < a->steps; ++k) {
+        if (!(top <= 3.5)) return XCONV_EUNSUPPORTED;
+        double next = 0.0;
+        for (int j = 0; j <= 512; ++j) {
+            const double v = top * j / 512, l = v * v, q = a->a + (a->b + a->c * l) * l;
+            if (!(std::fabs(q) <= 12.0)) return XCONV_EUNSUPPORTED;
+            next = std::max(next, std::fabs(v * q));
+        }
+        top = next;
+    }
+    return XCONV_OK;
+}
+xconv_status run_orth(const xconv_orth_item *items, int count, const xconv_orth_args *args, const xconv_muon_args *muon, void *ws_dev, size_t ws_bytes,
+                      void *stream)
+{
+    const xconv_status s = check_orth(items, count, args, muon, true);
+    if (s != XCONV_OK || count == 0) return s;
+    if (!ws_dev || !aligned_to(ws_dev, 256)) return XCONV_EINVAL;
+    if (ws_bytes < orth_ws_bytes(items, count)) return XCONV_EWORKSPACE;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    XC_LAUNCH(K_ORTH, st, launch_orth(items, count, args, muon, ws_dev, st));
+    return XCONV_OK;
+}
+}  // namespace
+
+size_t xconv_orth_workspace_bytes(const xconv_orth_item *items, int count, const xconv_orth_args *args)
+{
+    return check_orth(items, count, args, nullptr, false) == XCONV_OK ? orth_ws_bytes(items, count) : 0;
+}
+
+xconv_status xconv_orth(const xconv_orth_item *items, int count, const xconv_orth_args *args, void *ws_dev, size_t ws_bytes, void *stream)
+{
+    return run_orth(items, count, args, nullptr, ws_dev, ws_bytes, stream);
+}
+
+xconv_status xconv_muon_step(const xconv_orth_item *items, int count, const xconv_orth_args *args, const xconv_muon_args *muon, void *ws_dev,
+                             size_t ws_bytes, void *stream)
+{
+    if (!muon) return XCONV_EINVAL;
+    return run_orth(items, count, args, muon, ws_dev, ws_bytes, stream);
+}
+
 xconv_status xconv_diag_mfma_rate(int dtype, int iters, float *out_dev, size_t out_bytes, double *flops, void *stream)
 {
     if (dtype < XCONV_F32 || dtype > XCONV_F16 || iters < 1 || iters > (1 << 24) || !out_dev) return XCONV_EINVAL;
@@ -1382,6 +1503,8 @@ const char *xconv_prof_kernel_name(int id)
     case K_GEN_ZIMG: return "gen_zimg_kernel";
     case K_SCALE: return "scale_kernel";
     case K_PIXEL_FWD: return "pixel_fwd_kernel";
+    case K_NORM: return "norm_kernel";
+    case K_ORTH: return "orth_kernel";
     case K_RELU: return "relu_sign_kernel";
     default: return "unknown";
     }
