@@ -6,11 +6,11 @@
 // summed from the centred values (a mean far from zero costs no digits), every output is rounded once.
 // Bound by HBM: every tensor is read once, its values stay in registers between the statistics and the output.
 //
-// Rows: a group of G lanes (part of a wave, a wave, or a workgroup) holds a row, K 16-byte vectors a lane, and sums across
-// lanes.  Planes: 16 lanes lie along the positions (256 consecutive bytes of a plane), the other threads along the channels,
+// Rows: a group of G lanes (part of a wave, a wave, or a workgroup) holds R rows, K 16-byte vectors a row and lane, and sums
+// across lanes.  Planes: 8 lanes lie along the positions (one 128-byte line of a plane), the other threads along the channels,
 // K channels each; sums across threads go through LDS.  Longer rows and more channels than the registers hold are read
-// again from the cache (K == 0).  Rows of any length are read as vectors at the alignment of an element, which the memory
-// system takes; only the last vector of a row or plane is read value by value.
+// again from the cache (K == 0).  Rows and planes of any length are read as vectors at the alignment of an element, which the
+// memory system takes; the last vector of one whose length is no multiple of V starts earlier and overlaps the one before it.
 //
 // Backward: a fixed number of workgroups walks the positions and adds up dgamma and dbeta in registers, in fixed order; their
 // partial sums are added up in order by a second launch, so that results do not depend on timing.
@@ -49,28 +49,63 @@ template <int DT> __device__ inline void store_loose(typename NormElem<DT>::t *p
     *reinterpret_cast<Loose<DT> *>(p) = Loose<DT>{{v.x, v.y, v.z, v.w}};
 }
 
-// the first n (1 .. V) values of a vector; the others are zero / left alone
-template <int DT> __device__ inline uint4 load_some(const typename NormElem<DT>::t *p, int n)
+struct NormArgs {
+    const void *x, *dy, *gamma, *beta;
+    void *y;              // y or dx
+    float *mean, *rstd;   // written (forward, may be null) or read (backward)
+    float *part;          // backward: [workgroups][2][C] partial sums of dgamma and dbeta, null when neither is wanted
+    long long outer;
+    int C, inner;
+    float eps, inv_c, count;   // count = C, inv_c = 1 / C
+    int nvi;              // vectors a plane
+    long long tiles;      // tiles of kNormTX vectors of positions (planes)
+    int exact;            // last vectors do not overlap (shorter than a vector; outputs over inputs that are read again)
+};
+
+// Vector v of a run of n values: values lo .. hi - 1 of the V from `at` on are the vector's own.  Those below lo belong to the
+// vector before it as well: they are computed twice, with the same result, and count once in every sum.
+struct Part {
+    int at, lo, hi;
+};
+template <int V> __device__ inline Part part_of(int v, int n, int exact)
 {
-    constexpr int V = NormElem<DT>::V;
-    if (n >= V) return load_loose<DT>(p);
-    typename NormElem<DT>::t e[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) e[i] = i < n ? p[i] : typename NormElem<DT>::t(0);
-    return __builtin_bit_cast(uint4, e);
+    if (exact) return {v * V, 0, min(V, n - v * V)};
+    const int at = min(v * V, n - V);
+    return {at, v * V - at, V};
 }
-template <int DT> __device__ inline void store_some(typename NormElem<DT>::t *p, const uint4 &v, int n)
+__device__ inline bool own(const Part &p, int i) { return i >= p.lo && i < p.hi; }
+
+// the first n < V values, in runs of 4, 2 and 1
+template <int DT> __device__ inline uint4 load_short(const typename NormElem<DT>::t *p, int n)
+{
+    uint4 v{0, 0, 0, 0};
+    if constexpr (DT == XCONV_F32) {
+        v.x = n > 0 ? __float_as_uint(p[0]) : 0u;
+        v.y = n > 1 ? __float_as_uint(p[1]) : 0u;
+        v.z = n > 2 ? __float_as_uint(p[2]) : 0u;
+    } else {
+        auto pair = [&](int i) { return (n > i ? (uint32_t)p[i] : 0u) | (n > i + 1 ? (uint32_t)p[i + 1] << 16 : 0u); };
+        v = uint4{pair(0), pair(2), pair(4), pair(6)};
+    }
+    return v;
+}
+template <int DT> __device__ inline void store_short(typename NormElem<DT>::t *p, const uint4 v, int n)
 {
     constexpr int V = NormElem<DT>::V;
-    if (n >= V) {
-        store_loose<DT>(p, v);
-        return;
-    }
     struct Pack { typename NormElem<DT>::t e[V]; };
     const Pack k = __builtin_bit_cast(Pack, v);
 #pragma unroll
-    for (int i = 0; i < V; ++i)
+    for (int i = 0; i < V - 1; ++i)
         if (i < n) p[i] = k.e[i];
+}
+template <int DT> __device__ inline uint4 load_part(const typename NormElem<DT>::t *run, const Part &p)
+{
+    return p.hi == NormElem<DT>::V ? load_loose<DT>(run + p.at) : load_short<DT>(run + p.at, p.hi);
+}
+template <int DT> __device__ inline void store_part(typename NormElem<DT>::t *run, const uint4 &v, const Part &p)
+{
+    if (p.hi == NormElem<DT>::V) store_loose<DT>(run + p.at, v);
+    else store_short<DT>(run + p.at, v, p.hi);
 }
 template <int DT> __device__ inline void unpack(const uint4 &v, float (&x)[NormElem<DT>::V])
 {
@@ -95,26 +130,35 @@ template <int DT> __device__ inline uint4 pack(const float (&x)[NormElem<DT>::V]
     }
     return uint4{w[0], w[1], w[2], w[3]};
 }
-// V parameters from channel c on (n of them exist), in the type WT
-template <int WT, int V> __device__ inline void load_params(const void *p, int c, int n, float none, float (&out)[V])
+// Keeps 16 bytes as they are: what follows unpacks them again instead of holding the unpacked values in twice the registers.
+// The sums that were just made of them are operands too, so that those come first.
+template <int N> __device__ inline void keep_packed(uint4 &v, float (&sums)[N])
+{
+    asm volatile("" : "+v"(v.x), "+v"(v.y), "+v"(v.z), "+v"(v.w));
+#pragma unroll
+    for (int i = 0; i < N; i += 4) asm volatile("" : "+v"(v.x), "+v"(v.y), "+v"(v.z), "+v"(v.w), "+v"(sums[i]), "+v"(sums[i + 1]), "+v"(sums[i + 2]), "+v"(sums[i + 3]));
+}
+
+// V parameters of the type WT from p.at on, those that exist
+template <int WT, int V> __device__ inline void load_params(const void *q, const Part &p, float none, float (&out)[V], long long from = 0)
 {
     typedef typename NormElem<WT>::t elem_t;
-    const elem_t *q = static_cast<const elem_t *>(p) + c;
+    const elem_t *e = static_cast<const elem_t *>(q) + from + p.at;
     constexpr int VW = NormElem<WT>::V;
-    if (!p) {
+    if (!q) {
 #pragma unroll
         for (int i = 0; i < V; ++i) out[i] = none;
-    } else if (n >= V && V >= VW) {
+    } else if (p.hi == V && V >= VW) {
 #pragma unroll
         for (int j = 0; j < V; j += VW) {
             float t[VW];
-            unpack<WT>(load_loose<WT>(q + j), t);
+            unpack<WT>(load_loose<WT>(e + j), t);
 #pragma unroll
             for (int i = 0; i < VW; ++i) out[j + i] = t[i];
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < V; ++i) out[i] = i < n ? norm_val<WT>(q[i]) : none;
+        for (int i = 0; i < V; ++i) out[i] = i < p.hi ? norm_val<WT>(e[i]) : none;
     }
 }
 template <int WT> __device__ inline float load_param(const void *p, int c, float none)
@@ -122,324 +166,388 @@ template <int WT> __device__ inline float load_param(const void *p, int c, float
     return p ? norm_val<WT>(static_cast<const typename NormElem<WT>::t *>(p)[c]) : none;
 }
 
-// sum over a group of G lanes of a wave, or over the workgroup's G threads through `red` (two slots of G / 64 floats, taken in
-// turn so that one barrier a sum is enough)
-template <int G> __device__ inline float group_sum(float s, float *red, int &turn)
+// sums of R values over a group of G lanes of a wave, or over the workgroup's G threads through `red` (two slots of R * G / 64
+// floats, taken in turn so that one barrier a sum is enough)
+template <int G, int R> __device__ inline void group_sum(float (&s)[R], float *red, int &turn)
 {
 #pragma unroll
-    for (int o = (G < 64 ? G : 64) / 2; o >= 1; o >>= 1) s += __shfl_xor(s, o);
+    for (int o = (G < 64 ? G : 64) / 2; o >= 1; o >>= 1)
+#pragma unroll
+        for (int r = 0; r < R; ++r) s[r] += __shfl_xor(s[r], o);
     if constexpr (G > 64) {
         constexpr int W = G / 64;
-        float *slot = red + turn * W;
+        float *slot = red + turn * W * R;
         turn ^= 1;
-        if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = s;
-        __syncthreads();
-        s = 0.f;
+        if ((threadIdx.x & 63) == 0)
 #pragma unroll
-        for (int i = 0; i < W; ++i) s += slot[i];
+            for (int r = 0; r < R; ++r) slot[(threadIdx.x >> 6) * R + r] = s[r];
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < R; ++r) s[r] = 0.f;
+#pragma unroll
+        for (int i = 0; i < W; ++i)
+#pragma unroll
+            for (int r = 0; r < R; ++r) s[r] += slot[i * R + r];
     }
-    return s;
 }
 
-struct NormArgs {
-    const void *x, *dy, *gamma, *beta;
-    void *y;              // y or dx
-    float *mean, *rstd;   // written (forward, may be null) or read (backward)
-    float *part;          // backward: [workgroups][2][C] partial sums of dgamma and dbeta, null when neither is wanted
-    long long outer;
-    int C, inner;
-    float eps, inv_c, count;   // count = C, inv_c = 1 / C
-    int nvi;              // vectors a plane
-    long long tiles;      // tiles of 16 vectors of positions (planes)
-};
-
 // ---- rows ----------------------------------------------------------------------------------------------------------
-// G lanes a row, K vectors a lane (lane l holds vectors l, l + G, ...); K == 0: the row is read once a pass.
-template <int DT, int WT, int G, int K>
-__global__ __launch_bounds__(G > 256 ? G : 256) void norm_rows_fwd_kernel(NormArgs a)
+// G lanes a row, K vectors a lane (lane l holds vectors l, l + G, ...), R rows at once; K == 0: a row is read once a pass.
+template <int G> constexpr int row_threads = G > 256 ? G : 256;
+
+template <int DT, int WT, int G, int K, int R>
+__global__ __launch_bounds__(row_threads<G>) void norm_rows_fwd_kernel(NormArgs a)
 {
     typedef typename NormElem<DT>::t elem_t;
-    constexpr int V = NormElem<DT>::V, T = G > 256 ? G : 256, RP = T / G;
-    __shared__ float red[G > 64 ? 2 * (G / 64) : 1];
+    constexpr int V = NormElem<DT>::V, RP = row_threads<G> / G, KR = K > 0 ? K : 1;
+    __shared__ float red[G > 64 ? 2 * R * (G / 64) : 1];
     int turn = 0;
-    const int lane = threadIdx.x % G;
+    const int lane = threadIdx.x % G, grp = threadIdx.x / G;
     const int nv = (a.C + V - 1) / V;
-    auto left = [&](int v) { return a.C - v * V; };
-    for (long long r0 = (long long)blockIdx.x * RP; r0 < a.outer; r0 += (long long)gridDim.x * RP) {   // (the same count for all threads)
-        const long long row = r0 + threadIdx.x / G;
-        const bool on = row < a.outer;
-        const elem_t *x = static_cast<const elem_t *>(a.x) + (size_t)(on ? row : 0) * a.C;
-        elem_t *y = static_cast<elem_t *>(a.y) + (size_t)(on ? row : 0) * a.C;
-        uint4 raw[K > 0 ? K : 1];
-        // the rounds of vectors: k of the registers, or all that there are
-        auto rounds = [&](auto &&body) {
-            if constexpr (K > 0) {
+    const elem_t *X = static_cast<const elem_t *>(a.x);
+    elem_t *Y = static_cast<elem_t *>(a.y);
+    // the rounds of vectors: k of the registers, or all that there are
+    auto rounds = [&](auto &&body) {
+        if constexpr (K > 0) {
 #pragma unroll
-                for (int k = 0; k < K; ++k) body(k, lane + k * G);
-            } else {
-                for (int v = lane; v < nv; v += G) body(0, v);
-            }
+            for (int k = 0; k < K; ++k) body(k, lane + k * G);
+        } else {
+            for (int v = lane; v < nv; v += G) body(0, v);
+        }
+    };
+    for (long long r0 = (long long)blockIdx.x * (RP * R); r0 < a.outer; r0 += (long long)gridDim.x * (RP * R)) {   // (the same count for all threads)
+        uint4 raw[R][KR];
+        long long row[R];
+        bool on[R];
+        const elem_t *x[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            row[r] = r0 + r * RP + grp;
+            on[r] = row[r] < a.outer;
+            x[r] = X + (size_t)(on[r] ? row[r] : 0) * a.C;
+        }
+        if constexpr (K > 0)
+            rounds([&](int k, int v) {
+                const Part p = part_of<V>(v, a.C, a.exact);
+#pragma unroll
+                for (int r = 0; r < R; ++r) raw[r][k] = v < nv ? load_part<DT>(x[r], p) : uint4{0, 0, 0, 0};
+            });
+        auto value = [&](int r, int k, const Part &p) -> uint4 {
+            if constexpr (K > 0) return raw[r][k];
+            else return load_part<DT>(x[r], p);
         };
-        if constexpr (K > 0) rounds([&](int k, int v) { raw[k] = v < nv ? load_some<DT>(x + v * V, left(v)) : uint4{0, 0, 0, 0}; });
-        auto value = [&](int k, int v) -> uint4 {
-            if constexpr (K > 0) return raw[k];
-            else return load_some<DT>(x + v * V, left(v));
-        };
-        float s = 0.f;
-        rounds([&](int k, int v) {
-            float t[V];
-            unpack<DT>(value(k, v), t);
+        float s[R], mean[R], rstd[R];
 #pragma unroll
-            for (int i = 0; i < V; ++i) s += t[i];
-        });
-        const float mean = group_sum<G>(s, red, turn) / a.count;
-        s = 0.f;
+        for (int r = 0; r < R; ++r) s[r] = 0.f;
         rounds([&](int k, int v) {
-            const int n = left(v);
-            float t[V];
-            unpack<DT>(value(k, v), t);
+            const Part p = part_of<V>(v, a.C, a.exact);
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float d = i < n ? t[i] - mean : 0.f;
-                s += d * d;
+            for (int r = 0; r < R; ++r) {
+                float t[V];
+                unpack<DT>(value(r, k, p), t);
+#pragma unroll
+                for (int i = 0; i < V; ++i) s[r] += v < nv && own(p, i) ? t[i] : 0.f;
             }
         });
-        const float rstd = 1.0f / sqrtf(group_sum<G>(s, red, turn) * a.inv_c + a.eps);
-        if (!on) continue;
+        group_sum<G>(s, red, turn);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            mean[r] = s[r] / a.count;
+            s[r] = 0.f;
+        }
+        rounds([&](int k, int v) {
+            const Part p = part_of<V>(v, a.C, a.exact);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                float t[V];
+                unpack<DT>(value(r, k, p), t);
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const float d = v < nv && own(p, i) ? t[i] - mean[r] : 0.f;
+                    s[r] += d * d;
+                }
+            }
+        });
+        group_sum<G>(s, red, turn);
+#pragma unroll
+        for (int r = 0; r < R; ++r) rstd[r] = 1.0f / sqrtf(s[r] * a.inv_c + a.eps);
         rounds([&](int k, int v) {
             if (v >= nv) return;
-            float t[V], g[V], b[V];
-            unpack<DT>(value(k, v), t);
-            load_params<WT, V>(a.gamma, v * V, left(v), 1.f, g);
-            load_params<WT, V>(a.beta, v * V, left(v), 0.f, b);
+            const Part p = part_of<V>(v, a.C, a.exact);
+            float g[V], b[V];
+            load_params<WT, V>(a.gamma, p, 1.f, g);
+            load_params<WT, V>(a.beta, p, 0.f, b);
 #pragma unroll
-            for (int i = 0; i < V; ++i) t[i] = (t[i] - mean) * rstd * g[i] + b[i];
-            store_some<DT>(y + v * V, pack<DT>(t), left(v));
+            for (int r = 0; r < R; ++r) {
+                if (!on[r]) continue;
+                float t[V];
+                unpack<DT>(value(r, k, p), t);
+#pragma unroll
+                for (int i = 0; i < V; ++i) t[i] = (t[i] - mean[r]) * rstd[r] * g[i] + b[i];
+                store_part<DT>(Y + (size_t)row[r] * a.C, pack<DT>(t), p);
+            }
         });
         if (lane == 0) {
-            if (a.mean) a.mean[row] = mean;
-            if (a.rstd) a.rstd[row] = rstd;
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                if (on[r]) {
+                    if (a.mean) a.mean[row[r]] = mean[r];
+                    if (a.rstd) a.rstd[row[r]] = rstd[r];
+                }
         }
     }
 }
 
 // A workgroup's groups walk the rows; every lane adds up dgamma and dbeta of its own columns.  K == 0: one row a workgroup at
 // a time, dgamma and dbeta in the workgroup's own slots of `part`.
-template <int DT, int WT, int G, int K>
-__global__ __launch_bounds__(G > 256 ? G : 256) void norm_rows_bwd_kernel(NormArgs a)
+template <int DT, int WT, int G, int K, int R>
+__global__ __launch_bounds__(row_threads<G>) void norm_rows_bwd_kernel(NormArgs a)
 {
     typedef typename NormElem<DT>::t elem_t;
-    constexpr int V = NormElem<DT>::V, T = G > 256 ? G : 256, RP = T / G;
-    __shared__ float red[G > 64 ? 2 * (G / 64) : 1];
+    constexpr int V = NormElem<DT>::V, T = row_threads<G>, RP = T / G, KR = K > 0 ? K : 1;
+    __shared__ float red[G > 64 ? 4 * R * (G / 64) : 1];
     int turn = 0;
     const int lane = threadIdx.x % G, grp = threadIdx.x / G;
     const elem_t *X = static_cast<const elem_t *>(a.x), *DY = static_cast<const elem_t *>(a.dy);
     elem_t *DX = static_cast<elem_t *>(a.y);
     const int nv = (a.C + V - 1) / V;
-    auto left = [&](int v) { return a.C - v * V; };
     float *part = a.part ? a.part + (size_t)blockIdx.x * 2 * a.C : nullptr;
-    if constexpr (K > 0) {
-        float g[K][V], ag[K][V], ab[K][V];
+    auto rounds = [&](auto &&body) {
+        if constexpr (K > 0) {
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            const int v = lane + k * G;
-            load_params<WT, V>(a.gamma, v * V, left(v), 1.f, g[k]);
-#pragma unroll
-            for (int i = 0; i < V; ++i) ag[k][i] = ab[k][i] = 0.f;
-        }
-        for (long long r0 = (long long)blockIdx.x * RP; r0 < a.outer; r0 += (long long)gridDim.x * RP) {   // (the same count for all threads)
-            const long long row = r0 + grp;
-            const bool on = row < a.outer;
-            const size_t at = (size_t)(on ? row : 0) * a.C;
-            const float mean = a.mean[on ? row : 0], rstd = a.rstd[on ? row : 0];
-            uint4 rx[K], rd[K];
-#pragma unroll
-            for (int k = 0; k < K; ++k) {
-                const int v = lane + k * G;
-                const bool has = on && v < nv;
-                rx[k] = has ? load_some<DT>(X + at + v * V, left(v)) : uint4{0, 0, 0, 0};
-                rd[k] = has ? load_some<DT>(DY + at + v * V, left(v)) : uint4{0, 0, 0, 0};
-            }
-            float c1 = 0.f, c2 = 0.f;
-#pragma unroll
-            for (int k = 0; k < K; ++k) {
-                float x[V], d[V];
-                unpack<DT>(rx[k], x);
-                unpack<DT>(rd[k], d);
-                const int n = on ? left(lane + k * G) : 0;
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float xh = i < n ? (x[i] - mean) * rstd : 0.f, gd = i < n ? d[i] * g[k][i] : 0.f;
-                    c1 += gd;
-                    c2 += gd * xh;
-                    ag[k][i] += d[i] * xh;
-                    ab[k][i] += d[i];
-                }
-            }
-            c1 = group_sum<G>(c1, red, turn) * a.inv_c;
-            c2 = group_sum<G>(c2, red, turn) * a.inv_c;
-            if (DX && on) {
-#pragma unroll
-                for (int k = 0; k < K; ++k) {
-                    const int v = lane + k * G;
-                    if (v >= nv) continue;
-                    float x[V], d[V];
-                    unpack<DT>(rx[k], x);
-                    unpack<DT>(rd[k], d);
-#pragma unroll
-                    for (int i = 0; i < V; ++i) x[i] = rstd * (d[i] * g[k][i] - c1 - (x[i] - mean) * rstd * c2);
-                    store_some<DT>(DX + at + v * V, pack<DT>(x), left(v));
-                }
-            }
-        }
-        if (!part) return;
-        // groups of one workgroup hold the same columns: added up in order of the groups
-        if constexpr (RP > 1) {
-            extern __shared__ float cols[];     // [RP][2][G * K * V]
-            constexpr int W = G * K * V;
-#pragma unroll
-            for (int k = 0; k < K; ++k)
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const int c = (lane + k * G) * V + i;
-                    cols[(grp * 2) * W + c] = ag[k][i];
-                    cols[(grp * 2 + 1) * W + c] = ab[k][i];
-                }
-            __syncthreads();
-            for (int q = threadIdx.x; q < 2 * W; q += T) {
-                const int c = q % W;
-                if (c >= a.C) continue;
-                float s = 0.f;
-                for (int r = 0; r < RP; ++r) s += cols[r * 2 * W + q];
-                part[(size_t)(q / W) * a.C + c] = s;
-            }
+            for (int k = 0; k < K; ++k) body(k, lane + k * G);
         } else {
+            for (int v = lane; v < nv; v += G) body(0, v);
+        }
+    };
+    float ag[KR][V], ab[KR][V];
 #pragma unroll
-            for (int k = 0; k < K; ++k)
+    for (int k = 0; k < KR; ++k)
+#pragma unroll
+        for (int i = 0; i < V; ++i) ag[k][i] = ab[k][i] = 0.f;
+    bool first = true;
+    for (long long r0 = (long long)blockIdx.x * (RP * R); r0 < a.outer; r0 += (long long)gridDim.x * (RP * R), first = false) {   // (the same count for all threads)
+        uint4 rx[R][KR], rd[R][KR];
+        float mean[R], rstd[R], c[2 * R];
+        size_t at[R];
+        bool on[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const long long row = r0 + r * RP + grp;
+            on[r] = row < a.outer;
+            at[r] = (size_t)(on[r] ? row : 0) * a.C;
+            mean[r] = a.mean[on[r] ? row : 0];
+            rstd[r] = a.rstd[on[r] ? row : 0];
+            c[2 * r] = c[2 * r + 1] = 0.f;
+        }
+        auto get = [&](int r, int k, int v, const Part &p) {
+            const bool has = on[r] && v < nv;
+            rx[r][k] = has ? load_part<DT>(X + at[r], p) : uint4{0, 0, 0, 0};
+            rd[r][k] = has ? load_part<DT>(DY + at[r], p) : uint4{0, 0, 0, 0};
+        };
+        if constexpr (K > 0)
+            rounds([&](int k, int v) {
+                const Part p = part_of<V>(v, a.C, a.exact);
+#pragma unroll
+                for (int r = 0; r < R; ++r) get(r, k, v, p);
+            });
+        rounds([&](int k, int v) {
+            const Part p = part_of<V>(v, a.C, a.exact);
+            float g[V];
+            if (v < nv) {
+                load_params<WT, V>(a.gamma, p, 1.f, g);
+            } else {
+#pragma unroll
+                for (int i = 0; i < V; ++i) g[i] = 0.f;
+            }
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                if constexpr (K == 0) get(r, k, v, p);
+                float x[V], d[V];
+                unpack<DT>(rx[r][k], x);
+                unpack<DT>(rd[r][k], d);
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    const int c = (lane + k * G) * V + i;
-                    if (c < a.C) {
-                        part[c] = ag[k][i];
-                        part[(size_t)a.C + c] = ab[k][i];
+                    const bool mine = on[r] && v < nv && own(p, i);
+                    const float xh = mine ? (x[i] - mean[r]) * rstd[r] : 0.f, di = mine ? d[i] : 0.f, gd = di * g[i];
+                    c[2 * r] += gd;
+                    c[2 * r + 1] += gd * xh;
+                    if constexpr (K > 0) {
+                        ag[k][i] += di * xh;
+                        ab[k][i] += di;
+                    } else if (part && mine) {
+                        float *pg = part + p.at + i, *pb = pg + a.C;
+                        *pg = (first ? 0.f : *pg) + di * xh;
+                        *pb = (first ? 0.f : *pb) + di;
                     }
                 }
+                if constexpr (K > 1) {
+                    keep_packed(rx[r][k], ag[k]);
+                    keep_packed(rd[r][k], ab[k]);
+                }
+            }
+        });
+        if (!DX) continue;
+        group_sum<G>(c, red, turn);
+        rounds([&](int k, int v) {
+            if (v >= nv) return;
+            const Part p = part_of<V>(v, a.C, a.exact);
+            float g[V];
+            load_params<WT, V>(a.gamma, p, 1.f, g);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                if (!on[r]) continue;
+                if constexpr (K == 0) get(r, k, v, p);
+                const float c1 = c[2 * r] * a.inv_c, c2 = c[2 * r + 1] * a.inv_c;
+                float x[V], d[V];
+                unpack<DT>(rx[r][k], x);
+                unpack<DT>(rd[r][k], d);
+#pragma unroll
+                for (int i = 0; i < V; ++i) x[i] = rstd[r] * (d[i] * g[i] - c1 - (x[i] - mean[r]) * rstd[r] * c2);
+                store_part<DT>(DX + at[r], pack<DT>(x), p);
+            }
+        });
+    }
+    if (K == 0 || !part) return;
+    // groups of one workgroup hold the same columns: added up in order of the groups
+    constexpr int W = G * KR * V;
+    if constexpr (RP > 1) {
+        extern __shared__ float cols[];     // [RP][2][W]
+        rounds([&](int k, int v) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                cols[(grp * 2) * W + v * V + i] = ag[k][i];
+                cols[(grp * 2 + 1) * W + v * V + i] = ab[k][i];
+            }
+        });
+        __syncthreads();
+        for (int q = threadIdx.x; q < 2 * W; q += T) {
+            const int slot = q % W;
+            if (slot / V >= nv) continue;
+            const Part p = part_of<V>(slot / V, a.C, a.exact);
+            if (!own(p, slot % V)) continue;
+            float s = 0.f;
+            for (int r = 0; r < RP; ++r) s += cols[r * 2 * W + q];
+            part[(size_t)(q / W) * a.C + p.at + slot % V] = s;
         }
     } else {
-        bool first = true;
-        for (long long row = blockIdx.x; row < a.outer; row += gridDim.x, first = false) {
-            const size_t at = (size_t)row * a.C;
-            const float mean = a.mean[row], rstd = a.rstd[row];
-            float c1 = 0.f, c2 = 0.f;
-            for (int v = lane; v < nv; v += G) {
-                float x[V], d[V], g[V];
-                unpack<DT>(load_some<DT>(X + at + v * V, left(v)), x);
-                unpack<DT>(load_some<DT>(DY + at + v * V, left(v)), d);
-                load_params<WT, V>(a.gamma, v * V, left(v), 1.f, g);
+        rounds([&](int k, int v) {
+            if (v >= nv) return;
+            const Part p = part_of<V>(v, a.C, a.exact);
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float xh = i < left(v) ? (x[i] - mean) * rstd : 0.f, gd = i < left(v) ? d[i] * g[i] : 0.f;
-                    c1 += gd;
-                    c2 += gd * xh;
-                    if (part && i < left(v)) {
-                        float *pg = part + v * V + i, *pb = pg + a.C;
-                        *pg = (first ? 0.f : *pg) + d[i] * xh;
-                        *pb = (first ? 0.f : *pb) + d[i];
-                    }
+            for (int i = 0; i < V; ++i)
+                if (own(p, i)) {
+                    part[p.at + i] = ag[k][i];
+                    part[(size_t)a.C + p.at + i] = ab[k][i];
                 }
-            }
-            c1 = group_sum<G>(c1, red, turn) * a.inv_c;
-            c2 = group_sum<G>(c2, red, turn) * a.inv_c;
-            if (!DX) continue;
-            for (int v = lane; v < nv; v += G) {
-                float x[V], d[V], g[V];
-                unpack<DT>(load_some<DT>(X + at + v * V, left(v)), x);
-                unpack<DT>(load_some<DT>(DY + at + v * V, left(v)), d);
-                load_params<WT, V>(a.gamma, v * V, left(v), 1.f, g);
-#pragma unroll
-                for (int i = 0; i < V; ++i) x[i] = rstd * (d[i] * g[i] - c1 - (x[i] - mean) * rstd * c2);
-                store_some<DT>(DX + at + v * V, pack<DT>(x), left(v));
-            }
-        }
+        });
     }
 }
 
 // ---- planes --------------------------------------------------------------------------------------------------------
-constexpr int kNormTX = 16;     // lanes along the positions
+constexpr int kNormTX = 8;               // lanes along the positions
+constexpr int kNormTYW = 64 / kNormTX;   // channels of a wave
 
-// sums over the TY threads of each of the 16 columns of vectors, V positions each; `red` [NW][16][V]
-template <int V, int NW> __device__ inline void column_sum(float (&s)[V], float *red)
+// sums over the threads along the channels of N columns of V positions each; `red` [NW][kNormTX][N * V]
+template <int N, int NW> __device__ inline void column_sum(float (&s)[N], float *red)
 {
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        s[i] += __shfl_xor(s[i], 16);
-        s[i] += __shfl_xor(s[i], 32);
-    }
+    for (int o = kNormTX; o < 64; o <<= 1)
+#pragma unroll
+        for (int i = 0; i < N; ++i) s[i] += __shfl_xor(s[i], o);
     const int tx = threadIdx.x % kNormTX;
     __syncthreads();                     // whoever still reads the last sum
     if ((threadIdx.x & 63) < kNormTX)
 #pragma unroll
-        for (int i = 0; i < V; ++i) red[((threadIdx.x >> 6) * kNormTX + tx) * V + i] = s[i];
+        for (int i = 0; i < N; ++i) red[((threadIdx.x >> 6) * kNormTX + tx) * N + i] = s[i];
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < V; ++i) s[i] = 0.f;
-#pragma unroll
+    for (int i = 0; i < N; ++i) s[i] = 0.f;
+#pragma unroll 2
     for (int w = 0; w < NW; ++w)
 #pragma unroll
-        for (int i = 0; i < V; ++i) s[i] += red[(w * kNormTX + tx) * V + i];
+        for (int i = 0; i < N; ++i) s[i] += red[(w * kNormTX + tx) * N + i];
 }
 
-// where the thread's vector of positions lies: first value of channel 0, values that exist (0: past the end), first position
+// where the thread's vector of positions lies: first value of channel 0 of the image, its first position, the vector's part
 struct PlaneAt {
     size_t base;
     long long pos;
-    int n;
+    Part p;
+    bool on;
 };
 template <int V> __device__ inline PlaneAt plane_at(const NormArgs &a, long long tile)
 {
     const long long q = tile * kNormTX + threadIdx.x % kNormTX;
-    const long long img = q / a.nvi;
-    if (img >= a.outer) return {0, 0, 0};
-    const int p = (int)(q - img * a.nvi) * V;
-    return {(size_t)img * a.C * a.inner + p, img * a.inner + p, min(V, a.inner - p)};
+    const long long img = a.tiles * kNormTX < (1LL << 31) ? (long long)((uint32_t)q / (uint32_t)a.nvi) : q / a.nvi;
+    if (img >= a.outer) return {0, 0, {0, 0, V}, false};
+    const Part p = part_of<V>((int)(q - img * a.nvi), a.inner, a.exact);
+    return {(size_t)img * a.C * a.inner, img * a.inner + p.at, p, true};
+}
+// channel c of the vector; WHOLE: the planes are whole or overlapping vectors, and every lane loads (zeros where there is nothing)
+template <int DT, bool WHOLE> __device__ inline uint4 plane_get(const NormArgs &a, const typename NormElem<DT>::t *x, const PlaneAt &at, int c)
+{
+    const bool on = at.on && c < a.C;
+    if constexpr (WHOLE) {
+        const uint4 v = load_loose<DT>(x + (size_t)min(c, a.C - 1) * a.inner + at.p.at);
+        return uint4{on ? v.x : 0u, on ? v.y : 0u, on ? v.z : 0u, on ? v.w : 0u};
+    } else {
+        return on ? load_part<DT>(x + (size_t)c * a.inner, at.p) : uint4{0, 0, 0, 0};
+    }
+}
+template <int DT, bool WHOLE> __device__ inline void plane_put(const NormArgs &a, typename NormElem<DT>::t *y, const PlaneAt &at, int c, const uint4 &v)
+{
+    if constexpr (WHOLE) store_loose<DT>(y + (size_t)c * a.inner + at.p.at, v);
+    else store_part<DT>(y + (size_t)c * a.inner, v, at.p);
+}
+// the run of tiles of a workgroup: neighbouring tiles share lines of memory, so a workgroup takes neighbours, and the
+// workgroups of one die the neighbouring runs
+__device__ inline void tiles_of(const NormArgs &a, long long &from, long long &to)
+{
+    const long long w = xcd_block(blockIdx.x, gridDim.x);
+    from = a.tiles * w / gridDim.x;
+    to = a.tiles * (w + 1) / gridDim.x;
 }
 
-template <int DT, int WT, int NW, int K>
+// WHOLE: planes of at least one vector whose last vectors overlap, the ordinary case
+template <int DT, int WT, int NW, int K, bool WHOLE>
 __global__ __launch_bounds__(NW * 64) void norm_planes_fwd_kernel(NormArgs a)
 {
     typedef typename NormElem<DT>::t elem_t;
-    constexpr int V = NormElem<DT>::V, TY = NW * 4;
+    constexpr int V = NormElem<DT>::V, TY = NW * kNormTYW;
     __shared__ float red[NW * kNormTX * V];
     const int ty = threadIdx.x / kNormTX;
-    for (long long tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
+    long long tile, end;
+    tiles_of(a, tile, end);
+    // the rounds of channels: k of the registers, or all that there are
+    auto rounds = [&](auto &&body) {
+        if constexpr (K > 0) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) body(k, ty + k * TY);
+        } else {
+            for (int c = ty; c < a.C; c += TY) body(0, c);
+        }
+    };
+    for (; tile < end; ++tile) {
         const PlaneAt at = plane_at<V>(a, tile);
         const elem_t *x = static_cast<const elem_t *>(a.x) + at.base;
         elem_t *y = static_cast<elem_t *>(a.y) + at.base;
-        const bool on = at.n > 0;
         uint4 raw[K > 0 ? K : 1];
         float s[V], mean[V], rstd[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) s[i] = 0.f;
-        // the rounds of channels: k of the registers, or all that there are
-        auto rounds = [&](auto &&body) {
-            if constexpr (K > 0) {
-#pragma unroll
-                for (int k = 0; k < K; ++k) body(k, ty + k * TY);
-            } else {
-                for (int c = ty; c < a.C; c += TY) body(0, c);
-            }
-        };
+        auto get = [&](int c) { return plane_get<DT, WHOLE>(a, x, at, c); };
         auto value = [&](int k, int c) -> uint4 {
             if constexpr (K > 0) return raw[k];
-            else return on ? load_some<DT>(x + (size_t)c * a.inner, at.n) : uint4{0, 0, 0, 0};
+            else return get(c);
         };
-        if constexpr (K > 0)
-            rounds([&](int k, int c) { raw[k] = on && c < a.C ? load_some<DT>(x + (size_t)c * a.inner, at.n) : uint4{0, 0, 0, 0}; });
+        if constexpr (K > 0) rounds([&](int k, int c) { raw[k] = get(c); });
         rounds([&](int k, int c) {
             float t[V];
             unpack<DT>(value(k, c), t);
 #pragma unroll
             for (int i = 0; i < V; ++i) s[i] += t[i];
+            if constexpr (K > 0) keep_packed(raw[k], s);
         });
         column_sum<V, NW>(s, red);
 #pragma unroll
@@ -455,11 +563,12 @@ __global__ __launch_bounds__(NW * 64) void norm_planes_fwd_kernel(NormArgs a)
                 const float d = c < a.C ? t[i] - mean[i] : 0.f;
                 s[i] += d * d;
             }
+            if constexpr (K > 0) keep_packed(raw[k], s);
         });
         column_sum<V, NW>(s, red);
 #pragma unroll
         for (int i = 0; i < V; ++i) rstd[i] = 1.0f / sqrtf(s[i] * a.inv_c + a.eps);
-        if (!on) continue;
+        if (!at.on) continue;
         rounds([&](int k, int c) {
             if (c >= a.C) return;
             float t[V];
@@ -467,12 +576,12 @@ __global__ __launch_bounds__(NW * 64) void norm_planes_fwd_kernel(NormArgs a)
             const float g = load_param<WT>(a.gamma, c, 1.f), b = load_param<WT>(a.beta, c, 0.f);
 #pragma unroll
             for (int i = 0; i < V; ++i) t[i] = (t[i] - mean[i]) * rstd[i] * g + b;
-            store_some<DT>(y + (size_t)c * a.inner, pack<DT>(t), at.n);
+            plane_put<DT, WHOLE>(a, y, at, c, pack<DT>(t));
         });
         if (ty == 0) {
 #pragma unroll
             for (int i = 0; i < V; ++i)
-                if (i < at.n) {
+                if (own(at.p, i)) {
                     if (a.mean) a.mean[at.pos + i] = mean[i];
                     if (a.rstd) a.rstd[at.pos + i] = rstd[i];
                 }
@@ -480,19 +589,22 @@ __global__ __launch_bounds__(NW * 64) void norm_planes_fwd_kernel(NormArgs a)
     }
 }
 
-template <int DT, int WT, int NW, int K>
+template <int DT, int WT, int NW, int K, bool WHOLE>
 __global__ __launch_bounds__(NW * 64) void norm_planes_bwd_kernel(NormArgs a)
 {
     typedef typename NormElem<DT>::t elem_t;
-    constexpr int V = NormElem<DT>::V, TY = NW * 4, KR = K > 0 ? K : 1;
-    __shared__ float red[NW * kNormTX * V];
+    constexpr int V = NormElem<DT>::V, TY = NW * kNormTYW, KR = K > 0 ? K : 1;
+    __shared__ float red[NW * kNormTX * 2 * V];
     const int ty = threadIdx.x / kNormTX, tx = threadIdx.x % kNormTX;
     const elem_t *X = static_cast<const elem_t *>(a.x), *DY = static_cast<const elem_t *>(a.dy);
     elem_t *DX = static_cast<elem_t *>(a.y);
     float *part = a.part ? a.part + (size_t)blockIdx.x * 2 * a.C : nullptr;
-    float ag[KR], ab[KR];
+    float ag[KR], ab[KR], gk[KR];
 #pragma unroll
-    for (int k = 0; k < KR; ++k) ag[k] = ab[k] = 0.f;
+    for (int k = 0; k < KR; ++k) {
+        ag[k] = ab[k] = 0.f;
+        gk[k] = load_param<WT>(a.gamma, min(ty + k * TY, a.C - 1), 1.f);
+    }
     auto rounds = [&](auto &&body) {
         if constexpr (K > 0) {
 #pragma unroll
@@ -502,39 +614,57 @@ __global__ __launch_bounds__(NW * 64) void norm_planes_bwd_kernel(NormArgs a)
         }
     };
     bool first = true;
-    for (long long tile = blockIdx.x; tile < a.tiles; tile += gridDim.x, first = false) {
+    long long tile, end;
+    tiles_of(a, tile, end);
+    for (; tile < end; ++tile, first = false) {
         const PlaneAt at = plane_at<V>(a, tile);
-        const bool on = at.n > 0;
         uint4 rx[KR], rd[KR];
-        auto get = [&](const elem_t *t, int c) { return on && c < a.C ? load_some<DT>(t + at.base + (size_t)c * a.inner, at.n) : uint4{0, 0, 0, 0}; };
-        if constexpr (K > 0) rounds([&](int k, int c) { rx[k] = get(X, c); rd[k] = get(DY, c); });
-        float mean[V], rstd[V], c1[V], c2[V];
+        auto get = [&](const elem_t *t, int c) { return plane_get<DT, WHOLE>(a, t + at.base, at, c); };
+        if constexpr (K > 0)
+            rounds([&](int k, int c) {
+                rx[k] = get(X, c);
+                rd[k] = get(DY, c);
+            });
+        float mean[V], rstd[V], c12[2 * V];
+        if constexpr (WHOLE) {
+            load_params<XCONV_F32, V>(a.mean, Part{0, 0, V}, 0.f, mean, at.pos);
+            load_params<XCONV_F32, V>(a.rstd, Part{0, 0, V}, 0.f, rstd, at.pos);
+        } else {
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            mean[i] = i < at.n ? a.mean[at.pos + i] : 0.f;
-            rstd[i] = i < at.n ? a.rstd[at.pos + i] : 0.f;
-            c1[i] = c2[i] = 0.f;
+            for (int i = 0; i < V; ++i) {
+                const bool there = at.on && i < at.p.hi;
+                mean[i] = there ? a.mean[at.pos + i] : 0.f;
+                rstd[i] = there ? a.rstd[at.pos + i] : 0.f;
+            }
         }
+#pragma unroll
+        for (int i = 0; i < V; ++i) c12[i] = c12[V + i] = 0.f;
         rounds([&](int k, int c) {
-            if constexpr (K == 0) { rx[0] = get(X, c); rd[0] = get(DY, c); }
+            if constexpr (K == 0) {
+                rx[0] = get(X, c);
+                rd[0] = get(DY, c);
+            }
             float x[V], d[V], sg = 0.f, sb = 0.f;
             unpack<DT>(rx[k], x);
             unpack<DT>(rd[k], d);
-            const float g = c < a.C ? load_param<WT>(a.gamma, c, 1.f) : 0.f;
+            const float g = K > 0 ? gk[k] : load_param<WT>(a.gamma, c, 1.f);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const float xh = (x[i] - mean[i]) * rstd[i], gd = d[i] * g;
-                c1[i] += gd;
-                c2[i] += gd * xh;
-                sg += d[i] * xh;
-                sb += d[i];
+                c12[i] += gd;
+                c12[V + i] += gd * xh;
+                sg += i >= at.p.lo ? d[i] * xh : 0.f;
+                sb += i >= at.p.lo ? d[i] : 0.f;
             }
             if constexpr (K > 0) {
                 ag[k] += sg;
                 ab[k] += sb;
+                asm volatile("" : "+v"(ag[k]), "+v"(ab[k]), "+v"(rx[k].x), "+v"(rd[k].x));
+                keep_packed(rx[k], c12);
+                keep_packed(rd[k], c12);
             } else if (part) {
 #pragma unroll
-                for (int o = 8; o >= 1; o >>= 1) {
+                for (int o = kNormTX / 2; o >= 1; o >>= 1) {
                     sg += __shfl_xor(sg, o);
                     sb += __shfl_xor(sb, o);
                 }
@@ -545,58 +675,62 @@ __global__ __launch_bounds__(NW * 64) void norm_planes_bwd_kernel(NormArgs a)
             }
         });
         if (!DX) continue;
-        column_sum<V, NW>(c1, red);
-        column_sum<V, NW>(c2, red);
-        if (!on) continue;
+        column_sum<2 * V, NW>(c12, red);
+        if (!at.on) continue;
+#pragma unroll
+        for (int i = 0; i < 2 * V; ++i) c12[i] *= a.inv_c;
         rounds([&](int k, int c) {
             if (c >= a.C) return;
-            if constexpr (K == 0) { rx[0] = get(X, c); rd[0] = get(DY, c); }
+            if constexpr (K == 0) {
+                rx[0] = get(X, c);
+                rd[0] = get(DY, c);
+            }
             float x[V], d[V];
             unpack<DT>(rx[k], x);
             unpack<DT>(rd[k], d);
-            const float g = load_param<WT>(a.gamma, c, 1.f);
+            const float g = K > 0 ? gk[k] : load_param<WT>(a.gamma, c, 1.f);
 #pragma unroll
-            for (int i = 0; i < V; ++i) x[i] = rstd[i] * (d[i] * g - c1[i] * a.inv_c - (x[i] - mean[i]) * rstd[i] * (c2[i] * a.inv_c));
-            store_some<DT>(DX + at.base + (size_t)c * a.inner, pack<DT>(x), at.n);
+            for (int i = 0; i < V; ++i) x[i] = rstd[i] * (d[i] * g - c12[i] - (x[i] - mean[i]) * rstd[i] * c12[V + i]);
+            plane_put<DT, WHOLE>(a, DX + at.base, at, c, pack<DT>(x));
         });
     }
-    if constexpr (K > 0) {
-        if (!part) return;
+    if (K == 0 || !part) return;
+    rounds([&](int k, int c) {
+        float sg = ag[k], sb = ab[k];
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            float sg = ag[k], sb = ab[k];
-#pragma unroll
-            for (int o = 8; o >= 1; o >>= 1) {
-                sg += __shfl_xor(sg, o);
-                sb += __shfl_xor(sb, o);
-            }
-            const int c = ty + k * TY;
-            if (tx == 0 && c < a.C) {
-                part[c] = sg;
-                part[(size_t)a.C + c] = sb;
-            }
+        for (int o = kNormTX / 2; o >= 1; o >>= 1) {
+            sg += __shfl_xor(sg, o);
+            sb += __shfl_xor(sb, o);
         }
-    }
+        if (tx == 0 && c < a.C) {
+            part[c] = sg;
+            part[(size_t)a.C + c] = sb;
+        }
+    });
 }
 
-// out[c] = sum over the n workgroups' partial sums, in order: 64 columns a workgroup, its four waves share the workgroups
+// out[c] = sum over the n workgroups' partial sums, in order: a workgroup takes 16 columns, its 64 rows of threads share the sums
+constexpr int kJoinCols = 16, kJoinThreads = 1024;
 template <int WT>
-__global__ __launch_bounds__(kThreads) void norm_join_kernel(const float *part, int n, int C, void *dgamma, void *dbeta)
+__global__ __launch_bounds__(kJoinThreads) void norm_join_kernel(const float *part, int n, int C, void *dgamma, void *dbeta)
 {
-    __shared__ float red[kThreads];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, q = blockIdx.x * 64 + lane;
-    float s[4] = {0.f, 0.f, 0.f, 0.f};
-    if (q < 2 * C) {
-        int b = w;
-        for (; b + 12 < n; b += 16)
-#pragma unroll
-            for (int u = 0; u < 4; ++u) s[u] += part[(size_t)(b + 4 * u) * 2 * C + q];
-        for (; b < n; b += 4) s[0] += part[(size_t)b * 2 * C + q];
+    constexpr int RW = kJoinThreads / kJoinCols;
+    __shared__ float red[kJoinThreads / 64][kJoinCols];
+    const int col = threadIdx.x % kJoinCols, w = threadIdx.x / kJoinCols;
+    const long long q = (long long)blockIdx.x * kJoinCols + col;
+    float s = 0.f;
+    if (q < 2LL * C) {
+#pragma unroll 16
+        for (int b = w; b < n; b += RW) s += part[(size_t)b * 2 * C + q];
     }
-    red[threadIdx.x] = (s[0] + s[1]) + (s[2] + s[3]);
+    s += __shfl_xor(s, 16);
+    s += __shfl_xor(s, 32);
+    if ((threadIdx.x & 63) < kJoinCols) red[threadIdx.x >> 6][col] = s;
     __syncthreads();
-    if (w != 0 || q >= 2 * C) return;
-    const float t = (red[lane] + red[64 + lane]) + (red[128 + lane] + red[192 + lane]);
+    if (threadIdx.x >= kJoinCols || q >= 2LL * C) return;
+    float t = 0.f;
+#pragma unroll
+    for (int i = 0; i < kJoinThreads / 64; ++i) t += red[i][col];
     typedef typename NormElem<WT>::t elem_t;
     elem_t *out = static_cast<elem_t *>(q < C ? dgamma : dbeta);
     if (out) out[q < C ? q : q - C] = norm_round<WT>(t);
@@ -604,79 +738,88 @@ __global__ __launch_bounds__(kThreads) void norm_join_kernel(const float *part, 
 
 // ---- launches ------------------------------------------------------------------------------------------------------
 struct NormShape {
-    int G, K;       // rows: lanes a row, vectors a lane (0: read again)
+    int G, K, R;    // rows: lanes a row, vectors a lane (0: read again), rows at once
     int NW;         // planes: waves a workgroup
     int V;
 };
 
-// The smallest group that holds a row with one vector a lane; past a wave, two and four vectors a lane (more would spill the
-// backward pass's sums), then groups of several waves.
-NormShape rows_shape(int dtype, int C)
+// The smallest group that holds a row with one vector a lane; past a wave, two and four vectors a lane, then groups of several
+// waves.  Few vectors a row: several rows at once, so that enough loads are under way.
+NormShape rows_shape(int dtype, int C, bool backward)
 {
     const int V = dtype == XCONV_F32 ? 4 : 8, nv = ceil_div(C, V);
     for (int G : {4, 8, 16, 32, 64})
-        if (nv <= G) return {G, 1, 0, V};
-    if (nv <= 128) return {64, 2, 0, V};
-    if (nv <= 256) return {64, 4, 0, V};
+        if (nv <= G) return {G, 1, backward ? 2 : 4, 0, V};
+    if (nv <= 128) return {64, 2, backward ? 1 : 2, 0, V};
+    if (nv <= 256) return {64, 4, 1, 0, V};
     for (int G : {256, 512, 1024})
-        if (nv <= 2 * G) return {G, 2, 0, V};
-    if (nv <= 4096) return {1024, 4, 0, V};
-    return {1024, 0, 0, V};
+        if (nv <= 2 * G) return {G, 2, 1, 0, V};
+    if (!backward && nv <= 4096) return {1024, 4, 1, 0, V};
+    return {1024, 0, 1, 0, V};
 }
-// 4 channels a wave and round: enough waves for 8 rounds, then 16 rounds in the forward pass (the backward pass holds two tensors)
-NormShape planes_shape(int dtype, int C, bool backward)
+// 8 channels a wave and round: enough waves for 4 rounds, 8 with 16 waves
+NormShape planes_shape(int dtype, int C)
 {
     const int V = dtype == XCONV_F32 ? 4 : 8;
     for (int NW : {4, 8, 16})
-        for (int K : {1, 2, 4, 8})
-            if (C <= 4 * NW * K) return {0, K, NW, V};
-    if (!backward && C <= 1024) return {0, 16, 16, V};
-    return {0, 0, 16, V};
+        for (int K : {1, 2, 4})
+            if (C <= kNormTYW * NW * K) return {0, K, 1, NW, V};
+    if (C <= kNormTYW * 16 * 8) return {0, 8, 1, 16, V};
+    return {0, 0, 1, 16, V};
 }
 
-constexpr long long kNormGrid = 1 << 20;   // most workgroups of the forward pass
-constexpr int kNormBlocks = 1024;   // most workgroups that leave partial sums
+constexpr int kNormBlocks = 1024;           // most workgroups that leave partial sums
+constexpr long long kNormGrid = 1 << 20;    // most workgroups of the forward pass
 
-int bwd_blocks(const xconv_norm_desc *d, const NormShape &s, bool planes)
+long long plane_tiles(const xconv_norm_desc *d, int V) { return (d->outer * ceil_div((int)d->inner, V) + kNormTX - 1) / kNormTX; }
+
+// workgroups of a pass: one piece of work each in the forward pass, of the backward pass at most kNormBlocks
+int norm_blocks(const xconv_norm_desc *d, const NormShape &s, bool bwd)
 {
-    const long long want = planes ? (d->outer * ceil_div((int)d->inner, s.V) + kNormTX - 1) / kNormTX
-                                  : (d->outer + std::max(1, 256 / std::max(1, s.G)) - 1) / std::max(1, 256 / std::max(1, s.G));
-    return (int)std::min<long long>(want, kNormBlocks);
+    const int rows = s.G ? std::max(256, s.G) / s.G * s.R : 1;
+    const long long want = d->inner > 1 ? plane_tiles(d, s.V) : (d->outer + rows - 1) / rows;
+    return (int)std::min<long long>(want, bwd ? kNormBlocks : kNormGrid);
 }
 
-template <int DT, int WT, int G, int K> hipError_t go_rows(const NormArgs &a, bool bwd, int blocks, hipStream_t st)
+template <int DT, int WT, int G, int K, int RF, int RB> hipError_t go_rows(const NormArgs &a, bool bwd, int blocks, hipStream_t st)
 {
-    constexpr int T = G > 256 ? G : 256, RP = T / G;
+    constexpr int T = row_threads<G>, RP = T / G;
     if (!bwd) {
-        const long long grid = (a.outer + RP - 1) / RP;
-        hipLaunchKernelGGL((norm_rows_fwd_kernel<DT, WT, G, K>), dim3((unsigned)std::min<long long>(grid, kNormGrid)), dim3(T), 0, st, a);
-    } else {
+        hipLaunchKernelGGL((norm_rows_fwd_kernel<DT, WT, G, K, RF>), dim3((unsigned)blocks), dim3(T), 0, st, a);
+    } else if constexpr (RB > 0) {
         const size_t lds = RP > 1 && a.part ? (size_t)RP * 2 * G * K * NormElem<DT>::V * 4 : 0;
-        hipLaunchKernelGGL((norm_rows_bwd_kernel<DT, WT, G, K>), dim3((unsigned)blocks), dim3(T), lds, st, a);
+        hipLaunchKernelGGL((norm_rows_bwd_kernel<DT, WT, G, K, RB>), dim3((unsigned)blocks), dim3(T), lds, st, a);
     }
     return hipGetLastError();
 }
+// (rows at once of the two passes as rows_shape says; 0: that shape is not a backward one)
 template <int DT, int WT> hipError_t go_rows_shape(const NormArgs &a, const NormShape &s, bool bwd, int blocks, hipStream_t st)
 {
     switch (s.G * 8 + s.K) {
-    case 4 * 8 + 1: return go_rows<DT, WT, 4, 1>(a, bwd, blocks, st);
-    case 8 * 8 + 1: return go_rows<DT, WT, 8, 1>(a, bwd, blocks, st);
-    case 16 * 8 + 1: return go_rows<DT, WT, 16, 1>(a, bwd, blocks, st);
-    case 32 * 8 + 1: return go_rows<DT, WT, 32, 1>(a, bwd, blocks, st);
-    case 64 * 8 + 1: return go_rows<DT, WT, 64, 1>(a, bwd, blocks, st);
-    case 64 * 8 + 2: return go_rows<DT, WT, 64, 2>(a, bwd, blocks, st);
-    case 64 * 8 + 4: return go_rows<DT, WT, 64, 4>(a, bwd, blocks, st);
-    case 256 * 8 + 2: return go_rows<DT, WT, 256, 2>(a, bwd, blocks, st);
-    case 512 * 8 + 2: return go_rows<DT, WT, 512, 2>(a, bwd, blocks, st);
-    case 1024 * 8 + 2: return go_rows<DT, WT, 1024, 2>(a, bwd, blocks, st);
-    case 1024 * 8 + 4: return go_rows<DT, WT, 1024, 4>(a, bwd, blocks, st);
-    default: return go_rows<DT, WT, 1024, 0>(a, bwd, blocks, st);
+    case 4 * 8 + 1: return go_rows<DT, WT, 4, 1, 4, 2>(a, bwd, blocks, st);
+    case 8 * 8 + 1: return go_rows<DT, WT, 8, 1, 4, 2>(a, bwd, blocks, st);
+    case 16 * 8 + 1: return go_rows<DT, WT, 16, 1, 4, 2>(a, bwd, blocks, st);
+    case 32 * 8 + 1: return go_rows<DT, WT, 32, 1, 4, 2>(a, bwd, blocks, st);
+    case 64 * 8 + 1: return go_rows<DT, WT, 64, 1, 4, 2>(a, bwd, blocks, st);
+    case 64 * 8 + 2: return go_rows<DT, WT, 64, 2, 2, 1>(a, bwd, blocks, st);
+    case 64 * 8 + 4: return go_rows<DT, WT, 64, 4, 1, 1>(a, bwd, blocks, st);
+    case 256 * 8 + 2: return go_rows<DT, WT, 256, 2, 1, 1>(a, bwd, blocks, st);
+    case 512 * 8 + 2: return go_rows<DT, WT, 512, 2, 1, 1>(a, bwd, blocks, st);
+    case 1024 * 8 + 2: return go_rows<DT, WT, 1024, 2, 1, 1>(a, bwd, blocks, st);
+    case 1024 * 8 + 4: return go_rows<DT, WT, 1024, 4, 1, 0>(a, bwd, blocks, st);
+    default: return go_rows<DT, WT, 1024, 0, 1, 1>(a, bwd, blocks, st);
     }
 }
 template <int DT, int WT, int NW, int K> hipError_t go_planes(const NormArgs &a, bool bwd, int blocks, hipStream_t st)
 {
-    if (!bwd) hipLaunchKernelGGL((norm_planes_fwd_kernel<DT, WT, NW, K>), dim3((unsigned)std::min<long long>(a.tiles, kNormGrid)), dim3(NW * 64), 0, st, a);
-    else if constexpr (K <= 8) hipLaunchKernelGGL((norm_planes_bwd_kernel<DT, WT, NW, K>), dim3((unsigned)blocks), dim3(NW * 64), 0, st, a);
+    const dim3 grid((unsigned)blocks), block(NW * 64);
+    if (a.exact) {
+        if (!bwd) hipLaunchKernelGGL((norm_planes_fwd_kernel<DT, WT, NW, K, false>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((norm_planes_bwd_kernel<DT, WT, NW, K, false>), grid, block, 0, st, a);
+    } else {
+        if (!bwd) hipLaunchKernelGGL((norm_planes_fwd_kernel<DT, WT, NW, K, true>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((norm_planes_bwd_kernel<DT, WT, NW, K, true>), grid, block, 0, st, a);
+    }
     return hipGetLastError();
 }
 template <int DT, int WT> hipError_t go_planes_shape(const NormArgs &a, const NormShape &s, bool bwd, int blocks, hipStream_t st)
@@ -685,18 +828,28 @@ template <int DT, int WT> hipError_t go_planes_shape(const NormArgs &a, const No
     case 4 * 32 + 1: return go_planes<DT, WT, 4, 1>(a, bwd, blocks, st);
     case 4 * 32 + 2: return go_planes<DT, WT, 4, 2>(a, bwd, blocks, st);
     case 4 * 32 + 4: return go_planes<DT, WT, 4, 4>(a, bwd, blocks, st);
-    case 4 * 32 + 8: return go_planes<DT, WT, 4, 8>(a, bwd, blocks, st);
-    case 8 * 32 + 8: return go_planes<DT, WT, 8, 8>(a, bwd, blocks, st);
+    case 8 * 32 + 4: return go_planes<DT, WT, 8, 4>(a, bwd, blocks, st);
+    case 16 * 32 + 4: return go_planes<DT, WT, 16, 4>(a, bwd, blocks, st);
     case 16 * 32 + 8: return go_planes<DT, WT, 16, 8>(a, bwd, blocks, st);
-    case 16 * 32 + 16: return go_planes<DT, WT, 16, 16>(a, bwd, blocks, st);
     default: return go_planes<DT, WT, 16, 0>(a, bwd, blocks, st);
     }
+}
+
+bool overlap(const void *a, const void *b, size_t bytes)
+{
+    const uintptr_t p = reinterpret_cast<uintptr_t>(a), q = reinterpret_cast<uintptr_t>(b);
+    return a && b && p < q + bytes && q < p + bytes;
 }
 
 template <int DT, int WT> hipError_t launch_norm_dt(const xconv_norm_desc *d, NormArgs a, bool bwd, void *dgamma, void *dbeta, hipStream_t st)
 {
     const bool planes = d->inner > 1;
-    const NormShape s = planes ? planes_shape(DT, d->C, bwd) : rows_shape(DT, d->C);
+    constexpr int V = NormElem<DT>::V;
+    // outputs over inputs: the overlapping part of a plane may be another workgroup's, that of a row read again another lane's
+    const size_t bytes = (size_t)d->outer * d->C * d->inner * (DT == XCONV_F32 ? 4 : 2);
+    const bool over = overlap(a.y, a.x, bytes) || overlap(a.y, a.dy, bytes);
+    const NormShape s = planes ? planes_shape(DT, d->C) : rows_shape(DT, d->C, bwd);
+    a.exact = planes ? over || d->inner < V : d->C < V || (s.K == 0 && over);
     a.outer = d->outer;
     a.C = d->C;
     a.inner = (int)d->inner;
@@ -704,12 +857,12 @@ template <int DT, int WT> hipError_t launch_norm_dt(const xconv_norm_desc *d, No
     a.count = (float)d->C;
     a.inv_c = 1.0f / a.count;
     a.nvi = ceil_div((int)d->inner, s.V);
-    a.tiles = (d->outer * a.nvi + kNormTX - 1) / kNormTX;
-    const int blocks = bwd ? bwd_blocks(d, s, planes) : 0;
+    a.tiles = plane_tiles(d, s.V);
+    const int blocks = norm_blocks(d, s, bwd);
     hipError_t e = hipSuccess;
     if (d->outer > 0) e = planes ? go_planes_shape<DT, WT>(a, s, bwd, blocks, st) : go_rows_shape<DT, WT>(a, s, bwd, blocks, st);
-    if (e != hipSuccess || !a.part) return e;
-    hipLaunchKernelGGL(norm_join_kernel<WT>, dim3((unsigned)ceil_div(2 * d->C, 64)), dim3(kThreads), 0, st, a.part, blocks, d->C, dgamma, dbeta);
+    if (e != hipSuccess || !bwd || !(dgamma || dbeta)) return e;
+    hipLaunchKernelGGL(norm_join_kernel<WT>, dim3((unsigned)ceil_div(2 * d->C, kJoinCols)), dim3(kJoinThreads), 0, st, a.part, blocks, d->C, dgamma, dbeta);
     return hipGetLastError();
 }
 
@@ -727,8 +880,8 @@ hipError_t launch_norm(const xconv_norm_desc *d, const NormArgs &a, bool bwd, vo
 size_t norm_ws_bytes(const xconv_norm_desc *d)
 {
     const bool planes = d->inner > 1;
-    const NormShape s = planes ? planes_shape(d->dtype, d->C, true) : rows_shape(d->dtype, d->C);
-    return (size_t)bwd_blocks(d, s, planes) * 2 * d->C * sizeof(float);
+    const NormShape s = planes ? planes_shape(d->dtype, d->C) : rows_shape(d->dtype, d->C, true);
+    return (size_t)norm_blocks(d, s, true) * 2 * d->C * sizeof(float);
 }
 
 hipError_t launch_norm_fwd(const xconv_norm_desc *d, const void *X, const void *gamma, const void *beta, void *Y, float *mean, float *rstd, hipStream_t st)
