@@ -59,6 +59,7 @@ struct NormArgs {
     float eps, inv_c, count;   // count = C, inv_c = 1 / C
     int nvi;              // vectors a plane
     long long tiles;      // tiles of kNormTX vectors of positions (planes)
+    int ragged;           // rows (planes) are no whole number of vectors: values that are not a vector's own are masked
     int exact;            // last vectors do not overlap (shorter than a vector; outputs over inputs that are read again)
 };
 
@@ -126,6 +127,7 @@ template <int DT> __device__ inline uint4 pack(const float (&x)[NormElem<DT>::V]
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         if constexpr (DT == XCONV_F32) w[i] = __float_as_uint(x[i]);
+        else if constexpr (DT == XCONV_BF16) w[i] = bf16_pair(x[2 * i], x[2 * i + 1]);
         else w[i] = (uint32_t)f32_to_st16<DT>(x[2 * i]) | (uint32_t)f32_to_st16<DT>(x[2 * i + 1]) << 16;
     }
     return uint4{w[0], w[1], w[2], w[3]};
@@ -245,8 +247,13 @@ __global__ __launch_bounds__(row_threads<G>) void norm_rows_fwd_kernel(NormArgs 
             for (int r = 0; r < R; ++r) {
                 float t[V];
                 unpack<DT>(value(r, k, p), t);
+                if (!a.ragged) {
 #pragma unroll
-                for (int i = 0; i < V; ++i) s[r] += v < nv && own(p, i) ? t[i] : 0.f;
+                    for (int i = 0; i < V; ++i) s[r] += t[i];       // (zeros past the last vector)
+                } else {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) s[r] += v < nv && own(p, i) ? t[i] : 0.f;
+                }
             }
         });
         group_sum<G>(s, red, turn);
@@ -261,11 +268,18 @@ __global__ __launch_bounds__(row_threads<G>) void norm_rows_fwd_kernel(NormArgs 
             for (int r = 0; r < R; ++r) {
                 float t[V];
                 unpack<DT>(value(r, k, p), t);
+                float q = 0.f;
+                if (!a.ragged) {
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float d = v < nv && own(p, i) ? t[i] - mean[r] : 0.f;
-                    s[r] += d * d;
+                    for (int i = 0; i < V; ++i) q += (t[i] - mean[r]) * (t[i] - mean[r]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        const float d = own(p, i) ? t[i] - mean[r] : 0.f;
+                        q += d * d;
+                    }
                 }
+                s[r] += v < nv ? q : 0.f;
             }
         });
         group_sum<G>(s, red, turn);
@@ -336,8 +350,8 @@ __global__ __launch_bounds__(row_threads<G>) void norm_rows_bwd_kernel(NormArgs 
             const long long row = r0 + r * RP + grp;
             on[r] = row < a.outer;
             at[r] = (size_t)(on[r] ? row : 0) * a.C;
-            mean[r] = a.mean[on[r] ? row : 0];
-            rstd[r] = a.rstd[on[r] ? row : 0];
+            mean[r] = on[r] ? a.mean[row] : 0.f;
+            rstd[r] = on[r] ? a.rstd[row] : 0.f;
             c[2 * r] = c[2 * r + 1] = 0.f;
         }
         auto get = [&](int r, int k, int v, const Part &p) {
@@ -366,19 +380,27 @@ __global__ __launch_bounds__(row_threads<G>) void norm_rows_bwd_kernel(NormArgs 
                 float x[V], d[V];
                 unpack<DT>(rx[r][k], x);
                 unpack<DT>(rd[r][k], d);
+                // (rows and vectors that do not exist are zeros with statistics of zero, or columns that nobody reads)
+                if (a.ragged) {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        const bool mine = on[r] && v < nv && own(p, i);
+                        x[i] = mine ? x[i] : mean[r];
+                        d[i] = mine ? d[i] : 0.f;
+                    }
+                }
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    const bool mine = on[r] && v < nv && own(p, i);
-                    const float xh = mine ? (x[i] - mean[r]) * rstd[r] : 0.f, di = mine ? d[i] : 0.f, gd = di * g[i];
-                    c[2 * r] += gd;
-                    c[2 * r + 1] += gd * xh;
+                    const float t = d[i] * ((x[i] - mean[r]) * rstd[r]);
+                    c[2 * r] += d[i] * g[i];
+                    c[2 * r + 1] += t * g[i];
                     if constexpr (K > 0) {
-                        ag[k][i] += di * xh;
-                        ab[k][i] += di;
-                    } else if (part && mine) {
+                        ag[k][i] += t;
+                        ab[k][i] += d[i];
+                    } else if (part && (!a.ragged || own(p, i))) {
                         float *pg = part + p.at + i, *pb = pg + a.C;
-                        *pg = (first ? 0.f : *pg) + di * xh;
-                        *pb = (first ? 0.f : *pb) + di;
+                        *pg = (first ? 0.f : *pg) + t;
+                        *pb = (first ? 0.f : *pb) + d[i];
                     }
                 }
                 if constexpr (K > 1) {
@@ -398,12 +420,12 @@ __global__ __launch_bounds__(row_threads<G>) void norm_rows_bwd_kernel(NormArgs 
             for (int r = 0; r < R; ++r) {
                 if (!on[r]) continue;
                 if constexpr (K == 0) get(r, k, v, p);
-                const float c1 = c[2 * r] * a.inv_c, c2 = c[2 * r + 1] * a.inv_c;
+                const float c1 = c[2 * r] * a.inv_c * rstd[r], c2 = c[2 * r + 1] * a.inv_c * rstd[r] * rstd[r];
                 float x[V], d[V];
                 unpack<DT>(rx[r][k], x);
                 unpack<DT>(rd[r][k], d);
 #pragma unroll
-                for (int i = 0; i < V; ++i) x[i] = rstd[r] * (d[i] * g[i] - c1 - (x[i] - mean[r]) * rstd[r] * c2);
+                for (int i = 0; i < V; ++i) x[i] = (d[i] * (g[i] * rstd[r]) - c1) - (x[i] - mean[r]) * c2;
                 store_part<DT>(DX + at[r], pack<DT>(x), p);
             }
         });
@@ -559,10 +581,7 @@ __global__ __launch_bounds__(NW * 64) void norm_planes_fwd_kernel(NormArgs a)
             float t[V];
             unpack<DT>(value(k, c), t);
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float d = c < a.C ? t[i] - mean[i] : 0.f;
-                s[i] += d * d;
-            }
+            for (int i = 0; i < V; ++i) s[i] += c < a.C ? (t[i] - mean[i]) * (t[i] - mean[i]) : 0.f;
             if constexpr (K > 0) keep_packed(raw[k], s);
         });
         column_sum<V, NW>(s, red);
@@ -590,7 +609,7 @@ __global__ __launch_bounds__(NW * 64) void norm_planes_fwd_kernel(NormArgs a)
 }
 
 template <int DT, int WT, int NW, int K, bool WHOLE>
-__global__ __launch_bounds__(NW * 64) void norm_planes_bwd_kernel(NormArgs a)
+__global__ __launch_bounds__(NW * 64, 4) void norm_planes_bwd_kernel(NormArgs a)
 {
     typedef typename NormElem<DT>::t elem_t;
     constexpr int V = NormElem<DT>::V, TY = NW * kNormTYW, KR = K > 0 ? K : 1;
@@ -648,13 +667,24 @@ __global__ __launch_bounds__(NW * 64) void norm_planes_bwd_kernel(NormArgs a)
             unpack<DT>(rx[k], x);
             unpack<DT>(rd[k], d);
             const float g = K > 0 ? gk[k] : load_param<WT>(a.gamma, c, 1.f);
+            if (!a.ragged) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float xh = (x[i] - mean[i]) * rstd[i], gd = d[i] * g;
-                c12[i] += gd;
-                c12[V + i] += gd * xh;
-                sg += i >= at.p.lo ? d[i] * xh : 0.f;
-                sb += i >= at.p.lo ? d[i] : 0.f;
+                for (int i = 0; i < V; ++i) {
+                    const float t = d[i] * ((x[i] - mean[i]) * rstd[i]);
+                    c12[i] += d[i] * g;
+                    c12[V + i] += t * g;
+                    sg += t;
+                    sb += d[i];
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const float t = d[i] * ((x[i] - mean[i]) * rstd[i]);
+                    c12[i] += d[i] * g;
+                    c12[V + i] += t * g;
+                    sg += i >= at.p.lo ? t : 0.f;
+                    sb += i >= at.p.lo ? d[i] : 0.f;
+                }
             }
             if constexpr (K > 0) {
                 ag[k] += sg;
@@ -678,7 +708,10 @@ __global__ __launch_bounds__(NW * 64) void norm_planes_bwd_kernel(NormArgs a)
         column_sum<2 * V, NW>(c12, red);
         if (!at.on) continue;
 #pragma unroll
-        for (int i = 0; i < 2 * V; ++i) c12[i] *= a.inv_c;
+        for (int i = 0; i < V; ++i) {
+            c12[i] *= a.inv_c * rstd[i];
+            c12[V + i] *= a.inv_c * rstd[i] * rstd[i];
+        }
         rounds([&](int k, int c) {
             if (c >= a.C) return;
             if constexpr (K == 0) {
@@ -690,7 +723,7 @@ __global__ __launch_bounds__(NW * 64) void norm_planes_bwd_kernel(NormArgs a)
             unpack<DT>(rd[k], d);
             const float g = K > 0 ? gk[k] : load_param<WT>(a.gamma, c, 1.f);
 #pragma unroll
-            for (int i = 0; i < V; ++i) x[i] = rstd[i] * (d[i] * g - c12[i] - (x[i] - mean[i]) * rstd[i] * c12[V + i]);
+            for (int i = 0; i < V; ++i) x[i] = (d[i] * (g * rstd[i]) - c12[i]) - (x[i] - mean[i]) * c12[V + i];
             plane_put<DT, WHOLE>(a, DX + at.base, at, c, pack<DT>(x));
         });
     }
@@ -753,8 +786,8 @@ NormShape rows_shape(int dtype, int C, bool backward)
     if (nv <= 128) return {64, 2, backward ? 1 : 2, 0, V};
     if (nv <= 256) return {64, 4, 1, 0, V};
     for (int G : {256, 512, 1024})
-        if (nv <= 2 * G) return {G, 2, 1, 0, V};
-    if (!backward && nv <= 4096) return {1024, 4, 1, 0, V};
+        for (int K : {2, 3, 4})
+            if (nv <= K * G && (G == 256 || K > 2) && !(backward && G == 1024 && K > 3)) return {G, K, 1, 0, V};
     return {1024, 0, 1, 0, V};
 }
 // 8 channels a wave and round: enough waves for 4 rounds, 8 with 16 waves
@@ -804,8 +837,11 @@ template <int DT, int WT> hipError_t go_rows_shape(const NormArgs &a, const Norm
     case 64 * 8 + 2: return go_rows<DT, WT, 64, 2, 2, 1>(a, bwd, blocks, st);
     case 64 * 8 + 4: return go_rows<DT, WT, 64, 4, 1, 1>(a, bwd, blocks, st);
     case 256 * 8 + 2: return go_rows<DT, WT, 256, 2, 1, 1>(a, bwd, blocks, st);
-    case 512 * 8 + 2: return go_rows<DT, WT, 512, 2, 1, 1>(a, bwd, blocks, st);
-    case 1024 * 8 + 2: return go_rows<DT, WT, 1024, 2, 1, 1>(a, bwd, blocks, st);
+    case 256 * 8 + 3: return go_rows<DT, WT, 256, 3, 1, 1>(a, bwd, blocks, st);
+    case 256 * 8 + 4: return go_rows<DT, WT, 256, 4, 1, 1>(a, bwd, blocks, st);
+    case 512 * 8 + 3: return go_rows<DT, WT, 512, 3, 1, 1>(a, bwd, blocks, st);
+    case 512 * 8 + 4: return go_rows<DT, WT, 512, 4, 1, 1>(a, bwd, blocks, st);
+    case 1024 * 8 + 3: return go_rows<DT, WT, 1024, 3, 1, 1>(a, bwd, blocks, st);
     case 1024 * 8 + 4: return go_rows<DT, WT, 1024, 4, 1, 0>(a, bwd, blocks, st);
     default: return go_rows<DT, WT, 1024, 0, 1, 1>(a, bwd, blocks, st);
     }
@@ -849,6 +885,7 @@ template <int DT, int WT> hipError_t launch_norm_dt(const xconv_norm_desc *d, No
     const size_t bytes = (size_t)d->outer * d->C * d->inner * (DT == XCONV_F32 ? 4 : 2);
     const bool over = overlap(a.y, a.x, bytes) || overlap(a.y, a.dy, bytes);
     const NormShape s = planes ? planes_shape(DT, d->C) : rows_shape(DT, d->C, bwd);
+    a.ragged = (planes ? d->inner : (int64_t)d->C) % V != 0;
     a.exact = planes ? over || d->inner < V : d->C < V || (s.K == 0 && over);
     a.outer = d->outer;
     a.C = d->C;
