@@ -25,7 +25,7 @@ namespace xc {
 namespace {
 
 constexpr float kOrthScale = 4096.f, kOrthUnscale = 1.f / (4096.f * 4096.f);
-constexpr int kOrthItems = 20;      // matrices of one launch (as many as kernel arguments hold)
+constexpr int kOrthItems = 24;      // matrices of one launch (as many as kernel arguments hold)
 constexpr int kOrthTile = 64;       // extents are padded to this or twice this
 constexpr int kOrthNorms = 512;     // most partial sums of a matrix' squares
 constexpr int kBlockHalfs = 1024;   // 32 x 16 values, both numbers
@@ -43,11 +43,9 @@ struct OrthMat {
     double *sq;                         // partial sums of squares
     float *part;                        // partial products of X X^T, [tile][split][tile values]
     int rows, cols, m, n, mp, np;       // m <= n
-    int first[4];                       // first workgroup in launches over elements, tiles of A, tiles of X, 64 x 64 tiles of X
     int nsq;
-    int big;                            // tiles of 128 x 128 (else 64 x 64)
-    int splits, kbs;                    // X X^T: runs of kbs blocks of 16 columns
-    int gfirst, jfirst;                 // first workgroup in the launch of X X^T and of the one that joins it
+    int big_a, big_x;                   // tiles of 128 x 128 (else 64 x 64) of A and P, of X
+    int gsplits, gkbs, psplits, pkbs;   // X X^T and A A: runs of blocks of 16 along the sum, and their length
     float wscale;                       // lr sqrt(max(1, rows / cols))
 };
 struct OrthScalars {
@@ -56,26 +54,29 @@ struct OrthScalars {
 };
 struct OrthList {
     OrthScalars s;
+    int first[kOrthItems];
     OrthMat mat[kOrthItems];
 };
 static_assert(sizeof(OrthList) <= 4096, "kernel arguments");
 // What the launches after the first are given: the list lies in the scratch
 struct OrthRef {
     OrthScalars s;
+    int total;                          // workgroups that have work
+    int first[kOrthItems];              // each matrix' first workgroup
     const OrthMat *mat;
 };
 
-// the matrix of workgroup b in a launch whose first workgroups are `first`; b becomes the workgroup's number in the matrix
-template <class F> __device__ inline const OrthMat &find_mat(const OrthMat *mat, int count, F &&first, int &b)
+// which matrix workgroup b belongs to (one without workgroups starts where the next one does); b becomes its number in there
+__device__ inline int find_mat(const int *first, int count, int &b)
 {
     int lo = 0, hi = count - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
-        if (first(mat[mid]) <= b) lo = mid;
+        if (first[mid] <= b) lo = mid;
         else hi = mid - 1;
     }
-    b -= first(mat[lo]);
-    return mat[lo];
+    b -= first[lo];
+    return lo;
 }
 
 __device__ inline float orth_get(const void *p, int dtype, size_t i)
@@ -88,6 +89,42 @@ __device__ inline void orth_put(void *p, int dtype, size_t i, float v)
 {
     if (dtype == XCONV_F32) static_cast<float *>(p)[i] = v;
     else static_cast<uint16_t *>(p)[i] = dtype == XCONV_BF16 ? f32_to_bf16_rne(v) : f32_to_f16_rne(v);
+}
+// N values whose places `at(k)` gives, zero where it is negative: one branch on the type for all of them, so that the loads go
+// out together
+__device__ inline float half_value(uint16_t h, bool bf) { return bf ? bf16_to_f32(h) : f16_to_f32(h); }
+template <int N, class At> __device__ inline void orth_gather(const void *p, int dtype, At &&at, float (&v)[N])
+{
+    if (dtype == XCONV_F32) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const long long i = at(k);
+            v[k] = static_cast<const float *>(p)[i < 0 ? 0 : i];
+        }
+    } else {
+        uint16_t h[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const long long i = at(k);
+            h[k] = static_cast<const uint16_t *>(p)[i < 0 ? 0 : i];
+        }
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] = half_value(h[k], dtype == XCONV_BF16);
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = at(k) < 0 ? 0.f : v[k];
+}
+template <int N, class At> __device__ inline void orth_scatter(void *p, int dtype, At &&at, const float (&v)[N])
+{
+    if (dtype == XCONV_F32) {
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+            if (at(k) >= 0) static_cast<float *>(p)[at(k)] = v[k];
+    } else {
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+            if (at(k) >= 0) static_cast<uint16_t *>(p)[at(k)] = dtype == XCONV_BF16 ? f32_to_bf16_rne(v[k]) : f32_to_f16_rne(v[k]);
+    }
 }
 __device__ inline float update_of(float g, float m, const OrthScalars &L) { return L.nesterov ? g + L.mu * (m - g) : m; }
 
@@ -135,7 +172,7 @@ __global__ __launch_bounds__(kThreads) void orth_norm_kernel(OrthList L, OrthMat
         uint32_t *to = reinterpret_cast<uint32_t *>(list);
         for (int i = threadIdx.x; i < (int)(L.s.count * sizeof(OrthMat) / 4); i += kThreads) to[i] = from[i];
     }
-    const OrthMat &q = find_mat(L.mat, L.s.count, [](const OrthMat &m) { return m.first[0]; }, b);
+    const OrthMat &q = L.mat[find_mat(L.first, L.s.count, b)];
     const size_t n = (size_t)q.rows * q.cols, step = (size_t)q.nsq * kThreads * 4;
     double s = 0.0;
     for (size_t i = ((size_t)b * kThreads + threadIdx.x) * 4; i < n; i += step) {
@@ -215,32 +252,30 @@ __global__ __launch_bounds__(kThreads) void orth_start_kernel(OrthRef L)
 {
     __shared__ float t[kOrthTile][kOrthTile + 1];
     int b = blockIdx.x;
-    const OrthMat &q = find_mat(L.mat, L.s.count, [](const OrthMat &m) { return m.first[3]; }, b);
+    const OrthMat &q = L.mat[find_mat(L.first, L.s.count, b)];
     const TileAt at = tile_at<kOrthTile, kOrthTile>(q, b);
-    const double norm = sqrt(sum_squares(q)), d = norm < (double)L.s.eps ? (double)L.s.eps : norm;      // (a NaN stays one)
-    const double inv = d == 0.0 ? 0.0 : 1.0 / d;                                                         // (eps = 0 and a zero matrix)
     const bool tall = q.rows > q.cols;
     const int r0 = tall ? at.n0 : at.m0, c0 = tall ? at.m0 : at.n0;
-    constexpr int kRound = 4;
+    constexpr int kRound = 16;
+    float v[kRound], m[kRound];
+    auto place = [&](int k) -> long long {
+        const int u = k * kThreads + threadIdx.x, r = r0 + u / kOrthTile, c = c0 + u % kOrthTile;
+        return r < q.rows && c < q.cols ? (long long)r * q.cols + c : -1;
+    };
+    orth_gather(q.G, L.s.g_dtype, place, v);
+    if (L.s.muon) {
+        orth_gather(q.M, XCONV_F32, place, m);
 #pragma unroll
-    for (int j = 0; j < kOrthTile * kOrthTile / kThreads; j += kRound) {
-        float v[kRound], m[kRound];
+        for (int k = 0; k < kRound; ++k) v[k] = update_of(v[k], m[k], L.s);
+    }
+    const double norm = sqrt(sum_squares(q)), d = norm < (double)L.s.eps ? (double)L.s.eps : norm;      // (a NaN stays one)
+    const double inv = d == 0.0 ? 0.0 : 1.0 / d;                                                         // (eps = 0 and a zero matrix)
 #pragma unroll
-        for (int k = 0; k < kRound; ++k) {
-            const int u = (j + k) * kThreads + threadIdx.x, r = r0 + u / kOrthTile, c = c0 + u % kOrthTile;
-            const bool on = r < q.rows && c < q.cols;
-            const size_t i = (size_t)r * q.cols + c;
-            v[k] = on ? orth_get(q.G, L.s.g_dtype, i) : 0.f;
-            m[k] = on && L.s.muon ? q.M[i] : 0.f;
-        }
-#pragma unroll
-        for (int k = 0; k < kRound; ++k) {
-            const int u = (j + k) * kThreads + threadIdx.x, r = u / kOrthTile, c = u % kOrthTile;
-            if (L.s.muon) v[k] = update_of(v[k], m[k], L.s);
-            const float x = r0 + r < q.rows && c0 + c < q.cols ? (float)((double)v[k] * inv) : 0.f;
-            if (tall) t[c][r] = x;
-            else t[r][c] = x;
-        }
+    for (int k = 0; k < kRound; ++k) {
+        const int u = k * kThreads + threadIdx.x, r = u / kOrthTile, c = u % kOrthTile;
+        const float x = place(k) >= 0 ? (float)((double)v[k] * inv) : 0.f;
+        if (tall) t[c][r] = x;
+        else t[r][c] = x;
     }
     __syncthreads();
     emit_x<kOrthTile, kOrthTile>(t, q, q.Xt, at.m0, at.n0);
@@ -383,17 +418,21 @@ __device__ inline void pair_of(int b, int &i, int &j)
     i = b - j * (j + 1) / 2;
 }
 
-// t is tile (i0, j0) of A = X X^T (POLY = 0; also kept as plain floats) or of A A (1; becomes P = a I + b A + c A A): stored on
-// both sides of the diagonal
-template <int T, int POLY> __device__ inline void put_square(float (*t)[T + 1], const OrthMat &q, const OrthScalars &s, int i0, int j0)
+// t is part of A = X X^T (POLY = 0; also kept as plain floats) or of A A (1; becomes P = a I + b A + c A A).  Its rows are i0 on
+// and its columns j0 on (STEP = 32), or, when it is the part (i, j) of a tile of 128, every other run of 32 of them (STEP = 64).
+// What lies on and above the diagonal blocks of 32 x 32 is stored on both sides of the diagonal, so that A and P are symmetric
+// to the last bit whatever the tiles.
+template <int T, int POLY, int STEP> __device__ inline void put_square(float (*t)[T + 1], const OrthMat &q, const OrthScalars &s, int i0, int j0)
 {
     _Float16 *out = POLY ? q.P : q.A;
+    auto along = [](int from, int r) { return from + STEP * (r >> 5) + (r & 31); };
     for (int u = threadIdx.x; u < T * T; u += kThreads) {
-        const int r = u / T, c = u % T;
-        float *p = q.A32 + (size_t)(i0 + r) * q.mp + j0 + c;
+        const int r = u / T, c = u % T, row = along(i0, r), col = along(j0, c);
+        if (row >> 5 > col >> 5) continue;
+        float *p = q.A32 + (size_t)row * q.mp + col;
         if constexpr (POLY == 1) {
             float v = s.b * *p + s.c * t[r][c];
-            if (i0 + r == j0 + c && i0 + r < q.m) v += s.a;
+            if (row == col && row < q.m) v += s.a;
             t[r][c] = v;
         } else {
             *p = t[r][c];
@@ -402,80 +441,70 @@ template <int T, int POLY> __device__ inline void put_square(float (*t)[T + 1], 
     __syncthreads();
     for (int u = threadIdx.x; u < T * T / 8; u += kThreads) {
         const int r = u % T, c = u / T * 8;
-        float v[8], w[8];
+        float v[8];
+        {
+            const int row = along(i0, r), col = along(j0, c);
+            const bool diagonal = row >> 5 == col >> 5;
+            if (row >> 5 <= col >> 5) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            v[i] = t[r][c + i];
-            w[i] = t[c + i][r];
+                for (int i = 0; i < 8; ++i) v[i] = diagonal && (c + i & 31) < (r & 31) ? t[(r & ~31) + (c + i & 31)][(c & ~31) + (r & 31)] : t[r][c + i];
+                put_pieces(out, row, col, q.mp / 16, v);
+            }
         }
-        put_pieces(out, i0 + r, j0 + c, q.mp / 16, v);
-        if (i0 != j0) put_pieces(out, j0 + r, i0 + c, q.mp / 16, w);
+        {
+            // (r runs along the columns here)
+            const int row = along(i0, c), col = along(j0, r);
+            if (row >> 5 < col >> 5) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = t[c + i][r];
+                put_pieces(out, col, row, q.mp / 16, v);
+            }
+        }
     }
 }
 
-template <int T> __device__ inline void gram_tile(const OrthMat &q, const OrthScalars &s, int b, OrthLds &lds)
+// POLY 0: a tile of X X^T, 1: of A A; b: number of the pair of rows of tiles and of the run along the sum
+template <int T, int POLY> __device__ inline void square_tile(const OrthMat &q, const OrthScalars &s, int b, OrthLds &lds)
 {
-    const int split = b % q.splits, pair = b / q.splits;
+    const int splits = POLY ? q.psplits : q.gsplits, run = POLY ? q.pkbs : q.gkbs, kblocks = (POLY ? q.mp : q.np) / 16;
+    const int split = b % splits, pair = b / splits;
+    const _Float16 *F = POLY ? q.A : q.X;
     int ti, tj;
     pair_of(pair, ti, tj);
     Tile<T / 64, T / 64> t;
-    const int kblocks = q.np / 16, kb0 = split * q.kbs, kb1 = min(kblocks, kb0 + q.kbs);
-    t.product(q.X, ti * T, q.X, tj * T, kblocks, kb0, kb1, lds.stage);
-    if (q.splits > 1) {
+    t.product(F, ti * T, F, tj * T, kblocks, split * run, min(kblocks, (split + 1) * run), lds.stage);
+    if (splits > 1) {
         t.put_part(q.part + (size_t)b * T * T);
         return;
     }
     t.spread(tile_of<T>(lds));
-    put_square<T, 0>(tile_of<T>(lds), q, s, ti * T, tj * T);
+    put_square<T, POLY, 32>(tile_of<T>(lds), q, s, ti * T, tj * T);
 }
-__global__ __launch_bounds__(kThreads, 2) void orth_gram_kernel(OrthRef L, int total)
+template <int POLY> __global__ __launch_bounds__(kThreads, 2) void orth_square_kernel(OrthRef L)
 {
     __shared__ OrthLds lds;
     int b = xcd_block(blockIdx.x, gridDim.x);
-    if (b >= total) return;
-    const OrthMat &q = find_mat(L.mat, L.s.count, [](const OrthMat &m) { return m.gfirst; }, b);
-    if (q.big) gram_tile<128>(q, L.s, b, lds);
-    else gram_tile<64>(q, L.s, b, lds);
+    if (b >= L.total) return;
+    const OrthMat &q = L.mat[find_mat(L.first, L.s.count, b)];
+    if (q.big_a) square_tile<128, POLY>(q, L.s, b, lds);
+    else square_tile<64, POLY>(q, L.s, b, lds);
 }
 
-// adds up the runs of X X^T of the matrices that were split, in order
-template <int T> __device__ inline void join_tile(const OrthMat &q, const OrthScalars &s, int pair, OrthLds &lds)
+// adds up the runs of a product, in order: 64 x 64 values a workgroup
+template <int POLY> __global__ __launch_bounds__(kThreads) void orth_join_kernel(OrthRef L)
 {
+    __shared__ float t[64][64 + 1];
+    int b = blockIdx.x;
+    const OrthMat &q = L.mat[find_mat(L.first, L.s.count, b)];
+    const int splits = POLY ? q.psplits : q.gsplits, parts = q.big_a ? 4 : 1, pair = b / parts, part = b % parts;
     int ti, tj;
     pair_of(pair, ti, tj);
-    Tile<T / 64, T / 64> t;
-    t.clear();
-    for (int k = 0; k < q.splits; ++k) t.add_part(q.part + ((size_t)pair * q.splits + k) * T * T);
-    t.spread(tile_of<T>(lds));
-    put_square<T, 0>(tile_of<T>(lds), q, s, ti * T, tj * T);
-}
-__global__ __launch_bounds__(kThreads, 2) void orth_join_kernel(OrthRef L)
-{
-    __shared__ OrthLds lds;
-    int b = blockIdx.x;
-    // (a matrix that was not split has no workgroups here: its first is the next one's)
-    const OrthMat &q = find_mat(L.mat, L.s.count, [](const OrthMat &m) { return m.jfirst; }, b);
-    if (q.big) join_tile<128>(q, L.s, b, lds);
-    else join_tile<64>(q, L.s, b, lds);
-}
-
-template <int T> __device__ inline void poly_tile(const OrthMat &q, const OrthScalars &s, int b, OrthLds &lds)
-{
-    int ti, tj;
-    pair_of(b, ti, tj);
-    Tile<T / 64, T / 64> t;
-    t.product(q.A, ti * T, q.A, tj * T, q.mp / 16, 0, q.mp / 16, lds.stage);
-    t.spread(tile_of<T>(lds));
-    put_square<T, 1>(tile_of<T>(lds), q, s, ti * T, tj * T);
-}
-__global__ __launch_bounds__(kThreads, 2) void orth_poly_kernel(OrthRef L, int total)
-{
-    __shared__ OrthLds lds;
-    int b = xcd_block(blockIdx.x, gridDim.x);
-    if (b >= total) return;
-    const OrthMat &q = find_mat(L.mat, L.s.count, [](const OrthMat &m) { return m.first[1]; }, b);
-    if (q.big) poly_tile<128>(q, L.s, b, lds);
-    else poly_tile<64>(q, L.s, b, lds);
+    Tile<1, 1> sum;
+    sum.clear();
+    for (int k = 0; k < splits; ++k) sum.add_part(q.part + ((size_t)(pair * splits + k) * parts + part) * 64 * 64);
+    sum.spread(t);
+    if (q.big_a) put_square<64, POLY, 64>(t, q, L.s, ti * 128 + 32 * (part >> 1), tj * 128 + 32 * (part & 1));
+    else put_square<64, POLY, 32>(t, q, L.s, ti * 64, tj * 64);
 }
 
 // t, part (m0, n0) of the result of the last step, becomes O or the update of W
@@ -483,13 +512,21 @@ template <int T> __device__ inline void finish(const float (*t)[T + 1], const Or
 {
     const bool tall = q.rows > q.cols;
     const int r0 = tall ? n0 : m0, c0 = tall ? m0 : n0;
-    for (int u = threadIdx.x; u < T * T; u += kThreads) {
-        const int r = u / T, c = u % T;
-        if (r0 + r >= q.rows || c0 + c >= q.cols) continue;
-        const size_t i = (size_t)(r0 + r) * q.cols + c0 + c;
-        float v = tall ? t[c][r] : t[r][c];
-        if (s.muon) v = orth_get(q.out, s.out_dtype, i) * s.keep - q.wscale * v;
-        orth_put(q.out, s.out_dtype, i, v);
+    constexpr int kRound = 16;
+    for (int base = threadIdx.x; base < T * T; base += kRound * kThreads) {
+        auto place = [&](int k) -> long long {
+            const int u = base + k * kThreads, r = r0 + u / T, c = c0 + u % T;
+            return r < q.rows && c < q.cols ? (long long)r * q.cols + c : -1;
+        };
+        float v[kRound];
+        if (s.muon) orth_gather(q.out, s.out_dtype, place, v);
+#pragma unroll
+        for (int k = 0; k < kRound; ++k) {
+            const int u = base + k * kThreads, r = u / T, c = u % T;
+            const float x = tall ? t[c][r] : t[r][c];
+            v[k] = s.muon ? v[k] * s.keep - q.wscale * x : x;
+        }
+        orth_scatter(q.out, s.out_dtype, place, v);
     }
 }
 
@@ -503,13 +540,13 @@ template <int T> __device__ inline void apply_tile(const OrthMat &q, const OrthS
     if (last) finish<T>(tile_of<T>(lds), q, s, at.m0, at.n0);
     else emit_x<T, T>(tile_of<T>(lds), q, odd ? q.Xt : q.Xt2, at.m0, at.n0);
 }
-__global__ __launch_bounds__(kThreads, 2) void orth_apply_kernel(OrthRef L, int total, int odd, int last)
+__global__ __launch_bounds__(kThreads, 2) void orth_apply_kernel(OrthRef L, int odd, int last)
 {
     __shared__ OrthLds lds;
     int b = xcd_block(blockIdx.x, gridDim.x);
-    if (b >= total) return;
-    const OrthMat &q = find_mat(L.mat, L.s.count, [](const OrthMat &m) { return m.first[2]; }, b);
-    if (q.big) apply_tile<128>(q, L.s, b, odd, last, lds);
+    if (b >= L.total) return;
+    const OrthMat &q = L.mat[find_mat(L.first, L.s.count, b)];
+    if (q.big_x) apply_tile<128>(q, L.s, b, odd, last, lds);
     else apply_tile<64>(q, L.s, b, odd, last, lds);
 }
 
@@ -518,7 +555,7 @@ __global__ __launch_bounds__(kThreads) void orth_none_kernel(OrthRef L)
 {
     __shared__ float t[kOrthTile][kOrthTile + 1];
     int b = blockIdx.x;
-    const OrthMat &q = find_mat(L.mat, L.s.count, [](const OrthMat &m) { return m.first[3]; }, b);
+    const OrthMat &q = L.mat[find_mat(L.first, L.s.count, b)];
     const TileAt at = tile_at<kOrthTile, kOrthTile>(q, b);
     for (int u = threadIdx.x; u < 64 * 64; u += kThreads) {
         const int r = u / 64, c = u % 64, row = at.n0 + c, k = at.m0 + r;
@@ -529,56 +566,332 @@ __global__ __launch_bounds__(kThreads) void orth_none_kernel(OrthRef L)
     finish<kOrthTile>(t, q, L.s, at.m0, at.n0);
 }
 
+// ---- small matrices: all steps in one workgroup -------------------------------------------------------------------
+// m <= 64 and n <= 768: eight waves hold X in registers, 64 rows x 32 columns a tile and up to three tiles a wave, in the layout
+// in which the matrix instruction leaves its result: a lane has one column of 32 and half of the rows.  Read as an operand, that
+// is the column's part of P X (k runs over rows, in the order in which the lane has them; P is laid out in the same order), and
+// with the operands changed over it gives the same product transposed, a lane having one row of A and columns along k, which
+// is what X X^T takes.  So X never leaves the registers; the waves' parts of X X^T are added up through LDS.
+// What bounds it is latency and one unit's matrix instructions; a launch a product (15 of them) takes four times as long.
+constexpr int kNarrowThreads = 512, kNarrowWaves = 8, kNarrowTiles = 3, kNarrowItems = 64;
+constexpr int kNarrowM = 64, kNarrowN = 32 * kNarrowWaves * kNarrowTiles;
+
+struct NarrowMat {
+    const void *G;
+    void *out;
+    float *M;
+    int rows, cols;
+    float wscale;
+};
+struct NarrowList {
+    OrthScalars s;
+    int steps;
+    NarrowMat mat[kNarrowItems];
+};
+static_assert(sizeof(NarrowList) <= 4096, "kernel arguments");
+
+struct NarrowLds {
+    union {
+        float gram[kNarrowWaves][3][16][64];
+        struct {
+            h8 af[2][2][2][2][64];
+            float p[64][65];
+        };
+    };
+    float a[64][65];
+    h8 pf[2][2][2][2][64];     // [rows / 32][k / 32][half][number][lane]
+    double red[kNarrowWaves];
+};
+
+__device__ inline void split_pieces(const float (&v)[8], h8 &h, h8 &l)
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float s = v[i] * kOrthScale;
+        h[i] = (_Float16)s;
+        l[i] = (_Float16)(s - (float)h[i]);
+    }
+}
+// registers 8 kq .. 8 kq + 7 of a result tile as an operand
+__device__ inline void tile_pieces(const f32x16 &x, int kq, h8 &h, h8 &l)
+{
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = x[8 * kq + j];
+    split_pieces(v, h, l);
+}
+__device__ inline int result_row(int e, int lane) { return 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3); }
+__device__ inline f32x16 mfma3(const h8 &ah, const h8 &al, const h8 &bh, const h8 &bl, f32x16 c)
+{
+    c = __builtin_amdgcn_mfma_f32_32x32x16_f16(al, bh, c, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_f32_32x32x16_f16(ah, bl, c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(ah, bh, c, 0, 0, 0);
+}
+// the thread's fragment (one of 512) of a symmetric matrix t, k in the order of result_row
+__device__ inline void build_fragments(const float (*t)[65], h8 (*f)[2][2][2][64])
+{
+    const int lane = threadIdx.x & 63, kq = (threadIdx.x >> 6) & 1, mb = (threadIdx.x >> 7) & 1, rb = threadIdx.x >> 8;
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = t[32 * rb + (lane & 31)][32 * mb + 16 * kq + result_row(j, lane)];
+    split_pieces(v, f[rb][mb][kq][0][lane], f[rb][mb][kq][1][lane]);
+}
+
+// P times a tile of X, in true scale; ACROSS: transposed
+template <bool ACROSS> __device__ inline void tile_product(const f32x16 (&x)[2], const h8 (*pf)[2][2][2][64], int lane, f32x16 (&y)[2])
+{
+    f32x16 s[2];
+#pragma unroll
+    for (int rb = 0; rb < 2; ++rb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[rb][e] = 0.f;
+#pragma unroll
+    for (int mb = 0; mb < 2; ++mb)
+#pragma unroll
+        for (int kq = 0; kq < 2; ++kq) {
+            h8 xh, xl;
+            tile_pieces(x[mb], kq, xh, xl);
+#pragma unroll
+            for (int rb = 0; rb < 2; ++rb) {
+                const h8 ph = pf[rb][mb][kq][0][lane], pl = pf[rb][mb][kq][1][lane];
+                s[rb] = ACROSS ? mfma3(xh, xl, ph, pl, s[rb]) : mfma3(ph, pl, xh, xl, s[rb]);
+            }
+        }
+#pragma unroll
+    for (int rb = 0; rb < 2; ++rb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) y[rb][e] = s[rb][e] * kOrthUnscale;
+}
+
+__global__ __launch_bounds__(kNarrowThreads, 2) void orth_narrow_kernel(NarrowList L)
+{
+    extern __shared__ char narrow_lds[];
+    NarrowLds &S = *reinterpret_cast<NarrowLds *>(narrow_lds);
+    const NarrowMat &q = L.mat[blockIdx.x];
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 31;
+    const bool tall = q.rows > q.cols;
+    const int m = tall ? q.cols : q.rows, n = tall ? q.rows : q.cols;
+    const int rstride = tall ? 1 : q.cols, cstride = tall ? q.cols : 1;
+    auto place = [&](int r, int col) { return (uint32_t)(r * rstride + col * cstride); };
+    f32x16 x[kNarrowTiles][2];
+    double sq = 0.0;
+#pragma unroll
+    for (int i = 0; i < kNarrowTiles; ++i) {
+        const int n0 = 32 * (wave + kNarrowWaves * i);
+#pragma unroll
+        for (int mb = 0; mb < 2; ++mb)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[i][mb][e] = 0.f;
+        if (n0 >= n) continue;
+#pragma unroll
+        for (int mb = 0; mb < 2; ++mb) {
+            auto at = [&](int e) -> long long {
+                const int r = 32 * mb + result_row(e, lane), col = n0 + c;
+                return r < m && col < n ? (long long)place(r, col) : -1;
+            };
+            float v[16], mo[16];
+            orth_gather(q.G, L.s.g_dtype, at, v);
+            if (L.s.muon) {
+                orth_gather(q.M, XCONV_F32, at, mo);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) mo[e] = mo[e] + (v[e] - mo[e]) * (1.f - L.s.mu);
+                orth_scatter(q.M, XCONV_F32, at, mo);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) v[e] = update_of(v[e], mo[e], L.s);
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                x[i][mb][e] = v[e];
+                sq += (double)v[e] * v[e];
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) sq += __shfl_xor(sq, o);
+    if (lane == 0) S.red[wave] = sq;
+    // P = I for the first X X^T, which needs X the other way round only
+    for (int u = tid; u < 64 * 64; u += kNarrowThreads) S.a[u >> 6][u & 63] = (u >> 6) == (u & 63) ? 1.f : 0.f;
+    __syncthreads();
+    build_fragments(S.a, S.pf);
+    sq = 0.0;
+#pragma unroll
+    for (int w = 0; w < kNarrowWaves; ++w) sq += S.red[w];
+    const double norm = sqrt(sq), d = norm < (double)L.s.eps ? (double)L.s.eps : norm;      // (a NaN stays one)
+    const double inv = d == 0.0 ? 0.0 : 1.0 / d;                                             // (eps = 0 and a zero matrix)
+#pragma unroll
+    for (int i = 0; i < kNarrowTiles; ++i)
+#pragma unroll
+        for (int mb = 0; mb < 2; ++mb)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[i][mb][e] = (float)((double)x[i][mb][e] * inv);
+    __syncthreads();
+
+    for (int step = 0; step < L.steps; ++step) {
+        // X <- P X, and the wave's part of X X^T
+        f32x16 g[3];
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) g[k][e] = 0.f;
+#pragma unroll
+        for (int i = 0; i < kNarrowTiles; ++i) {
+            if (32 * (wave + kNarrowWaves * i) >= n) continue;
+            // transposed first, for X X^T: one product's sums are live at a time
+            {
+                f32x16 z[2];
+                tile_product<true>(x[i], S.pf, lane, z);
+#pragma unroll
+                for (int kq = 0; kq < 2; ++kq) {
+                    h8 h[2], l[2];
+#pragma unroll
+                    for (int rb = 0; rb < 2; ++rb) tile_pieces(z[rb], kq, h[rb], l[rb]);
+                    g[0] = mfma3(h[0], l[0], h[0], l[0], g[0]);
+                    g[1] = mfma3(h[0], l[0], h[1], l[1], g[1]);
+                    g[2] = mfma3(h[1], l[1], h[1], l[1], g[2]);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if (step > 0) {
+                f32x16 y[2];
+                tile_product<false>(x[i], S.pf, lane, y);
+                x[i][0] = y[0];
+                x[i][1] = y[1];
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) S.gram[wave][k][e][lane] = g[k][e];
+        __syncthreads();
+        // A, added up in order of the waves
+        for (int u = tid; u < 3 * 16 * 64; u += kNarrowThreads) {
+            const int k = u >> 10, e = (u >> 6) & 15, l = u & 63;
+            float v = 0.f;
+#pragma unroll
+            for (int w = 0; w < kNarrowWaves; ++w) v += S.gram[w][k][e][l];
+            v *= kOrthUnscale;
+            const int r = (k == 2 ? 32 : 0) + result_row(e, l), col = (k > 0 ? 32 : 0) + (l & 31);
+            S.a[r][col] = v;
+            if (k == 1) S.a[col][r] = v;
+        }
+        __syncthreads();
+        build_fragments(S.a, S.af);
+        __syncthreads();
+        // P = a I + b A + c A A: one block of 32 x 32 a wave
+        if (wave < 3) {
+            const int r0 = wave == 2, c0 = wave > 0;
+            f32x16 t;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) t[e] = 0.f;
+#pragma unroll
+            for (int mb = 0; mb < 2; ++mb)
+#pragma unroll
+                for (int kq = 0; kq < 2; ++kq)
+                    t = mfma3(S.af[r0][mb][kq][0][lane], S.af[r0][mb][kq][1][lane], S.af[c0][mb][kq][0][lane], S.af[c0][mb][kq][1][lane], t);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int r = 32 * r0 + result_row(e, lane), col = 32 * c0 + c;
+                float v = L.s.b * S.a[r][col] + L.s.c * (t[e] * kOrthUnscale);
+                if (r == col) v += L.s.a;
+                S.p[r][col] = v;
+                if (r0 != c0) S.p[col][r] = v;
+            }
+        }
+        __syncthreads();
+        build_fragments(S.p, S.pf);
+        __syncthreads();
+    }
+
+    // the last P X, along the rows of the result; no step: X_0
+#pragma unroll
+    for (int i = 0; i < kNarrowTiles; ++i) {
+        const int n0 = 32 * (wave + kNarrowWaves * i);
+        if (n0 >= n) continue;
+        const bool across = tall && L.steps > 0;
+        f32x16 y[2] = {x[i][0], x[i][1]};
+        if (across) tile_product<true>(x[i], S.pf, lane, y);
+        else if (L.steps > 0) tile_product<false>(x[i], S.pf, lane, y);
+#pragma unroll
+        for (int rb = 0; rb < 2; ++rb) {
+            auto at = [&](int e) -> long long {
+                const int r = across ? 32 * rb + c : 32 * rb + result_row(e, lane), col = n0 + (across ? result_row(e, lane) : c);
+                return r < m && col < n ? (long long)place(r, col) : -1;
+            };
+            float v[16];
+            if (L.s.muon) orth_gather(q.out, L.s.out_dtype, at, v);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) v[e] = L.s.muon ? v[e] * L.s.keep - q.wscale * y[rb][e] : y[rb][e];
+            orth_scatter(q.out, L.s.out_dtype, at, v);
+        }
+    }
+}
+
 // ---- host ----------------------------------------------------------------------------------------------------------
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
 // Tiles of 128 x 128 read half as much for the same products, tiles of 64 x 64 waste less of a small matrix and are four times
-// as many.  128 where they leave X with enough tiles for the chip's 256 compute units, and for matrices that they do not pad to
-// more than half as many rows again.  The sum over columns of X X^T is split where there are too few tiles of A to fill the chip.
-constexpr int kFillUnits = 512, kFewestBlocks = 16;
+// as many.  X is taken in tiles of 128 where that leaves enough of them for the chip's 256 compute units, of matrices that it does
+// not pad to more than half as many rows again; A, which has fewer, where there are 128.
+//
+// Sums along k are split so that a matrix has about as many workgroups as the chip has compute units, or twice as many of the
+// large tiles: by the matrix' own extents, so that what else is in the call does not change its result.
+constexpr int kFewestBlocks = 24;
+int splits_of(int m, int kblocks)
+{
+    const int t64 = ceil_div(m, 64) * (ceil_div(m, 64) + 1) / 2, t128 = ceil_div(m, 128) * (ceil_div(m, 128) + 1) / 2;
+    const int want = m <= 1024 ? (224 + t64 / 2) / t64 : 448 / t128;
+    return std::max(1, std::min(want, kblocks / kFewestBlocks));
+}
+bool narrow(const xconv_orth_item &it) { return std::min(it.rows, it.cols) <= kNarrowM && std::max(it.rows, it.cols) <= kNarrowN; }
+
 struct OrthPlan {
     int count;
     struct Mat {
-        int m, n, mp, np, big, splits, kbs, tiles_a, tiles_x;
+        int m, n, mp, np, big_a, big_x, gsplits, gkbs, psplits, pkbs, tiles_a, tiles_x;
         size_t x, a, part, bytes;
     } mat[kOrthItems];
     size_t bytes;
 };
-OrthPlan plan_orth(const xconv_orth_item *items, int count)
+// items: the matrices of a run, all of them wide
+OrthPlan plan_orth(const xconv_orth_item *const *items, int count)
 {
     OrthPlan P{};
     P.count = count;
     auto can = [](int m) { return m > 64 && 2 * round_up(m, 128) <= 3 * m; };
-    long long large = 0;
+    long long large_x = 0, large_a = 0;
     for (int i = 0; i < count; ++i) {
-        const int m = std::min(items[i].rows, items[i].cols), n = std::max(items[i].rows, items[i].cols);
-        if (can(m)) large += (long long)ceil_div(m, 128) * ceil_div(n, 128);
+        const int m = std::min(items[i]->rows, items[i]->cols), n = std::max(items[i]->rows, items[i]->cols), tm = ceil_div(m, 128);
+        if (!can(m)) continue;
+        large_x += (long long)tm * ceil_div(n, 128);
+        large_a += tm * (tm + 1) / 2;
     }
-    long long blocks = 0;
-    for (int i = 0; i < count; ++i) {
-        OrthPlan::Mat &q = P.mat[i];
-        q.m = std::min(items[i].rows, items[i].cols);
-        q.n = std::max(items[i].rows, items[i].cols);
-        q.big = can(q.m) && large >= 256;
-        const int T = q.big ? 128 : 64;
-        q.mp = round_up(q.m, T);
-        q.np = round_up(q.n, T);
-        const int tm = q.mp / T;
-        q.tiles_a = tm * (tm + 1) / 2;
-        q.tiles_x = tm * (q.np / T);
-        blocks += (long long)q.tiles_a * (q.np / 16);
-    }
-    // runs of about as many blocks as give every compute unit two workgroups
-    const int run = (int)std::max<long long>(kFewestBlocks, round_up((int)std::min<long long>((blocks + kFillUnits - 1) / kFillUnits, 1 << 20), 4));
     P.bytes = up256(sizeof(OrthMat) * kOrthItems);
     for (int i = 0; i < count; ++i) {
         OrthPlan::Mat &q = P.mat[i];
-        const int kb = q.np / 16;
-        q.splits = kb >= 2 * run ? ceil_div(kb, run) : 1;
-        q.kbs = q.splits > 1 ? run : kb;
+        q.m = std::min(items[i]->rows, items[i]->cols);
+        q.n = std::max(items[i]->rows, items[i]->cols);
+        q.big_x = can(q.m) && large_x >= 256;
+        q.big_a = q.big_x && large_a >= 128;
+        const int T = q.big_x ? 128 : 64, ta = q.big_a ? 128 : 64;
+        q.mp = round_up(q.m, T);
+        q.np = round_up(q.n, T);
+        q.tiles_a = q.mp / ta * (q.mp / ta + 1) / 2;
+        q.tiles_x = q.mp / T * (q.np / T);
+        // (extents padded to 64 for the splits, runs of whole steps)
+        auto split = [&](int extent, int &splits, int &run) {
+            const int kb = round_up(extent, 64) / 16;
+            splits = splits_of(q.m, kb);
+            run = splits > 1 ? round_up(ceil_div(kb, splits), 4) : std::max(q.mp, q.np) / 16;
+            if (splits > 1) splits = ceil_div(kb, run);
+        };
+        split(q.n, q.gsplits, q.gkbs);
+        split(q.m, q.psplits, q.pkbs);
         q.x = up256((size_t)q.mp * q.np * 4);
         q.a = up256((size_t)q.mp * q.mp * 4);
-        q.part = q.splits > 1 ? up256((size_t)q.tiles_a * q.splits * (q.big ? 128 * 128 : 64 * 64) * 4) : 0;
+        const int most = std::max(q.gsplits, q.psplits);
+        q.part = most > 1 ? up256((size_t)q.tiles_a * most * ta * ta * 4) : 0;
         q.bytes = 3 * q.x + 3 * q.a + q.part + up256(kOrthNorms * sizeof(double));
         P.bytes += q.bytes;
     }
@@ -587,70 +900,131 @@ OrthPlan plan_orth(const xconv_orth_item *items, int count)
 
 }  // namespace
 
-// the matrices go through in runs of kOrthItems, one run after the other through the same scratch
+// Calls `run` with the next kOrthItems matrices that the narrow kernel does not take, in order, until there are none
+namespace {
+template <class F> bool wide_runs(const xconv_orth_item *items, int count, F &&run)
+{
+    const xconv_orth_item *list[kOrthItems];
+    int n = 0;
+    for (int i = 0; i <= count; ++i) {
+        if (i < count && !narrow(items[i])) list[n++] = items + i;
+        if (n == kOrthItems || (i == count && n)) {
+            if (!run(list, n)) return false;
+            n = 0;
+        }
+    }
+    return true;
+}
+
+OrthScalars scalars_of(const xconv_orth_args *args, const xconv_muon_args *muon)
+{
+    OrthScalars s{};
+    s.g_dtype = args->g_dtype; s.out_dtype = args->out_dtype;
+    s.a = args->a; s.b = args->b; s.c = args->c; s.eps = args->eps;
+    if (muon) {
+        s.muon = 1; s.nesterov = muon->nesterov != 0; s.mu = muon->momentum;
+        s.keep = (float)(1.0 - (double)muon->lr * muon->weight_decay);
+    }
+    return s;
+}
+float wscale_of(const xconv_orth_item &it, const xconv_muon_args *muon)
+{
+    return muon ? (float)((double)muon->lr * std::sqrt(std::max(1.0, (double)it.rows / it.cols))) : 0.f;
+}
+
+hipError_t launch_narrow(const xconv_orth_item *items, int count, const xconv_orth_args *args, const xconv_muon_args *muon, hipStream_t st)
+{
+    static const hipError_t set = hipFuncSetAttribute(reinterpret_cast<const void *>(orth_narrow_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(NarrowLds));
+    if (set != hipSuccess) return set;
+    NarrowList L{};
+    L.s = scalars_of(args, muon);
+    L.steps = args->steps;
+    int n = 0;
+    for (int i = 0; i <= count; ++i) {
+        if (i < count && narrow(items[i])) {
+            const xconv_orth_item &it = items[i];
+            L.mat[n++] = {it.G_dev, it.out_dev, it.M_dev, it.rows, it.cols, wscale_of(it, muon)};
+        }
+        if (n == kNarrowItems || (i == count && n)) {
+            hipLaunchKernelGGL(orth_narrow_kernel, dim3((unsigned)n), dim3(kNarrowThreads), sizeof(NarrowLds), st, L);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+            n = 0;
+        }
+    }
+    return hipSuccess;
+}
+
+hipError_t launch_wide(const xconv_orth_item *const *items, int count, const xconv_orth_args *args, const xconv_muon_args *muon, void *ws, hipStream_t st)
+{
+    const OrthPlan P = plan_orth(items, count);
+    OrthList L{};
+    L.s = scalars_of(args, muon);
+    L.s.count = count;
+    char *p = static_cast<char *>(ws);
+    auto take = [&](size_t bytes) { char *r = p; p += bytes; return r; };
+    OrthMat *list = (OrthMat *)take(up256(sizeof(OrthMat) * kOrthItems));
+    // the first workgroups of the matrices in the launches
+    enum { NORM, START, GRAM, GRAM_JOIN, POLY, POLY_JOIN, APPLY, KINDS };
+    OrthRef R[KINDS];
+    for (OrthRef &r : R) r = OrthRef{L.s, 0, {}, list};
+    for (int i = 0; i < count; ++i) {
+        const xconv_orth_item &it = *items[i];
+        const OrthPlan::Mat &f = P.mat[i];
+        OrthMat &q = L.mat[i];
+        q.G = it.G_dev; q.out = it.out_dev; q.M = it.M_dev;
+        q.rows = it.rows; q.cols = it.cols; q.m = f.m; q.n = f.n; q.mp = f.mp; q.np = f.np;
+        q.big_a = f.big_a; q.big_x = f.big_x;
+        q.gsplits = f.gsplits; q.gkbs = f.gkbs; q.psplits = f.psplits; q.pkbs = f.pkbs;
+        q.X = (_Float16 *)take(f.x); q.Xt = (_Float16 *)take(f.x); q.Xt2 = (_Float16 *)take(f.x);
+        q.A = (_Float16 *)take(f.a); q.P = (_Float16 *)take(f.a); q.A32 = (float *)take(f.a);
+        q.part = (float *)take(f.part);
+        q.sq = (double *)take(up256(kOrthNorms * sizeof(double)));
+        q.nsq = (int)std::min<size_t>(kOrthNorms, ((size_t)it.rows * it.cols + 4095) / 4096);
+        q.wscale = wscale_of(it, muon);
+        const int pieces = f.tiles_a * (f.big_a ? 4 : 1);
+        const int blocks[KINDS] = {q.nsq, (f.mp / kOrthTile) * (f.np / kOrthTile), f.tiles_a * f.gsplits, f.gsplits > 1 ? pieces : 0,
+                                   f.tiles_a * f.psplits, f.psplits > 1 ? pieces : 0, f.tiles_x};
+        for (int k = 0; k < KINDS; ++k) {
+            R[k].first[i] = R[k].total;
+            R[k].total += blocks[k];
+        }
+    }
+    for (int i = 0; i < count; ++i) L.first[i] = R[NORM].first[i];
+    const dim3 block(kThreads);
+    auto grid = [&](int k) { return dim3((unsigned)R[k].total); };
+    auto grid8 = [&](int k) { return dim3((unsigned)round_up(R[k].total, 8)); };      // (whole rounds of the eight dies)
+    hipLaunchKernelGGL(orth_norm_kernel, grid(NORM), block, 0, st, L, list);
+    hipLaunchKernelGGL(orth_start_kernel, grid(START), block, 0, st, R[START]);
+    if (args->steps == 0) hipLaunchKernelGGL(orth_none_kernel, grid(START), block, 0, st, R[START]);
+    for (int k = 0; k < args->steps; ++k) {
+        hipLaunchKernelGGL(orth_square_kernel<0>, grid8(GRAM), block, 0, st, R[GRAM]);
+        if (R[GRAM_JOIN].total) hipLaunchKernelGGL(orth_join_kernel<0>, grid(GRAM_JOIN), block, 0, st, R[GRAM_JOIN]);
+        hipLaunchKernelGGL(orth_square_kernel<1>, grid8(POLY), block, 0, st, R[POLY]);
+        if (R[POLY_JOIN].total) hipLaunchKernelGGL(orth_join_kernel<1>, grid(POLY_JOIN), block, 0, st, R[POLY_JOIN]);
+        hipLaunchKernelGGL(orth_apply_kernel, grid8(APPLY), block, 0, st, R[APPLY], k & 1, k + 1 == args->steps);
+    }
+    return hipGetLastError();
+}
+}  // namespace
+
+// the runs go one after the other through the same scratch
 size_t orth_ws_bytes(const xconv_orth_item *items, int count)
 {
     size_t most = 256;
-    for (int at = 0; at < count; at += kOrthItems) most = std::max(most, plan_orth(items + at, std::min(kOrthItems, count - at)).bytes);
+    wide_runs(items, count, [&](const xconv_orth_item *const *list, int n) {
+        most = std::max(most, plan_orth(list, n).bytes);
+        return true;
+    });
     return most;
 }
 
 hipError_t launch_orth(const xconv_orth_item *items, int count, const xconv_orth_args *args, const xconv_muon_args *muon, void *ws, hipStream_t st)
 {
-    for (int at = 0; at < count; at += kOrthItems) {
-        const OrthPlan P = plan_orth(items + at, std::min(kOrthItems, count - at));
-        OrthList L{};
-        OrthScalars &s = L.s;
-        s.count = P.count;
-        s.g_dtype = args->g_dtype; s.out_dtype = args->out_dtype;
-        s.a = args->a; s.b = args->b; s.c = args->c; s.eps = args->eps;
-        if (muon) {
-            s.muon = 1; s.nesterov = muon->nesterov != 0; s.mu = muon->momentum;
-            s.keep = (float)(1.0 - (double)muon->lr * muon->weight_decay);
-        }
-        char *p = static_cast<char *>(ws);
-        auto take = [&](size_t bytes) { char *r = p; p += bytes; return r; };
-        OrthMat *list = (OrthMat *)take(up256(sizeof(OrthMat) * kOrthItems));
-        int total[4] = {0, 0, 0, 0}, gram = 0, join = 0;
-        for (int i = 0; i < P.count; ++i) {
-            const xconv_orth_item &it = items[at + i];
-            const OrthPlan::Mat &f = P.mat[i];
-            OrthMat &q = L.mat[i];
-            q.G = it.G_dev; q.out = it.out_dev; q.M = it.M_dev;
-            q.rows = it.rows; q.cols = it.cols; q.m = f.m; q.n = f.n; q.mp = f.mp; q.np = f.np;
-            q.big = f.big; q.splits = f.splits; q.kbs = f.kbs;
-            q.X = (_Float16 *)take(f.x); q.Xt = (_Float16 *)take(f.x); q.Xt2 = (_Float16 *)take(f.x);
-            q.A = (_Float16 *)take(f.a); q.P = (_Float16 *)take(f.a); q.A32 = (float *)take(f.a);
-            q.part = (float *)take(f.part);
-            q.sq = (double *)take(up256(kOrthNorms * sizeof(double)));
-            q.nsq = (int)std::min<size_t>(kOrthNorms, ((size_t)it.rows * it.cols + 4095) / 4096);
-            if (muon) q.wscale = (float)((double)muon->lr * std::sqrt(std::max(1.0, (double)it.rows / it.cols)));
-            const int blocks[4] = {q.nsq, f.tiles_a, f.tiles_x, (f.mp / kOrthTile) * (f.np / kOrthTile)};
-            for (int k = 0; k < 4; ++k) {
-                q.first[k] = total[k];
-                total[k] += blocks[k];
-            }
-            q.gfirst = gram;
-            gram += f.tiles_a * f.splits;
-            q.jfirst = join;
-            join += f.splits > 1 ? f.tiles_a : 0;
-        }
-        const OrthRef R{s, list};
-        const dim3 block(kThreads);
-        auto grid8 = [](int n) { return dim3((unsigned)round_up(n, 8)); };
-        hipLaunchKernelGGL(orth_norm_kernel, dim3(total[0]), block, 0, st, L, list);
-        hipLaunchKernelGGL(orth_start_kernel, dim3(total[3]), block, 0, st, R);
-        if (args->steps == 0) hipLaunchKernelGGL(orth_none_kernel, dim3(total[3]), block, 0, st, R);
-        for (int k = 0; k < args->steps; ++k) {
-            hipLaunchKernelGGL(orth_gram_kernel, grid8(gram), block, 0, st, R, gram);
-            if (join) hipLaunchKernelGGL(orth_join_kernel, dim3(join), block, 0, st, R);
-            hipLaunchKernelGGL(orth_poly_kernel, grid8(total[1]), block, 0, st, R, total[1]);
-            hipLaunchKernelGGL(orth_apply_kernel, grid8(total[2]), block, 0, st, R, total[2], k & 1, k + 1 == args->steps);
-        }
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
-    return hipSuccess;
+    hipError_t e = launch_narrow(items, count, args, muon, st);
+    if (e != hipSuccess) return e;
+    wide_runs(items, count, [&](const xconv_orth_item *const *list, int n) { return (e = launch_wide(list, n, args, muon, ws, st)) == hipSuccess; });
+    return e;
 }
 
 }  // namespace xc

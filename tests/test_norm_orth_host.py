@@ -50,10 +50,10 @@ def test_orth_statuses():
     items = lambda *m: xb.make_orth_items([(r, c, 4096, 4096, 4096) for r, c in m])
     args = xb.make_orth_args()
     mu = ctypes.byref(xb.xconv_muon_args(0.1, 0.9, 0.0, 1))
-    size = xb.xconv_orth_workspace_bytes(items((64, 576), (10, 3)), 2, args)
-    assert size >= 64 * 576 * 4 and size % 256 == 0
+    size = xb.xconv_orth_workspace_bytes(items((128, 1152), (10, 3)), 2, args)
+    assert size >= 128 * 1152 * 4 and size % 256 == 0
     # the scratch of a long list is that of a launch, not of the list
-    many = xb.xconv_orth_workspace_bytes(items(*[(64, 576)] * 100), 100, args)
+    many = xb.xconv_orth_workspace_bytes(items(*[(128, 1152)] * 100), 100, args)
     assert size < many < 100 * size
 
     def both(it, n, a, status, ws=ONE, nbytes=1 << 40):
