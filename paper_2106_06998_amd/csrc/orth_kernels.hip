@@ -31,6 +31,7 @@ constexpr int kOrthNorms = 512;     // most partial sums of a matrix' squares
 constexpr int kBlockHalfs = 1024;   // 32 x 16 values, both numbers
 
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
@@ -128,16 +129,28 @@ template <int N, class At> __device__ inline void orth_scatter(void *p, int dtyp
 }
 __device__ inline float update_of(float g, float m, const OrthScalars &L) { return L.nesterov ? g + L.mu * (m - g) : m; }
 
-// eight values as two fp16 numbers each, stored at their place (row r, columns k .. k + 7) of a matrix in fragment order
+// eight values, already scaled, as two fp16 numbers each (rounded to nearest; the rest of the first is exact)
+__device__ inline void split8(const float (&s)[8], h8 &h, h8 &l)
+{
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+        const h2 hi = __builtin_convertvector(f32x2{s[i], s[i + 1]}, h2);
+        f32x2 rest;
+        asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(rest[0]) : "v"(hi), "v"(s[i]));
+        asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(rest[1]) : "v"(hi), "v"(s[i + 1]));
+        const h2 lo = __builtin_convertvector(rest, h2);
+        h[i] = hi[0]; h[i + 1] = hi[1];
+        l[i] = lo[0]; l[i + 1] = lo[1];
+    }
+}
+// eight values stored at their place (row r, columns k .. k + 7) of a matrix in fragment order
 __device__ inline void put_pieces(_Float16 *frag, int r, int k, int kblocks, const float (&v)[8])
 {
-    h8 h, l;
+    float s[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float s = v[i] * kOrthScale;
-        h[i] = (_Float16)s;
-        l[i] = (_Float16)(s - (float)h[i]);
-    }
+    for (int i = 0; i < 8; ++i) s[i] = v[i] * kOrthScale;
+    h8 h, l;
+    split8(s, h, l);
     _Float16 *p = frag + ((size_t)(r >> 5) * kblocks + (k >> 4)) * kBlockHalfs + ((r & 31) + 32 * ((k >> 3) & 1)) * 8;
     *reinterpret_cast<h8 *>(p) = h;
     *reinterpret_cast<h8 *>(p + 512) = l;
@@ -283,12 +296,16 @@ __global__ __launch_bounds__(kThreads) void orth_start_kernel(OrthRef L)
 
 // ---- products ------------------------------------------------------------------------------------------------------
 // A workgroup's tile: 64 MT rows of one matrix times 64 NT rows of another (rows along k, fragment order with kblocks blocks a
-// row of blocks), blocks kb0 .. kb1 - 1; wave w computes rows 32 MT (w / 2), columns 32 NT (w % 2).  Steps of KS blocks are
-// staged through registers into one of two buffers while the other one is used: one barrier a step.
-constexpr int kStageUnits = 2048;     // 16-byte units of a step, 8 a thread
+// row of blocks), blocks kb0 .. kb1 - 1; wave w computes rows 32 MT (w / 2), columns 32 NT (w % 2).  Steps of KS blocks.  The first
+// matrix' fragments go through LDS (staged through registers into one of two buffers while the other one is used: one barrier a
+// step), the second one's straight into the registers of the two waves that use them, a step ahead: both ways through LDS, its
+// bandwidth is what the matrix instructions wait for.
 template <int MT, int NT> struct Tile {
-    static constexpr int TM = 64 * MT, TN = 64 * NT, KS = kStageUnits / (2 * (MT + NT) * 128);
+    static constexpr int TM = 64 * MT, TN = 64 * NT, KS = 4 / MT, kUnits = 2 * MT * KS * 128, kPer = kUnits / kThreads;
     f32x16 acc[MT][NT];
+    struct Right {
+        h8 f[KS][2][NT];
+    };
 
     __device__ void clear()
     {
@@ -299,62 +316,82 @@ template <int MT, int NT> struct Tile {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
     }
-    static constexpr int kRun = KS * 128, kPer = kStageUnits / kThreads;
-    __device__ static void load(u32x4 (&r)[kPer], const _Float16 *Fa, int ra, const _Float16 *Fb, int rb, int kblocks, int kb)
+    __device__ static void load(u32x4 (&r)[kPer], const _Float16 *Fa, int ra, int kblocks, int kb)
     {
+        constexpr int kRun = KS * 128;
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
-            // (a run is a whole number of rounds of the workgroup, or half of one)
+            // (a run is a whole number of rounds of the workgroup)
             const int blk = j * kThreads / kRun, off = (j * kThreads) % kRun + (int)threadIdx.x;
-            const bool second = blk >= 2 * MT;
-            const int row = second ? rb / 32 + blk - 2 * MT : ra / 32 + blk;
-            r[j] = reinterpret_cast<const u32x4 *>((second ? Fb : Fa) + ((size_t)row * kblocks + kb) * kBlockHalfs)[off];
+            r[j] = reinterpret_cast<const u32x4 *>(Fa + ((size_t)(ra / 32 + blk) * kblocks + kb) * kBlockHalfs)[off];
         }
+    }
+    __device__ static void load(Right &r, const _Float16 *Fb, int rb, int kblocks, int kb)
+    {
+        const int wb = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) & 1), lane = threadIdx.x & 63;
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int k = 0; k < KS; ++k)
+#pragma unroll
+                for (int p = 0; p < 2; ++p)
+                    r.f[k][p][j] = reinterpret_cast<const h8 *>(Fb + ((size_t)(rb / 32 + wb * NT + j) * kblocks + kb + k) * kBlockHalfs + p * 512)[lane];
     }
     __device__ static void store(const u32x4 (&r)[kPer], u32x4 *lds)
     {
 #pragma unroll
         for (int j = 0; j < kPer; ++j) lds[j * kThreads + threadIdx.x] = r[j];
     }
-    __device__ void multiply(const u32x4 *lds)
+    __device__ void multiply(const u32x4 *lds, const Right &b)
     {
-        const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wa = wave >> 1, wb = wave & 1;
+        const int wa = threadIdx.x >> 7, lane = threadIdx.x & 63;
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
-            h8 a[2][MT], b[2][NT];
+            h8 a[2][MT];
 #pragma unroll
-            for (int p = 0; p < 2; ++p) {
+            for (int p = 0; p < 2; ++p)
 #pragma unroll
                 for (int i = 0; i < MT; ++i) a[p][i] = __builtin_bit_cast(h8, lds[((wa * MT + i) * KS + k) * 128 + p * 64 + lane]);
-#pragma unroll
-                for (int j = 0; j < NT; ++j) b[p][j] = __builtin_bit_cast(h8, lds[((2 * MT + wb * NT + j) * KS + k) * 128 + p * 64 + lane]);
-            }
             // the small products first
 #pragma unroll
             for (int p = 0; p < 3; ++p)
 #pragma unroll
                 for (int i = 0; i < MT; ++i)
 #pragma unroll
-                    for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[p == 0][i], b[p == 1][j], acc[i][j], 0, 0, 0);
+                    for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[p == 0][i], b.f[k][p == 1][j], acc[i][j], 0, 0, 0);
         }
     }
-    // lds: two stages
+    // lds: two steps
     __device__ void product(const _Float16 *Fa, int ra, const _Float16 *Fb, int rb, int kblocks, int kb0, int kb1, u32x4 *lds)
     {
         clear();
         u32x4 r[kPer];
-        load(r, Fa, ra, Fb, rb, kblocks, kb0);
+        Right b0, b1;
+        load(b0, Fb, rb, kblocks, kb0);
+        load(r, Fa, ra, kblocks, kb0);
         store(r, lds);
         __syncthreads();
         int at = 0;
-        for (int kb = kb0 + KS; kb < kb1; kb += KS) {
-            load(r, Fa, ra, Fb, rb, kblocks, kb);
-            multiply(lds + at * kStageUnits);
+        // one step with the next one's loads under way
+        auto step = [&](const Right &now, Right &next, int kb) {
+            load(next, Fb, rb, kblocks, kb);
+            load(r, Fa, ra, kblocks, kb);
+            multiply(lds + at * kUnits, now);
             at ^= 1;
-            store(r, lds + at * kStageUnits);
+            store(r, lds + at * kUnits);
             __syncthreads();
+        };
+        int kb = kb0 + KS;
+        for (; kb + KS < kb1; kb += 2 * KS) {
+            step(b0, b1, kb);
+            step(b1, b0, kb + KS);
         }
-        multiply(lds + at * kStageUnits);
+        if (kb < kb1) {
+            step(b0, b1, kb);
+            multiply(lds + at * kUnits, b1);
+        } else {
+            multiply(lds + at * kUnits, b0);
+        }
         __syncthreads();
     }
     // the sums, in true scale, as t[row][column]
@@ -399,7 +436,7 @@ template <int MT, int NT> struct Tile {
 };
 
 union OrthLds {
-    u32x4 stage[2 * kStageUnits];
+    u32x4 stage[2 * 1024];      // (1024 units a step, with either tile)
     float small[64][64 + 1];
     float large[128][128 + 1];
 };
@@ -603,23 +640,18 @@ struct NarrowLds {
     double red[kNarrowWaves];
 };
 
-__device__ inline void split_pieces(const float (&v)[8], h8 &h, h8 &l)
-{
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float s = v[i] * kOrthScale;
-        h[i] = (_Float16)s;
-        l[i] = (_Float16)(s - (float)h[i]);
-    }
-}
-// registers 8 kq .. 8 kq + 7 of a result tile as an operand
-__device__ inline void tile_pieces(const f32x16 &x, int kq, h8 &h, h8 &l)
+// registers 8 kq .. 8 kq + 7 of a result, scaled, as an operand
+__device__ inline void result_pieces(const f32x16 &x, int kq, float scale, h8 &h, h8 &l)
 {
     float v[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = x[8 * kq + j];
-    split_pieces(v, h, l);
+    for (int j = 0; j < 8; ++j) v[j] = x[8 * kq + j] * scale;
+    split8(v, h, l);
 }
+// a tile of X: [rows / 32][half], both numbers
+struct Pieces {
+    h8 h[2][2], l[2][2];
+};
 __device__ inline int result_row(int e, int lane) { return 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3); }
 __device__ inline f32x16 mfma3(const h8 &ah, const h8 &al, const h8 &bh, const h8 &bl, f32x16 c)
 {
@@ -633,34 +665,32 @@ __device__ inline void build_fragments(const float (*t)[65], h8 (*f)[2][2][2][64
     const int lane = threadIdx.x & 63, kq = (threadIdx.x >> 6) & 1, mb = (threadIdx.x >> 7) & 1, rb = threadIdx.x >> 8;
     float v[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = t[32 * rb + (lane & 31)][32 * mb + 16 * kq + result_row(j, lane)];
-    split_pieces(v, f[rb][mb][kq][0][lane], f[rb][mb][kq][1][lane]);
+    for (int j = 0; j < 8; ++j) v[j] = t[32 * rb + (lane & 31)][32 * mb + 16 * kq + result_row(j, lane)] * kOrthScale;
+    split8(v, f[rb][mb][kq][0][lane], f[rb][mb][kq][1][lane]);
 }
 
-// P times a tile of X, in true scale; ACROSS: transposed
-template <bool ACROSS> __device__ inline void tile_product(const f32x16 (&x)[2], const h8 (*pf)[2][2][2][64], int lane, f32x16 (&y)[2])
+// P times a tile of X, scaled twice; ACROSS: transposed
+template <bool ACROSS> __device__ inline void tile_product(const Pieces &x, const h8 (*pf)[2][2][2][64], int lane, f32x16 (&y)[2])
 {
-    f32x16 s[2];
 #pragma unroll
     for (int rb = 0; rb < 2; ++rb)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) s[rb][e] = 0.f;
+        for (int e = 0; e < 16; ++e) y[rb][e] = 0.f;
 #pragma unroll
     for (int mb = 0; mb < 2; ++mb)
 #pragma unroll
         for (int kq = 0; kq < 2; ++kq) {
-            h8 xh, xl;
-            tile_pieces(x[mb], kq, xh, xl);
+            const h8 xh = x.h[mb][kq], xl = x.l[mb][kq];
+            const h8 ph[2] = {pf[0][mb][kq][0][lane], pf[1][mb][kq][0][lane]}, pl[2] = {pf[0][mb][kq][1][lane], pf[1][mb][kq][1][lane]};
+            // the two results in turn
 #pragma unroll
-            for (int rb = 0; rb < 2; ++rb) {
-                const h8 ph = pf[rb][mb][kq][0][lane], pl = pf[rb][mb][kq][1][lane];
-                s[rb] = ACROSS ? mfma3(xh, xl, ph, pl, s[rb]) : mfma3(ph, pl, xh, xl, s[rb]);
-            }
+            for (int p = 0; p < 3; ++p)
+#pragma unroll
+                for (int rb = 0; rb < 2; ++rb) {
+                    const h8 a = p == 0 ? xl : xh, b = p == 1 ? pl[rb] : ph[rb];
+                    y[rb] = ACROSS ? __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, y[rb], 0, 0, 0) : __builtin_amdgcn_mfma_f32_32x32x16_f16(b, a, y[rb], 0, 0, 0);
+                }
         }
-#pragma unroll
-    for (int rb = 0; rb < 2; ++rb)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) y[rb][e] = s[rb][e] * kOrthUnscale;
 }
 
 __global__ __launch_bounds__(kNarrowThreads, 2) void orth_narrow_kernel(NarrowList L)
@@ -673,7 +703,7 @@ __global__ __launch_bounds__(kNarrowThreads, 2) void orth_narrow_kernel(NarrowLi
     const int m = tall ? q.cols : q.rows, n = tall ? q.rows : q.cols;
     const int rstride = tall ? 1 : q.cols, cstride = tall ? q.cols : 1;
     auto place = [&](int r, int col) { return (uint32_t)(r * rstride + col * cstride); };
-    f32x16 x[kNarrowTiles][2];
+    f32x16 u[kNarrowTiles][2];
     double sq = 0.0;
 #pragma unroll
     for (int i = 0; i < kNarrowTiles; ++i) {
@@ -681,7 +711,7 @@ __global__ __launch_bounds__(kNarrowThreads, 2) void orth_narrow_kernel(NarrowLi
 #pragma unroll
         for (int mb = 0; mb < 2; ++mb)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) x[i][mb][e] = 0.f;
+            for (int e = 0; e < 16; ++e) u[i][mb][e] = 0.f;
         if (n0 >= n) continue;
 #pragma unroll
         for (int mb = 0; mb < 2; ++mb) {
@@ -701,7 +731,7 @@ __global__ __launch_bounds__(kNarrowThreads, 2) void orth_narrow_kernel(NarrowLi
             }
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                x[i][mb][e] = v[e];
+                u[i][mb][e] = v[e];
                 sq += (double)v[e] * v[e];
             }
         }
@@ -719,12 +749,17 @@ __global__ __launch_bounds__(kNarrowThreads, 2) void orth_narrow_kernel(NarrowLi
     for (int w = 0; w < kNarrowWaves; ++w) sq += S.red[w];
     const double norm = sqrt(sq), d = norm < (double)L.s.eps ? (double)L.s.eps : norm;      // (a NaN stays one)
     const double inv = d == 0.0 ? 0.0 : 1.0 / d;                                             // (eps = 0 and a zero matrix)
+    const double scale = inv * (double)kOrthScale;
+    Pieces x[kNarrowTiles];
 #pragma unroll
     for (int i = 0; i < kNarrowTiles; ++i)
 #pragma unroll
-        for (int mb = 0; mb < 2; ++mb)
+        for (int mb = 0; mb < 2; ++mb) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) x[i][mb][e] = (float)((double)x[i][mb][e] * inv);
+            for (int e = 0; e < 16; ++e) u[i][mb][e] = (float)((double)u[i][mb][e] * scale);
+#pragma unroll
+            for (int kq = 0; kq < 2; ++kq) result_pieces(u[i][mb], kq, 1.f, x[i].h[mb][kq], x[i].l[mb][kq]);
+        }
     __syncthreads();
 
     for (int step = 0; step < L.steps; ++step) {
@@ -745,18 +780,22 @@ __global__ __launch_bounds__(kNarrowThreads, 2) void orth_narrow_kernel(NarrowLi
                 for (int kq = 0; kq < 2; ++kq) {
                     h8 h[2], l[2];
 #pragma unroll
-                    for (int rb = 0; rb < 2; ++rb) tile_pieces(z[rb], kq, h[rb], l[rb]);
-                    g[0] = mfma3(h[0], l[0], h[0], l[0], g[0]);
-                    g[1] = mfma3(h[0], l[0], h[1], l[1], g[1]);
-                    g[2] = mfma3(h[1], l[1], h[1], l[1], g[2]);
+                    for (int rb = 0; rb < 2; ++rb) result_pieces(z[rb], kq, 1.f / kOrthScale, h[rb], l[rb]);
+#pragma unroll
+                    for (int p = 0; p < 3; ++p)
+#pragma unroll
+                        for (int k = 0; k < 3; ++k)
+                            g[k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(p == 0 ? l[k == 2] : h[k == 2], p == 1 ? l[k > 0] : h[k > 0], g[k], 0, 0, 0);
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
             if (step > 0) {
                 f32x16 y[2];
                 tile_product<false>(x[i], S.pf, lane, y);
-                x[i][0] = y[0];
-                x[i][1] = y[1];
+#pragma unroll
+                for (int rb = 0; rb < 2; ++rb)
+#pragma unroll
+                    for (int kq = 0; kq < 2; ++kq) result_pieces(y[rb], kq, 1.f / kOrthScale, x[i].h[rb][kq], x[i].l[rb][kq]);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -810,9 +849,17 @@ __global__ __launch_bounds__(kNarrowThreads, 2) void orth_narrow_kernel(NarrowLi
         const int n0 = 32 * (wave + kNarrowWaves * i);
         if (n0 >= n) continue;
         const bool across = tall && L.steps > 0;
-        f32x16 y[2] = {x[i][0], x[i][1]};
-        if (across) tile_product<true>(x[i], S.pf, lane, y);
-        else if (L.steps > 0) tile_product<false>(x[i], S.pf, lane, y);
+        f32x16 y[2];
+        if (across) {
+            tile_product<true>(x[i], S.pf, lane, y);
+        } else if (L.steps > 0) {
+            tile_product<false>(x[i], S.pf, lane, y);
+        } else {
+#pragma unroll
+            for (int rb = 0; rb < 2; ++rb)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) y[rb][e] = ((float)x[i].h[rb][e >> 3][e & 7] + (float)x[i].l[rb][e >> 3][e & 7]) * kOrthScale;
+        }
 #pragma unroll
         for (int rb = 0; rb < 2; ++rb) {
             auto at = [&](int e) -> long long {
@@ -822,7 +869,7 @@ __global__ __launch_bounds__(kNarrowThreads, 2) void orth_narrow_kernel(NarrowLi
             float v[16];
             if (L.s.muon) orth_gather(q.out, L.s.out_dtype, at, v);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) v[e] = L.s.muon ? v[e] * L.s.keep - q.wscale * y[rb][e] : y[rb][e];
+            for (int e = 0; e < 16; ++e) v[e] = L.s.muon ? v[e] * L.s.keep - q.wscale * (y[rb][e] * kOrthUnscale) : y[rb][e] * kOrthUnscale;
             orth_scatter(q.out, L.s.out_dtype, at, v);
         }
     }
