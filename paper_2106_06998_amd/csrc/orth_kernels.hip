@@ -40,12 +40,11 @@ struct OrthMat {
     void *out;
     float *M;
     _Float16 *X, *Xt, *Xt2, *A, *P;     // fragment order
-    float *A32;                         // [mp][mp]
     double *sq;                         // partial sums of squares
     float *part;                        // partial products of X X^T, [tile][split][tile values]
     int rows, cols, m, n, mp, np;       // m <= n
     int nsq;
-    int big_a, big_x;                   // tiles of 128 x 128 (else 64 x 64) of A and P, of X
+    int big[3];                         // tiles of 128 x 128 (else 64 x 64) of A, of P, of X
     int gsplits, gkbs, psplits, pkbs;   // X X^T and A A: runs of blocks of 16 along the sum, and their length
     float wscale;                       // lr sqrt(max(1, rows / cols))
 };
@@ -99,14 +98,14 @@ template <int N, class At> __device__ inline void orth_gather(const void *p, int
     if (dtype == XCONV_F32) {
 #pragma unroll
         for (int k = 0; k < N; ++k) {
-            const long long i = at(k);
+            const auto i = at(k);
             v[k] = static_cast<const float *>(p)[i < 0 ? 0 : i];
         }
     } else {
         uint16_t h[N];
 #pragma unroll
         for (int k = 0; k < N; ++k) {
-            const long long i = at(k);
+            const auto i = at(k);
             h[k] = static_cast<const uint16_t *>(p)[i < 0 ? 0 : i];
         }
 #pragma unroll
@@ -114,6 +113,18 @@ template <int N, class At> __device__ inline void orth_gather(const void *p, int
     }
 #pragma unroll
     for (int k = 0; k < N; ++k) v[k] = at(k) < 0 ? 0.f : v[k];
+}
+// the same of a matrix and of one of floats, all loads together
+template <int N, class At> __device__ inline void orth_gather2(const void *p, int dtype, const float *p2, At &&at, float (&v)[N], float (&v2)[N])
+{
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const auto i = at(k);
+        v2[k] = p2[i < 0 ? 0 : i];
+    }
+    orth_gather(p, dtype, at, v);
+#pragma unroll
+    for (int k = 0; k < N; ++k) v2[k] = at(k) < 0 ? 0.f : v2[k];
 }
 template <int N, class At> __device__ inline void orth_scatter(void *p, int dtype, At &&at, const float (&v)[N])
 {
@@ -143,7 +154,11 @@ __device__ inline void split8(const float (&s)[8], h8 &h, h8 &l)
         l[i] = lo[0]; l[i + 1] = lo[1];
     }
 }
-// eight values stored at their place (row r, columns k .. k + 7) of a matrix in fragment order
+// where row r, columns k .. k + 7 of a matrix in fragment order lie (the second numbers 512 values on)
+__device__ inline _Float16 *place_of(_Float16 *frag, int r, int k, int kblocks)
+{
+    return frag + ((size_t)(r >> 5) * kblocks + (k >> 4)) * kBlockHalfs + ((r & 31) + 32 * ((k >> 3) & 1)) * 8;
+}
 __device__ inline void put_pieces(_Float16 *frag, int r, int k, int kblocks, const float (&v)[8])
 {
     float s[8];
@@ -151,7 +166,7 @@ __device__ inline void put_pieces(_Float16 *frag, int r, int k, int kblocks, con
     for (int i = 0; i < 8; ++i) s[i] = v[i] * kOrthScale;
     h8 h, l;
     split8(s, h, l);
-    _Float16 *p = frag + ((size_t)(r >> 5) * kblocks + (k >> 4)) * kBlockHalfs + ((r & 31) + 32 * ((k >> 3) & 1)) * 8;
+    _Float16 *p = place_of(frag, r, k, kblocks);
     *reinterpret_cast<h8 *>(p) = h;
     *reinterpret_cast<h8 *>(p + 512) = l;
 }
@@ -275,11 +290,12 @@ __global__ __launch_bounds__(kThreads) void orth_start_kernel(OrthRef L)
         const int u = k * kThreads + threadIdx.x, r = r0 + u / kOrthTile, c = c0 + u % kOrthTile;
         return r < q.rows && c < q.cols ? (long long)r * q.cols + c : -1;
     };
-    orth_gather(q.G, L.s.g_dtype, place, v);
     if (L.s.muon) {
-        orth_gather(q.M, XCONV_F32, place, m);
+        orth_gather2(q.G, L.s.g_dtype, q.M, place, v, m);
 #pragma unroll
         for (int k = 0; k < kRound; ++k) v[k] = update_of(v[k], m[k], L.s);
+    } else {
+        orth_gather(q.G, L.s.g_dtype, place, v);
     }
     const double norm = sqrt(sum_squares(q)), d = norm < (double)L.s.eps ? (double)L.s.eps : norm;      // (a NaN stays one)
     const double inv = d == 0.0 ? 0.0 : 1.0 / d;                                                         // (eps = 0 and a zero matrix)
@@ -301,7 +317,7 @@ __global__ __launch_bounds__(kThreads) void orth_start_kernel(OrthRef L)
 // step), the second one's straight into the registers of the two waves that use them, a step ahead: both ways through LDS, its
 // bandwidth is what the matrix instructions wait for.
 template <int MT, int NT> struct Tile {
-    static constexpr int TM = 64 * MT, TN = 64 * NT, KS = 4 / MT, kUnits = 2 * MT * KS * 128, kPer = kUnits / kThreads;
+    static constexpr int TM = 64 * MT, TN = 64 * NT, KS = MT == 1 ? 8 : 2, kUnits = 2 * MT * KS * 128, kPer = kUnits / kThreads;
     f32x16 acc[MT][NT];
     struct Right {
         h8 f[KS][2][NT];
@@ -316,17 +332,21 @@ template <int MT, int NT> struct Tile {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
     }
-    __device__ static void load(u32x4 (&r)[kPer], const _Float16 *Fa, int ra, int kblocks, int kb)
+    // (blocks from kb1 on are zeros)
+    __device__ static void load(u32x4 (&r)[kPer], const _Float16 *Fa, int ra, int kblocks, int kb, int kb1)
     {
         constexpr int kRun = KS * 128;
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
             // (a run is a whole number of rounds of the workgroup)
             const int blk = j * kThreads / kRun, off = (j * kThreads) % kRun + (int)threadIdx.x;
-            r[j] = reinterpret_cast<const u32x4 *>(Fa + ((size_t)(ra / 32 + blk) * kblocks + kb) * kBlockHalfs)[off];
+            const bool on = KS <= 4 || kb + off / 128 < kb1;
+            const u32x4 v = reinterpret_cast<const u32x4 *>(Fa + ((size_t)(ra / 32 + blk) * kblocks + kb) * kBlockHalfs)[on ? off : 0];
+            r[j] = on ? v : u32x4{0, 0, 0, 0};
         }
     }
-    __device__ static void load(Right &r, const _Float16 *Fb, int rb, int kblocks, int kb)
+    // (any values from kb1 on)
+    template <int PRODUCTS> __device__ static void load(Right &r, const _Float16 *Fb, int rb, int kblocks, int kb, int kb1)
     {
         const int wb = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) & 1), lane = threadIdx.x & 63;
 #pragma unroll
@@ -334,49 +354,49 @@ template <int MT, int NT> struct Tile {
 #pragma unroll
             for (int k = 0; k < KS; ++k)
 #pragma unroll
-                for (int p = 0; p < 2; ++p)
-                    r.f[k][p][j] = reinterpret_cast<const h8 *>(Fb + ((size_t)(rb / 32 + wb * NT + j) * kblocks + kb + k) * kBlockHalfs + p * 512)[lane];
+                for (int p = 0; p < (PRODUCTS > 1 ? 2 : 1); ++p)
+                    r.f[k][p][j] = reinterpret_cast<const h8 *>(Fb + ((size_t)(rb / 32 + wb * NT + j) * kblocks + (KS <= 4 ? kb + k : min(kb + k, kb1 - 1))) * kBlockHalfs + p * 512)[lane];
     }
     __device__ static void store(const u32x4 (&r)[kPer], u32x4 *lds)
     {
 #pragma unroll
         for (int j = 0; j < kPer; ++j) lds[j * kThreads + threadIdx.x] = r[j];
     }
-    __device__ void multiply(const u32x4 *lds, const Right &b)
+    template <int PRODUCTS> __device__ void multiply(const u32x4 *lds, const Right &b)
     {
         const int wa = threadIdx.x >> 7, lane = threadIdx.x & 63;
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
             h8 a[2][MT];
 #pragma unroll
-            for (int p = 0; p < 2; ++p)
+            for (int p = 0; p < (PRODUCTS > 1 ? 2 : 1); ++p)
 #pragma unroll
                 for (int i = 0; i < MT; ++i) a[p][i] = __builtin_bit_cast(h8, lds[((wa * MT + i) * KS + k) * 128 + p * 64 + lane]);
             // the small products first
 #pragma unroll
-            for (int p = 0; p < 3; ++p)
+            for (int p = 3 - PRODUCTS; p < 3; ++p)
 #pragma unroll
                 for (int i = 0; i < MT; ++i)
 #pragma unroll
                     for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[p == 0][i], b.f[k][p == 1][j], acc[i][j], 0, 0, 0);
         }
     }
-    // lds: two steps
-    __device__ void product(const _Float16 *Fa, int ra, const _Float16 *Fb, int rb, int kblocks, int kb0, int kb1, u32x4 *lds)
+    // lds: two steps; PRODUCTS = 1: the first numbers' product only
+    template <int PRODUCTS = 3> __device__ void product(const _Float16 *Fa, int ra, const _Float16 *Fb, int rb, int kblocks, int kb0, int kb1, u32x4 *lds)
     {
         clear();
         u32x4 r[kPer];
         Right b0, b1;
-        load(b0, Fb, rb, kblocks, kb0);
-        load(r, Fa, ra, kblocks, kb0);
+        load<PRODUCTS>(b0, Fb, rb, kblocks, kb0, kb1);
+        load(r, Fa, ra, kblocks, kb0, kb1);
         store(r, lds);
         __syncthreads();
         int at = 0;
         // one step with the next one's loads under way
         auto step = [&](const Right &now, Right &next, int kb) {
-            load(next, Fb, rb, kblocks, kb);
-            load(r, Fa, ra, kblocks, kb);
-            multiply(lds + at * kUnits, now);
+            load<PRODUCTS>(next, Fb, rb, kblocks, kb, kb1);
+            load(r, Fa, ra, kblocks, kb, kb1);
+            multiply<PRODUCTS>(lds + at * kUnits, now);
             at ^= 1;
             store(r, lds + at * kUnits);
             __syncthreads();
@@ -388,9 +408,9 @@ template <int MT, int NT> struct Tile {
         }
         if (kb < kb1) {
             step(b0, b1, kb);
-            multiply(lds + at * kUnits, b1);
+            multiply<PRODUCTS>(lds + at * kUnits, b1);
         } else {
-            multiply(lds + at * kUnits, b0);
+            multiply<PRODUCTS>(lds + at * kUnits, b0);
         }
         __syncthreads();
     }
@@ -436,7 +456,7 @@ template <int MT, int NT> struct Tile {
 };
 
 union OrthLds {
-    u32x4 stage[2 * 1024];      // (1024 units a step, with either tile)
+    u32x4 stage[2 * 2048];
     float small[64][64 + 1];
     float large[128][128 + 1];
 };
@@ -455,7 +475,7 @@ __device__ inline void pair_of(int b, int &i, int &j)
     i = b - j * (j + 1) / 2;
 }
 
-// t is part of A = X X^T (POLY = 0; also kept as plain floats) or of A A (1; becomes P = a I + b A + c A A).  Its rows are i0 on
+// t is part of A = X X^T (POLY = 0) or of A A (1: P = a I + b A + c A A is stored).  Its rows are i0 on
 // and its columns j0 on (STEP = 32), or, when it is the part (i, j) of a tile of 128, every other run of 32 of them (STEP = 64).
 // What lies on and above the diagonal blocks of 32 x 32 is stored on both sides of the diagonal, so that A and P are symmetric
 // to the last bit whatever the tiles.
@@ -463,19 +483,19 @@ template <int T, int POLY, int STEP> __device__ inline void put_square(float (*t
 {
     _Float16 *out = POLY ? q.P : q.A;
     auto along = [](int from, int r) { return from + STEP * (r >> 5) + (r & 31); };
-    for (int u = threadIdx.x; u < T * T; u += kThreads) {
-        const int r = u / T, c = u % T, row = along(i0, r), col = along(j0, c);
-        if (row >> 5 > col >> 5) continue;
-        float *p = q.A32 + (size_t)row * q.mp + col;
+    // eight values of the result, A A's being v, at (row, col) and right of it
+    auto put = [&](int row, int col, float (&v)[8]) {
         if constexpr (POLY == 1) {
-            float v = s.b * *p + s.c * t[r][c];
-            if (row == col && row < q.m) v += s.a;
-            t[r][c] = v;
-        } else {
-            *p = t[r][c];
+            const _Float16 *p = place_of(q.A, row, col, q.mp / 16);
+            const h8 h = *reinterpret_cast<const h8 *>(p), l = *reinterpret_cast<const h8 *>(p + 512);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                v[i] = s.b * (((float)h[i] + (float)l[i]) * (1.f / kOrthScale)) + s.c * v[i];
+                if (row == col + i && row < q.m) v[i] += s.a;
+            }
         }
-    }
-    __syncthreads();
+        put_pieces(out, row, col, q.mp / 16, v);
+    };
     for (int u = threadIdx.x; u < T * T / 8; u += kThreads) {
         const int r = u % T, c = u / T * 8;
         float v[8];
@@ -485,7 +505,7 @@ template <int T, int POLY, int STEP> __device__ inline void put_square(float (*t
             if (row >> 5 <= col >> 5) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[i] = diagonal && (c + i & 31) < (r & 31) ? t[(r & ~31) + (c + i & 31)][(c & ~31) + (r & 31)] : t[r][c + i];
-                put_pieces(out, row, col, q.mp / 16, v);
+                put(row, col, v);
             }
         }
         {
@@ -494,7 +514,7 @@ template <int T, int POLY, int STEP> __device__ inline void put_square(float (*t
             if (row >> 5 < col >> 5) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[i] = t[c + i][r];
-                put_pieces(out, col, row, q.mp / 16, v);
+                put(col, row, v);
             }
         }
     }
@@ -517,14 +537,13 @@ template <int T, int POLY> __device__ inline void square_tile(const OrthMat &q, 
     t.spread(tile_of<T>(lds));
     put_square<T, POLY, 32>(tile_of<T>(lds), q, s, ti * T, tj * T);
 }
-template <int POLY> __global__ __launch_bounds__(kThreads, 2) void orth_square_kernel(OrthRef L)
+template <int T, int POLY> __global__ __launch_bounds__(kThreads, 2) void orth_square_kernel(OrthRef L)
 {
     __shared__ OrthLds lds;
     int b = xcd_block(blockIdx.x, gridDim.x);
     if (b >= L.total) return;
     const OrthMat &q = L.mat[find_mat(L.first, L.s.count, b)];
-    if (q.big_a) square_tile<128, POLY>(q, L.s, b, lds);
-    else square_tile<64, POLY>(q, L.s, b, lds);
+    square_tile<T, POLY>(q, L.s, b, lds);
 }
 
 // adds up the runs of a product, in order: 64 x 64 values a workgroup
@@ -533,14 +552,14 @@ template <int POLY> __global__ __launch_bounds__(kThreads) void orth_join_kernel
     __shared__ float t[64][64 + 1];
     int b = blockIdx.x;
     const OrthMat &q = L.mat[find_mat(L.first, L.s.count, b)];
-    const int splits = POLY ? q.psplits : q.gsplits, parts = q.big_a ? 4 : 1, pair = b / parts, part = b % parts;
+    const int splits = POLY ? q.psplits : q.gsplits, parts = q.big[POLY] ? 4 : 1, pair = b / parts, part = b % parts;
     int ti, tj;
     pair_of(pair, ti, tj);
     Tile<1, 1> sum;
     sum.clear();
     for (int k = 0; k < splits; ++k) sum.add_part(q.part + ((size_t)(pair * splits + k) * parts + part) * 64 * 64);
     sum.spread(t);
-    if (q.big_a) put_square<64, POLY, 64>(t, q, L.s, ti * 128 + 32 * (part >> 1), tj * 128 + 32 * (part & 1));
+    if (q.big[POLY]) put_square<64, POLY, 64>(t, q, L.s, ti * 128 + 32 * (part >> 1), tj * 128 + 32 * (part & 1));
     else put_square<64, POLY, 32>(t, q, L.s, ti * 64, tj * 64);
 }
 
@@ -567,24 +586,21 @@ template <int T> __device__ inline void finish(const float (*t)[T + 1], const Or
     }
 }
 
-// X <- P X, from the transposed X (Xt, or Xt2 when odd) to X and the other transposed one; last: to the result instead
-template <int T> __device__ inline void apply_tile(const OrthMat &q, const OrthScalars &s, int b, int odd, int last, OrthLds &lds)
-{
-    const TileAt at = tile_at<T, T>(q, b);
-    Tile<T / 64, T / 64> t;
-    t.product(q.P, at.m0, odd ? q.Xt2 : q.Xt, at.n0, q.mp / 16, 0, q.mp / 16, lds.stage);
-    t.spread(tile_of<T>(lds));
-    if (last) finish<T>(tile_of<T>(lds), q, s, at.m0, at.n0);
-    else emit_x<T, T>(tile_of<T>(lds), q, odd ? q.Xt : q.Xt2, at.m0, at.n0);
-}
-__global__ __launch_bounds__(kThreads, 2) void orth_apply_kernel(OrthRef L, int odd, int last)
+// X <- P X, from the transposed X (Xt, or Xt2 when odd) to X and the other transposed one.  LAST 1: to the result instead.  2: the
+// same with the first fp16 numbers alone.  What that drops, 2^-12 of P and of X, goes into no further step: it is an eighth of what
+// rounding O to bf16 drops, and far below the rounding of 16-bit weights, of which the update is a small part.
+template <int T, int LAST> __global__ __launch_bounds__(kThreads, 2) void orth_apply_kernel(OrthRef L, int odd)
 {
     __shared__ OrthLds lds;
     int b = xcd_block(blockIdx.x, gridDim.x);
     if (b >= L.total) return;
     const OrthMat &q = L.mat[find_mat(L.first, L.s.count, b)];
-    if (q.big_x) apply_tile<128>(q, L.s, b, odd, last, lds);
-    else apply_tile<64>(q, L.s, b, odd, last, lds);
+    const TileAt at = tile_at<T, T>(q, b);
+    Tile<T / 64, T / 64> t;
+    t.template product<LAST == 2 ? 1 : 3>(q.P, at.m0, odd ? q.Xt2 : q.Xt, at.n0, q.mp / 16, 0, q.mp / 16, lds.stage);
+    t.spread(tile_of<T>(lds));
+    if constexpr (LAST > 0) finish<T>(tile_of<T>(lds), q, L.s, at.m0, at.n0);
+    else emit_x<T, T>(tile_of<T>(lds), q, odd ? q.Xt : q.Xt2, at.m0, at.n0);
 }
 
 // no steps: X_0 is the result
@@ -629,16 +645,12 @@ static_assert(sizeof(NarrowList) <= 4096, "kernel arguments");
 
 struct NarrowLds {
     union {
-        float gram[kNarrowWaves][3][16][64];
-        struct {
-            h8 af[2][2][2][2][64];
-            float p[64][65];
-        };
+        f32x4 gram[kNarrowWaves][4][4][64];     // [wave][block][registers / 4][lane] of X X^T
+        double red[kNarrowWaves];
     };
-    float a[64][65];
-    h8 pf[2][2][2][2][64];     // [rows / 32][k / 32][half][number][lane]
-    double red[kNarrowWaves];
+    h8 af[2][2][2][2][64], pf[2][2][2][2][64];  // A and P: [rows / 32][k / 32][half][number][lane]
 };
+static_assert(sizeof(NarrowLds) <= 160 * 1024, "LDS of a compute unit");
 
 // registers 8 kq .. 8 kq + 7 of a result, scaled, as an operand
 __device__ inline void result_pieces(const f32x16 &x, int kq, float scale, h8 &h, h8 &l)
@@ -659,16 +671,6 @@ __device__ inline f32x16 mfma3(const h8 &ah, const h8 &al, const h8 &bh, const h
     c = __builtin_amdgcn_mfma_f32_32x32x16_f16(ah, bl, c, 0, 0, 0);
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(ah, bh, c, 0, 0, 0);
 }
-// the thread's fragment (one of 512) of a symmetric matrix t, k in the order of result_row
-__device__ inline void build_fragments(const float (*t)[65], h8 (*f)[2][2][2][64])
-{
-    const int lane = threadIdx.x & 63, kq = (threadIdx.x >> 6) & 1, mb = (threadIdx.x >> 7) & 1, rb = threadIdx.x >> 8;
-    float v[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = t[32 * rb + (lane & 31)][32 * mb + 16 * kq + result_row(j, lane)] * kOrthScale;
-    split8(v, f[rb][mb][kq][0][lane], f[rb][mb][kq][1][lane]);
-}
-
 // P times a tile of X, scaled twice; ACROSS: transposed
 template <bool ACROSS> __device__ inline void tile_product(const Pieces &x, const h8 (*pf)[2][2][2][64], int lane, f32x16 (&y)[2])
 {
@@ -693,80 +695,115 @@ template <bool ACROSS> __device__ inline void tile_product(const Pieces &x, cons
         }
 }
 
-__global__ __launch_bounds__(kNarrowThreads, 2) void orth_narrow_kernel(NarrowList L)
+// One value of a buffer at a lane's byte offset plus a uniform one; past the end: zero, or nothing stored
+template <int DT> __device__ inline float buffer_get(__amdgpu_buffer_rsrc_t b, int lane_off, int off)
+{
+    if constexpr (DT == XCONV_F32) return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(b, lane_off, off, 0));
+    else return st16_to_f32<DT>((uint16_t)__builtin_amdgcn_raw_buffer_load_b16(b, lane_off, off, 0));
+}
+template <int DT> __device__ inline void buffer_put(__amdgpu_buffer_rsrc_t b, int lane_off, int off, float v)
+{
+    if constexpr (DT == XCONV_F32) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), b, lane_off, off, 0);
+    else if constexpr (DT == XCONV_BF16) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(short, (__bf16)v), b, lane_off, off, 0);
+    else __builtin_amdgcn_raw_buffer_store_b16((short)f32_to_f16_rne(v), b, lane_off, off, 0);
+}
+constexpr int kNarrowOut = 0x40000000;      // a lane's offset of what does not exist
+
+// GT, OT: types of G and of the result.  A call of a small matrix is latency, of the code's own fetching too: loads and stores are
+// buffer instructions, whose bounds checks take the place of masks, and all loads go out before the first is waited for.
+template <int GT, int OT, bool MUON> __global__ __launch_bounds__(kNarrowThreads, 2) void orth_narrow_kernel(NarrowList L)
 {
     extern __shared__ char narrow_lds[];
     NarrowLds &S = *reinterpret_cast<NarrowLds *>(narrow_lds);
     const NarrowMat &q = L.mat[blockIdx.x];
-    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 31;
+    constexpr int GE = GT == XCONV_F32 ? 4 : 2, OE = OT == XCONV_F32 ? 4 : 2;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 31, hrow = 4 * (lane >> 5);
     const bool tall = q.rows > q.cols;
     const int m = tall ? q.cols : q.rows, n = tall ? q.rows : q.cols;
-    const int rstride = tall ? 1 : q.cols, cstride = tall ? q.cols : 1;
-    auto place = [&](int r, int col) { return (uint32_t)(r * rstride + col * cstride); };
-    f32x16 u[kNarrowTiles][2];
-    double sq = 0.0;
+    const int rstride = tall ? 1 : q.cols, cstride = tall ? q.cols : 1, count = q.rows * q.cols;
+    const auto G = __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(q.G), 0, count * GE, 0x00020000);
+    const auto M = __builtin_amdgcn_make_buffer_rsrc(q.M, 0, MUON ? count * 4 : 0, 0x00020000);
+    const auto O = __builtin_amdgcn_make_buffer_rsrc(q.out, 0, count * OE, 0x00020000);
+    // a wave's part of A and P between the products: rows 32 mb + 16 kq .. of columns 32 rb ..
+    const int rb0 = wave >> 2, mb0 = (wave >> 1) & 1, kq0 = wave & 1;
+    // register e of rows 32 mb .. lies a multiple of the rows' distance, the same for all lanes, behind the lane's own place
+    auto row_of = [](int mb, int e) { return 32 * mb + 8 * (e >> 2) + (e & 3); };
+    auto first_of = [&](int i) { return 32 * (wave + kNarrowWaves * i); };
+    f32x16 u[kNarrowTiles][2], mo[MUON ? kNarrowTiles : 1][2];
 #pragma unroll
     for (int i = 0; i < kNarrowTiles; ++i) {
-        const int n0 = 32 * (wave + kNarrowWaves * i);
+        if (first_of(i) >= n) continue;
+        const int col = first_of(i) + c, place = col < n ? hrow * rstride + col * cstride : kNarrowOut / 4;
 #pragma unroll
         for (int mb = 0; mb < 2; ++mb)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) u[i][mb][e] = 0.f;
-        if (n0 >= n) continue;
-#pragma unroll
-        for (int mb = 0; mb < 2; ++mb) {
-            auto at = [&](int e) -> long long {
-                const int r = 32 * mb + result_row(e, lane), col = n0 + c;
-                return r < m && col < n ? (long long)place(r, col) : -1;
-            };
-            float v[16], mo[16];
-            orth_gather(q.G, L.s.g_dtype, at, v);
-            if (L.s.muon) {
-                orth_gather(q.M, XCONV_F32, at, mo);
-#pragma unroll
-                for (int e = 0; e < 16; ++e) mo[e] = mo[e] + (v[e] - mo[e]) * (1.f - L.s.mu);
-                orth_scatter(q.M, XCONV_F32, at, mo);
-#pragma unroll
-                for (int e = 0; e < 16; ++e) v[e] = update_of(v[e], mo[e], L.s);
+            for (int e = 0; e < 16; ++e) {
+                const int at = hrow + row_of(mb, e) < m ? place : kNarrowOut / 4, off = row_of(mb, e) * rstride;
+                u[i][mb][e] = buffer_get<GT>(G, at * GE, off * GE);
+                if constexpr (MUON) mo[i][mb][e] = buffer_get<XCONV_F32>(M, at * 4, off * 4);
             }
+    }
+    double sq = 0.0;
+#pragma unroll
+    for (int i = 0; i < kNarrowTiles; ++i) {
+        if (first_of(i) >= n) continue;
+        const int col = first_of(i) + c, place = col < n ? hrow * rstride + col * cstride : kNarrowOut / 4;
+#pragma unroll
+        for (int mb = 0; mb < 2; ++mb)
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                u[i][mb][e] = v[e];
-                sq += (double)v[e] * v[e];
+                if constexpr (MUON) {
+                    const float g = u[i][mb][e], w = mo[i][mb][e] + (g - mo[i][mb][e]) * (1.f - L.s.mu);
+                    const int at = hrow + row_of(mb, e) < m ? place : kNarrowOut / 4, off = row_of(mb, e) * rstride;
+                    buffer_put<XCONV_F32>(M, at * 4, off * 4, w);
+                    u[i][mb][e] = update_of(g, w, L.s);
+                }
+                sq += (double)u[i][mb][e] * u[i][mb][e];
             }
-        }
-        __builtin_amdgcn_sched_barrier(0);
     }
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) sq += __shfl_xor(sq, o);
     if (lane == 0) S.red[wave] = sq;
-    // P = I for the first X X^T, which needs X the other way round only
-    for (int u = tid; u < 64 * 64; u += kNarrowThreads) S.a[u >> 6][u & 63] = (u >> 6) == (u & 63) ? 1.f : 0.f;
+    {
+        // P = I for the first X X^T, which needs X the other way round only
+        h8 one, none;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            one[j] = (_Float16)(32 * mb0 + 16 * kq0 + result_row(j, lane) == 32 * rb0 + c ? kOrthScale : 0.f);
+            none[j] = (_Float16)0.f;
+        }
+        S.pf[rb0][mb0][kq0][0][lane] = one;
+        S.pf[rb0][mb0][kq0][1][lane] = none;
+    }
     __syncthreads();
-    build_fragments(S.a, S.pf);
     sq = 0.0;
 #pragma unroll
     for (int w = 0; w < kNarrowWaves; ++w) sq += S.red[w];
     const double norm = sqrt(sq), d = norm < (double)L.s.eps ? (double)L.s.eps : norm;      // (a NaN stays one)
-    const double inv = d == 0.0 ? 0.0 : 1.0 / d;                                             // (eps = 0 and a zero matrix)
-    const double scale = inv * (double)kOrthScale;
+    // 4096 / d in two factors, the first a power of two: a norm far from one takes a single float out of its range
+    const int power = d > 0.0 && d < 1e300 ? max(-126, min(126, -ilogb(d))) : 0;
+    const float s1 = ldexpf(1.f, power), s2 = d == 0.0 ? 0.f : (float)((double)kOrthScale / d / (double)s1);      // (eps = 0 and a zero matrix)
     Pieces x[kNarrowTiles];
 #pragma unroll
-    for (int i = 0; i < kNarrowTiles; ++i)
+    for (int i = 0; i < kNarrowTiles; ++i) {
+        if (first_of(i) >= n) continue;
 #pragma unroll
-        for (int mb = 0; mb < 2; ++mb) {
+        for (int mb = 0; mb < 2; ++mb)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) u[i][mb][e] = (float)((double)u[i][mb][e] * scale);
+            for (int kq = 0; kq < 2; ++kq) {
+                float v[8];
 #pragma unroll
-            for (int kq = 0; kq < 2; ++kq) result_pieces(u[i][mb], kq, 1.f, x[i].h[mb][kq], x[i].l[mb][kq]);
-        }
-    __syncthreads();
+                for (int j = 0; j < 8; ++j) v[j] = u[i][mb][8 * kq + j] * s1 * s2;
+                split8(v, x[i].h[mb][kq], x[i].l[mb][kq]);
+            }
+    }
+    __syncthreads();     // (the sums of squares lie where X X^T goes)
 
     for (int step = 0; step < L.steps; ++step) {
         // X <- P X, and the wave's part of X X^T
-        f32x16 g[3];
+        f32x16 g[4];
 #pragma unroll
-        for (int k = 0; k < 3; ++k)
+        for (int k = 0; k < 4; ++k)
 #pragma unroll
             for (int e = 0; e < 16; ++e) g[k][e] = 0.f;
 #pragma unroll
@@ -784,8 +821,8 @@ __global__ __launch_bounds__(kNarrowThreads, 2) void orth_narrow_kernel(NarrowLi
 #pragma unroll
                     for (int p = 0; p < 3; ++p)
 #pragma unroll
-                        for (int k = 0; k < 3; ++k)
-                            g[k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(p == 0 ? l[k == 2] : h[k == 2], p == 1 ? l[k > 0] : h[k > 0], g[k], 0, 0, 0);
+                        for (int k = 0; k < 4; ++k)
+                            g[k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(p == 0 ? l[k >> 1] : h[k >> 1], p == 1 ? l[k & 1] : h[k & 1], g[k], 0, 0, 0);
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
@@ -800,56 +837,73 @@ __global__ __launch_bounds__(kNarrowThreads, 2) void orth_narrow_kernel(NarrowLi
             __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll
-        for (int k = 0; k < 3; ++k)
+        for (int k = 0; k < 4; ++k)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) S.gram[wave][k][e][lane] = g[k][e];
+            for (int e = 0; e < 4; ++e) S.gram[wave][k][e][lane] = f32x4{g[k][4 * e], g[k][4 * e + 1], g[k][4 * e + 2], g[k][4 * e + 3]};
         __syncthreads();
-        // A, added up in order of the waves
-        for (int u = tid; u < 3 * 16 * 64; u += kNarrowThreads) {
-            const int k = u >> 10, e = (u >> 6) & 15, l = u & 63;
-            float v = 0.f;
+        // The wave's part of A, added up in order of the waves: eight registers of a block, which are a fragment of A as an
+        // operand as well (A is symmetric)
+        float part[8], v[8];
 #pragma unroll
-            for (int w = 0; w < kNarrowWaves; ++w) v += S.gram[w][k][e][l];
-            v *= kOrthUnscale;
-            const int r = (k == 2 ? 32 : 0) + result_row(e, l), col = (k > 0 ? 32 : 0) + (l & 31);
-            S.a[r][col] = v;
-            if (k == 1) S.a[col][r] = v;
-        }
-        __syncthreads();
-        build_fragments(S.a, S.af);
-        __syncthreads();
-        // P = a I + b A + c A A: one block of 32 x 32 a wave
-        if (wave < 3) {
-            const int r0 = wave == 2, c0 = wave > 0;
-            f32x16 t;
+        for (int j = 0; j < 8; ++j) part[j] = 0.f;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) t[e] = 0.f;
+        for (int w = 0; w < kNarrowWaves; ++w)
 #pragma unroll
-            for (int mb = 0; mb < 2; ++mb)
+            for (int j = 0; j < 8; j += 4) {
+                const f32x4 t = S.gram[w][2 * mb0 + rb0][2 * kq0 + j / 4][lane];
 #pragma unroll
-                for (int kq = 0; kq < 2; ++kq)
-                    t = mfma3(S.af[r0][mb][kq][0][lane], S.af[r0][mb][kq][1][lane], S.af[c0][mb][kq][0][lane], S.af[c0][mb][kq][1][lane], t);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int r = 32 * r0 + result_row(e, lane), col = 32 * c0 + c;
-                float v = L.s.b * S.a[r][col] + L.s.c * (t[e] * kOrthUnscale);
-                if (r == col) v += L.s.a;
-                S.p[r][col] = v;
-                if (r0 != c0) S.p[col][r] = v;
+                for (int i = 0; i < 4; ++i) part[j + i] += t[i];
             }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            part[j] *= kOrthUnscale;
+            v[j] = part[j] * kOrthScale;
         }
+        split8(v, S.af[rb0][mb0][kq0][0][lane], S.af[rb0][mb0][kq0][1][lane]);
         __syncthreads();
-        build_fragments(S.p, S.pf);
+        // the same part of P = a I + b A + c A A (two waves make a block of A A, each takes its half)
+        f32x16 t;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) t[e] = 0.f;
+#pragma unroll
+        for (int mb = 0; mb < 2; ++mb)
+#pragma unroll
+            for (int kq = 0; kq < 2; ++kq)
+                t = mfma3(S.af[mb0][mb][kq][0][lane], S.af[mb0][mb][kq][1][lane], S.af[rb0][mb][kq][0][lane], S.af[rb0][mb][kq][1][lane], t);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float square = (kq0 ? t[8 + j] : t[j]) * kOrthUnscale;
+            v[j] = L.s.b * part[j] + L.s.c * square;
+            if (32 * mb0 + 16 * kq0 + result_row(j, lane) == 32 * rb0 + c) v[j] += L.s.a;
+            v[j] *= kOrthScale;
+        }
+        split8(v, S.pf[rb0][mb0][kq0][0][lane], S.pf[rb0][mb0][kq0][1][lane]);
         __syncthreads();
     }
 
     // the last P X, along the rows of the result; no step: X_0
+    const bool across = tall && L.steps > 0;
 #pragma unroll
     for (int i = 0; i < kNarrowTiles; ++i) {
-        const int n0 = 32 * (wave + kNarrowWaves * i);
+        const int n0 = first_of(i);
         if (n0 >= n) continue;
-        const bool across = tall && L.steps > 0;
-        f32x16 y[2];
+        // registers run along the rows from the lane's column, or (across) along the columns from the lane's row
+        const int stride = across ? cstride : rstride, most = (across ? n - n0 : m) - hrow;
+        int place[2], next[2];
+#pragma unroll
+        for (int rb = 0; rb < 2; ++rb) {
+            place[rb] = across ? (32 * rb + c) * rstride + (n0 + hrow) * cstride : hrow * rstride + (n0 + c) * cstride;
+            next[rb] = across ? 0 : 32 * rb;
+            if (across ? 32 * rb + c >= m : n0 + c >= n) place[rb] = kNarrowOut / 4;
+        }
+        auto at = [&](int rb, int e) { return next[rb] + row_of(0, e) < most ? place[rb] : kNarrowOut / 4; };
+        f32x16 w[2], y[2];
+        if constexpr (MUON) {
+#pragma unroll
+            for (int rb = 0; rb < 2; ++rb)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) w[rb][e] = buffer_get<OT>(O, at(rb, e) * OE, (next[rb] + row_of(0, e)) * stride * OE);
+        }
         if (across) {
             tile_product<true>(x[i], S.pf, lane, y);
         } else if (L.steps > 0) {
@@ -861,17 +915,12 @@ __global__ __launch_bounds__(kNarrowThreads, 2) void orth_narrow_kernel(NarrowLi
                 for (int e = 0; e < 16; ++e) y[rb][e] = ((float)x[i].h[rb][e >> 3][e & 7] + (float)x[i].l[rb][e >> 3][e & 7]) * kOrthScale;
         }
 #pragma unroll
-        for (int rb = 0; rb < 2; ++rb) {
-            auto at = [&](int e) -> long long {
-                const int r = across ? 32 * rb + c : 32 * rb + result_row(e, lane), col = n0 + (across ? result_row(e, lane) : c);
-                return r < m && col < n ? (long long)place(r, col) : -1;
-            };
-            float v[16];
-            if (L.s.muon) orth_gather(q.out, L.s.out_dtype, at, v);
+        for (int rb = 0; rb < 2; ++rb)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) v[e] = L.s.muon ? v[e] * L.s.keep - q.wscale * (y[rb][e] * kOrthUnscale) : y[rb][e] * kOrthUnscale;
-            orth_scatter(q.out, L.s.out_dtype, at, v);
-        }
+            for (int e = 0; e < 16; ++e) {
+                const float o = y[rb][e] * kOrthUnscale;
+                buffer_put<OT>(O, at(rb, e) * OE, (next[rb] + row_of(0, e)) * stride * OE, MUON ? w[rb][e] * L.s.keep - q.wscale * o : o);
+            }
     }
 }
 
@@ -879,8 +928,8 @@ __global__ __launch_bounds__(kNarrowThreads, 2) void orth_narrow_kernel(NarrowLi
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
 // Tiles of 128 x 128 read half as much for the same products, tiles of 64 x 64 waste less of a small matrix and are four times
-// as many.  X is taken in tiles of 128 where that leaves enough of them for the chip's 256 compute units, of matrices that it does
-// not pad to more than half as many rows again; A, which has fewer, where there are 128.
+// as many.  A product is taken in tiles of 128 where that leaves enough workgroups for the chip's 256 compute units, of matrices
+// that it does not pad to more than half as many rows again.
 //
 // Sums along k are split so that a matrix has about as many workgroups as the chip has compute units, or twice as many of the
 // large tiles: by the matrix' own extents, so that what else is in the call does not change its result.
@@ -896,7 +945,7 @@ bool narrow(const xconv_orth_item &it) { return std::min(it.rows, it.cols) <= kN
 struct OrthPlan {
     int count;
     struct Mat {
-        int m, n, mp, np, big_a, big_x, gsplits, gkbs, psplits, pkbs, tiles_a, tiles_x;
+        int m, n, mp, np, big[3], gsplits, gkbs, psplits, pkbs, tiles[3];
         size_t x, a, part, bytes;
     } mat[kOrthItems];
     size_t bytes;
@@ -907,39 +956,45 @@ OrthPlan plan_orth(const xconv_orth_item *const *items, int count)
     OrthPlan P{};
     P.count = count;
     auto can = [](int m) { return m > 64 && 2 * round_up(m, 128) <= 3 * m; };
-    long long large_x = 0, large_a = 0;
+    auto splits = [](int m, int extent) { return splits_of(m, round_up(extent, 64) / 16); };
+    long long large[3] = {0, 0, 0};     // workgroups with tiles of 128
     for (int i = 0; i < count; ++i) {
         const int m = std::min(items[i]->rows, items[i]->cols), n = std::max(items[i]->rows, items[i]->cols), tm = ceil_div(m, 128);
         if (!can(m)) continue;
-        large_x += (long long)tm * ceil_div(n, 128);
-        large_a += tm * (tm + 1) / 2;
+        large[0] += (long long)tm * (tm + 1) / 2 * splits(m, n);
+        large[1] += (long long)tm * (tm + 1) / 2 * splits(m, m);
+        large[2] += (long long)tm * ceil_div(n, 128);
     }
     P.bytes = up256(sizeof(OrthMat) * kOrthItems);
     for (int i = 0; i < count; ++i) {
         OrthPlan::Mat &q = P.mat[i];
         q.m = std::min(items[i]->rows, items[i]->cols);
         q.n = std::max(items[i]->rows, items[i]->cols);
-        q.big_x = can(q.m) && large_x >= 256;
-        q.big_a = q.big_x && large_a >= 128;
-        const int T = q.big_x ? 128 : 64, ta = q.big_a ? 128 : 64;
+        int T = 64;
+        for (int k = 0; k < 3; ++k) {
+            q.big[k] = can(q.m) && large[k] >= 256;
+            if (q.big[k]) T = 128;
+        }
         q.mp = round_up(q.m, T);
         q.np = round_up(q.n, T);
-        q.tiles_a = q.mp / ta * (q.mp / ta + 1) / 2;
-        q.tiles_x = q.mp / T * (q.np / T);
+        for (int k = 0; k < 3; ++k) {
+            const int t = q.big[k] ? 128 : 64;
+            q.tiles[k] = k < 2 ? q.mp / t * (q.mp / t + 1) / 2 : q.mp / t * (q.np / t);
+        }
         // (extents padded to 64 for the splits, runs of whole steps)
-        auto split = [&](int extent, int &splits, int &run) {
+        auto split = [&](int extent, int &count, int &run) {
             const int kb = round_up(extent, 64) / 16;
-            splits = splits_of(q.m, kb);
-            run = splits > 1 ? round_up(ceil_div(kb, splits), 4) : std::max(q.mp, q.np) / 16;
-            if (splits > 1) splits = ceil_div(kb, run);
+            count = splits(q.m, extent);
+            run = count > 1 ? round_up(ceil_div(kb, count), 4) : std::max(q.mp, q.np) / 16;
+            if (count > 1) count = ceil_div(kb, run);
         };
         split(q.n, q.gsplits, q.gkbs);
         split(q.m, q.psplits, q.pkbs);
         q.x = up256((size_t)q.mp * q.np * 4);
         q.a = up256((size_t)q.mp * q.mp * 4);
-        const int most = std::max(q.gsplits, q.psplits);
-        q.part = most > 1 ? up256((size_t)q.tiles_a * most * ta * ta * 4) : 0;
-        q.bytes = 3 * q.x + 3 * q.a + q.part + up256(kOrthNorms * sizeof(double));
+        auto partial = [&](int k, int count) { return count > 1 ? (size_t)q.tiles[k] * count * (q.big[k] ? 128 * 128 : 64 * 64) * 4 : 0; };
+        q.part = up256(std::max(partial(0, q.gsplits), partial(1, q.psplits)));
+        q.bytes = 3 * q.x + 2 * q.a + q.part + up256(kOrthNorms * sizeof(double));
         P.bytes += q.bytes;
     }
     return P;
@@ -981,8 +1036,23 @@ float wscale_of(const xconv_orth_item &it, const xconv_muon_args *muon)
 
 hipError_t launch_narrow(const xconv_orth_item *items, int count, const xconv_orth_args *args, const xconv_muon_args *muon, hipStream_t st)
 {
-    static const hipError_t set = hipFuncSetAttribute(reinterpret_cast<const void *>(orth_narrow_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(NarrowLds));
+    typedef void (*Kernel)(NarrowList);
+    // [muon][type of G][type of the result]
+    static const Kernel kernels[2][3][3] = {
+        {{orth_narrow_kernel<0, 0, false>, orth_narrow_kernel<0, 1, false>, orth_narrow_kernel<0, 2, false>},
+         {orth_narrow_kernel<1, 0, false>, orth_narrow_kernel<1, 1, false>, orth_narrow_kernel<1, 2, false>},
+         {orth_narrow_kernel<2, 0, false>, orth_narrow_kernel<2, 1, false>, orth_narrow_kernel<2, 2, false>}},
+        {{orth_narrow_kernel<0, 0, true>, orth_narrow_kernel<0, 1, true>, orth_narrow_kernel<0, 2, true>},
+         {orth_narrow_kernel<1, 0, true>, orth_narrow_kernel<1, 1, true>, orth_narrow_kernel<1, 2, true>},
+         {orth_narrow_kernel<2, 0, true>, orth_narrow_kernel<2, 1, true>, orth_narrow_kernel<2, 2, true>}}};
+    static const hipError_t set = [] {
+        hipError_t e = hipSuccess;
+        for (const Kernel *k1 = &kernels[0][0][0]; k1 < &kernels[0][0][0] + 18; ++k1)
+            if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void *>(*k1), hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(NarrowLds));
+        return e;
+    }();
     if (set != hipSuccess) return set;
+    const Kernel kernel = kernels[muon != nullptr][args->g_dtype][args->out_dtype];
     NarrowList L{};
     L.s = scalars_of(args, muon);
     L.steps = args->steps;
@@ -993,7 +1063,7 @@ hipError_t launch_narrow(const xconv_orth_item *items, int count, const xconv_or
             L.mat[n++] = {it.G_dev, it.out_dev, it.M_dev, it.rows, it.cols, wscale_of(it, muon)};
         }
         if (n == kNarrowItems || (i == count && n)) {
-            hipLaunchKernelGGL(orth_narrow_kernel, dim3((unsigned)n), dim3(kNarrowThreads), sizeof(NarrowLds), st, L);
+            hipLaunchKernelGGL(kernel, dim3((unsigned)n), dim3(kNarrowThreads), sizeof(NarrowLds), st, L);
             const hipError_t e = hipGetLastError();
             if (e != hipSuccess) return e;
             n = 0;
@@ -1011,8 +1081,8 @@ hipError_t launch_wide(const xconv_orth_item *const *items, int count, const xco
     char *p = static_cast<char *>(ws);
     auto take = [&](size_t bytes) { char *r = p; p += bytes; return r; };
     OrthMat *list = (OrthMat *)take(up256(sizeof(OrthMat) * kOrthItems));
-    // the first workgroups of the matrices in the launches
-    enum { NORM, START, GRAM, GRAM_JOIN, POLY, POLY_JOIN, APPLY, KINDS };
+    // the first workgroups of the matrices in the launches (products: tiles of 64, of 128)
+    enum { NORM, START, GRAM, GRAM_JOIN = GRAM + 2, POLY, POLY_JOIN = POLY + 2, APPLY, KINDS = APPLY + 2 };
     OrthRef R[KINDS];
     for (OrthRef &r : R) r = OrthRef{L.s, 0, {}, list};
     for (int i = 0; i < count; ++i) {
@@ -1021,17 +1091,22 @@ hipError_t launch_wide(const xconv_orth_item *const *items, int count, const xco
         OrthMat &q = L.mat[i];
         q.G = it.G_dev; q.out = it.out_dev; q.M = it.M_dev;
         q.rows = it.rows; q.cols = it.cols; q.m = f.m; q.n = f.n; q.mp = f.mp; q.np = f.np;
-        q.big_a = f.big_a; q.big_x = f.big_x;
+        for (int k = 0; k < 3; ++k) q.big[k] = f.big[k];
         q.gsplits = f.gsplits; q.gkbs = f.gkbs; q.psplits = f.psplits; q.pkbs = f.pkbs;
         q.X = (_Float16 *)take(f.x); q.Xt = (_Float16 *)take(f.x); q.Xt2 = (_Float16 *)take(f.x);
-        q.A = (_Float16 *)take(f.a); q.P = (_Float16 *)take(f.a); q.A32 = (float *)take(f.a);
+        q.A = (_Float16 *)take(f.a); q.P = (_Float16 *)take(f.a);
         q.part = (float *)take(f.part);
         q.sq = (double *)take(up256(kOrthNorms * sizeof(double)));
         q.nsq = (int)std::min<size_t>(kOrthNorms, ((size_t)it.rows * it.cols + 4095) / 4096);
         q.wscale = wscale_of(it, muon);
-        const int pieces = f.tiles_a * (f.big_a ? 4 : 1);
-        const int blocks[KINDS] = {q.nsq, (f.mp / kOrthTile) * (f.np / kOrthTile), f.tiles_a * f.gsplits, f.gsplits > 1 ? pieces : 0,
-                                   f.tiles_a * f.psplits, f.psplits > 1 ? pieces : 0, f.tiles_x};
+        int blocks[KINDS] = {};
+        blocks[NORM] = q.nsq;
+        blocks[START] = (f.mp / kOrthTile) * (f.np / kOrthTile);
+        blocks[GRAM + f.big[0]] = f.tiles[0] * f.gsplits;
+        blocks[GRAM_JOIN] = f.gsplits > 1 ? f.tiles[0] * (f.big[0] ? 4 : 1) : 0;
+        blocks[POLY + f.big[1]] = f.tiles[1] * f.psplits;
+        blocks[POLY_JOIN] = f.psplits > 1 ? f.tiles[1] * (f.big[1] ? 4 : 1) : 0;
+        blocks[APPLY + f.big[2]] = f.tiles[2];
         for (int k = 0; k < KINDS; ++k) {
             R[k].first[i] = R[k].total;
             R[k].total += blocks[k];
@@ -1039,17 +1114,34 @@ hipError_t launch_wide(const xconv_orth_item *const *items, int count, const xco
     }
     for (int i = 0; i < count; ++i) L.first[i] = R[NORM].first[i];
     const dim3 block(kThreads);
-    auto grid = [&](int k) { return dim3((unsigned)R[k].total); };
-    auto grid8 = [&](int k) { return dim3((unsigned)round_up(R[k].total, 8)); };      // (whole rounds of the eight dies)
-    hipLaunchKernelGGL(orth_norm_kernel, grid(NORM), block, 0, st, L, list);
-    hipLaunchKernelGGL(orth_start_kernel, grid(START), block, 0, st, R[START]);
-    if (args->steps == 0) hipLaunchKernelGGL(orth_none_kernel, grid(START), block, 0, st, R[START]);
+    // (products: whole rounds of the eight dies)
+    auto go = [&](auto kernel, int k, auto... more) {
+        if (!R[k].total) return;
+        const int blocks = (k >= GRAM && k < GRAM_JOIN) || (k >= POLY && k < POLY_JOIN) || k >= APPLY ? round_up(R[k].total, 8) : R[k].total;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), block, 0, st, R[k], more...);
+    };
+    hipLaunchKernelGGL(orth_norm_kernel, dim3((unsigned)R[NORM].total), block, 0, st, L, list);
+    go(orth_start_kernel, START);
+    if (args->steps == 0) go(orth_none_kernel, START);
     for (int k = 0; k < args->steps; ++k) {
-        hipLaunchKernelGGL(orth_square_kernel<0>, grid8(GRAM), block, 0, st, R[GRAM]);
-        if (R[GRAM_JOIN].total) hipLaunchKernelGGL(orth_join_kernel<0>, grid(GRAM_JOIN), block, 0, st, R[GRAM_JOIN]);
-        hipLaunchKernelGGL(orth_square_kernel<1>, grid8(POLY), block, 0, st, R[POLY]);
-        if (R[POLY_JOIN].total) hipLaunchKernelGGL(orth_join_kernel<1>, grid(POLY_JOIN), block, 0, st, R[POLY_JOIN]);
-        hipLaunchKernelGGL(orth_apply_kernel, grid8(APPLY), block, 0, st, R[APPLY], k & 1, k + 1 == args->steps);
+        const int odd = k & 1;
+        const bool last = k + 1 == args->steps;
+        go(orth_square_kernel<64, 0>, GRAM);
+        go(orth_square_kernel<128, 0>, GRAM + 1);
+        go(orth_join_kernel<0>, GRAM_JOIN);
+        go(orth_square_kernel<64, 1>, POLY);
+        go(orth_square_kernel<128, 1>, POLY + 1);
+        go(orth_join_kernel<1>, POLY_JOIN);
+        if (!last) {
+            go(orth_apply_kernel<64, 0>, APPLY, odd);
+            go(orth_apply_kernel<128, 0>, APPLY + 1, odd);
+        } else if (args->out_dtype == XCONV_BF16 || (muon && args->out_dtype == XCONV_F16)) {
+            go(orth_apply_kernel<64, 2>, APPLY, odd);
+            go(orth_apply_kernel<128, 2>, APPLY + 1, odd);
+        } else {
+            go(orth_apply_kernel<64, 1>, APPLY, odd);
+            go(orth_apply_kernel<128, 1>, APPLY + 1, odd);
+        }
     }
     return hipGetLastError();
 }
