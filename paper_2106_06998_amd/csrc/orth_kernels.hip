@@ -64,6 +64,7 @@ struct OrthRef {
     int total;                          // workgroups that have work
     int first[kOrthItems];              // each matrix' first workgroup
     const OrthMat *mat;
+    OrthMat one;                        // the matrix of a list of one
 };
 
 // which matrix workgroup b belongs to (one without workgroups starts where the next one does); b becomes its number in there
@@ -77,6 +78,12 @@ __device__ inline int find_mat(const int *first, int count, int &b)
     }
     b -= first[lo];
     return lo;
+}
+
+__device__ inline OrthMat the_mat(const OrthRef &L, int &b)
+{
+    if (L.s.count == 1) return L.one;
+    return L.mat[find_mat(L.first, L.s.count, b)];
 }
 
 __device__ inline float orth_get(const void *p, int dtype, size_t i)
@@ -280,7 +287,7 @@ __global__ __launch_bounds__(kThreads) void orth_start_kernel(OrthRef L)
 {
     __shared__ float t[kOrthTile][kOrthTile + 1];
     int b = blockIdx.x;
-    const OrthMat &q = L.mat[find_mat(L.first, L.s.count, b)];
+    const OrthMat q = the_mat(L, b);
     const TileAt at = tile_at<kOrthTile, kOrthTile>(q, b);
     const bool tall = q.rows > q.cols;
     const int r0 = tall ? at.n0 : at.m0, c0 = tall ? at.m0 : at.n0;
@@ -317,7 +324,7 @@ __global__ __launch_bounds__(kThreads) void orth_start_kernel(OrthRef L)
 // step), the second one's straight into the registers of the two waves that use them, a step ahead: both ways through LDS, its
 // bandwidth is what the matrix instructions wait for.
 template <int MT, int NT> struct Tile {
-    static constexpr int TM = 64 * MT, TN = 64 * NT, KS = MT == 1 ? 8 : 2, kUnits = 2 * MT * KS * 128, kPer = kUnits / kThreads;
+    static constexpr int TM = 64 * MT, TN = 64 * NT, KS = 2, kUnits = 2 * MT * KS * 128, kPer = kUnits / kThreads;
     f32x16 acc[MT][NT];
     struct Right {
         h8 f[KS][2][NT];
@@ -332,21 +339,17 @@ template <int MT, int NT> struct Tile {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
     }
-    // (blocks from kb1 on are zeros)
-    __device__ static void load(u32x4 (&r)[kPer], const _Float16 *Fa, int ra, int kblocks, int kb, int kb1)
+    __device__ static void load(u32x4 (&r)[kPer], const _Float16 *Fa, int ra, int kblocks, int kb)
     {
         constexpr int kRun = KS * 128;
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
             // (a run is a whole number of rounds of the workgroup)
             const int blk = j * kThreads / kRun, off = (j * kThreads) % kRun + (int)threadIdx.x;
-            const bool on = KS <= 4 || kb + off / 128 < kb1;
-            const u32x4 v = reinterpret_cast<const u32x4 *>(Fa + ((size_t)(ra / 32 + blk) * kblocks + kb) * kBlockHalfs)[on ? off : 0];
-            r[j] = on ? v : u32x4{0, 0, 0, 0};
+            r[j] = reinterpret_cast<const u32x4 *>(Fa + ((size_t)(ra / 32 + blk) * kblocks + kb) * kBlockHalfs)[off];
         }
     }
-    // (any values from kb1 on)
-    template <int PRODUCTS> __device__ static void load(Right &r, const _Float16 *Fb, int rb, int kblocks, int kb, int kb1)
+    template <int PRODUCTS> __device__ static void load(Right &r, const _Float16 *Fb, int rb, int kblocks, int kb)
     {
         const int wb = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) & 1), lane = threadIdx.x & 63;
 #pragma unroll
@@ -355,7 +358,7 @@ template <int MT, int NT> struct Tile {
             for (int k = 0; k < KS; ++k)
 #pragma unroll
                 for (int p = 0; p < (PRODUCTS > 1 ? 2 : 1); ++p)
-                    r.f[k][p][j] = reinterpret_cast<const h8 *>(Fb + ((size_t)(rb / 32 + wb * NT + j) * kblocks + (KS <= 4 ? kb + k : min(kb + k, kb1 - 1))) * kBlockHalfs + p * 512)[lane];
+                    r.f[k][p][j] = reinterpret_cast<const h8 *>(Fb + ((size_t)(rb / 32 + wb * NT + j) * kblocks + kb + k) * kBlockHalfs + p * 512)[lane];
     }
     __device__ static void store(const u32x4 (&r)[kPer], u32x4 *lds)
     {
@@ -381,21 +384,64 @@ template <int MT, int NT> struct Tile {
                     for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[p == 0][i], b.f[k][p == 1][j], acc[i][j], 0, 0, 0);
         }
     }
+    // 64 x 64: every wave loads its own fragments, four blocks ahead of the ones that it multiplies
+    template <int PRODUCTS> __device__ void product_direct(const _Float16 *Fa, int ra, const _Float16 *Fb, int rb, int kblocks, int kb0, int kb1)
+    {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+        const h8 *pa = reinterpret_cast<const h8 *>(Fa + ((size_t)(ra / 32 + (wave >> 1)) * kblocks + kb0) * kBlockHalfs) + lane;
+        const h8 *pb = reinterpret_cast<const h8 *>(Fb + ((size_t)(rb / 32 + (wave & 1)) * kblocks + kb0) * kBlockHalfs) + lane;
+        constexpr int P = PRODUCTS > 1 ? 2 : 1;
+        h8 a[2][4][P], b[2][4][P];
+        auto get = [&](int s) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+                    a[s][k][p] = pa[k * 128 + p * 64];
+                    b[s][k][p] = pb[k * 128 + p * 64];
+                }
+            pa += 4 * 128;
+            pb += 4 * 128;
+        };
+        auto use = [&](int s) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if constexpr (P > 1) {
+                    acc[0][0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[s][k][P - 1], b[s][k][0], acc[0][0], 0, 0, 0);
+                    acc[0][0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[s][k][0], b[s][k][P - 1], acc[0][0], 0, 0, 0);
+                }
+                acc[0][0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[s][k][0], b[s][k][0], acc[0][0], 0, 0, 0);
+            }
+        };
+        clear();
+        int left = (kb1 - kb0) / 4;
+        get(0);
+        if (left > 1) get(1);
+#pragma unroll 1
+        for (; left > 2; left -= 2) {
+            use(0);
+            get(0);
+            use(1);
+            if (left > 3) get(1);
+        }
+        use(0);
+        if (left > 1) use(1);
+    }
     // lds: two steps; PRODUCTS = 1: the first numbers' product only
     template <int PRODUCTS = 3> __device__ void product(const _Float16 *Fa, int ra, const _Float16 *Fb, int rb, int kblocks, int kb0, int kb1, u32x4 *lds)
     {
         clear();
         u32x4 r[kPer];
         Right b0, b1;
-        load<PRODUCTS>(b0, Fb, rb, kblocks, kb0, kb1);
-        load(r, Fa, ra, kblocks, kb0, kb1);
+        load<PRODUCTS>(b0, Fb, rb, kblocks, kb0);
+        load(r, Fa, ra, kblocks, kb0);
         store(r, lds);
         __syncthreads();
         int at = 0;
         // one step with the next one's loads under way
         auto step = [&](const Right &now, Right &next, int kb) {
-            load<PRODUCTS>(next, Fb, rb, kblocks, kb, kb1);
-            load(r, Fa, ra, kblocks, kb, kb1);
+            load<PRODUCTS>(next, Fb, rb, kblocks, kb);
+            load(r, Fa, ra, kblocks, kb);
             multiply<PRODUCTS>(lds + at * kUnits, now);
             at ^= 1;
             store(r, lds + at * kUnits);
@@ -455,15 +501,18 @@ template <int MT, int NT> struct Tile {
     }
 };
 
-union OrthLds {
-    u32x4 stage[2 * 2048];
-    float small[64][64 + 1];
-    float large[128][128 + 1];
+// A workgroup's LDS: two steps of the product, then the tile of the result
+template <int T> union TileLds {
+    u32x4 stage[T == 64 ? 1 : 2 * Tile<T / 64, T / 64>::kUnits];
+    float t[T][T + 1];
 };
-template <int T> __device__ inline float (*tile_of(OrthLds &l))[T + 1]
+// A tile's product: of 64 x 64 straight from memory, which a small matrix' few workgroups get through sooner; of 128 x 128 through
+// LDS, which takes less from the caches
+template <int T, int PRODUCTS> __device__ inline void tile_of_product(TileLds<T> &lds, Tile<T / 64, T / 64> &t, const _Float16 *Fa, int ra, const _Float16 *Fb, int rb,
+                                                                      int kblocks, int kb0, int kb1)
 {
-    if constexpr (T == 64) return l.small;
-    else return l.large;
+    if constexpr (T == 64) t.template product_direct<PRODUCTS>(Fa, ra, Fb, rb, kblocks, kb0, kb1);
+    else t.template product<PRODUCTS>(Fa, ra, Fb, rb, kblocks, kb0, kb1, lds.stage);
 }
 
 // pair (i <= j) of tiles of a symmetric matrix with T rows of tiles
@@ -521,7 +570,7 @@ template <int T, int POLY, int STEP> __device__ inline void put_square(float (*t
 }
 
 // POLY 0: a tile of X X^T, 1: of A A; b: number of the pair of rows of tiles and of the run along the sum
-template <int T, int POLY> __device__ inline void square_tile(const OrthMat &q, const OrthScalars &s, int b, OrthLds &lds)
+template <int T, int POLY> __device__ inline void square_tile(const OrthMat &q, const OrthScalars &s, int b, TileLds<T> &lds)
 {
     const int splits = POLY ? q.psplits : q.gsplits, run = POLY ? q.pkbs : q.gkbs, kblocks = (POLY ? q.mp : q.np) / 16;
     const int split = b % splits, pair = b / splits;
@@ -529,20 +578,20 @@ template <int T, int POLY> __device__ inline void square_tile(const OrthMat &q, 
     int ti, tj;
     pair_of(pair, ti, tj);
     Tile<T / 64, T / 64> t;
-    t.product(F, ti * T, F, tj * T, kblocks, split * run, min(kblocks, (split + 1) * run), lds.stage);
+    tile_of_product<T, 3>(lds, t, F, ti * T, F, tj * T, kblocks, split * run, min(kblocks, (split + 1) * run));
     if (splits > 1) {
         t.put_part(q.part + (size_t)b * T * T);
         return;
     }
-    t.spread(tile_of<T>(lds));
-    put_square<T, POLY, 32>(tile_of<T>(lds), q, s, ti * T, tj * T);
+    t.spread(lds.t);
+    put_square<T, POLY, 32>(lds.t, q, s, ti * T, tj * T);
 }
 template <int T, int POLY> __global__ __launch_bounds__(kThreads, 2) void orth_square_kernel(OrthRef L)
 {
-    __shared__ OrthLds lds;
+    __shared__ TileLds<T> lds;
     int b = xcd_block(blockIdx.x, gridDim.x);
     if (b >= L.total) return;
-    const OrthMat &q = L.mat[find_mat(L.first, L.s.count, b)];
+    const OrthMat q = the_mat(L, b);
     square_tile<T, POLY>(q, L.s, b, lds);
 }
 
@@ -551,7 +600,7 @@ template <int POLY> __global__ __launch_bounds__(kThreads) void orth_join_kernel
 {
     __shared__ float t[64][64 + 1];
     int b = blockIdx.x;
-    const OrthMat &q = L.mat[find_mat(L.first, L.s.count, b)];
+    const OrthMat q = the_mat(L, b);
     const int splits = POLY ? q.psplits : q.gsplits, parts = q.big[POLY] ? 4 : 1, pair = b / parts, part = b % parts;
     int ti, tj;
     pair_of(pair, ti, tj);
@@ -591,16 +640,16 @@ template <int T> __device__ inline void finish(const float (*t)[T + 1], const Or
 // rounding O to bf16 drops, and far below the rounding of 16-bit weights, of which the update is a small part.
 template <int T, int LAST> __global__ __launch_bounds__(kThreads, 2) void orth_apply_kernel(OrthRef L, int odd)
 {
-    __shared__ OrthLds lds;
+    __shared__ TileLds<T> lds;
     int b = xcd_block(blockIdx.x, gridDim.x);
     if (b >= L.total) return;
-    const OrthMat &q = L.mat[find_mat(L.first, L.s.count, b)];
+    const OrthMat q = the_mat(L, b);
     const TileAt at = tile_at<T, T>(q, b);
     Tile<T / 64, T / 64> t;
-    t.template product<LAST == 2 ? 1 : 3>(q.P, at.m0, odd ? q.Xt2 : q.Xt, at.n0, q.mp / 16, 0, q.mp / 16, lds.stage);
-    t.spread(tile_of<T>(lds));
-    if constexpr (LAST > 0) finish<T>(tile_of<T>(lds), q, L.s, at.m0, at.n0);
-    else emit_x<T, T>(tile_of<T>(lds), q, odd ? q.Xt : q.Xt2, at.m0, at.n0);
+    tile_of_product<T, LAST == 2 ? 1 : 3>(lds, t, q.P, at.m0, odd ? q.Xt2 : q.Xt, at.n0, q.mp / 16, 0, q.mp / 16);
+    t.spread(lds.t);
+    if constexpr (LAST > 0) finish<T>(lds.t, q, L.s, at.m0, at.n0);
+    else emit_x<T, T>(lds.t, q, odd ? q.Xt : q.Xt2, at.m0, at.n0);
 }
 
 // no steps: X_0 is the result
@@ -608,7 +657,7 @@ __global__ __launch_bounds__(kThreads) void orth_none_kernel(OrthRef L)
 {
     __shared__ float t[kOrthTile][kOrthTile + 1];
     int b = blockIdx.x;
-    const OrthMat &q = L.mat[find_mat(L.first, L.s.count, b)];
+    const OrthMat q = the_mat(L, b);
     const TileAt at = tile_at<kOrthTile, kOrthTile>(q, b);
     for (int u = threadIdx.x; u < 64 * 64; u += kThreads) {
         const int r = u / 64, c = u % 64, row = at.n0 + c, k = at.m0 + r;
@@ -1084,7 +1133,7 @@ hipError_t launch_wide(const xconv_orth_item *const *items, int count, const xco
     // the first workgroups of the matrices in the launches (products: tiles of 64, of 128)
     enum { NORM, START, GRAM, GRAM_JOIN = GRAM + 2, POLY, POLY_JOIN = POLY + 2, APPLY, KINDS = APPLY + 2 };
     OrthRef R[KINDS];
-    for (OrthRef &r : R) r = OrthRef{L.s, 0, {}, list};
+    for (OrthRef &r : R) r = OrthRef{L.s, 0, {}, list, {}};
     for (int i = 0; i < count; ++i) {
         const xconv_orth_item &it = *items[i];
         const OrthPlan::Mat &f = P.mat[i];
@@ -1113,6 +1162,7 @@ hipError_t launch_wide(const xconv_orth_item *const *items, int count, const xco
         }
     }
     for (int i = 0; i < count; ++i) L.first[i] = R[NORM].first[i];
+    for (OrthRef &r : R) r.one = L.mat[0];
     const dim3 block(kThreads);
     // (products: whole rounds of the eight dies)
     auto go = [&](auto kernel, int k, auto... more) {
