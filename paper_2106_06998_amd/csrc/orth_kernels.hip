@@ -197,6 +197,41 @@ __device__ inline void orth_get4(const void *p, int dtype, size_t i, float (&v)[
     }
 }
 
+// eight values from element i on, as they are (16 bits: in the first vector) and as floats
+struct __attribute__((packed, aligned(2))) Loose8 { uint32_t w[4]; };
+__device__ inline void raw_get8(const void *p, int dtype, size_t i, u32x4 (&v)[2])
+{
+    if (dtype == XCONV_F32) {
+        const Loose4 *q = reinterpret_cast<const Loose4 *>(static_cast<const float *>(p) + i);
+        const Loose4 a = q[0], b = q[1];
+        v[0] = u32x4{a.w[0], a.w[1], a.w[2], a.w[3]};
+        v[1] = u32x4{b.w[0], b.w[1], b.w[2], b.w[3]};
+    } else {
+        const Loose8 a = *reinterpret_cast<const Loose8 *>(static_cast<const uint16_t *>(p) + i);
+        v[0] = u32x4{a.w[0], a.w[1], a.w[2], a.w[3]};
+    }
+}
+__device__ inline void raw_values(const u32x4 (&r)[2], int dtype, float (&v)[8])
+{
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+        v[k] = dtype == XCONV_F32 ? __uint_as_float(r[k >> 2][k & 3]) : half_value((uint16_t)(r[0][k >> 1] >> (16 * (k & 1))), dtype == XCONV_BF16);
+}
+__device__ inline void orth_put8(void *p, int dtype, size_t i, const float (&v)[8])
+{
+    if (dtype == XCONV_F32) {
+        Loose4 *q = reinterpret_cast<Loose4 *>(static_cast<float *>(p) + i);
+        q[0] = Loose4{{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])}};
+        q[1] = Loose4{{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])}};
+        return;
+    }
+    Loose8 h;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        h.w[k] = dtype == XCONV_BF16 ? bf16_pair(v[2 * k], v[2 * k + 1]) : __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{v[2 * k], v[2 * k + 1]}, h2));
+    *reinterpret_cast<Loose8 *>(static_cast<uint16_t *>(p) + i) = h;
+}
+
 // ---- momentum and the sum of squares; the list of matrices goes to the scratch ------------------------------------
 __global__ __launch_bounds__(kThreads) void orth_norm_kernel(OrthList L, OrthMat *list)
 {
@@ -612,28 +647,60 @@ template <int POLY> __global__ __launch_bounds__(kThreads) void orth_join_kernel
     else put_square<64, POLY, 32>(t, q, L.s, ti * 64, tj * 64);
 }
 
-// t, part (m0, n0) of the result of the last step, becomes O or the update of W
-template <int T> __device__ inline void finish(const float (*t)[T + 1], const OrthMat &q, const OrthScalars &s, int m0, int n0)
-{
-    const bool tall = q.rows > q.cols;
-    const int r0 = tall ? n0 : m0, c0 = tall ? m0 : n0;
-    constexpr int kRound = 16;
-    for (int base = threadIdx.x; base < T * T; base += kRound * kThreads) {
-        auto place = [&](int k) -> long long {
-            const int u = base + k * kThreads, r = r0 + u / T, c = c0 + u % T;
-            return r < q.rows && c < q.cols ? (long long)r * q.cols + c : -1;
-        };
-        float v[kRound];
-        if (s.muon) orth_gather(q.out, s.out_dtype, place, v);
-#pragma unroll
-        for (int k = 0; k < kRound; ++k) {
-            const int u = base + k * kThreads, r = u / T, c = u % T;
-            const float x = tall ? t[c][r] : t[r][c];
-            v[k] = s.muon ? v[k] * s.keep - q.wscale * x : x;
-        }
-        orth_scatter(q.out, s.out_dtype, place, v);
+// Part (m0, n0) of the result of the last step becomes O or the update of W: eight values in the order of memory a thread and
+// round, four threads a row.  The weights are loaded for all rounds before the first is needed.
+template <int T> struct Finish {
+    static constexpr int N = T * T / 8 / kThreads;
+    const OrthMat &q;
+    const OrthScalars &s;
+    bool tall;
+    int r0, c0;
+    u32x4 w[N][2];
+
+    __device__ Finish(const OrthMat &q, const OrthScalars &s, int m0, int n0) : q(q), s(s)
+    {
+        tall = q.rows > q.cols;
+        r0 = tall ? n0 : m0;
+        c0 = tall ? m0 : n0;
     }
-}
+    __device__ static int row(int j) { return (j * kThreads + (int)threadIdx.x) / 4 % T; }
+    __device__ static int col(int j) { return ((j * kThreads + (int)threadIdx.x) / (4 * T) * 4 + (int)threadIdx.x % 4) * 8; }
+    // how many of the eight there are, and the first one's place
+    __device__ int there(int j) const { return r0 + row(j) < q.rows ? max(0, min(8, q.cols - (c0 + col(j)))) : 0; }
+    __device__ size_t place(int j) const { return (size_t)(r0 + row(j)) * q.cols + c0 + col(j); }
+    __device__ void load()
+    {
+        if (!s.muon) return;
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (there(j) == 8) raw_get8(q.out, s.out_dtype, place(j), w[j]);
+    }
+    __device__ void put(const float (*t)[T + 1])
+    {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const int n = there(j), r = row(j), c = col(j);
+            if (n == 8) {
+                float v[8], old[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] = tall ? t[c + k][r] : t[r][c + k];
+                if (s.muon) {
+                    raw_values(w[j], s.out_dtype, old);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) v[k] = old[k] * s.keep - q.wscale * v[k];
+                }
+                orth_put8(q.out, s.out_dtype, place(j), v);
+            } else {
+#pragma unroll 1
+                for (int k = 0; k < n; ++k) {
+                    float v = tall ? t[c + k][r] : t[r][c + k];
+                    if (s.muon) v = orth_get(q.out, s.out_dtype, place(j) + k) * s.keep - q.wscale * v;
+                    orth_put(q.out, s.out_dtype, place(j) + k, v);
+                }
+            }
+        }
+    }
+};
 
 // X <- P X, from the transposed X (Xt, or Xt2 when odd) to X and the other transposed one.  LAST 1: to the result instead.  2: the
 // same with the first fp16 numbers alone.  What that drops, 2^-12 of P and of X, goes into no further step: it is an eighth of what
@@ -647,9 +714,15 @@ template <int T, int LAST> __global__ __launch_bounds__(kThreads, 2) void orth_a
     const TileAt at = tile_at<T, T>(q, b);
     Tile<T / 64, T / 64> t;
     tile_of_product<T, LAST == 2 ? 1 : 3>(lds, t, q.P, at.m0, odd ? q.Xt2 : q.Xt, at.n0, q.mp / 16, 0, q.mp / 16);
-    t.spread(lds.t);
-    if constexpr (LAST > 0) finish<T>(lds.t, q, L.s, at.m0, at.n0);
-    else emit_x<T, T>(lds.t, q, odd ? q.Xt : q.Xt2, at.m0, at.n0);
+    if constexpr (LAST > 0) {
+        Finish<T> f(q, L.s, at.m0, at.n0);
+        f.load();
+        t.spread(lds.t);
+        f.put(lds.t);
+    } else {
+        t.spread(lds.t);
+        emit_x<T, T>(lds.t, q, odd ? q.Xt : q.Xt2, at.m0, at.n0);
+    }
 }
 
 // no steps: X_0 is the result
@@ -665,7 +738,9 @@ __global__ __launch_bounds__(kThreads) void orth_none_kernel(OrthRef L)
         t[r][c] = ((float)p[0] + (float)p[512]) / kOrthScale;
     }
     __syncthreads();
-    finish<kOrthTile>(t, q, L.s, at.m0, at.n0);
+    Finish<kOrthTile> f(q, L.s, at.m0, at.n0);
+    f.load();
+    f.put(t);
 }
 
 // ---- small matrices: all steps in one workgroup -------------------------------------------------------------------
