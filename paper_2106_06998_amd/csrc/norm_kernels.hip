@@ -168,6 +168,14 @@ template <int WT> __device__ inline float load_param(const void *p, int c, float
     return p ? norm_val<WT>(static_cast<const typename NormElem<WT>::t *>(p)[c]) : none;
 }
 
+// s / count to the last bit but rare ones, at a quarter of a division's instructions; 1 / sqrt(v) to one unit in the last place
+__device__ inline float mean_of(float s, const NormArgs &a)
+{
+    const float q = s * a.inv_c;
+    return fabsf(q) < 1e30f ? fmaf(fmaf(-q, a.count, s), a.inv_c, q) : q;
+}
+__device__ inline float rstd_of(float squares, const NormArgs &a) { return rsqrtf(squares * a.inv_c + a.eps); }
+
 // sums of R values over a group of G lanes of a wave, or over the workgroup's G threads through `red` (two slots of R * G / 64
 // floats, taken in turn so that one barrier a sum is enough)
 template <int G, int R> __device__ inline void group_sum(float (&s)[R], float *red, int &turn)
@@ -194,6 +202,13 @@ template <int G, int R> __device__ inline void group_sum(float (&s)[R], float *r
 }
 
 // ---- rows ----------------------------------------------------------------------------------------------------------
+// whether the wave's round k of vectors needs masks: rows that are no whole vectors, in the wave that has the last one
+template <int G> __device__ inline bool masked(const NormArgs &a, int k, int nv)
+{
+    if constexpr (G <= 64) return a.ragged;
+    else return a.ragged && __builtin_amdgcn_readfirstlane((int)(threadIdx.x % G) | 63) + k * G >= nv - 1;
+}
+
 // G lanes a row, K vectors a lane (lane l holds vectors l, l + G, ...), R rows at once; K == 0: a row is read once a pass.
 template <int G> constexpr int row_threads = G > 256 ? G : 256;
 
@@ -247,7 +262,7 @@ __global__ __launch_bounds__(row_threads<G>) void norm_rows_fwd_kernel(NormArgs 
             for (int r = 0; r < R; ++r) {
                 float t[V];
                 unpack<DT>(value(r, k, p), t);
-                if (!a.ragged) {
+                if (K > 0 ? !masked<G>(a, k, nv) : !a.ragged) {
 #pragma unroll
                     for (int i = 0; i < V; ++i) s[r] += t[i];       // (zeros past the last vector)
                 } else {
@@ -259,7 +274,7 @@ __global__ __launch_bounds__(row_threads<G>) void norm_rows_fwd_kernel(NormArgs 
         group_sum<G>(s, red, turn);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            mean[r] = s[r] / a.count;
+            mean[r] = mean_of(s[r], a);
             s[r] = 0.f;
         }
         rounds([&](int k, int v) {
@@ -269,7 +284,7 @@ __global__ __launch_bounds__(row_threads<G>) void norm_rows_fwd_kernel(NormArgs 
                 float t[V];
                 unpack<DT>(value(r, k, p), t);
                 float q = 0.f;
-                if (!a.ragged) {
+                if (K > 0 ? !masked<G>(a, k, nv) : !a.ragged) {
 #pragma unroll
                     for (int i = 0; i < V; ++i) q += (t[i] - mean[r]) * (t[i] - mean[r]);
                 } else {
@@ -284,7 +299,7 @@ __global__ __launch_bounds__(row_threads<G>) void norm_rows_fwd_kernel(NormArgs 
         });
         group_sum<G>(s, red, turn);
 #pragma unroll
-        for (int r = 0; r < R; ++r) rstd[r] = 1.0f / sqrtf(s[r] * a.inv_c + a.eps);
+        for (int r = 0; r < R; ++r) rstd[r] = rstd_of(s[r], a);
         rounds([&](int k, int v) {
             if (v >= nv) return;
             const Part p = part_of<V>(v, a.C, a.exact);
@@ -381,7 +396,7 @@ __global__ __launch_bounds__(row_threads<G>) void norm_rows_bwd_kernel(NormArgs 
                 unpack<DT>(rx[r][k], x);
                 unpack<DT>(rd[r][k], d);
                 // (rows and vectors that do not exist are zeros with statistics of zero, or columns that nobody reads)
-                if (a.ragged) {
+                if (K > 0 ? masked<G>(a, k, nv) : a.ragged) {
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
                         const bool mine = on[r] && v < nv && own(p, i);
@@ -522,13 +537,17 @@ template <int DT, bool WHOLE> __device__ inline void plane_put(const NormArgs &a
     if constexpr (WHOLE) store_loose<DT>(y + (size_t)c * a.inner + at.p.at, v);
     else store_part<DT>(y + (size_t)c * a.inner, v, at.p);
 }
-// the run of tiles of a workgroup: neighbouring tiles share lines of memory, so a workgroup takes neighbours, and the
-// workgroups of one die the neighbouring runs
-__device__ inline void tiles_of(const NormArgs &a, long long &from, long long &to)
+// The tiles of a workgroup.  Planes are rarely whole lines, so neighbouring tiles share lines of memory: each of the chip's eight
+// dies has a run of tiles of its own, and its workgroups take neighbours at the same time, so that the die's L2 cache has the
+// shared lines for both (256 x 28 x 28: a workgroup with a run of its own reads 1.9 times the tensors).
+struct TileRun {
+    long long from, to, step;
+};
+__device__ inline TileRun tiles_of(const NormArgs &a)
 {
-    const long long w = xcd_block(blockIdx.x, gridDim.x);
-    from = a.tiles * w / gridDim.x;
-    to = a.tiles * (w + 1) / gridDim.x;
+    const int b = blockIdx.x, grid = gridDim.x;
+    if (grid & 7) return {b, a.tiles, grid};
+    return {a.tiles * (b & 7) / 8 + (b >> 3), a.tiles * ((b & 7) + 1) / 8, grid >> 3};
 }
 
 // WHOLE: planes of at least one vector whose last vectors overlap, the ordinary case
@@ -539,8 +558,7 @@ __global__ __launch_bounds__(NW * 64) void norm_planes_fwd_kernel(NormArgs a)
     constexpr int V = NormElem<DT>::V, TY = NW * kNormTYW;
     __shared__ float red[NW * kNormTX * V];
     const int ty = threadIdx.x / kNormTX;
-    long long tile, end;
-    tiles_of(a, tile, end);
+    const TileRun run = tiles_of(a);
     // the rounds of channels: k of the registers, or all that there are
     auto rounds = [&](auto &&body) {
         if constexpr (K > 0) {
@@ -550,7 +568,7 @@ __global__ __launch_bounds__(NW * 64) void norm_planes_fwd_kernel(NormArgs a)
             for (int c = ty; c < a.C; c += TY) body(0, c);
         }
     };
-    for (; tile < end; ++tile) {
+    for (long long tile = run.from; tile < run.to; tile += run.step) {
         const PlaneAt at = plane_at<V>(a, tile);
         const elem_t *x = static_cast<const elem_t *>(a.x) + at.base;
         elem_t *y = static_cast<elem_t *>(a.y) + at.base;
@@ -574,7 +592,7 @@ __global__ __launch_bounds__(NW * 64) void norm_planes_fwd_kernel(NormArgs a)
         column_sum<V, NW>(s, red);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            mean[i] = s[i] / a.count;
+            mean[i] = mean_of(s[i], a);
             s[i] = 0.f;
         }
         rounds([&](int k, int c) {
@@ -586,7 +604,7 @@ __global__ __launch_bounds__(NW * 64) void norm_planes_fwd_kernel(NormArgs a)
         });
         column_sum<V, NW>(s, red);
 #pragma unroll
-        for (int i = 0; i < V; ++i) rstd[i] = 1.0f / sqrtf(s[i] * a.inv_c + a.eps);
+        for (int i = 0; i < V; ++i) rstd[i] = rstd_of(s[i], a);
         if (!at.on) continue;
         rounds([&](int k, int c) {
             if (c >= a.C) return;
@@ -633,9 +651,10 @@ __global__ __launch_bounds__(NW * 64, 4) void norm_planes_bwd_kernel(NormArgs a)
         }
     };
     bool first = true;
-    long long tile, end;
-    tiles_of(a, tile, end);
-    for (; tile < end; ++tile, first = false) {
+    const TileRun run = tiles_of(a);
+    if (K == 0 && part && run.from >= run.to)
+        for (int c = threadIdx.x; c < 2 * a.C; c += NW * 64) part[c] = 0.f;
+    for (long long tile = run.from; tile < run.to; tile += run.step, first = false) {
         const PlaneAt at = plane_at<V>(a, tile);
         uint4 rx[KR], rd[KR];
         auto get = [&](const elem_t *t, int c) { return plane_get<DT, WHOLE>(a, t + at.base, at, c); };
@@ -811,7 +830,7 @@ int norm_blocks(const xconv_norm_desc *d, const NormShape &s, bool bwd)
 {
     const int rows = s.G ? std::max(256, s.G) / s.G * s.R : 1;
     const long long want = d->inner > 1 ? plane_tiles(d, s.V) : (d->outer + rows - 1) / rows;
-    return (int)std::min<long long>(want, bwd ? kNormBlocks : kNormGrid);
+    return (int)std::min<long long>(d->inner > 1 && want > 8 ? (want + 7) / 8 * 8 : want, bwd ? kNormBlocks : kNormGrid);
 }
 
 template <int DT, int WT, int G, int K, int RF, int RB> hipError_t go_rows(const NormArgs &a, bool bwd, int blocks, hipStream_t st)
