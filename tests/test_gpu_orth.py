@@ -339,3 +339,51 @@ def test_refusals_on_the_device():
         optim.muon_step([w], [g], [m], float("inf"))
     torch.cuda.synchronize()
     assert torch.equal(w, g) and not m.any()
+
+
+@pytest.mark.parametrize("rows,cols", [(64, 768), (64, 769), (65, 768), (768, 64), (769, 20), (8, 900), (33, 257), (1, 769), (64, 2000)])
+def test_where_small_matrices_end(rows, cols):
+    """Around the extents up to which a matrix is one workgroup's."""
+    for dtype in ("f32", "f16"):
+        g = gradient(rows, cols, rows + cols, dtype)
+        o = optim.orthogonalize(g.to(DEV))
+        torch.cuda.synchronize()
+        check_orth(o, g, dtype)
+
+
+@pytest.mark.parametrize("rows,cols", [(256, 2304), (96, 3200), (1100, 1300), (1088, 2100)])
+def test_split_sums(rows, cols):
+    say("orthogonalize", rows, cols)
+    g = gradient(rows, cols, 5, "bf16")
+    o = optim.orthogonalize(g.to(DEV))
+    torch.cuda.synchronize()
+    check_orth(o, g, "bf16")
+
+
+@pytest.mark.parametrize("shape", [(256, 1152), (512, 1600), (130, 700), (120, 2000)])
+def test_larger_tiles_give_the_same_bits(shape):
+    """Enough equal matrices are taken in larger tiles: not one bit of a result depends on it."""
+    say("orthogonalize", shape, "alone and among others")
+    gs = [gradient(*shape, i).to(DEV) for i in range(20)]
+    many = optim.orthogonalize(gs)
+    torch.cuda.synchronize()
+    for i in (0, 7, 19):
+        one = optim.orthogonalize(gs[i])
+        torch.cuda.synchronize()
+        assert torch.equal(one, many[i])
+    check_orth(many[3], gs[3].cpu(), "f32")
+
+
+def test_muon_on_large_layers():
+    say("muon_step 6 x 300 x 1300")
+    ws = [gradient(300, 1300, i, scale=1.0) * 0.1 for i in range(6)]
+    gs = [gradient(300, 1300, 50 + i) for i in range(6)]
+    for dtype in ("f32", "bf16"):
+        wd = [w.to(TD[dtype]).to(DEV) for w in ws]
+        gd = [g.to(TD[dtype]).to(DEV) for g in gs]
+        md = [torch.zeros(300, 1300, device=DEV) for _ in ws]
+        optim.muon_step(wd, gd, md, 0.05, 0.9, 0.1)
+        torch.cuda.synchronize()
+        want, m1, bound = muon_reference(ws[2].to(TD[dtype]), gs[2].to(TD[dtype]), torch.zeros(300, 1300), 0.05, 0.9, 0.1, True)
+        off = np.linalg.norm(wd[2].cpu().double().numpy() - want)
+        assert off <= bound + (UOUT[dtype] + 3 * 2.0 ** -24) * np.linalg.norm(want)
