@@ -410,7 +410,7 @@ xconv_status xconv_layernorm_bwd(const xconv_norm_desc *desc, const void *dY_dev
  * XCONV_EINVAL: a null pointer, count < 0, rows or cols < 1, bad enum, steps < 0, eps, lr, momentum, weight_decay or a
  * coefficient not finite, eps < 0; XCONV_EUNSUPPORTED: min(rows, cols) above 32768, an extent above 2^24, rows * cols above
  * 2^31, steps above 64, and coefficients with which a singular value s that starts in [0, 1] passes 3.5 before the last step
- * or |a + b s^2 + c s^4| passes 12 (the fp16 numbers could overflow).  count == 0 is a no-op. */
+ * or |a + b s^2 + c s^4| or |b s + c s^3| passes 12 (the fp16 numbers could overflow).  count == 0 is a no-op. */
 typedef struct xconv_orth_item {
     int32_t rows, cols;
     const void *G_dev;

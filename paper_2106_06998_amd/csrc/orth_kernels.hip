@@ -32,6 +32,7 @@ constexpr int kBlockHalfs = 1024;   // 32 x 16 values, both numbers
 
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef _Float16 h4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
@@ -306,6 +307,26 @@ template <int TM, int TN> __device__ inline void emit_x(const float (*t)[TN + 1]
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = t[r + i][c];
         put_pieces(xt, n0 + c, m0 + r, q.mp / 16, v);
+    }
+}
+// the same for all rows and TN columns from n0 on, where the matrix may have fewer than TM rows
+template <int TM, int TN, int NTHR> __device__ inline void emit_rows(const float (*t)[TN + 1], const OrthMat &q, _Float16 *xt, int n0)
+{
+    for (int u = threadIdx.x; u < TM * TN / 8; u += NTHR) {
+        float v[8];
+        int r = u % TM, c = u / TM * 8;
+        if (r < q.mp) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = t[r][c + i];
+            put_pieces(q.X, r, n0 + c, q.np / 16, v);
+        }
+        r = u / TN * 8;
+        c = u % TN;
+        if (r < q.mp) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = t[r + i][c];
+            put_pieces(xt, n0 + c, r, q.mp / 16, v);
+        }
     }
 }
 // the part of tile b (of tm tiles along m)
@@ -649,8 +670,8 @@ template <int POLY> __global__ __launch_bounds__(kThreads) void orth_join_kernel
 
 // Part (m0, n0) of the result of the last step becomes O or the update of W: eight values in the order of memory a thread and
 // round, four threads a row.  The weights are loaded for all rounds before the first is needed.
-template <int T> struct Finish {
-    static constexpr int N = T * T / 8 / kThreads;
+template <int TM, int TN, int NTHR = kThreads> struct Finish {
+    static constexpr int N = TM * TN / 8 / NTHR;
     const OrthMat &q;
     const OrthScalars &s;
     bool tall;
@@ -663,8 +684,16 @@ template <int T> struct Finish {
         r0 = tall ? n0 : m0;
         c0 = tall ? m0 : n0;
     }
-    __device__ static int row(int j) { return (j * kThreads + (int)threadIdx.x) / 4 % T; }
-    __device__ static int col(int j) { return ((j * kThreads + (int)threadIdx.x) / (4 * T) * 4 + (int)threadIdx.x % 4) * 8; }
+    __device__ int row(int j) const
+    {
+        const int u = (j * NTHR + (int)threadIdx.x) / 4;
+        return tall ? u % TN : u % TM;
+    }
+    __device__ int col(int j) const
+    {
+        const int u = (j * NTHR + (int)threadIdx.x) / 4;
+        return ((tall ? u / TN : u / TM) * 4 + (int)threadIdx.x % 4) * 8;
+    }
     // how many of the eight there are, and the first one's place
     __device__ int there(int j) const { return r0 + row(j) < q.rows ? max(0, min(8, q.cols - (c0 + col(j)))) : 0; }
     __device__ size_t place(int j) const { return (size_t)(r0 + row(j)) * q.cols + c0 + col(j); }
@@ -675,7 +704,7 @@ template <int T> struct Finish {
         for (int j = 0; j < N; ++j)
             if (there(j) == 8) raw_get8(q.out, s.out_dtype, place(j), w[j]);
     }
-    __device__ void put(const float (*t)[T + 1])
+    __device__ void put(const float (*t)[TN + 1])
     {
 #pragma unroll
         for (int j = 0; j < N; ++j) {
@@ -715,13 +744,125 @@ template <int T, int LAST> __global__ __launch_bounds__(kThreads, 2) void orth_a
     Tile<T / 64, T / 64> t;
     tile_of_product<T, LAST == 2 ? 1 : 3>(lds, t, q.P, at.m0, odd ? q.Xt2 : q.Xt, at.n0, q.mp / 16, 0, q.mp / 16);
     if constexpr (LAST > 0) {
-        Finish<T> f(q, L.s, at.m0, at.n0);
+        Finish<T, T> f(q, L.s, at.m0, at.n0);
         f.load();
         t.spread(lds.t);
         f.put(lds.t);
     } else {
         t.spread(lds.t);
         emit_x<T, T>(lds.t, q, odd ? q.Xt : q.Xt2, at.m0, at.n0);
+    }
+}
+
+// ---- matrices of up to 256 rows: X <- a X + A (b X + c A X) in one launch -------------------------------------------
+// P costs such a matrix a launch of a few workgroups, which is latency.  Here a workgroup takes 32 CB columns of X through both
+// products by A: wave w holds rows 32 w .. of A in registers (read once, all loads together), the columns of X and then
+// Z = b X + c A X lie in LDS as the second operand, and a X is where the second product's sums start from.
+template <int MB, int CB> union MergeLds {
+    u32x4 frag[CB][2 * MB * 128];
+    float t[32 * MB][32 * CB + 1];
+};
+template <int MB, int CB, int LAST> __global__ __launch_bounds__(64 * MB, MB == 8 ? 2 : 1) void orth_merge_kernel(OrthRef L, int odd)
+{
+    extern __shared__ char merge_lds[];
+    MergeLds<MB, CB> &lds = *reinterpret_cast<MergeLds<MB, CB> *>(merge_lds);
+    constexpr int KB = 2 * MB, NTHR = 64 * MB;
+    int b = blockIdx.x;
+    const OrthMat q = the_mat(L, b);
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+    const int n0 = b * 32 * CB, kblocks = q.mp / 16;
+    const bool mine = 32 * wave < q.mp;          // (waves past the matrix' rows only help to copy)
+    // columns n0 .. of X, which are rows of the transposed X: whole kilobytes
+    const u32x4 *x = reinterpret_cast<const u32x4 *>((odd ? q.Xt2 : q.Xt) + (size_t)(n0 / 32) * kblocks * kBlockHalfs);
+    u32x4 r[CB * KB * 128 / NTHR];
+    const int units = kblocks * 128;
+#pragma unroll
+    for (int j = 0; j < CB * KB * 128 / NTHR; ++j) r[j] = j * NTHR + tid < CB * units ? x[j * NTHR + tid] : u32x4{0, 0, 0, 0};
+    h8 a[KB][2];
+    if (mine) {
+        const h8 *f = reinterpret_cast<const h8 *>(q.A + (size_t)wave * kblocks * kBlockHalfs) + lane;
+#pragma unroll
+        for (int k = 0; k < KB; ++k)
+            if (k < kblocks) {
+                a[k][0] = f[k * 128];
+                a[k][1] = f[k * 128 + 64];
+            }
+    }
+    u32x4 *frag = &lds.frag[0][0];               // [column block][block along k][number][lane], of the matrix' own extent
+#pragma unroll
+    for (int j = 0; j < CB * KB * 128 / NTHR; ++j)
+        if (j * NTHR + tid < CB * units) frag[j * NTHR + tid] = r[j];
+    __syncthreads();
+    f32x16 acc[CB];
+    auto product = [&] {
+#pragma unroll
+        for (int k = 0; k < KB; ++k)
+            if (k < kblocks) {
+                h8 v[CB][2];
+#pragma unroll
+                for (int j = 0; j < CB; ++j)
+#pragma unroll
+                    for (int p = 0; p < 2; ++p) v[j][p] = __builtin_bit_cast(h8, frag[j * units + k * 128 + p * 64 + lane]);
+#pragma unroll
+                for (int p = 0; p < 3; ++p)
+#pragma unroll
+                    for (int j = 0; j < CB; ++j) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[k][p == 0], v[j][p == 1], acc[j], 0, 0, 0);
+            }
+    };
+#pragma unroll
+    for (int j = 0; j < CB; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[j][e] = 0.f;
+    // registers 4 g .. of a lane are four of the eight values of one lane's fragment: its place in LDS
+    auto four = [&](int j, int g, int p) {
+        const int k = 2 * wave + (g >> 1), from = (lane & 31) + 32 * (g & 1);
+        return reinterpret_cast<h4 *>(frag + j * units + k * 128 + p * 64 + from) + (lane >> 5);
+    };
+    h4 zh[CB][4], zl[CB][4];
+    if (mine) {
+        product();
+#pragma unroll
+        for (int j = 0; j < CB; ++j)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const h4 xh = *four(j, g, 0), xl = *four(j, g, 1);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    // (X scaled once, the sums twice)
+                    const float v = (float)xh[i] + (float)xl[i], z = L.s.b * v + L.s.c * (acc[j][4 * g + i] * (1.f / kOrthScale));
+                    zh[j][g][i] = (_Float16)z;
+                    zl[j][g][i] = (_Float16)(z - (float)zh[j][g][i]);
+                    acc[j][4 * g + i] = L.s.a * v * kOrthScale;
+                }
+            }
+    }
+    __syncthreads();
+    if (mine) {
+#pragma unroll
+        for (int j = 0; j < CB; ++j)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                *four(j, g, 0) = zh[j][g];
+                *four(j, g, 1) = zl[j][g];
+            }
+    }
+    __syncthreads();
+    if (mine) product();
+    __syncthreads();
+    if (mine) {
+#pragma unroll
+        for (int j = 0; j < CB; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) lds.t[32 * wave + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3)][32 * j + (lane & 31)] = acc[j][e] * kOrthUnscale;
+    }
+    if constexpr (LAST) {
+        Finish<32 * MB, 32 * CB, NTHR> f(q, L.s, 0, n0);
+        f.load();
+        __syncthreads();
+        f.put(lds.t);
+    } else {
+        __syncthreads();
+        emit_rows<32 * MB, 32 * CB, NTHR>(lds.t, q, odd ? q.Xt : q.Xt2, n0);
     }
 }
 
@@ -738,7 +879,7 @@ __global__ __launch_bounds__(kThreads) void orth_none_kernel(OrthRef L)
         t[r][c] = ((float)p[0] + (float)p[512]) / kOrthScale;
     }
     __syncthreads();
-    Finish<kOrthTile> f(q, L.s, at.m0, at.n0);
+    Finish<kOrthTile, kOrthTile> f(q, L.s, at.m0, at.n0);
     f.load();
     f.put(t);
 }
@@ -1066,10 +1207,11 @@ int splits_of(int m, int kblocks)
 }
 bool narrow(const xconv_orth_item &it) { return std::min(it.rows, it.cols) <= kNarrowM && std::max(it.rows, it.cols) <= kNarrowN; }
 
+constexpr int kMergeM = 256;        // most rows of a matrix that takes both products by A in one launch
 struct OrthPlan {
-    int count;
+    int count, merge_mb, merge_cb;  // blocks of 32 rows and columns of the workgroups of that launch
     struct Mat {
-        int m, n, mp, np, big[3], gsplits, gkbs, psplits, pkbs, tiles[3];
+        int m, n, mp, np, big[3], merge, gsplits, gkbs, psplits, pkbs, tiles[3];
         size_t x, a, part, bytes;
     } mat[kOrthItems];
     size_t bytes;
@@ -1079,7 +1221,7 @@ OrthPlan plan_orth(const xconv_orth_item *const *items, int count)
 {
     OrthPlan P{};
     P.count = count;
-    auto can = [](int m) { return m > 64 && 2 * round_up(m, 128) <= 3 * m; };
+    auto can = [](int m) { return m > kMergeM && 2 * round_up(m, 128) <= 3 * m; };
     auto splits = [](int m, int extent) { return splits_of(m, round_up(extent, 64) / 16); };
     long long large[3] = {0, 0, 0};     // workgroups with tiles of 128
     for (int i = 0; i < count; ++i) {
@@ -1089,6 +1231,7 @@ OrthPlan plan_orth(const xconv_orth_item *const *items, int count)
         large[1] += (long long)tm * (tm + 1) / 2 * splits(m, m);
         large[2] += (long long)tm * ceil_div(n, 128);
     }
+    long long columns = 0;
     P.bytes = up256(sizeof(OrthMat) * kOrthItems);
     for (int i = 0; i < count; ++i) {
         OrthPlan::Mat &q = P.mat[i];
@@ -1101,6 +1244,11 @@ OrthPlan plan_orth(const xconv_orth_item *const *items, int count)
         }
         q.mp = round_up(q.m, T);
         q.np = round_up(q.n, T);
+        q.merge = q.m <= kMergeM;
+        if (q.merge) {
+            P.merge_mb = std::max(P.merge_mb, q.mp <= 128 ? 4 : 8);
+            columns += q.np;
+        }
         for (int k = 0; k < 3; ++k) {
             const int t = q.big[k] ? 128 : 64;
             q.tiles[k] = k < 2 ? q.mp / t * (q.mp / t + 1) / 2 : q.mp / t * (q.np / t);
@@ -1121,12 +1269,15 @@ OrthPlan plan_orth(const xconv_orth_item *const *items, int count)
         q.bytes = 3 * q.x + 2 * q.a + q.part + up256(kOrthNorms * sizeof(double));
         P.bytes += q.bytes;
     }
+    // (64 columns read A half as often; 32 are twice as many workgroups)
+    P.merge_cb = columns / 64 >= 192 ? 2 : 1;
     return P;
 }
 
 }  // namespace
 
-// Calls `run` with the next kOrthItems matrices that the narrow kernel does not take, in order, until there are none
+// Calls `run` with the next kOrthItems matrices that the narrow kernel does not take until there are none, those of few rows first:
+// their workgroups make room early for the last ones of a launch that has a few more than the chip holds
 namespace {
 template <class F> bool wide_runs(const xconv_orth_item *items, int count, F &&run)
 {
@@ -1135,6 +1286,7 @@ template <class F> bool wide_runs(const xconv_orth_item *items, int count, F &&r
     for (int i = 0; i <= count; ++i) {
         if (i < count && !narrow(items[i])) list[n++] = items + i;
         if (n == kOrthItems || (i == count && n)) {
+            std::stable_sort(list, list + n, [](const xconv_orth_item *a, const xconv_orth_item *b) { return std::min(a->rows, a->cols) < std::min(b->rows, b->cols); });
             if (!run(list, n)) return false;
             n = 0;
         }
@@ -1196,8 +1348,22 @@ hipError_t launch_narrow(const xconv_orth_item *items, int count, const xconv_or
     return hipSuccess;
 }
 
+template <int MB, int CB> hipError_t allow_merge()
+{
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(orth_merge_kernel<MB, CB, 0>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(MergeLds<MB, CB>));
+    return e != hipSuccess ? e : hipFuncSetAttribute(reinterpret_cast<const void *>(orth_merge_kernel<MB, CB, 1>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(MergeLds<MB, CB>));
+}
+template <int MB, int CB> void launch_merge(const OrthRef &R, int odd, bool last, hipStream_t st)
+{
+    const dim3 grid((unsigned)R.total), block(64 * MB);
+    if (last) hipLaunchKernelGGL((orth_merge_kernel<MB, CB, 1>), grid, block, sizeof(MergeLds<MB, CB>), st, R, odd);
+    else hipLaunchKernelGGL((orth_merge_kernel<MB, CB, 0>), grid, block, sizeof(MergeLds<MB, CB>), st, R, odd);
+}
+
 hipError_t launch_wide(const xconv_orth_item *const *items, int count, const xconv_orth_args *args, const xconv_muon_args *muon, void *ws, hipStream_t st)
 {
+    static const hipError_t set = allow_merge<8, 2>();      // (the others stay below 64 KB)
+    if (set != hipSuccess) return set;
     const OrthPlan P = plan_orth(items, count);
     OrthList L{};
     L.s = scalars_of(args, muon);
@@ -1206,7 +1372,7 @@ hipError_t launch_wide(const xconv_orth_item *const *items, int count, const xco
     auto take = [&](size_t bytes) { char *r = p; p += bytes; return r; };
     OrthMat *list = (OrthMat *)take(up256(sizeof(OrthMat) * kOrthItems));
     // the first workgroups of the matrices in the launches (products: tiles of 64, of 128)
-    enum { NORM, START, GRAM, GRAM_JOIN = GRAM + 2, POLY, POLY_JOIN = POLY + 2, APPLY, KINDS = APPLY + 2 };
+    enum { NORM, START, GRAM, GRAM_JOIN = GRAM + 2, POLY, POLY_JOIN = POLY + 2, APPLY, MERGE = APPLY + 2, KINDS };
     OrthRef R[KINDS];
     for (OrthRef &r : R) r = OrthRef{L.s, 0, {}, list, {}};
     for (int i = 0; i < count; ++i) {
@@ -1228,9 +1394,10 @@ hipError_t launch_wide(const xconv_orth_item *const *items, int count, const xco
         blocks[START] = (f.mp / kOrthTile) * (f.np / kOrthTile);
         blocks[GRAM + f.big[0]] = f.tiles[0] * f.gsplits;
         blocks[GRAM_JOIN] = f.gsplits > 1 ? f.tiles[0] * (f.big[0] ? 4 : 1) : 0;
-        blocks[POLY + f.big[1]] = f.tiles[1] * f.psplits;
-        blocks[POLY_JOIN] = f.psplits > 1 ? f.tiles[1] * (f.big[1] ? 4 : 1) : 0;
-        blocks[APPLY + f.big[2]] = f.tiles[2];
+        if (f.merge) blocks[MERGE] = f.np / (32 * P.merge_cb);
+        else blocks[POLY + f.big[1]] = f.tiles[1] * f.psplits;
+        blocks[POLY_JOIN] = !f.merge && f.psplits > 1 ? f.tiles[1] * (f.big[1] ? 4 : 1) : 0;
+        if (!f.merge) blocks[APPLY + f.big[2]] = f.tiles[2];
         for (int k = 0; k < KINDS; ++k) {
             R[k].first[i] = R[k].total;
             R[k].total += blocks[k];
@@ -1242,7 +1409,7 @@ hipError_t launch_wide(const xconv_orth_item *const *items, int count, const xco
     // (products: whole rounds of the eight dies)
     auto go = [&](auto kernel, int k, auto... more) {
         if (!R[k].total) return;
-        const int blocks = (k >= GRAM && k < GRAM_JOIN) || (k >= POLY && k < POLY_JOIN) || k >= APPLY ? round_up(R[k].total, 8) : R[k].total;
+        const int blocks = (k >= GRAM && k < GRAM_JOIN) || (k >= POLY && k < POLY_JOIN) || (k >= APPLY && k < MERGE) ? round_up(R[k].total, 8) : R[k].total;
         hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), block, 0, st, R[k], more...);
     };
     hipLaunchKernelGGL(orth_norm_kernel, dim3((unsigned)R[NORM].total), block, 0, st, L, list);
@@ -1257,6 +1424,12 @@ hipError_t launch_wide(const xconv_orth_item *const *items, int count, const xco
         go(orth_square_kernel<64, 1>, POLY);
         go(orth_square_kernel<128, 1>, POLY + 1);
         go(orth_join_kernel<1>, POLY_JOIN);
+        if (R[MERGE].total) {
+            if (P.merge_mb == 4 && P.merge_cb == 1) launch_merge<4, 1>(R[MERGE], odd, last, st);
+            else if (P.merge_mb == 4) launch_merge<4, 2>(R[MERGE], odd, last, st);
+            else if (P.merge_cb == 1) launch_merge<8, 1>(R[MERGE], odd, last, st);
+            else launch_merge<8, 2>(R[MERGE], odd, last, st);
+        }
         if (!last) {
             go(orth_apply_kernel<64, 0>, APPLY, odd);
             go(orth_apply_kernel<128, 0>, APPLY + 1, odd);

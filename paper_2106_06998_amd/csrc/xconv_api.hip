@@ -1403,14 +1403,14 @@ xconv_status check_orth(const xconv_orth_item *items, int count, const xconv_ort
         if (t.rows > (1 << 24) || t.cols > (1 << 24) || std::min(t.rows, t.cols) > 32768 || (long long)t.rows * t.cols > (1LL << 31)) return XCONV_EUNSUPPORTED;
     }
     if (a->steps > 64) return XCONV_EUNSUPPORTED;
-    // how far the steps take singular values from [0, 1]: the fp16 numbers hold entries below 16 of X, X X^T and the polynomial
+    // how far the steps take singular values from [0, 1]: the fp16 numbers hold entries below 16 of X, X X^T, the polynomial and b X + c A X
     double top = 1.0;
     for (int k = 0; k < a->steps; ++k) {
         if (!(top <= 3.5)) return XCONV_EUNSUPPORTED;
         double next = 0.0;
         for (int j = 0; j <= 512; ++j) {
             const double v = top * j / 512, l = v * v, q = a->a + (a->b + a->c * l) * l;
-            if (!(std::fabs(q) <= 12.0)) return XCONV_EUNSUPPORTED;
+            if (!(std::fabs(q) <= 12.0) || !(std::fabs(v * (a->b + a->c * l)) <= 12.0)) return XCONV_EUNSUPPORTED;
             next = std::max(next, std::fabs(v * q));
         }
         top = next;

@@ -75,7 +75,7 @@ def test_orth_statuses():
         both(items(bad), 1, args, xb.XCONV_EUNSUPPORTED)
     for kw, status in (({"g_dtype": 3}, 1), ({"out_dtype": -1}, 1), ({"steps": -1}, 1), ({"steps": 65}, 2), ({"eps": -1.0}, 1), ({"eps": float("nan")}, 1),
                        ({"coefficients": (float("inf"), 0, 0)}, 1), ({"coefficients": (13.0, 0, 0)}, 2), ({"coefficients": (4.0, 0, 0)}, 2),
-                       ({"coefficients": (1.5, 0.5, 0.0), "steps": 20}, 2)):
+                       ({"coefficients": (1.5, 0.5, 0.0), "steps": 20}, 2), ({"coefficients": (1.0, 40.0, -40.0)}, 2)):
         both(items((4, 4)), 1, xb.make_orth_args(**kw), status)
     # a last step may end anywhere: only what is split into fp16 numbers is bounded
     assert xb.xconv_orth_workspace_bytes(items((4, 4)), 1, xb.make_orth_args(coefficients=(4.0, 0, 0), steps=1)) > 0
