@@ -16,13 +16,14 @@
 // Launches cover all matrices of a call: a workgroup finds its matrix in the list of first tiles.
 //
 // Three ways, by the matrix' own extents: up to 64 x 768 all steps in one workgroup (orth_narrow_kernel); up to 256 rows two launches
-// a step, X X^T and both products by A (orth_merge_kernel); else three, X X^T, P and P X, in tiles of 64 x 64 or 128 x 128.  The sums
+// a step, X X^T and both products by A (orth_merge_kernel); else three, X X^T, P and P X, in tiles of 64 x 64 or 128 x 128, and where
+// n >= 2 m only the first and the last of them once for up to three steps (see `grouped`).  The sums
 // of X X^T and A A are split along k where their tiles are too few for the chip and joined in order by another launch.  What else
 // is in a call changes the tiles but not one bit of a result.
 //
 // Measured, five steps: 64 x 576 fp32 44 us (7.2 us a step, most of it one compute unit's matrix instructions), 200 x 147 88 us
-// (two launches of 6 to 9 us a step), 2048 x 4096 fp32 1.17 ms (three fp16 products for one: 0.8 to 0.98 PFLOP/s of them in the
-// three products, where a large library product reaches 1.2), 8 of 512 x 4608 0.88 ms.
+// (two launches of 6 to 9 us a step), 2048 x 4096 fp32 1.02 ms (three fp16 products for one: 0.8 to 0.98 PFLOP/s of them in the
+// large products, where a large library product reaches 1.2), 8 of 512 x 4608 bf16 with the weights' update 0.57 ms.
 #include <algorithm>
 #include <cmath>
 
@@ -49,7 +50,7 @@ struct OrthMat {
     const void *G;
     void *out;
     float *M;
-    _Float16 *X, *Xt, *Xt2, *A, *P;     // fragment order
+    _Float16 *X, *Xt, *Xt2, *S;         // fragment order; S: A and the other symmetric matrices, one after the other
     double *sq;                         // partial sums of squares
     float *part;                        // partial products of X X^T, [tile][split][tile values]
     int rows, cols, m, n, mp, np;       // m <= n
@@ -68,6 +69,11 @@ struct OrthList {
     OrthMat mat[kOrthItems];
 };
 static_assert(sizeof(OrthList) <= 4096, "kernel arguments");
+// A product of two symmetric matrices S_left S_right, symmetric itself, goes to S_out times `scale`
+struct Squares {
+    int left, right, out;
+    float scale;
+};
 // What the launches after the first are given: the list lies in the scratch
 struct OrthRef {
     OrthScalars s;
@@ -95,6 +101,8 @@ __device__ inline OrthMat the_mat(const OrthRef &L, int &b)
     if (L.s.count == 1) return L.one;
     return L.mat[find_mat(L.first, L.s.count, b)];
 }
+
+__device__ inline _Float16 *square_of(const OrthMat &q, int k) { return q.S + (size_t)k * q.mp * q.mp * 2; }
 
 __device__ inline float orth_get(const void *p, int dtype, size_t i)
 {
@@ -160,7 +168,7 @@ __device__ inline void split8(const float (&s)[8], h8 &h, h8 &l)
     }
 }
 // where row r, columns k .. k + 7 of a matrix in fragment order lie (the second numbers 512 values on)
-__device__ inline _Float16 *place_of(_Float16 *frag, int r, int k, int kblocks)
+template <class H> __device__ inline H *place_of(H *frag, int r, int k, int kblocks)
 {
     return frag + ((size_t)(r >> 5) * kblocks + (k >> 4)) * kBlockHalfs + ((r & 31) + 32 * ((k >> 3) & 1)) * 8;
 }
@@ -513,17 +521,18 @@ template <int MT, int NT> struct Tile {
         }
         __syncthreads();
     }
-    // the sums, in true scale, as t[row][column]
-    __device__ void spread(float (*t)[TN + 1]) const
+    // the sums, in true scale (times a factor), as t[row][column]
+    __device__ void spread(float (*t)[TN + 1], float factor = 1.f) const
     {
         const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+        const float unscale = kOrthUnscale * factor;
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
             for (int j = 0; j < NT; ++j)
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
-                    t[32 * (MT * (wave >> 1) + i) + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3)][32 * (NT * (wave & 1) + j) + (lane & 31)] = acc[i][j][e] * kOrthUnscale;
+                    t[32 * (MT * (wave >> 1) + i) + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3)][32 * (NT * (wave & 1) + j) + (lane & 31)] = acc[i][j][e] * unscale;
         __syncthreads();
     }
     // partial sums, in the order of the registers
@@ -577,18 +586,22 @@ __device__ inline void pair_of(int b, int &i, int &j)
     i = b - j * (j + 1) / 2;
 }
 
-// t is part of A = X X^T (POLY = 0) or of A A (1: P = a I + b A + c A A is stored).  Its rows are i0 on
+// What a product of symmetric tiles is: A = X X^T, P = a I + b A + c A A, or a product of two polynomials of X X^T
+enum { GRAM, POLY, MUL };
+
+// t is part of A (GRAM), of A A (POLY: P is stored) or of a product (MUL).  Its rows are i0 on
 // and its columns j0 on (STEP = 32), or, when it is the part (i, j) of a tile of 128, every other run of 32 of them (STEP = 64).
 // What lies on and above the diagonal blocks of 32 x 32 is stored on both sides of the diagonal, so that A and P are symmetric
 // to the last bit whatever the tiles.
-template <int T, int POLY, int STEP> __device__ inline void put_square(float (*t)[T + 1], const OrthMat &q, const OrthScalars &s, int i0, int j0)
+template <int T, int KIND, int STEP> __device__ inline void put_square(float (*t)[T + 1], const OrthMat &q, const OrthScalars &s, const Squares &u, int i0, int j0)
 {
-    _Float16 *out = POLY ? q.P : q.A;
+    _Float16 *out = square_of(q, u.out);
+    const _Float16 *A = square_of(q, u.left);
     auto along = [](int from, int r) { return from + STEP * (r >> 5) + (r & 31); };
     // eight values of the result, A A's being v, at (row, col) and right of it
     auto put = [&](int row, int col, float (&v)[8]) {
-        if constexpr (POLY == 1) {
-            const _Float16 *p = place_of(q.A, row, col, q.mp / 16);
+        if constexpr (KIND == POLY) {
+            const _Float16 *p = place_of(A, row, col, q.mp / 16);
             const h8 h = *reinterpret_cast<const h8 *>(p), l = *reinterpret_cast<const h8 *>(p + 512);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -598,8 +611,8 @@ template <int T, int POLY, int STEP> __device__ inline void put_square(float (*t
         }
         put_pieces(out, row, col, q.mp / 16, v);
     };
-    for (int u = threadIdx.x; u < T * T / 8; u += kThreads) {
-        const int r = u % T, c = u / T * 8;
+    for (int i = threadIdx.x; i < T * T / 8; i += kThreads) {
+        const int r = i % T, c = i / T * 8;
         float v[8];
         {
             const int row = along(i0, r), col = along(j0, c);
@@ -622,47 +635,45 @@ template <int T, int POLY, int STEP> __device__ inline void put_square(float (*t
     }
 }
 
-// POLY 0: a tile of X X^T, 1: of A A; b: number of the pair of rows of tiles and of the run along the sum
-template <int T, int POLY> __device__ inline void square_tile(const OrthMat &q, const OrthScalars &s, int b, TileLds<T> &lds)
-{
-    const int splits = POLY ? q.psplits : q.gsplits, run = POLY ? q.pkbs : q.gkbs, kblocks = (POLY ? q.mp : q.np) / 16;
-    const int split = b % splits, pair = b / splits;
-    const _Float16 *F = POLY ? q.A : q.X;
-    int ti, tj;
-    pair_of(pair, ti, tj);
-    Tile<T / 64, T / 64> t;
-    tile_of_product<T, 3>(lds, t, F, ti * T, F, tj * T, kblocks, split * run, min(kblocks, (split + 1) * run));
-    if (splits > 1) {
-        t.put_part(q.part + (size_t)b * T * T);
-        return;
-    }
-    t.spread(lds.t);
-    put_square<T, POLY, 32>(lds.t, q, s, ti * T, tj * T);
-}
-template <int T, int POLY> __global__ __launch_bounds__(kThreads, 2) void orth_square_kernel(OrthRef L)
+// a workgroup: a pair of rows of tiles and a run along the sum
+template <int T, int KIND> __global__ __launch_bounds__(kThreads, 2) void orth_square_kernel(OrthRef L, Squares u)
 {
     __shared__ TileLds<T> lds;
     int b = xcd_block(blockIdx.x, gridDim.x);
     if (b >= L.total) return;
     const OrthMat q = the_mat(L, b);
-    square_tile<T, POLY>(q, L.s, b, lds);
+    const bool gram = KIND == GRAM;
+    const int splits = gram ? q.gsplits : q.psplits, run = gram ? q.gkbs : q.pkbs, kblocks = (gram ? q.np : q.mp) / 16;
+    const int split = b % splits, pair = b / splits;
+    const _Float16 *left = gram ? q.X : square_of(q, u.left), *right = gram ? q.X : square_of(q, u.right);
+    int ti, tj;
+    pair_of(pair, ti, tj);
+    Tile<T / 64, T / 64> t;
+    tile_of_product<T, 3>(lds, t, left, ti * T, right, tj * T, kblocks, split * run, min(kblocks, (split + 1) * run));
+    if (splits > 1) {
+        t.put_part(q.part + (size_t)b * T * T);
+        return;
+    }
+    t.spread(lds.t, u.scale);
+    put_square<T, KIND, 32>(lds.t, q, L.s, u, ti * T, tj * T);
 }
 
 // adds up the runs of a product, in order: 64 x 64 values a workgroup
-template <int POLY> __global__ __launch_bounds__(kThreads) void orth_join_kernel(OrthRef L)
+template <int KIND> __global__ __launch_bounds__(kThreads) void orth_join_kernel(OrthRef L, Squares u)
 {
     __shared__ float t[64][64 + 1];
     int b = blockIdx.x;
     const OrthMat q = the_mat(L, b);
-    const int splits = POLY ? q.psplits : q.gsplits, parts = q.big[POLY] ? 4 : 1, pair = b / parts, part = b % parts;
+    const bool big = q.big[KIND == GRAM ? 0 : 1];
+    const int splits = KIND == GRAM ? q.gsplits : q.psplits, parts = big ? 4 : 1, pair = b / parts, part = b % parts;
     int ti, tj;
     pair_of(pair, ti, tj);
     Tile<1, 1> sum;
     sum.clear();
     for (int k = 0; k < splits; ++k) sum.add_part(q.part + ((size_t)(pair * splits + k) * parts + part) * 64 * 64);
-    sum.spread(t);
-    if (q.big[POLY]) put_square<64, POLY, 64>(t, q, L.s, ti * 128 + 32 * (part >> 1), tj * 128 + 32 * (part & 1));
-    else put_square<64, POLY, 32>(t, q, L.s, ti * 64, tj * 64);
+    sum.spread(t, u.scale);
+    if (big) put_square<64, KIND, 64>(t, q, L.s, u, ti * 128 + 32 * (part >> 1), tj * 128 + 32 * (part & 1));
+    else put_square<64, KIND, 32>(t, q, L.s, u, ti * 64, tj * 64);
 }
 
 // Part (m0, n0) of the result of the last step becomes O or the update of W: eight values in the order of memory a thread and
@@ -728,10 +739,10 @@ template <int TM, int TN, int NTHR = kThreads> struct Finish {
     }
 };
 
-// X <- P X, from the transposed X (Xt, or Xt2 when odd) to X and the other transposed one.  LAST 1: to the result instead.  2: the
+// X <- P X, P being `scale` times S_which, from the transposed X (Xt, or Xt2 when odd) to X and the other transposed one.  LAST 1: to the result instead.  2: the
 // same with the first fp16 numbers alone.  What that drops, 2^-12 of P and of X, goes into no further step: it is an eighth of what
 // rounding O to bf16 drops, and far below the rounding of 16-bit weights, of which the update is a small part.
-template <int T, int LAST> __global__ __launch_bounds__(kThreads, 2) void orth_apply_kernel(OrthRef L, int odd)
+template <int T, int LAST> __global__ __launch_bounds__(kThreads, 2) void orth_apply_kernel(OrthRef L, int odd, int which, float scale)
 {
     __shared__ TileLds<T> lds;
     int b = xcd_block(blockIdx.x, gridDim.x);
@@ -739,14 +750,14 @@ template <int T, int LAST> __global__ __launch_bounds__(kThreads, 2) void orth_a
     const OrthMat q = the_mat(L, b);
     const TileAt at = tile_at<T, T>(q, b);
     Tile<T / 64, T / 64> t;
-    tile_of_product<T, LAST == 2 ? 1 : 3>(lds, t, q.P, at.m0, odd ? q.Xt2 : q.Xt, at.n0, q.mp / 16, 0, q.mp / 16);
+    tile_of_product<T, LAST == 2 ? 1 : 3>(lds, t, square_of(q, which), at.m0, odd ? q.Xt2 : q.Xt, at.n0, q.mp / 16, 0, q.mp / 16);
     if constexpr (LAST > 0) {
         Finish<T, T> f(q, L.s, at.m0, at.n0);
         f.load();
-        t.spread(lds.t);
+        t.spread(lds.t, scale);
         f.put(lds.t);
     } else {
-        t.spread(lds.t);
+        t.spread(lds.t, scale);
         emit_x<T, T>(lds.t, q, odd ? q.Xt : q.Xt2, at.m0, at.n0);
     }
 }
@@ -778,7 +789,7 @@ template <int MB, int CB, int LAST> __global__ __launch_bounds__(64 * MB, MB == 
     for (int j = 0; j < CB * KB * 128 / NTHR; ++j) r[j] = j * NTHR + tid < CB * units ? x[j * NTHR + tid] : u32x4{0, 0, 0, 0};
     h8 a[KB][2];
     if (mine) {
-        const h8 *f = reinterpret_cast<const h8 *>(q.A + (size_t)wave * kblocks * kBlockHalfs) + lane;
+        const h8 *f = reinterpret_cast<const h8 *>(q.S + (size_t)wave * kblocks * kBlockHalfs) + lane;
 #pragma unroll
         for (int k = 0; k < KB; ++k)
             if (k < kblocks) {
@@ -1206,10 +1217,50 @@ int splits_of(int m, int kblocks)
 bool narrow(const xconv_orth_item &it) { return std::min(it.rows, it.cols) <= kNarrowM && std::max(it.rows, it.cols) <= kNarrowN; }
 
 constexpr int kMergeM = 256;        // most rows of a matrix that takes both products by A in one launch
+
+// Steps on A alone.  A step's polynomial P of A commutes with A, so the next step's A is P A P and two steps are one product
+// P' P by X: three products of m x m matrices take the place of X X^T and P X.  That is less work where n > m (five steps, one at a
+// time against groups: 8 of 512 x 4608 820 and 530 us, 8 of 512 x 1024 335 and 313, 2048 x 4096 1119 and 1010, but one of 512 x 1024
+// 176 and 187).
+bool grouped(const xconv_orth_item &it)
+{
+    const int m = std::min(it.rows, it.cols), n = std::max(it.rows, it.cols);
+    return m > kMergeM && n >= 2 * m;
+}
+// The steps in groups of at most three, then two.  An error of A is multiplied by up to |d (l q(l)^2) / dl| a step (l: an eigenvalue
+// of A, q the polynomial), 11.9 with a = 3.44, where it would fade with a new X X^T; products of P are kept as a sixteenth of
+// themselves, below 16.  With a = 3.44 and five steps, three and two steps: errors of 2e-6 to 4e-6 as with one at a time; two, two and
+// one: 4e-6 to 6e-6, four and one: 8e-6 to 15e-6 (512 x 4608, 1000 x 1100).
+int groups_of(const xconv_orth_args *args, int (&sizes)[64])
+{
+    int groups = 0;
+    double top = 1.0;
+    for (int k = 0; k < args->steps;) {
+        const int most = k == 0 ? 3 : 2;
+        double growth = 1.0, largest = 1.0;
+        int n = 0;
+        for (; n < most && k < args->steps; ++n, ++k) {
+            double g = 0.0, p = 0.0, next = 0.0;
+            for (int j = 0; j <= 512; ++j) {
+                const double v = top * j / 512, l = v * v, q = args->a + (args->b + args->c * l) * l, slope = args->b + 2.0 * args->c * l;
+                g = std::max(g, std::fabs(q * q + 2.0 * l * q * slope));
+                p = std::max(p, std::fabs(q));
+                next = std::max(next, std::fabs(v * q));
+            }
+            if (n > 0 && (growth > 160.0 || largest * p > 192.0)) break;
+            growth *= std::max(1.0, g);
+            largest *= p;
+            top = next;
+        }
+        sizes[groups++] = n;
+    }
+    return groups;
+}
+constexpr float kGroupScale = 1.f / 16.f;
 struct OrthPlan {
     int count, merge_mb, merge_cb;  // blocks of 32 rows and columns of the workgroups of that launch
     struct Mat {
-        int m, n, mp, np, big[3], merge, gsplits, gkbs, psplits, pkbs, tiles[3];
+        int m, n, mp, np, big[3], merge, squares, gsplits, gkbs, psplits, pkbs, tiles[3];
         size_t x, a, part, bytes;
     } mat[kOrthItems];
     size_t bytes;
@@ -1261,10 +1312,11 @@ OrthPlan plan_orth(const xconv_orth_item *const *items, int count)
         split(q.n, q.gsplits, q.gkbs);
         split(q.m, q.psplits, q.pkbs);
         q.x = up256((size_t)q.mp * q.np * 4);
-        q.a = up256((size_t)q.mp * q.mp * 4);
+        q.a = (size_t)q.mp * q.mp * 4;       // (a multiple of 256)
         auto partial = [&](int k, int count) { return count > 1 ? (size_t)q.tiles[k] * count * (q.big[k] ? 128 * 128 : 64 * 64) * 4 : 0; };
         q.part = up256(std::max(partial(0, q.gsplits), partial(1, q.psplits)));
-        q.bytes = 3 * q.x + 2 * q.a + q.part + up256(kOrthNorms * sizeof(double));
+        q.squares = grouped(*items[i]) ? 4 : q.merge ? 1 : 2;
+        q.bytes = 3 * q.x + q.squares * q.a + q.part + up256(kOrthNorms * sizeof(double));
         P.bytes += q.bytes;
     }
     // (64 columns read A half as often; 32 are twice as many workgroups)
@@ -1274,19 +1326,22 @@ OrthPlan plan_orth(const xconv_orth_item *const *items, int count)
 
 }  // namespace
 
-// Calls `run` with the next kOrthItems matrices that the narrow kernel does not take until there are none, those of few rows first:
-// their workgroups make room early for the last ones of a launch that has a few more than the chip holds
+// Calls `run` with the next kOrthItems matrices that the narrow kernel does not take until there are none, first those that take their
+// steps one at a time.  Within a run those of few rows come first: their workgroups make room early for the last ones of a launch that
+// has a few more than the chip holds.
 namespace {
 template <class F> bool wide_runs(const xconv_orth_item *items, int count, F &&run)
 {
     const xconv_orth_item *list[kOrthItems];
-    int n = 0;
-    for (int i = 0; i <= count; ++i) {
-        if (i < count && !narrow(items[i])) list[n++] = items + i;
-        if (n == kOrthItems || (i == count && n)) {
-            std::stable_sort(list, list + n, [](const xconv_orth_item *a, const xconv_orth_item *b) { return std::min(a->rows, a->cols) < std::min(b->rows, b->cols); });
-            if (!run(list, n)) return false;
-            n = 0;
+    for (bool group : {false, true}) {
+        int n = 0;
+        for (int i = 0; i <= count; ++i) {
+            if (i < count && !narrow(items[i]) && grouped(items[i]) == group) list[n++] = items + i;
+            if (n == kOrthItems || (i == count && n)) {
+                std::stable_sort(list, list + n, [](const xconv_orth_item *a, const xconv_orth_item *b) { return std::min(a->rows, a->cols) < std::min(b->rows, b->cols); });
+                if (!run(list, n)) return false;
+                n = 0;
+            }
         }
     }
     return true;
@@ -1370,7 +1425,7 @@ hipError_t launch_wide(const xconv_orth_item *const *items, int count, const xco
     auto take = [&](size_t bytes) { char *r = p; p += bytes; return r; };
     OrthMat *list = (OrthMat *)take(up256(sizeof(OrthMat) * kOrthItems));
     // the first workgroups of the matrices in the launches (products: tiles of 64, of 128)
-    enum { NORM, START, GRAM, GRAM_JOIN = GRAM + 2, POLY, POLY_JOIN = POLY + 2, APPLY, MERGE = APPLY + 2, KINDS };
+    enum { NORM, START, XX, XX_JOIN = XX + 2, SQUARE, SQUARE_JOIN = SQUARE + 2, APPLY, MERGE = APPLY + 2, KINDS };
     OrthRef R[KINDS];
     for (OrthRef &r : R) r = OrthRef{L.s, 0, {}, list, {}};
     for (int i = 0; i < count; ++i) {
@@ -1382,7 +1437,7 @@ hipError_t launch_wide(const xconv_orth_item *const *items, int count, const xco
         for (int k = 0; k < 3; ++k) q.big[k] = f.big[k];
         q.gsplits = f.gsplits; q.gkbs = f.gkbs; q.psplits = f.psplits; q.pkbs = f.pkbs;
         q.X = (_Float16 *)take(f.x); q.Xt = (_Float16 *)take(f.x); q.Xt2 = (_Float16 *)take(f.x);
-        q.A = (_Float16 *)take(f.a); q.P = (_Float16 *)take(f.a);
+        q.S = (_Float16 *)take(f.squares * f.a);
         q.part = (float *)take(f.part);
         q.sq = (double *)take(up256(kOrthNorms * sizeof(double)));
         q.nsq = (int)std::min<size_t>(kOrthNorms, ((size_t)it.rows * it.cols + 4095) / 4096);
@@ -1390,11 +1445,11 @@ hipError_t launch_wide(const xconv_orth_item *const *items, int count, const xco
         int blocks[KINDS] = {};
         blocks[NORM] = q.nsq;
         blocks[START] = (f.mp / kOrthTile) * (f.np / kOrthTile);
-        blocks[GRAM + f.big[0]] = f.tiles[0] * f.gsplits;
-        blocks[GRAM_JOIN] = f.gsplits > 1 ? f.tiles[0] * (f.big[0] ? 4 : 1) : 0;
+        blocks[XX + f.big[0]] = f.tiles[0] * f.gsplits;
+        blocks[XX_JOIN] = f.gsplits > 1 ? f.tiles[0] * (f.big[0] ? 4 : 1) : 0;
         if (f.merge) blocks[MERGE] = f.np / (32 * P.merge_cb);
-        else blocks[POLY + f.big[1]] = f.tiles[1] * f.psplits;
-        blocks[POLY_JOIN] = !f.merge && f.psplits > 1 ? f.tiles[1] * (f.big[1] ? 4 : 1) : 0;
+        else blocks[SQUARE + f.big[1]] = f.tiles[1] * f.psplits;
+        blocks[SQUARE_JOIN] = !f.merge && f.psplits > 1 ? f.tiles[1] * (f.big[1] ? 4 : 1) : 0;
         if (!f.merge) blocks[APPLY + f.big[2]] = f.tiles[2];
         for (int k = 0; k < KINDS; ++k) {
             R[k].first[i] = R[k].total;
@@ -1407,21 +1462,49 @@ hipError_t launch_wide(const xconv_orth_item *const *items, int count, const xco
     // (products: whole rounds of the eight dies)
     auto go = [&](auto kernel, int k, auto... more) {
         if (!R[k].total) return;
-        const int blocks = (k >= GRAM && k < GRAM_JOIN) || (k >= POLY && k < POLY_JOIN) || (k >= APPLY && k < MERGE) ? round_up(R[k].total, 8) : R[k].total;
+        const int blocks = (k >= XX && k < XX_JOIN) || (k >= SQUARE && k < SQUARE_JOIN) || (k >= APPLY && k < MERGE) ? round_up(R[k].total, 8) : R[k].total;
         hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), block, 0, st, R[k], more...);
     };
     hipLaunchKernelGGL(orth_norm_kernel, dim3((unsigned)R[NORM].total), block, 0, st, L, list);
     go(orth_start_kernel, START);
     if (args->steps == 0) go(orth_none_kernel, START);
-    for (int k = 0; k < args->steps; ++k) {
+    // S_out = polynomial of A, or S_left S_right
+    auto poly = [&](int out) {
+        const Squares u{0, 0, out, 1.f};
+        go(orth_square_kernel<64, POLY>, SQUARE, u);
+        go(orth_square_kernel<128, POLY>, SQUARE + 1, u);
+        go(orth_join_kernel<POLY>, SQUARE_JOIN, u);
+    };
+    auto mul = [&](int left, int right, int out, float scale = 1.f) {
+        const Squares u{left, right, out, scale};
+        go(orth_square_kernel<64, MUL>, SQUARE, u);
+        go(orth_square_kernel<128, MUL>, SQUARE + 1, u);
+        go(orth_join_kernel<MUL>, SQUARE_JOIN, u);
+    };
+    int sizes[64], groups = args->steps;
+    if (grouped(*items[0])) groups = groups_of(args, sizes);
+    else std::fill(sizes, sizes + groups, 1);
+    for (int k = 0; k < groups; ++k) {
         const int odd = k & 1;
-        const bool last = k + 1 == args->steps;
-        go(orth_square_kernel<64, 0>, GRAM);
-        go(orth_square_kernel<128, 0>, GRAM + 1);
-        go(orth_join_kernel<0>, GRAM_JOIN);
-        go(orth_square_kernel<64, 1>, POLY);
-        go(orth_square_kernel<128, 1>, POLY + 1);
-        go(orth_join_kernel<1>, POLY_JOIN);
+        const bool last = k + 1 == groups;
+        const Squares gram{0, 0, 0, 1.f};
+        go(orth_square_kernel<64, GRAM>, XX, gram);
+        go(orth_square_kernel<128, GRAM>, XX + 1, gram);
+        go(orth_join_kernel<GRAM>, XX_JOIN, gram);
+        // A is S_0, the last polynomial S_p, the product of all of the group S_q, and S_t is free
+        int p = 1, q = 1, t = 2;
+        poly(p);
+        for (int j = 1; j < sizes[k]; ++j) {
+            mul(0, p, t);
+            mul(t, p, 0);
+            poly(t);
+            const int out = j == 1 ? 3 : p, free = j == 1 ? p : q;
+            mul(t, q, out, j == 1 ? kGroupScale : 1.f);
+            p = t;
+            q = out;
+            t = free;
+        }
+        const float scale = sizes[k] > 1 ? 1.f / kGroupScale : 1.f;
         if (R[MERGE].total) {
             if (P.merge_mb == 4 && P.merge_cb == 1) launch_merge<4, 1>(R[MERGE], odd, last, st);
             else if (P.merge_mb == 4) launch_merge<4, 2>(R[MERGE], odd, last, st);
@@ -1429,14 +1512,14 @@ hipError_t launch_wide(const xconv_orth_item *const *items, int count, const xco
             else launch_merge<8, 2>(R[MERGE], odd, last, st);
         }
         if (!last) {
-            go(orth_apply_kernel<64, 0>, APPLY, odd);
-            go(orth_apply_kernel<128, 0>, APPLY + 1, odd);
+            go(orth_apply_kernel<64, 0>, APPLY, odd, q, scale);
+            go(orth_apply_kernel<128, 0>, APPLY + 1, odd, q, scale);
         } else if (args->out_dtype == XCONV_BF16 || (muon && args->out_dtype == XCONV_F16)) {
-            go(orth_apply_kernel<64, 2>, APPLY, odd);
-            go(orth_apply_kernel<128, 2>, APPLY + 1, odd);
+            go(orth_apply_kernel<64, 2>, APPLY, odd, q, scale);
+            go(orth_apply_kernel<128, 2>, APPLY + 1, odd, q, scale);
         } else {
-            go(orth_apply_kernel<64, 1>, APPLY, odd);
-            go(orth_apply_kernel<128, 1>, APPLY + 1, odd);
+            go(orth_apply_kernel<64, 1>, APPLY, odd, q, scale);
+            go(orth_apply_kernel<128, 1>, APPLY + 1, odd, q, scale);
         }
     }
     return hipGetLastError();

@@ -387,3 +387,54 @@ def test_muon_on_large_layers():
         want, m1, bound = muon_reference(ws[2].to(TD[dtype]), gs[2].to(TD[dtype]), torch.zeros(300, 1300), 0.05, 0.9, 0.1, True)
         off = np.linalg.norm(wd[2].cpu().double().numpy() - want)
         assert off <= bound + (UOUT[dtype] + 3 * 2.0 ** -24) * np.linalg.norm(want)
+
+
+# ---- steps in groups: the next A from this one (matrices of more than 256 rows that are at least twice as wide) ---------------
+def group_bound(g, steps, coef, eps=1e-7):
+    """The bound above where every step's A may come from the one before it: an error of A grows by at most
+    G = max |d (l q(l)^2) / dl| a step, and at most two steps lie between X X^T and the A that is used."""
+    a, b, c = coef
+    want, bound = exact_orth(g, steps, coef, eps)
+    l = np.linspace(0, 1.3, 400)
+    q, slope = a + b * l + c * l * l, b + 2 * c * l
+    grow = max(1.0, float(np.abs(q * q + 2 * l * q * slope).max()))
+    return want, bound * 3 * grow ** 2
+
+
+@pytest.mark.parametrize("shape", [(257, 514), (514, 257), (300, 1500), (390, 781)])
+@pytest.mark.parametrize("steps,coef", [(1, COEF), (2, COEF), (3, COEF), (4, COEF), (5, COEF), (6, COEF), (7, COEF), (9, (1.875, -1.25, 0.375)), (6, (1.5, -0.5, 0.0))])
+def test_steps_in_groups(shape, steps, coef):
+    say("orthogonalize", shape, steps, coef)
+    g = gradient(*shape, 5 + steps)
+    o = optim.orthogonalize(g.to(DEV), steps, coef)
+    torch.cuda.synchronize()
+    want, bound = group_bound(g.double().numpy(), steps, coef)
+    off = np.linalg.norm(o.cpu().double().numpy() - want)
+    size = np.linalg.norm(want)
+    assert off <= bound + 2.0 ** -24 * size
+    assert off <= 2e-5 * size       # a large matrix' bound says little: of the order of fp32 products
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_groups_of_sixteen_bits(dtype):
+    for shape in ((260, 600), (600, 260)):
+        say("orthogonalize", shape, dtype)
+        g = gradient(*shape, 8, dtype)
+        o = optim.orthogonalize(g.to(DEV))
+        torch.cuda.synchronize()
+        want, bound = group_bound(g.double().numpy(), 5, COEF)
+        size = np.linalg.norm(want)
+        assert np.linalg.norm(o.cpu().double().numpy() - want) <= min(bound, 2e-5 * size) + (2.0 ** -8 if dtype == "bf16" else 2.0 ** -11) * size
+
+
+def test_groups_beside_single_steps():
+    """A list of both kinds and of small matrices: the same bits as alone, in any order."""
+    shapes = [(300, 700), (64, 90), (300, 400), (1000, 270), (130, 900), (257, 514)]
+    gs = [gradient(*s, 40 + i).to(DEV) for i, s in enumerate(shapes)]
+    many = optim.orthogonalize(gs)
+    turned = optim.orthogonalize(gs[::-1])[::-1]
+    torch.cuda.synchronize()
+    for i, g in enumerate(gs):
+        one = optim.orthogonalize(g)
+        torch.cuda.synchronize()
+        assert torch.equal(one, many[i]) and torch.equal(one, turned[i]), shapes[i]
