@@ -16,8 +16,8 @@
 // Launches cover all matrices of a call: a workgroup finds its matrix in the list of first tiles.
 //
 // Three ways, by the matrix' own extents: up to 64 x 768 all steps in one workgroup (orth_narrow_kernel); up to 256 rows two launches
-// a step, X X^T and both products by A (orth_merge_kernel); else three, X X^T, P and P X, in tiles of 64 x 64 or 128 x 128, and where
-// n >= 2 m only the first and the last of them once for up to three steps (see `grouped`).  The sums
+// a step, X X^T and both products by A (orth_merge_kernel); else three, X X^T, P and P X, in tiles of 64 x 64 or 128 x 128.  Wide
+// matrices of 128 rows and 2^18 values or more take only the first and the last of these three once for up to three steps (see `grouped`).  The sums
 // of X X^T and A A are split along k where their tiles are too few for the chip and joined in order by another launch.  What else
 // is in a call changes the tiles but not one bit of a result.
 //
@@ -26,6 +26,8 @@
 // large products, where a large library product reaches 1.2), 8 of 512 x 4608 bf16 with the weights' update 0.57 ms.
 #include <algorithm>
 #include <cmath>
+#include <mutex>
+#include <vector>
 
 #include "common.h"
 #include "launch.h"
@@ -1206,31 +1208,34 @@ size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 // X X^T 43 us in tiles of 128 and 62 us in tiles of 64; A A, which has 80 tiles of 128 there, 43 and 17 us).
 //
 // Sums along k are split so that a matrix has about as many workgroups as the chip has compute units, or twice as many of the
-// large tiles: by the matrix' own extents, so that what else is in the call does not change its result.
-constexpr int kFewestBlocks = 24;
+// large tiles: by the matrix' own extents, so that what else is in the call does not change its result.  A run of fewer than 24 (large
+// tiles: 40) blocks costs more in the launch that joins than it gives.  Products of square matrices are split from 1536 rows on
+// (five steps of 2048 x 4096: 1022 us with three runs, 1203 with one; 1024 x 2048: 364 us with two runs, 311 with one).
 int splits_of(int m, int kblocks)
 {
     const int t64 = ceil_div(m, 64) * (ceil_div(m, 64) + 1) / 2, t128 = ceil_div(m, 128) * (ceil_div(m, 128) + 1) / 2;
     const int want = m <= 1024 ? (224 + t64 / 2) / t64 : 448 / t128;
-    return std::max(1, std::min(want, kblocks / kFewestBlocks));
+    return std::max(1, std::min(want, kblocks / (m <= 1024 ? 24 : 40)));
 }
 bool narrow(const xconv_orth_item &it) { return std::min(it.rows, it.cols) <= kNarrowM && std::max(it.rows, it.cols) <= kNarrowN; }
 
 constexpr int kMergeM = 256;        // most rows of a matrix that takes both products by A in one launch
 
 // Steps on A alone.  A step's polynomial P of A commutes with A, so the next step's A is P A P and two steps are one product
-// P' P by X: three products of m x m matrices take the place of X X^T and P X.  That is less work where n > m (five steps, one at a
-// time against groups: 8 of 512 x 4608 820 and 530 us, 8 of 512 x 1024 335 and 313, 2048 x 4096 1119 and 1010, but one of 512 x 1024
-// 176 and 187).
+// P' P by X: three products of m x m matrices take the place of X X^T and P X.  That is less work where n > m, but more launches: a
+// matrix alone gains from about 700000 values on (five steps, one at a time against groups: 512 x 4608 238 and 210 us, 512 x 1024 176
+// and 187, 256 x 2304 137 and 147), several at once earlier (8 of 512 x 4608 820 and 530, 8 of 512 x 1024 335 and 313, 6 of 256 x 2304
+// 209 and 181, 16 of 256 x 1152 293 and 193, 4 of 700 x 1100 358 and 350).
 bool grouped(const xconv_orth_item &it)
 {
     const int m = std::min(it.rows, it.cols), n = std::max(it.rows, it.cols);
-    return m > kMergeM && n >= 2 * m;
+    return m >= 128 && n >= 2 * m && (long long)m * n >= 1 << 18;
 }
 // The steps in groups of at most three, then two.  An error of A is multiplied by up to |d (l q(l)^2) / dl| a step (l: an eigenvalue
-// of A, q the polynomial), 11.9 with a = 3.44, where it would fade with a new X X^T; products of P are kept as a sixteenth of
-// themselves, below 16.  With a = 3.44 and five steps, three and two steps: errors of 2e-6 to 4e-6 as with one at a time; two, two and
-// one: 4e-6 to 6e-6, four and one: 8e-6 to 15e-6 (512 x 4608, 1000 x 1100).
+// of A, q the polynomial), 11.9 with a = 3.44, where it would fade with a new X X^T; at the start A is small.  Products of P are kept as
+// a sixteenth of themselves, below 16.  Five steps with a = 3.44, simulated: gradients of 200 to 800 rows 2.2e-6 to 3.2e-6 in groups of
+// three and two, 1.3e-6 to 2.3e-6 one at a time and with fp32 products; matrices of equal singular values 2.7e-6 to 7.4e-6 against
+// 1.5e-6 to 2.1e-6; below 128 rows up to 1e-5 against 1.3e-6.
 int groups_of(const xconv_orth_args *args, int (&sizes)[64])
 {
     int groups = 0;
@@ -1271,13 +1276,14 @@ OrthPlan plan_orth(const xconv_orth_item *const *items, int count)
     OrthPlan P{};
     P.count = count;
     auto can = [](int m) { return m > kMergeM; };
-    auto splits = [](int m, int extent) { return splits_of(m, round_up(extent, 64) / 16); };
+    auto runs = [](int m, int n) { return splits_of(m, round_up(n, 64) / 16); };              // of X X^T
+    auto runs_square = [&](int m) { return m <= 1536 ? 1 : runs(m, m); };                    // of the others
     long long large[3] = {0, 0, 0};     // workgroups with tiles of 128
     for (int i = 0; i < count; ++i) {
         const int m = std::min(items[i]->rows, items[i]->cols), n = std::max(items[i]->rows, items[i]->cols), tm = ceil_div(m, 128);
         if (!can(m)) continue;
-        large[0] += (long long)tm * (tm + 1) / 2 * splits(m, n);
-        large[1] += (long long)tm * (tm + 1) / 2 * splits(m, m);
+        large[0] += (long long)tm * (tm + 1) / 2 * runs(m, n);
+        large[1] += (long long)tm * (tm + 1) / 2 * runs_square(m);
         large[2] += (long long)tm * ceil_div(n, 128);
     }
     long long columns = 0;
@@ -1293,7 +1299,7 @@ OrthPlan plan_orth(const xconv_orth_item *const *items, int count)
         }
         q.mp = round_up(q.m, T);
         q.np = round_up(q.n, T);
-        q.merge = q.m <= kMergeM;
+        q.merge = q.m <= kMergeM && !grouped(*items[i]);
         if (q.merge) {
             P.merge_mb = std::max(P.merge_mb, q.mp <= 128 ? 4 : 8);
             columns += q.np;
@@ -1305,10 +1311,11 @@ OrthPlan plan_orth(const xconv_orth_item *const *items, int count)
         // (extents padded to 64 for the splits, runs of whole steps)
         auto split = [&](int extent, int &count, int &run) {
             const int kb = round_up(extent, 64) / 16;
-            count = splits(q.m, extent);
             run = count > 1 ? round_up(ceil_div(kb, count), 4) : std::max(q.mp, q.np) / 16;
             if (count > 1) count = ceil_div(kb, run);
         };
+        q.gsplits = runs(q.m, q.n);
+        q.psplits = runs_square(q.m);
         split(q.n, q.gsplits, q.gkbs);
         split(q.m, q.psplits, q.pkbs);
         q.x = up256((size_t)q.mp * q.np * 4);
@@ -1326,25 +1333,36 @@ OrthPlan plan_orth(const xconv_orth_item *const *items, int count)
 
 }  // namespace
 
-// Calls `run` with the next kOrthItems matrices that the narrow kernel does not take until there are none, first those that take their
-// steps one at a time.  Within a run those of few rows come first: their workgroups make room early for the last ones of a launch that
-// has a few more than the chip holds.
 namespace {
-template <class F> bool wide_runs(const xconv_orth_item *items, int count, F &&run)
+// What a matrix takes: one workgroup, a step at a time, steps in groups
+enum { NARROW, SINGLE, GROUPED };
+int kind_of(const xconv_orth_item &it) { return narrow(it) ? NARROW : grouped(it) ? GROUPED : SINGLE; }
+
+// Calls `run` with the next kOrthItems matrices of a kind until there are none.  Within a run those of few rows come first: their
+// workgroups make room early for the last ones of a launch that has a few more than the chip holds.
+template <class F> bool wide_runs(const xconv_orth_item *items, int count, int kind, F &&run)
 {
     const xconv_orth_item *list[kOrthItems];
-    for (bool group : {false, true}) {
-        int n = 0;
-        for (int i = 0; i <= count; ++i) {
-            if (i < count && !narrow(items[i]) && grouped(items[i]) == group) list[n++] = items + i;
-            if (n == kOrthItems || (i == count && n)) {
-                std::stable_sort(list, list + n, [](const xconv_orth_item *a, const xconv_orth_item *b) { return std::min(a->rows, a->cols) < std::min(b->rows, b->cols); });
-                if (!run(list, n)) return false;
-                n = 0;
-            }
+    int n = 0;
+    for (int i = 0; i <= count; ++i) {
+        if (i < count && kind_of(items[i]) == kind) list[n++] = items + i;
+        if (n == kOrthItems || (i == count && n)) {
+            std::stable_sort(list, list + n, [](const xconv_orth_item *a, const xconv_orth_item *b) { return std::min(a->rows, a->cols) < std::min(b->rows, b->cols); });
+            if (!run(list, n)) return false;
+            n = 0;
         }
     }
     return true;
+}
+// the scratch of the runs of a kind, which go one after the other through it
+size_t kind_ws(const xconv_orth_item *items, int count, int kind)
+{
+    size_t most = 0;
+    wide_runs(items, count, kind, [&](const xconv_orth_item *const *list, int n) {
+        most = std::max(most, plan_orth(list, n).bytes);
+        return true;
+    });
+    return most;
 }
 
 OrthScalars scalars_of(const xconv_orth_args *args, const xconv_muon_args *muon)
@@ -1526,22 +1544,110 @@ hipError_t launch_wide(const xconv_orth_item *const *items, int count, const xco
 }
 }  // namespace
 
-// the runs go one after the other through the same scratch
+namespace {
+// Streams beside the caller's for the kinds of matrices of a call: each kind is a chain of launches that leave most of the chip idle
+// (18 layers of three kinds: 379 us one kind after the other, 215 us beside each other; 64 x 576 and 128 x 1152: 146 and 111).  They start after what the caller's stream holds
+// and it goes on after them, so a call looks as if all of it ran there.  Kept for later calls; one call at a time has them.
+struct Sides {
+    int device;
+    hipStream_t stream[2];
+    hipEvent_t start, done[2];
+};
+std::mutex g_sides_mu;
+std::vector<Sides> &free_sides()
+{
+    static std::vector<Sides> *sides = new std::vector<Sides>;       // (never destroyed: the runtime may be gone by then)
+    return *sides;
+}
+bool take_sides(Sides &out)
+{
+    int device = 0;
+    if (hipGetDevice(&device) != hipSuccess) return false;
+    {
+        std::lock_guard<std::mutex> lk(g_sides_mu);
+        std::vector<Sides> &f = free_sides();
+        for (size_t i = 0; i < f.size(); ++i)
+            if (f[i].device == device) {
+                out = f[i];
+                f.erase(f.begin() + i);
+                return true;
+            }
+    }
+    Sides s{device, {nullptr, nullptr}, nullptr, {nullptr, nullptr}};
+    bool ok = hipEventCreateWithFlags(&s.start, hipEventDisableTiming) == hipSuccess;
+    for (int i = 0; i < 2; ++i)
+        ok = ok && hipStreamCreateWithFlags(&s.stream[i], hipStreamNonBlocking) == hipSuccess && hipEventCreateWithFlags(&s.done[i], hipEventDisableTiming) == hipSuccess;
+    if (ok) {
+        out = s;
+        return true;
+    }
+    for (int i = 0; i < 2; ++i) {
+        if (s.done[i]) (void)hipEventDestroy(s.done[i]);
+        if (s.stream[i]) (void)hipStreamDestroy(s.stream[i]);
+    }
+    if (s.start) (void)hipEventDestroy(s.start);
+    return false;
+}
+void give_sides(const Sides &s)
+{
+    std::lock_guard<std::mutex> lk(g_sides_mu);
+    free_sides().push_back(s);
+}
+}  // namespace
+
 size_t orth_ws_bytes(const xconv_orth_item *items, int count)
 {
-    size_t most = 256;
-    wide_runs(items, count, [&](const xconv_orth_item *const *list, int n) {
-        most = std::max(most, plan_orth(list, n).bytes);
-        return true;
-    });
-    return most;
+    return std::max<size_t>(256, kind_ws(items, count, SINGLE) + kind_ws(items, count, GROUPED));
 }
 
 hipError_t launch_orth(const xconv_orth_item *items, int count, const xconv_orth_args *args, const xconv_muon_args *muon, void *ws, hipStream_t st)
 {
-    hipError_t e = launch_narrow(items, count, args, muon, st);
-    if (e != hipSuccess) return e;
-    wide_runs(items, count, [&](const xconv_orth_item *const *list, int n) { return (e = launch_wide(list, n, args, muon, ws, st)) == hipSuccess; });
+    bool any[3] = {};
+    for (int i = 0; i < count; ++i) any[kind_of(items[i])] = true;
+    auto run = [&](int kind, hipStream_t on) {
+        if (kind == NARROW) return launch_narrow(items, count, args, muon, on);
+        void *at = kind == GROUPED ? static_cast<char *>(ws) + kind_ws(items, count, SINGLE) : ws;
+        hipError_t e = hipSuccess;
+        wide_runs(items, count, kind, [&](const xconv_orth_item *const *list, int n) { return (e = launch_wide(list, n, args, muon, at, on)) == hipSuccess; });
+        return e;
+    };
+    // (not while the caller's stream is captured: streams of a capture are not to be used by other calls until its end)
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    Sides sides;
+    bool beside = false;
+    if (any[NARROW] + any[SINGLE] + any[GROUPED] > 1) {
+        beside = hipStreamIsCapturing(st, &capture) == hipSuccess && capture == hipStreamCaptureStatusNone && take_sides(sides);
+        if (!beside) (void)hipGetLastError();
+    }
+    hipError_t e = hipSuccess;
+    if (!beside) {
+        for (int kind : {NARROW, GROUPED, SINGLE})
+            if (any[kind] && e == hipSuccess) e = run(kind, st);
+        return e;
+    }
+    // the longest chain stays on the caller's stream
+    const int own = any[GROUPED] ? GROUPED : SINGLE;
+    int used = 0;
+    e = hipEventRecord(sides.start, st);
+    for (int kind : {NARROW, GROUPED, SINGLE}) {
+        if (!any[kind] || e != hipSuccess) continue;
+        hipStream_t on = st;
+        if (kind != own) {
+            on = sides.stream[used];
+            e = hipStreamWaitEvent(on, sides.start, 0);
+            if (e != hipSuccess) break;
+            ++used;
+        }
+        e = run(kind, on);
+    }
+    // also after an error: what was launched ends before the caller's stream goes on
+    for (int i = 0; i < used; ++i) {
+        hipError_t j = hipEventRecord(sides.done[i], sides.stream[i]);
+        if (j == hipSuccess) j = hipStreamWaitEvent(st, sides.done[i], 0);
+        if (j != hipSuccess) (void)hipStreamSynchronize(sides.stream[i]);
+        if (e == hipSuccess) e = j;
+    }
+    give_sides(sides);
     return e;
 }
 

@@ -438,3 +438,101 @@ def test_groups_beside_single_steps():
         one = optim.orthogonalize(g)
         torch.cuda.synchronize()
         assert torch.equal(one, many[i]) and torch.equal(one, turned[i]), shapes[i]
+
+
+@pytest.mark.parametrize("shape,dtype", [((70, 4000), "f32"), ((4000, 70), "bf16"), ((200, 1400), "f16"), ((256, 1100), "f32"), ((300, 900), "f16"), ((1025, 2100), "f32")])
+def test_groups_of_few_and_of_many_rows(shape, dtype):
+    say("orthogonalize", shape, dtype)
+    g = gradient(*shape, 9, dtype)
+    o = optim.orthogonalize(g.to(DEV))
+    torch.cuda.synchronize()
+    want, bound = group_bound(g.double().numpy(), 5, COEF)
+    size = np.linalg.norm(want)
+    assert np.linalg.norm(o.cpu().double().numpy() - want) <= min(bound, 2e-5 * size) + UOUT[dtype] * size
+
+
+KINDS = [(300, 900), (64, 90), (130, 200), (16, 144), (600, 500), (64, 4200)]
+
+
+def kinds_alone(seed):
+    """Weights, gradients and momenta of all kinds of matrices, and the step of each by itself."""
+    g = [gradient(*s, seed + i).to(DEV) for i, s in enumerate(KINDS)]
+    w = [0.1 * torch.ones_like(t) for t in g]
+    m = [0.5 * t for t in g]
+    one = [(a.clone(), b.clone()) for a, b in zip(w, m)]
+    for (a, b), t in zip(one, g):
+        optim.muon_step([a], [t], [b], lr=0.02)
+    torch.cuda.synchronize()
+    return w, g, m, one
+
+
+def test_kinds_beside_each_other_follow_the_stream():
+    """What the call reads is made just before it on its stream, and what it writes is used just after it."""
+    w, g, m, one = kinds_alone(60)
+    say("muon_step, kinds", KINDS)
+    side = torch.cuda.Stream()
+    slow = torch.ones(2048, 2048, device=DEV)
+    torch.cuda.synchronize()
+    for turn in range(8):
+        with torch.cuda.stream(side):
+            made = [torch.zeros_like(t) for t in g]
+            for _ in range(3):
+                slow = slow @ slow * (1.0 / 2048)
+            for a, b in zip(made, g):
+                a.copy_(b)
+            ws, ms = [t.clone() for t in w], [t.clone() for t in m]
+            optim.muon_step(ws, made, ms, lr=0.02)
+            for t in made:
+                t.fill_(float("nan"))
+            got = [(a.clone(), b.clone()) for a, b in zip(ws, ms)]
+            for t in ws + ms:
+                t.fill_(float("nan"))
+        side.synchronize()
+        assert all(torch.equal(a, c) and torch.equal(b, d) for (a, b), (c, d) in zip(got, one)), turn
+
+
+def test_kinds_in_a_graph_and_eager_calls_between():
+    w, g, m, one = kinds_alone(70)
+    say("muon_step in a graph, kinds", KINDS)
+    ws, ms = [t.clone() for t in w], [t.clone() for t in m]
+    optim.muon_step(ws, g, ms, lr=0.02)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        optim.muon_step(ws, g, ms, lr=0.02)
+    for turn in range(4):
+        for a, b in zip(ws + ms, w + m):
+            a.copy_(b)
+        graph.replay()
+        w2, m2 = [t.clone() for t in w], [t.clone() for t in m]
+        optim.muon_step(w2, g, m2, lr=0.02)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, c) and torch.equal(b, d) for a, b, (c, d) in zip(ws, ms, one)), turn
+        assert all(torch.equal(a, c) and torch.equal(b, d) for a, b, (c, d) in zip(w2, m2, one)), turn
+
+
+def test_kinds_from_several_threads():
+    import threading
+
+    w, g, m, one = kinds_alone(80)
+    say("muon_step from three threads, kinds", KINDS)
+    good = [None] * 3
+
+    def work(k):
+        with torch.cuda.stream(torch.cuda.Stream()) as _:
+            s = torch.cuda.current_stream()
+            same = True
+            for _ in range(6):
+                ws, ms = [t.clone() for t in w], [t.clone() for t in m]
+                optim.muon_step(ws, g, ms, lr=0.02)
+                s.synchronize()
+                same = same and all(torch.equal(a, c) and torch.equal(b, d) for a, b, (c, d) in zip(ws, ms, one))
+            good[k] = same
+
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(3)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert good == [True] * 3
