@@ -971,7 +971,8 @@ template <bool ACROSS> __device__ inline void tile_product(const Pieces &x, cons
         }
 }
 
-// One value of a buffer at a lane's byte offset plus a uniform one; past the end: zero, or nothing stored
+// One value of a buffer at a lane's byte offset plus a uniform one; past the end: zero, or nothing stored.  The bounds check is one of the
+// lane's offset; the uniform one has to lie inside the buffer by itself.
 template <int DT> __device__ inline float buffer_get(__amdgpu_buffer_rsrc_t b, int lane_off, int off)
 {
     if constexpr (DT == XCONV_F32) return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(b, lane_off, off, 0));
@@ -1014,7 +1015,7 @@ template <int GT, int OT, bool MUON> __global__ __launch_bounds__(kNarrowThreads
         for (int mb = 0; mb < 2; ++mb)
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                const int at = hrow + row_of(mb, e) < m ? place : kNarrowOut / 4, off = row_of(mb, e) * rstride;
+                const int at = hrow + row_of(mb, e) < m ? place : kNarrowOut / 4, off = min(row_of(mb, e), m - 1) * rstride;
                 u[i][mb][e] = buffer_get<GT>(G, at * GE, off * GE);
                 if constexpr (MUON) mo[i][mb][e] = buffer_get<XCONV_F32>(M, at * 4, off * 4);
             }
@@ -1030,7 +1031,7 @@ template <int GT, int OT, bool MUON> __global__ __launch_bounds__(kNarrowThreads
             for (int e = 0; e < 16; ++e) {
                 if constexpr (MUON) {
                     const float g = u[i][mb][e], w = mo[i][mb][e] + (g - mo[i][mb][e]) * (1.f - L.s.mu);
-                    const int at = hrow + row_of(mb, e) < m ? place : kNarrowOut / 4, off = row_of(mb, e) * rstride;
+                    const int at = hrow + row_of(mb, e) < m ? place : kNarrowOut / 4, off = min(row_of(mb, e), m - 1) * rstride;
                     buffer_put<XCONV_F32>(M, at * 4, off * 4, w);
                     u[i][mb][e] = update_of(g, w, L.s);
                 }
@@ -1173,12 +1174,14 @@ template <int GT, int OT, bool MUON> __global__ __launch_bounds__(kNarrowThreads
             if (across ? 32 * rb + c >= m : n0 + c >= n) place[rb] = kNarrowOut / 4;
         }
         auto at = [&](int rb, int e) { return next[rb] + row_of(0, e) < most ? place[rb] : kNarrowOut / 4; };
+        const int end = (across ? n - n0 : m) - 1;
+        auto along = [&](int rb, int e) { return min(next[rb] + row_of(0, e), end) * stride * OE; };
         f32x16 w[2], y[2];
         if constexpr (MUON) {
 #pragma unroll
             for (int rb = 0; rb < 2; ++rb)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) w[rb][e] = buffer_get<OT>(O, at(rb, e) * OE, (next[rb] + row_of(0, e)) * stride * OE);
+                for (int e = 0; e < 16; ++e) w[rb][e] = buffer_get<OT>(O, at(rb, e) * OE, along(rb, e));
         }
         if (across) {
             tile_product<true>(x[i], S.pf, lane, y);
@@ -1195,7 +1198,7 @@ template <int GT, int OT, bool MUON> __global__ __launch_bounds__(kNarrowThreads
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 const float o = y[rb][e] * kOrthUnscale;
-                buffer_put<OT>(O, at(rb, e) * OE, (next[rb] + row_of(0, e)) * stride * OE, MUON ? w[rb][e] * L.s.keep - q.wscale * o : o);
+                buffer_put<OT>(O, at(rb, e) * OE, along(rb, e), MUON ? w[rb][e] * L.s.keep - q.wscale * o : o);
             }
     }
 }
