@@ -400,18 +400,19 @@ __global__ __launch_bounds__(row_threads<G>) void norm_rows_bwd_kernel(NormArgs 
                 float x[V], d[V];
                 unpack<DT>(rx[r][k], x);
                 unpack<DT>(rd[r][k], d);
-                // (rows and vectors that do not exist are zeros with statistics of zero, or columns that nobody reads)
+                // (rows and vectors that do not exist are zeros with a mean of zero)
+                const float mu = v < nv ? mean[r] : 0.f;
                 if (K > 0 ? masked<G>(a, k, nv) : a.ragged) {
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
                         const bool mine = on[r] && v < nv && own(p, i);
-                        x[i] = mine ? x[i] : mean[r];
+                        x[i] = mine ? x[i] : mu;
                         d[i] = mine ? d[i] : 0.f;
                     }
                 }
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    const float t = d[i] * ((x[i] - mean[r]) * rstd[r]);
+                    const float t = d[i] * ((x[i] - mu) * rstd[r]);
                     c[2 * r] += d[i] * g[i];
                     c[2 * r + 1] += t * g[i];
                     if constexpr (K > 0) {
@@ -526,12 +527,14 @@ template <int V> __device__ inline PlaneAt plane_at(const NormArgs &a, long long
     const Part p = part_of<V>((int)(q - img * a.nvi), a.inner, a.exact);
     return {(size_t)img * a.C * a.inner, img * a.inner + p.at, p, true};
 }
-// channel c of the vector; WHOLE: the planes are whole or overlapping vectors, and every lane loads (zeros where there is nothing)
-template <int DT, bool WHOLE> __device__ inline uint4 plane_get(const NormArgs &a, const typename NormElem<DT>::t *x, const PlaneAt &at, int c)
+// channel c of the vector; WHOLE: the planes are whole or overlapping vectors, and every lane loads (where there is nothing: zeros, or
+// with ANY the values of another channel or position)
+template <int DT, bool WHOLE, bool ANY = false> __device__ inline uint4 plane_get(const NormArgs &a, const typename NormElem<DT>::t *x, const PlaneAt &at, int c)
 {
     const bool on = at.on && c < a.C;
     if constexpr (WHOLE) {
         const uint4 v = load_loose<DT>(x + (size_t)min(c, a.C - 1) * a.inner + at.p.at);
+        if constexpr (ANY) return v;
         return uint4{on ? v.x : 0u, on ? v.y : 0u, on ? v.z : 0u, on ? v.w : 0u};
     } else {
         return on ? load_part<DT>(x + (size_t)c * a.inner, at.p) : uint4{0, 0, 0, 0};
@@ -662,12 +665,12 @@ __global__ __launch_bounds__(NW * 64, 4) void norm_planes_bwd_kernel(NormArgs a)
     for (long long tile = run.from; tile < run.to; tile += run.step, first = false) {
         const PlaneAt at = plane_at<V>(a, tile);
         uint4 rx[KR], rd[KR];
-        auto get = [&](const elem_t *t, int c) { return plane_get<DT, WHOLE>(a, t + at.base, at, c); };
-        if constexpr (K > 0)
-            rounds([&](int k, int c) {
-                rx[k] = get(X, c);
-                rd[k] = get(DY, c);
-            });
+        // (a gradient of zero drops what does not exist from the sums; values of X that are near their mean keep the product zero)
+        auto get = [&](int k, int c) {
+            rx[k] = plane_get<DT, WHOLE, true>(a, X + at.base, at, c);
+            rd[k] = plane_get<DT, WHOLE>(a, DY + at.base, at, c);
+        };
+        if constexpr (K > 0) rounds(get);
         float mean[V], rstd[V], c12[2 * V];
         if constexpr (WHOLE) {
             load_params<XCONV_F32, V>(a.mean, Part{0, 0, V}, 0.f, mean, at.pos);
@@ -683,10 +686,7 @@ __global__ __launch_bounds__(NW * 64, 4) void norm_planes_bwd_kernel(NormArgs a)
 #pragma unroll
         for (int i = 0; i < V; ++i) c12[i] = c12[V + i] = 0.f;
         rounds([&](int k, int c) {
-            if constexpr (K == 0) {
-                rx[0] = get(X, c);
-                rd[0] = get(DY, c);
-            }
+            if constexpr (K == 0) get(0, c);
             float x[V], d[V], sg = 0.f, sb = 0.f;
             unpack<DT>(rx[k], x);
             unpack<DT>(rd[k], d);
@@ -694,7 +694,7 @@ __global__ __launch_bounds__(NW * 64, 4) void norm_planes_bwd_kernel(NormArgs a)
             if (!a.ragged) {
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    const float t = d[i] * ((x[i] - mean[i]) * rstd[i]);
+                    const float t = d[i] * ((x[i] - (WHOLE || c < a.C ? mean[i] : 0.f)) * rstd[i]);
                     c12[i] += d[i] * g;
                     c12[V + i] += t * g;
                     sg += t;
@@ -703,7 +703,7 @@ __global__ __launch_bounds__(NW * 64, 4) void norm_planes_bwd_kernel(NormArgs a)
             } else {
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    const float t = d[i] * ((x[i] - mean[i]) * rstd[i]);
+                    const float t = d[i] * ((x[i] - (WHOLE || c < a.C ? mean[i] : 0.f)) * rstd[i]);
                     c12[i] += d[i] * g;
                     c12[V + i] += t * g;
                     sg += i >= at.p.lo ? t : 0.f;
@@ -738,10 +738,7 @@ __global__ __launch_bounds__(NW * 64, 4) void norm_planes_bwd_kernel(NormArgs a)
         }
         rounds([&](int k, int c) {
             if (c >= a.C) return;
-            if constexpr (K == 0) {
-                rx[0] = get(X, c);
-                rd[0] = get(DY, c);
-            }
+            if constexpr (K == 0) get(0, c);
             float x[V], d[V];
             unpack<DT>(rx[k], x);
             unpack<DT>(rd[k], d);

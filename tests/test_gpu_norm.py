@@ -362,3 +362,21 @@ def test_refusals_on_the_device():
         norm.layer_norm_backward(x, x, mean[:3], rstd)
     with pytest.raises(RuntimeError, match="8 channels"):
         norm.XLayerNorm(8)(torch.zeros(2, 9, device=DEV))
+
+
+@pytest.mark.parametrize("shape,axis", [((6, 37), -1), ((9, 500), -1), ((5, 1300), -1), ((2, 37, 5, 5), 1), ((1, 1100, 3, 4), 1)])
+def test_backward_where_mean_times_rstd_leaves_the_range(shape, axis):
+    """Positions with one value of 2^122 in all channels and an rstd of 10^5: x - mean and what follows from it is 0, everything
+    is finite.  Lanes that have no channel see that mean as well."""
+    say("layer norm", shape, "constant positions")
+    x = torch.full(shape, 2.0 ** 122)
+    dy = draw(shape, 4, "f32", axis)[1]
+    stat = [s for i, s in enumerate(shape) if i != axis % len(shape)]
+    mean, rstd = torch.full(stat, 2.0 ** 122), torch.full(stat, 1e5)
+    dx, dw, db = norm.layer_norm_backward(dy.to(DEV), x.to(DEV), mean.to(DEV), rstd.to(DEV), None, axis)
+    torch.cuda.synchronize()
+    assert not dw.any()
+    size = dy.double()
+    want = 1e5 * (size - size.mean(axis, keepdim=True))
+    tol = 1e5 * U * (8 * size.abs() + chain(shape[axis]) * size.abs().mean(axis, keepdim=True)) + 4 * U * want.abs()
+    assert ((dx.cpu().double() - want).abs() <= tol).all()
