@@ -405,8 +405,8 @@ xconv_status xconv_layernorm_bwd(const xconv_norm_desc *desc, const void *dY_dev
  * xconv_orth).  Row-major, aligned to the element size; outputs of one call do not overlap anything else it is given.
  * Products run on the 16-bit matrix cores with every float as the sum of two fp16 numbers (22 bits; three products, fp32
  * sums).  Matrices of at least 128 rows and 2^18 values that are at least twice as wide take up to three steps on A alone.  Results are
- * as far from 64 bits as those of fp32 products, with such steps up to four times as far (a few 1e-6 of O).  The last product takes
- * 11 bits where the result is bf16 or a 16-bit weight.  O and W are rounded once.  A zero matrix gives zeros; a matrix with an infinity
+ * as far from 64 bits as those of fp32 products, with such steps up to four times as far (a few 1e-6 of O).  O and W are
+ * rounded once, from fp32 sums.  A zero matrix gives zeros; a matrix with an infinity
  * or a NaN gives NaN (its momentum keeps the value).  Deterministic.
  * The work of a call is ordered on `stream`.  Where it has matrices that take different kernels, two streams of the library's own work
  * beside it: they start after what `stream` holds, and it goes on after them (while it is captured, all launches are on it).

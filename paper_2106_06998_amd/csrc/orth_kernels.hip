@@ -23,7 +23,7 @@
 //
 // Measured, five steps: 64 x 576 fp32 44 us (7.2 us a step, most of it one compute unit's matrix instructions), 200 x 147 88 us
 // (two launches of 6 to 9 us a step), 2048 x 4096 fp32 1.02 ms (three fp16 products for one: 0.8 to 0.98 PFLOP/s of them in the
-// large products, where a large library product reaches 1.2), 8 of 512 x 4608 bf16 with the weights' update 0.57 ms.
+// large products, where a large library product reaches 1.2), 8 of 512 x 4608 bf16 with the weights' update 0.60 ms.
 #include <algorithm>
 #include <cmath>
 #include <mutex>
@@ -412,7 +412,7 @@ template <int MT, int NT> struct Tile {
             r[j] = reinterpret_cast<const u32x4 *>(Fa + ((size_t)(ra / 32 + blk) * kblocks + kb) * kBlockHalfs)[off];
         }
     }
-    template <int PRODUCTS> __device__ static void load(Right &r, const _Float16 *Fb, int rb, int kblocks, int kb)
+    __device__ static void load(Right &r, const _Float16 *Fb, int rb, int kblocks, int kb)
     {
         const int wb = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) & 1), lane = threadIdx.x & 63;
 #pragma unroll
@@ -420,7 +420,7 @@ template <int MT, int NT> struct Tile {
 #pragma unroll
             for (int k = 0; k < KS; ++k)
 #pragma unroll
-                for (int p = 0; p < (PRODUCTS > 1 ? 2 : 1); ++p)
+                for (int p = 0; p < 2; ++p)
                     r.f[k][p][j] = reinterpret_cast<const h8 *>(Fb + ((size_t)(rb / 32 + wb * NT + j) * kblocks + kb + k) * kBlockHalfs + p * 512)[lane];
     }
     __device__ static void store(const u32x4 (&r)[kPer], u32x4 *lds)
@@ -428,19 +428,19 @@ template <int MT, int NT> struct Tile {
 #pragma unroll
         for (int j = 0; j < kPer; ++j) lds[j * kThreads + threadIdx.x] = r[j];
     }
-    template <int PRODUCTS> __device__ void multiply(const u32x4 *lds, const Right &b)
+    __device__ void multiply(const u32x4 *lds, const Right &b)
     {
         const int wa = threadIdx.x >> 7, lane = threadIdx.x & 63;
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
             h8 a[2][MT];
 #pragma unroll
-            for (int p = 0; p < (PRODUCTS > 1 ? 2 : 1); ++p)
+            for (int p = 0; p < 2; ++p)
 #pragma unroll
                 for (int i = 0; i < MT; ++i) a[p][i] = __builtin_bit_cast(h8, lds[((wa * MT + i) * KS + k) * 128 + p * 64 + lane]);
             // the small products first
 #pragma unroll
-            for (int p = 3 - PRODUCTS; p < 3; ++p)
+            for (int p = 0; p < 3; ++p)
 #pragma unroll
                 for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -448,18 +448,17 @@ template <int MT, int NT> struct Tile {
         }
     }
     // 64 x 64: every wave loads its own fragments, four blocks ahead of the ones that it multiplies
-    template <int PRODUCTS> __device__ void product_direct(const _Float16 *Fa, int ra, const _Float16 *Fb, int rb, int kblocks, int kb0, int kb1)
+    __device__ void product_direct(const _Float16 *Fa, int ra, const _Float16 *Fb, int rb, int kblocks, int kb0, int kb1)
     {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
         const h8 *pa = reinterpret_cast<const h8 *>(Fa + ((size_t)(ra / 32 + (wave >> 1)) * kblocks + kb0) * kBlockHalfs) + lane;
         const h8 *pb = reinterpret_cast<const h8 *>(Fb + ((size_t)(rb / 32 + (wave & 1)) * kblocks + kb0) * kBlockHalfs) + lane;
-        constexpr int P = PRODUCTS > 1 ? 2 : 1;
-        h8 a[2][4][P], b[2][4][P];
+        h8 a[2][4][2], b[2][4][2];
         auto get = [&](int s) {
 #pragma unroll
             for (int k = 0; k < 4; ++k)
 #pragma unroll
-                for (int p = 0; p < P; ++p) {
+                for (int p = 0; p < 2; ++p) {
                     a[s][k][p] = pa[k * 128 + p * 64];
                     b[s][k][p] = pb[k * 128 + p * 64];
                 }
@@ -469,10 +468,8 @@ template <int MT, int NT> struct Tile {
         auto use = [&](int s) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                if constexpr (P > 1) {
-                    acc[0][0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[s][k][P - 1], b[s][k][0], acc[0][0], 0, 0, 0);
-                    acc[0][0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[s][k][0], b[s][k][P - 1], acc[0][0], 0, 0, 0);
-                }
+                acc[0][0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[s][k][1], b[s][k][0], acc[0][0], 0, 0, 0);
+                acc[0][0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[s][k][0], b[s][k][1], acc[0][0], 0, 0, 0);
                 acc[0][0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[s][k][0], b[s][k][0], acc[0][0], 0, 0, 0);
             }
         };
@@ -490,22 +487,22 @@ template <int MT, int NT> struct Tile {
         use(0);
         if (left > 1) use(1);
     }
-    // lds: two steps; PRODUCTS = 1: the first numbers' product only
-    template <int PRODUCTS = 3> __device__ void product(const _Float16 *Fa, int ra, const _Float16 *Fb, int rb, int kblocks, int kb0, int kb1, u32x4 *lds)
+    // lds: two steps
+    __device__ void product(const _Float16 *Fa, int ra, const _Float16 *Fb, int rb, int kblocks, int kb0, int kb1, u32x4 *lds)
     {
         clear();
         u32x4 r[kPer];
         Right b0, b1;
-        load<PRODUCTS>(b0, Fb, rb, kblocks, kb0);
+        load(b0, Fb, rb, kblocks, kb0);
         load(r, Fa, ra, kblocks, kb0);
         store(r, lds);
         __syncthreads();
         int at = 0;
         // one step with the next one's loads under way
         auto step = [&](const Right &now, Right &next, int kb) {
-            load<PRODUCTS>(next, Fb, rb, kblocks, kb);
+            load(next, Fb, rb, kblocks, kb);
             load(r, Fa, ra, kblocks, kb);
-            multiply<PRODUCTS>(lds + at * kUnits, now);
+            multiply(lds + at * kUnits, now);
             at ^= 1;
             store(r, lds + at * kUnits);
             __syncthreads();
@@ -517,9 +514,9 @@ template <int MT, int NT> struct Tile {
         }
         if (kb < kb1) {
             step(b0, b1, kb);
-            multiply<PRODUCTS>(lds + at * kUnits, b1);
+            multiply(lds + at * kUnits, b1);
         } else {
-            multiply<PRODUCTS>(lds + at * kUnits, b0);
+            multiply(lds + at * kUnits, b0);
         }
         __syncthreads();
     }
@@ -572,11 +569,11 @@ template <int T> union TileLds {
 };
 // A tile's product: of 64 x 64 straight from memory, which a small matrix' few workgroups get through sooner; of 128 x 128 through
 // LDS, which takes less from the caches
-template <int T, int PRODUCTS> __device__ inline void tile_of_product(TileLds<T> &lds, Tile<T / 64, T / 64> &t, const _Float16 *Fa, int ra, const _Float16 *Fb, int rb,
-                                                                      int kblocks, int kb0, int kb1)
+template <int T> __device__ inline void tile_of_product(TileLds<T> &lds, Tile<T / 64, T / 64> &t, const _Float16 *Fa, int ra, const _Float16 *Fb, int rb,
+                                                        int kblocks, int kb0, int kb1)
 {
-    if constexpr (T == 64) t.template product_direct<PRODUCTS>(Fa, ra, Fb, rb, kblocks, kb0, kb1);
-    else t.template product<PRODUCTS>(Fa, ra, Fb, rb, kblocks, kb0, kb1, lds.stage);
+    if constexpr (T == 64) t.product_direct(Fa, ra, Fb, rb, kblocks, kb0, kb1);
+    else t.product(Fa, ra, Fb, rb, kblocks, kb0, kb1, lds.stage);
 }
 
 // pair (i <= j) of tiles of a symmetric matrix with T rows of tiles
@@ -651,7 +648,7 @@ template <int T, int KIND> __global__ __launch_bounds__(kThreads, 2) void orth_s
     int ti, tj;
     pair_of(pair, ti, tj);
     Tile<T / 64, T / 64> t;
-    tile_of_product<T, 3>(lds, t, left, ti * T, right, tj * T, kblocks, split * run, min(kblocks, (split + 1) * run));
+    tile_of_product<T>(lds, t, left, ti * T, right, tj * T, kblocks, split * run, min(kblocks, (split + 1) * run));
     if (splits > 1) {
         t.put_part(q.part + (size_t)b * T * T);
         return;
@@ -741,9 +738,9 @@ template <int TM, int TN, int NTHR = kThreads> struct Finish {
     }
 };
 
-// X <- P X, P being `scale` times S_which, from the transposed X (Xt, or Xt2 when odd) to X and the other transposed one.  LAST 1: to the result instead.  2: the
-// same with the first fp16 numbers alone.  What that drops, 2^-12 of P and of X, goes into no further step: it is an eighth of what
-// rounding O to bf16 drops, and far below the rounding of 16-bit weights, of which the update is a small part.
+// X <- P X, P being `scale` times S_which, from the transposed X (Xt, or Xt2 when odd) to X and the other transposed one.  LAST: to the result instead.
+// All three products for results of 16 bits too: the first numbers' product alone takes 8 of 512 x 4608 from 603 to 580 us, but it is
+// 3e-4 of O away, more than rounding to fp16, and for a falling spectrum as far as rounding to bf16.
 template <int T, int LAST> __global__ __launch_bounds__(kThreads, 2) void orth_apply_kernel(OrthRef L, int odd, int which, float scale)
 {
     __shared__ TileLds<T> lds;
@@ -752,8 +749,8 @@ template <int T, int LAST> __global__ __launch_bounds__(kThreads, 2) void orth_a
     const OrthMat q = the_mat(L, b);
     const TileAt at = tile_at<T, T>(q, b);
     Tile<T / 64, T / 64> t;
-    tile_of_product<T, LAST == 2 ? 1 : 3>(lds, t, square_of(q, which), at.m0, odd ? q.Xt2 : q.Xt, at.n0, q.mp / 16, 0, q.mp / 16);
-    if constexpr (LAST > 0) {
+    tile_of_product<T>(lds, t, square_of(q, which), at.m0, odd ? q.Xt2 : q.Xt, at.n0, q.mp / 16, 0, q.mp / 16);
+    if constexpr (LAST) {
         Finish<T, T> f(q, L.s, at.m0, at.n0);
         f.load();
         t.spread(lds.t, scale);
@@ -1535,9 +1532,6 @@ hipError_t launch_wide(const xconv_orth_item *const *items, int count, const xco
         if (!last) {
             go(orth_apply_kernel<64, 0>, APPLY, odd, q, scale);
             go(orth_apply_kernel<128, 0>, APPLY + 1, odd, q, scale);
-        } else if (args->out_dtype == XCONV_BF16 || (muon && args->out_dtype == XCONV_F16)) {
-            go(orth_apply_kernel<64, 2>, APPLY, odd, q, scale);
-            go(orth_apply_kernel<128, 2>, APPLY + 1, odd, q, scale);
         } else {
             go(orth_apply_kernel<64, 1>, APPLY, odd, q, scale);
             go(orth_apply_kernel<128, 1>, APPLY + 1, odd, q, scale);
