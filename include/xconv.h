@@ -412,7 +412,7 @@ xconv_status xconv_layernorm_bwd(const xconv_norm_desc *desc, const void *dY_dev
  * beside it: they start after what `stream` holds, and it goes on after them (while it is captured, all launches are on it).
  * ws_dev: xconv_orth_workspace_bytes() bytes, 256-byte aligned.
  * XCONV_EINVAL: a null pointer, count < 0, rows or cols < 1, bad enum, steps < 0, eps, lr, momentum, weight_decay or a
- * coefficient not finite, eps < 0; XCONV_EUNSUPPORTED: min(rows, cols) above 32768, an extent above 2^24, rows * cols above
+ * coefficient not a finite float, eps < 0; XCONV_EUNSUPPORTED: min(rows, cols) above 32768, an extent above 2^24, rows * cols above
  * 2^31, steps above 64, and coefficients with which a singular value s that starts in [0, 1] passes 3.5 before the last step
  * or |a + b s^2 + c s^4| or |b s + c s^3| passes 12 (the fp16 numbers could overflow).  count == 0 is a no-op. */
 typedef struct xconv_orth_item {
@@ -429,10 +429,16 @@ typedef struct xconv_muon_args {
     float lr, momentum, weight_decay;
     int32_t nesterov;
 } xconv_muon_args;
+typedef struct xconv_muon_args64 {      /* the same in 64 bits: 1 - 0.95 is 0.05 to the last bit of a float, 1 - 0.95f is not */
+    double lr, momentum, weight_decay;
+    int32_t nesterov;
+} xconv_muon_args64;
 size_t xconv_orth_workspace_bytes(const xconv_orth_item *items, int count, const xconv_orth_args *args);   /* reads rows and cols; 0: not valid */
 xconv_status xconv_orth(const xconv_orth_item *items, int count, const xconv_orth_args *args, void *ws_dev, size_t ws_bytes, void *stream);
 xconv_status xconv_muon_step(const xconv_orth_item *items, int count, const xconv_orth_args *args, const xconv_muon_args *muon, void *ws_dev,
                              size_t ws_bytes, void *stream);
+xconv_status xconv_muon_step64(const xconv_orth_item *items, int count, const xconv_orth_args *args, const xconv_muon_args64 *muon, void *ws_dev,
+                               size_t ws_bytes, void *stream);
 
 /* Reference measurement for the roofline figures (not part of the method): enqueues a loop of `iters` x 4
  * independent 32x32 matrix instructions per wave (32x32x16 for the 16-bit types, 32x32x2 for fp32) on every

@@ -54,6 +54,10 @@ class xconv_muon_args(ctypes.Structure):
     _fields_ = [("lr", ctypes.c_float), ("momentum", ctypes.c_float), ("weight_decay", ctypes.c_float), ("nesterov", ctypes.c_int32)]
 
 
+class xconv_muon_args64(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("momentum", ctypes.c_double), ("weight_decay", ctypes.c_double), ("nesterov", ctypes.c_int32)]
+
+
 class XConvError(RuntimeError):
     def __init__(self, status, where):
         self.status = status
@@ -169,6 +173,8 @@ def lib():
         L.xconv_orth.argtypes = [PI, i32, PA, vp, sz, vp]
         L.xconv_muon_step.restype = i32
         L.xconv_muon_step.argtypes = [PI, i32, PA, PM, vp, sz, vp]
+        L.xconv_muon_step64.restype = i32
+        L.xconv_muon_step64.argtypes = [PI, i32, PA, ctypes.POINTER(xconv_muon_args64), vp, sz, vp]
         L.xconv_diag_mfma_rate.restype = i32
         L.xconv_diag_mfma_rate.argtypes = [i32, i32, vp, sz, ctypes.POINTER(ctypes.c_double), vp]
         L.xconv_prof_enable.restype = None
@@ -530,3 +536,8 @@ def xconv_orth(items, count, args, ws_dev, stream=None):
 def xconv_muon_step(items, count, args, muon, ws_dev, stream=None):
     _check(lib().xconv_muon_step(items, int(count), ctypes.byref(args), ctypes.byref(muon), _ptr(ws_dev), _nbytes(ws_dev), _stream(stream)),
            "xconv_muon_step")
+
+
+def xconv_muon_step64(items, count, args, muon, ws_dev, stream=None):
+    _check(lib().xconv_muon_step64(items, int(count), ctypes.byref(args), ctypes.byref(muon), _ptr(ws_dev), _nbytes(ws_dev), _stream(stream)),
+           "xconv_muon_step64")

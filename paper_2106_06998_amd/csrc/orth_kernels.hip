@@ -63,7 +63,7 @@ struct OrthMat {
 };
 struct OrthScalars {
     int count, g_dtype, out_dtype, muon, nesterov;
-    float a, b, c, eps, mu, keep;       // keep = 1 - lr decay
+    float a, b, c, eps, mu, rest, keep;     // rest = 1 - mu, keep = 1 - lr decay, both rounded once from 64 bits
 };
 struct OrthList {
     OrthScalars s;
@@ -268,7 +268,7 @@ __global__ __launch_bounds__(kThreads) void orth_norm_kernel(OrthList L, OrthMat
         if (L.s.muon) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                m[k] = m[k] + (u[k] - m[k]) * (1.f - L.s.mu);
+                m[k] = m[k] + (u[k] - m[k]) * L.s.rest;
                 u[k] = update_of(u[k], m[k], L.s);
             }
             if (k1 == 4) {
@@ -1027,7 +1027,7 @@ template <int GT, int OT, bool MUON> __global__ __launch_bounds__(kNarrowThreads
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 if constexpr (MUON) {
-                    const float g = u[i][mb][e], w = mo[i][mb][e] + (g - mo[i][mb][e]) * (1.f - L.s.mu);
+                    const float g = u[i][mb][e], w = mo[i][mb][e] + (g - mo[i][mb][e]) * L.s.rest;
                     const int at = hrow + row_of(mb, e) < m ? place : kNarrowOut / 4, off = min(row_of(mb, e), m - 1) * rstride;
                     buffer_put<XCONV_F32>(M, at * 4, off * 4, w);
                     u[i][mb][e] = update_of(g, w, L.s);
@@ -1365,23 +1365,24 @@ size_t kind_ws(const xconv_orth_item *items, int count, int kind)
     return most;
 }
 
-OrthScalars scalars_of(const xconv_orth_args *args, const xconv_muon_args *muon)
+OrthScalars scalars_of(const xconv_orth_args *args, const xconv_muon_args64 *muon)
 {
     OrthScalars s{};
     s.g_dtype = args->g_dtype; s.out_dtype = args->out_dtype;
     s.a = args->a; s.b = args->b; s.c = args->c; s.eps = args->eps;
     if (muon) {
-        s.muon = 1; s.nesterov = muon->nesterov != 0; s.mu = muon->momentum;
-        s.keep = (float)(1.0 - (double)muon->lr * muon->weight_decay);
+        s.muon = 1; s.nesterov = muon->nesterov != 0; s.mu = (float)muon->momentum;
+        s.rest = (float)(1.0 - muon->momentum);
+        s.keep = (float)(1.0 - muon->lr * muon->weight_decay);
     }
     return s;
 }
-float wscale_of(const xconv_orth_item &it, const xconv_muon_args *muon)
+float wscale_of(const xconv_orth_item &it, const xconv_muon_args64 *muon)
 {
-    return muon ? (float)((double)muon->lr * std::sqrt(std::max(1.0, (double)it.rows / it.cols))) : 0.f;
+    return muon ? (float)(muon->lr * std::sqrt(std::max(1.0, (double)it.rows / it.cols))) : 0.f;
 }
 
-hipError_t launch_narrow(const xconv_orth_item *items, int count, const xconv_orth_args *args, const xconv_muon_args *muon, hipStream_t st)
+hipError_t launch_narrow(const xconv_orth_item *items, int count, const xconv_orth_args *args, const xconv_muon_args64 *muon, hipStream_t st)
 {
     typedef void (*Kernel)(NarrowList);
     // [muon][type of G][type of the result]
@@ -1431,7 +1432,7 @@ template <int MB, int CB> void launch_merge(const OrthRef &R, int odd, bool last
     else hipLaunchKernelGGL((orth_merge_kernel<MB, CB, 0>), grid, block, sizeof(MergeLds<MB, CB>), st, R, odd);
 }
 
-hipError_t launch_wide(const xconv_orth_item *const *items, int count, const xconv_orth_args *args, const xconv_muon_args *muon, void *ws, hipStream_t st)
+hipError_t launch_wide(const xconv_orth_item *const *items, int count, const xconv_orth_args *args, const xconv_muon_args64 *muon, void *ws, hipStream_t st)
 {
     static const hipError_t set = allow_merge<8, 2>();      // (the others stay below 64 KB)
     if (set != hipSuccess) return set;
@@ -1597,7 +1598,7 @@ size_t orth_ws_bytes(const xconv_orth_item *items, int count)
     return std::max<size_t>(256, kind_ws(items, count, SINGLE) + kind_ws(items, count, GROUPED));
 }
 
-hipError_t launch_orth(const xconv_orth_item *items, int count, const xconv_orth_args *args, const xconv_muon_args *muon, void *ws, hipStream_t st)
+hipError_t launch_orth(const xconv_orth_item *items, int count, const xconv_orth_args *args, const xconv_muon_args64 *muon, void *ws, hipStream_t st)
 {
     bool any[3] = {};
     for (int i = 0; i < count; ++i) any[kind_of(items[i])] = true;

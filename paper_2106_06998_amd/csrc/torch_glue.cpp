@@ -46,7 +46,7 @@ struct Lib {
     decltype(&xconv_layernorm_bwd) layernorm_bwd;
     decltype(&xconv_orth_workspace_bytes) orth_workspace_bytes;
     decltype(&xconv_orth) orth;
-    decltype(&xconv_muon_step) muon_step;
+    decltype(&xconv_muon_step64) muon_step;
     decltype(&xconv_status_string) status_string;
 } L;
 bool g_ready = false;
@@ -596,7 +596,7 @@ PyObject *muon_step(PyObject *, PyObject *const *args, Py_ssize_t nargs)
                 j.m = in_order(m[i]);
                 jobs.push_back(std::move(j));
             }
-            const xconv_muon_args mu{(float)h[0], (float)h[1], (float)h[2], (int32_t)(v[0] != 0)};
+            const xconv_muon_args64 mu{h[0], h[1], h[2], (int32_t)(v[0] != 0)};
             in_groups(jobs, [&](const std::vector<xconv_orth_item> &items, int gt, int ot) {
                 const xconv_orth_args a{gt, ot, (int32_t)v[1], (float)f[0], (float)f[1], (float)f[2], (float)f[3]};
                 const Tensor ws = orth_scratch(items, a, w[0]);
@@ -661,7 +661,7 @@ PyObject *glue_init(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     get(L.layernorm_bwd, "xconv_layernorm_bwd");
     get(L.orth_workspace_bytes, "xconv_orth_workspace_bytes");
     get(L.orth, "xconv_orth");
-    get(L.muon_step, "xconv_muon_step");
+    get(L.muon_step, "xconv_muon_step64");
     get(L.status_string, "xconv_status_string");
     if (missing) {
         PyErr_Format(PyExc_RuntimeError, "%s has no %s", path, missing);

@@ -1385,12 +1385,12 @@ xconv_status xconv_layernorm_bwd(const xconv_norm_desc *desc, const void *dY_dev
 // ---- orthogonalised weight updates ------------------------------------------------------
 namespace {
 // pointers: also those of the matrices
-xconv_status check_orth(const xconv_orth_item *items, int count, const xconv_orth_args *a, const xconv_muon_args *mu, bool pointers)
+xconv_status check_orth(const xconv_orth_item *items, int count, const xconv_orth_args *a, const xconv_muon_args64 *mu, bool pointers)
 {
     if (count < 0 || !a || (count > 0 && !items)) return XCONV_EINVAL;
     if (a->g_dtype < XCONV_F32 || a->g_dtype > XCONV_F16 || a->out_dtype < XCONV_F32 || a->out_dtype > XCONV_F16 || a->steps < 0) return XCONV_EINVAL;
     if (!std::isfinite(a->a) || !std::isfinite(a->b) || !std::isfinite(a->c) || !std::isfinite(a->eps) || a->eps < 0.f) return XCONV_EINVAL;
-    if (mu && (!std::isfinite(mu->lr) || !std::isfinite(mu->momentum) || !std::isfinite(mu->weight_decay))) return XCONV_EINVAL;
+    if (mu && (!std::isfinite((float)mu->lr) || !std::isfinite((float)mu->momentum) || !std::isfinite((float)mu->weight_decay))) return XCONV_EINVAL;
     for (int i = 0; i < count; ++i) {
         const xconv_orth_item &t = items[i];
         if (t.rows < 1 || t.cols < 1) return XCONV_EINVAL;
@@ -1417,7 +1417,7 @@ xconv_status check_orth(const xconv_orth_item *items, int count, const xconv_ort
     }
     return XCONV_OK;
 }
-xconv_status run_orth(const xconv_orth_item *items, int count, const xconv_orth_args *args, const xconv_muon_args *muon, void *ws_dev, size_t ws_bytes,
+xconv_status run_orth(const xconv_orth_item *items, int count, const xconv_orth_args *args, const xconv_muon_args64 *muon, void *ws_dev, size_t ws_bytes,
                       void *stream)
 {
     const xconv_status s = check_orth(items, count, args, muon, true);
@@ -1442,6 +1442,14 @@ xconv_status xconv_orth(const xconv_orth_item *items, int count, const xconv_ort
 
 xconv_status xconv_muon_step(const xconv_orth_item *items, int count, const xconv_orth_args *args, const xconv_muon_args *muon, void *ws_dev,
                              size_t ws_bytes, void *stream)
+{
+    if (!muon) return XCONV_EINVAL;
+    const xconv_muon_args64 m{muon->lr, muon->momentum, muon->weight_decay, muon->nesterov};
+    return run_orth(items, count, args, &m, ws_dev, ws_bytes, stream);
+}
+
+xconv_status xconv_muon_step64(const xconv_orth_item *items, int count, const xconv_orth_args *args, const xconv_muon_args64 *muon, void *ws_dev,
+                               size_t ws_bytes, void *stream)
 {
     if (!muon) return XCONV_EINVAL;
     return run_orth(items, count, args, muon, ws_dev, ws_bytes, stream);
