@@ -62,6 +62,27 @@ class Muon(torch.optim.Optimizer):
                 if p.dim() < 2:
                     raise ValueError("Muon: parameters of two and more axes only, got one of shape %s" % (tuple(p.shape),))
 
+    def load_state_dict(self, state_dict):
+        """As of any optimiser, but that the momenta stay float32 whatever the parameters' type: torch brings floating state to the
+        type of its parameter, which drops digits that a checkpoint holds."""
+        # what is loaded is known after the other hooks, and is put right before theirs
+        loaded = {}
+        hooks = [self.register_load_state_dict_pre_hook(lambda _, state: loaded.update(state)),
+                 self.register_load_state_dict_post_hook(lambda _: self._restore_momenta(loaded), prepend=True)]
+        try:
+            super().load_state_dict(state_dict)
+        finally:
+            for h in hooks:
+                h.remove()
+
+    def _restore_momenta(self, loaded):
+        keys = [k for group in loaded["param_groups"] for k in group["params"]]
+        params = [p for group in self.param_groups for p in group["params"]]
+        for key, p in zip(keys, params):
+            m = loaded["state"].get(key, {}).get("momentum_buffer")
+            if m is not None:
+                self.state[p]["momentum_buffer"] = m.to(device=p.device, dtype=torch.float32)
+
     @torch.no_grad()
     def step(self, closure=None):
         loss = None
