@@ -51,16 +51,29 @@ class Muon(torch.optim.Optimizer):
     axes (weights of convolutions and linear layers; give norms and biases to another optimiser)."""
 
     def __init__(self, params, lr=0.02, momentum=0.95, weight_decay=0.0, nesterov=True, steps=5, coefficients=COEFFICIENTS, eps=1e-7):
-        if not lr >= 0 or not 0 <= momentum <= 1 or not weight_decay >= 0 or not eps >= 0:
+        options = dict(lr=lr, momentum=momentum, weight_decay=weight_decay, nesterov=nesterov, steps=steps, coefficients=coefficients, eps=eps)
+        self._check_options(options)
+        super().__init__(params, options)
+
+    @staticmethod
+    def _check_options(group):
+        if not group["lr"] >= 0 or not 0 <= group["momentum"] <= 1 or not group["weight_decay"] >= 0 or not group["eps"] >= 0:
             raise ValueError("Muon: lr, weight_decay and eps must not be negative, momentum lies in [0, 1]")
-        if int(steps) != steps or steps < 0 or len(coefficients) != 3:
+        if int(group["steps"]) != group["steps"] or group["steps"] < 0 or len(group["coefficients"]) != 3:
             raise ValueError("Muon: steps is a count, coefficients are three numbers")
-        super().__init__(params, dict(lr=lr, momentum=momentum, weight_decay=weight_decay, nesterov=nesterov, steps=int(steps),
-                                      coefficients=tuple(coefficients), eps=eps))
-        for group in self.param_groups:
+        group["steps"], group["coefficients"] = int(group["steps"]), tuple(group["coefficients"])
+
+    def add_param_group(self, param_group):
+        super().add_param_group(param_group)
+        group = self.param_groups[-1]
+        try:
+            self._check_options(group)
             for p in group["params"]:
                 if p.dim() < 2:
                     raise ValueError("Muon: parameters of two and more axes only, got one of shape %s" % (tuple(p.shape),))
+        except ValueError:
+            self.param_groups.pop()
+            raise
 
     def load_state_dict(self, state_dict):
         """As of any optimiser, but that the momenta stay float32 whatever the parameters' type: torch brings floating state to the

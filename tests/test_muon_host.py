@@ -72,3 +72,25 @@ def test_checkpoints_with_several_groups_missing_and_changed_state():
     assert new.state[y]["momentum_buffer"].dtype == torch.float32 and torch.equal(new.state[y]["momentum_buffer"], m[b].bfloat16().float())
     with pytest.raises(ValueError):
         new.load_state_dict(optim.Muon([torch.nn.Parameter(torch.zeros(2, 2))]).state_dict())
+
+
+def weight(*shape):
+    return torch.nn.Parameter(torch.zeros(*shape))
+
+
+def test_every_group_is_checked_not_only_the_defaults():
+    for kw in ({"lr": -1}, {"lr": float("nan")}, {"momentum": 2.0}, {"weight_decay": -1}, {"steps": -1}, {"steps": 1.5}, {"coefficients": (1, 2)}, {"eps": -1.0}):
+        with pytest.raises(ValueError, match="Muon"):
+            optim.Muon([{"params": [weight(3, 4)]}, {"params": [weight(3, 4)], **kw}])
+        opt = optim.Muon([weight(3, 4)])
+        with pytest.raises(ValueError, match="Muon"):
+            opt.add_param_group({"params": [weight(3, 4)], **kw})
+        assert len(opt.param_groups) == 1          # nothing is left of what was refused
+    with pytest.raises(ValueError, match="two and more axes"):
+        opt.add_param_group({"params": weight(3)})
+    with pytest.raises(ValueError, match="two and more axes"):
+        opt.add_param_group({"params": iter([weight(3, 3), weight(3)])})
+    assert len(opt.param_groups) == 1
+    opt.add_param_group({"params": iter([weight(3, 3)]), "steps": 3.0, "coefficients": [1.5, -0.5, 0.0]})
+    assert opt.param_groups[1]["steps"] == 3 and isinstance(opt.param_groups[1]["steps"], int) and opt.param_groups[1]["coefficients"] == (1.5, -0.5, 0.0)
+    opt.step()
