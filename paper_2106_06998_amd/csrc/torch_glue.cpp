@@ -10,8 +10,11 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
+#include <cmath>
 #include <exception>
 #include <string>
+#include <vector>
 
 #include "../../include/xconv.h"
 
@@ -517,20 +520,37 @@ struct OrthJob {
     Tensor g, out, m;
 };
 // one call of the library for all jobs of equal types
-template <class F> void in_groups(const std::vector<OrthJob> &jobs, F &&call)
+struct OrthCall {
+    std::vector<xconv_orth_item> items;
+    xconv_orth_args args;
+};
+std::vector<OrthCall> calls_of(const std::vector<OrthJob> &jobs, long long steps, const double (&f)[4])
 {
+    std::vector<OrthCall> calls;
     for (int gt = 0; gt < 3; ++gt)
         for (int ot = 0; ot < 3; ++ot) {
-            std::vector<xconv_orth_item> items;
+            OrthCall c{{}, {gt, ot, (int32_t)steps, (float)f[0], (float)f[1], (float)f[2], (float)f[3]}};
             for (const OrthJob &j : jobs)
                 if (j.g.numel() > 0 && dtype_code(j.g.scalar_type()) == gt && dtype_code(j.out.scalar_type()) == ot)
-                    items.push_back({(int32_t)j.g.size(0), (int32_t)(j.g.numel() / j.g.size(0)), ptr(j.g), ptr(j.out), j.m.defined() ? j.m.data_ptr<float>() : nullptr});
-            if (!items.empty()) call(items, gt, ot);
+                    c.items.push_back({(int32_t)j.g.size(0), (int32_t)(j.g.numel() / j.g.size(0)), ptr(j.g), ptr(j.out), j.m.defined() ? j.m.data_ptr<float>() : nullptr});
+            if (!c.items.empty()) calls.push_back(std::move(c));
         }
+    return calls;
 }
-Tensor orth_scratch(const std::vector<xconv_orth_item> &items, const xconv_orth_args &a, const Tensor &like)
+// Makes the calls, which share one scratch.  What can be refused, and the memory, is settled for all of them before the first one runs:
+// a step is taken as a whole or not at all.  call(items, count, args, scratch, its bytes); begin() is called before the first one
+template <class F, class B> void make_calls(const std::vector<OrthCall> &calls, const Tensor &like, const char *where, F &&call, B &&begin)
 {
-    return bytes_on(L.orth_workspace_bytes(items.data(), (int)items.size(), &a), like);    // (0: the call below says why)
+    if (calls.empty()) return;
+    size_t most = 0;
+    for (const OrthCall &c : calls) {
+        const size_t n = L.orth_workspace_bytes(c.items.data(), (int)c.items.size(), &c.args);
+        if (n == 0) check(call(c, nullptr, 0), where);     // (refused before anything is launched, with the reason)
+        most = std::max(most, n);
+    }
+    const Tensor ws = bytes_on(most, like);
+    begin();
+    for (const OrthCall &c : calls) check(call(c, ptr(ws), (size_t)ws.numel()), where);
 }
 
 // orthogonalize([G ...], steps, a, b, c, eps, stream) -> [O ...]
@@ -551,11 +571,12 @@ PyObject *orthogonalize(PyObject *, PyObject *const *args, Py_ssize_t nargs)
                 const Tensor c = dense_rows(t) ? t : t.contiguous();
                 jobs.push_back({c, at::empty_like(c), Tensor()});
             }
-            in_groups(jobs, [&](const std::vector<xconv_orth_item> &items, int gt, int ot) {
-                const xconv_orth_args a{gt, ot, (int32_t)steps, (float)f[0], (float)f[1], (float)f[2], (float)f[3]};
-                const Tensor ws = orth_scratch(items, a, g[0]);
-                check(L.orth(items.data(), (int)items.size(), &a, ptr(ws), (size_t)ws.numel(), reinterpret_cast<void *>(s)), "xconv_orth");
-            });
+            make_calls(
+                calls_of(jobs, steps, f), g[0], "xconv_orth",
+                [&](const OrthCall &c, void *ws, size_t bytes) {
+                    return L.orth(c.items.data(), (int)c.items.size(), &c.args, ws, bytes, reinterpret_cast<void *>(s));
+                },
+                [] {});
         }))
         return nullptr;
     PyObject *out = PyList_New((Py_ssize_t)jobs.size());
@@ -576,7 +597,8 @@ PyObject *muon_step(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     if (!run([&] {
             if (w.size() != g.size() || w.size() != m.size()) refuse("muon_step: as many gradients and momenta as weights are expected");
             if (w.empty()) return;
-            if (v[1] < 0 || v[1] > INT32_MAX) throw Failed{XCONV_EINVAL, "xconv_muon_step"};
+            if (v[1] < 0 || v[1] > INT32_MAX || !std::isfinite((float)h[0]) || !std::isfinite((float)h[1]) || !std::isfinite((float)h[2]))
+                throw Failed{XCONV_EINVAL, "xconv_muon_step"};
             for (size_t i = 0; i < w.size(); ++i) {
                 for (const Tensor *t : {&w[i], &g[i], &m[i]}) check_matrix(*t, w[0], "muon_step");
                 if (g[i].sizes() != w[i].sizes() || m[i].sizes() != w[i].sizes()) refuse("muon_step: a gradient or a momentum has another shape than its weight");
@@ -597,16 +619,20 @@ PyObject *muon_step(PyObject *, PyObject *const *args, Py_ssize_t nargs)
                 jobs.push_back(std::move(j));
             }
             const xconv_muon_args64 mu{h[0], h[1], h[2], (int32_t)(v[0] != 0)};
-            in_groups(jobs, [&](const std::vector<xconv_orth_item> &items, int gt, int ot) {
-                const xconv_orth_args a{gt, ot, (int32_t)v[1], (float)f[0], (float)f[1], (float)f[2], (float)f[3]};
-                const Tensor ws = orth_scratch(items, a, w[0]);
-                check(L.muon_step(items.data(), (int)items.size(), &a, &mu, ptr(ws), (size_t)ws.numel(), reinterpret_cast<void *>(s)), "xconv_muon_step");
-            });
+            make_calls(
+                calls_of(jobs, v[1], f), w[0], "xconv_muon_step",
+                [&](const OrthCall &c, void *ws, size_t bytes) {
+                    return L.muon_step(c.items.data(), (int)c.items.size(), &c.args, &mu, ws, bytes, reinterpret_cast<void *>(s));
+                },
+                [&] {
+                    for (size_t i = 0; i < w.size(); ++i) {
+                        if (jobs[i].out.is_same(w[i])) w[i].unsafeGetTensorImpl()->bump_version();
+                        if (jobs[i].m.is_same(m[i])) m[i].unsafeGetTensorImpl()->bump_version();
+                    }
+                });
             for (size_t i = 0; i < w.size(); ++i) {
                 if (!jobs[i].out.is_same(w[i])) w[i].copy_(jobs[i].out);
-                else w[i].unsafeGetTensorImpl()->bump_version();
                 if (!jobs[i].m.is_same(m[i])) m[i].copy_(jobs[i].m);
-                else m[i].unsafeGetTensorImpl()->bump_version();
             }
         }))
         return nullptr;

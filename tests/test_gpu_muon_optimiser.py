@@ -4,6 +4,7 @@ import io
 import pytest
 import torch
 
+from paper_2106_06998_amd import binding as xb
 from paper_2106_06998_amd import optim
 from test_gpu_orth import DEV, TD, gradient, say
 
@@ -40,3 +41,52 @@ def test_a_resumed_run_goes_on_with_the_same_bits(dtype):
     steps(rest, new, range(2, 4))
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(whole, rest))
+
+
+def some(rows, cols, dtype, seed=1):
+    """A weight, a gradient and a momentum, and copies of the first and the last."""
+    w, g = (gradient(rows, cols, seed + i, dtype).to(DEV) for i in range(2))
+    m = gradient(rows, cols, seed + 2).to(DEV)
+    return (w, g, m), (w.clone(), m.clone())
+
+
+def untouched(tensors, copies, versions):
+    torch.cuda.synchronize()
+    (w, _, m), (w0, m0) = tensors, copies
+    return torch.equal(w, w0) and torch.equal(m, m0) and (w._version, m._version) == versions
+
+
+def test_a_refused_step_changes_nothing():
+    """Weights of two types are two calls of the library: when the second one's shape is refused, the first one has not run."""
+    small, copies = some(40, 60, "f32")
+    versions = (small[0]._version, small[2]._version)
+    n = (1 << 24) + 1
+    far = [torch.zeros(1, n, dtype=torch.float16, device=DEV) for _ in range(2)] + [torch.zeros(1, n, device=DEV)]
+    with pytest.raises(xb.XConvError):
+        optim.muon_step([small[0]], [small[1]], [small[2]], float("inf"))
+    assert untouched(small, copies, versions)
+    say("muon_step, f32 40 x 60 and a refused f16 1 x %d" % n)
+    with pytest.raises(xb.XConvError, match="unsupported"):
+        optim.muon_step([small[0], far[0]], [small[1], far[1]], [small[2], far[2]], 0.1)
+    assert untouched(small, copies, versions)
+
+
+def test_a_step_without_room_for_its_scratch_changes_nothing():
+    small, copies = some(40, 60, "f32")
+    versions = (small[0]._version, small[2]._version)
+    large = [torch.zeros(2048, 4096, dtype=torch.float16, device=DEV) for _ in range(2)] + [torch.zeros(2048, 4096, device=DEV)]
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    say("muon_step, f32 40 x 60 and f16 2048 x 4096 without room for its scratch")
+    total = torch.cuda.get_device_properties(0).total_memory
+    try:
+        # (the scratch of 2048 x 4096 takes over 100 MB)
+        torch.cuda.set_per_process_memory_fraction((torch.cuda.memory_reserved() + (32 << 20)) / total)
+        with pytest.raises(torch.OutOfMemoryError):
+            optim.muon_step([small[0], large[0]], [small[1], large[1]], [small[2], large[2]], 0.1)
+    finally:
+        torch.cuda.set_per_process_memory_fraction(1.0)
+    assert untouched(small, copies, versions)
+    optim.muon_step([small[0], large[0]], [small[1], large[1]], [small[2], large[2]], 0.1)
+    torch.cuda.synchronize()
+    assert small[0]._version > versions[0] and small[2]._version > versions[1] and not torch.equal(small[0], copies[0])
