@@ -625,9 +625,10 @@ PyObject *muon_step(PyObject *, PyObject *const *args, Py_ssize_t nargs)
                     return L.muon_step(c.items.data(), (int)c.items.size(), &c.args, &mu, ws, bytes, reinterpret_cast<void *>(s));
                 },
                 [&] {
+                    // (also what is copied back below: copies made from here do not count themselves)
                     for (size_t i = 0; i < w.size(); ++i) {
-                        if (jobs[i].out.is_same(w[i])) w[i].unsafeGetTensorImpl()->bump_version();
-                        if (jobs[i].m.is_same(m[i])) m[i].unsafeGetTensorImpl()->bump_version();
+                        w[i].unsafeGetTensorImpl()->bump_version();
+                        m[i].unsafeGetTensorImpl()->bump_version();
                     }
                 });
             for (size_t i = 0; i < w.size(); ++i) {

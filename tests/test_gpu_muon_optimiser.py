@@ -90,3 +90,17 @@ def test_a_step_without_room_for_its_scratch_changes_nothing():
     optim.muon_step([small[0], large[0]], [small[1], large[1]], [small[2], large[2]], 0.1)
     torch.cuda.synchronize()
     assert small[0]._version > versions[0] and small[2]._version > versions[1] and not torch.equal(small[0], copies[0])
+
+
+def test_a_graph_knows_that_a_strided_weight_has_changed():
+    """Weights and momenta whose memory has gaps are updated through a copy: their versions count as well."""
+    big = torch.randn(12, 40, device=DEV)
+    w = big[:, ::2].requires_grad_(True)
+    m = torch.zeros(12, 40, device=DEV)[:, ::2]
+    y = (w * w).sum()
+    before, before_m = w._version, m._version
+    optim.muon_step([w.detach()], [torch.ones(12, 20, device=DEV)], [m], 0.1)
+    torch.cuda.synchronize()
+    assert w._version > before and m._version > before_m and bool(m.any())
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
