@@ -6,6 +6,7 @@
 #include <dlfcn.h>
 
 #include <ATen/ATen.h>
+#include <ATen/MemoryOverlap.h>
 #include <c10/core/DeviceGuard.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -603,6 +604,8 @@ PyObject *muon_step(PyObject *, PyObject *const *args, Py_ssize_t nargs)
                 for (const Tensor *t : {&w[i], &g[i], &m[i]}) check_matrix(*t, w[0], "muon_step");
                 if (g[i].sizes() != w[i].sizes() || m[i].sizes() != w[i].sizes()) refuse("muon_step: a gradient or a momentum has another shape than its weight");
                 if (m[i].scalar_type() != at::kFloat) refuse("muon_step: momenta are float32");
+                at::assert_no_internal_overlap(w[i]);       // (copies back to such tensors would be refused after the step)
+                at::assert_no_internal_overlap(m[i]);
             }
             const c10::DeviceGuard guard(w[0].device());
             std::vector<OrthJob> jobs;

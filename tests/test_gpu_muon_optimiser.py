@@ -104,3 +104,16 @@ def test_a_graph_knows_that_a_strided_weight_has_changed():
     assert w._version > before and m._version > before_m and bool(m.any())
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         y.backward()
+
+
+def test_an_expanded_momentum_or_weight_is_refused_before_anything_runs():
+    small, copies = some(40, 60, "f32")
+    versions = (small[0]._version, small[2]._version)
+    w, g, m = (torch.zeros(12, 20, device=DEV) for _ in range(3))
+    one = torch.zeros(1, 20, device=DEV).expand(12, 20)
+    for bad in ((w, g, one), (one, g, m)):
+        with pytest.raises(RuntimeError, match="single memory location"):
+            optim.muon_step([small[0], bad[0]], [small[1], bad[1]], [small[2], bad[2]], 0.1)
+        assert untouched(small, copies, versions)
+    optim.muon_step([w], [torch.ones(1, 20, device=DEV).expand(12, 20)], [m], 0.1)        # (a gradient may be)
+    assert bool(w.any())
