@@ -585,6 +585,35 @@ PyObject *orthogonalize(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     return out;
 }
 
+// Refuses a list whose outputs (weights and momenta) lie over each other or over an input: the workgroups of one launch would race.
+// Of a tensor with gaps in its memory, which is updated through a copy, only the first value counts.
+void check_apart(const std::vector<Tensor> &w, const std::vector<Tensor> &g, const std::vector<Tensor> &m)
+{
+    struct Span {
+        uintptr_t from, to;
+        bool out;
+    };
+    std::vector<Span> spans;
+    spans.reserve(3 * w.size());
+    auto add = [&](const Tensor &t, bool out) {
+        if (t.numel() == 0) return;
+        const uintptr_t from = reinterpret_cast<uintptr_t>(t.data_ptr());
+        spans.push_back({from, from + (size_t)t.element_size() * (t.is_non_overlapping_and_dense() ? (size_t)t.numel() : 1), out});
+    };
+    for (size_t i = 0; i < w.size(); ++i) {
+        add(w[i], true);
+        add(g[i], false);
+        add(m[i], true);
+    }
+    std::sort(spans.begin(), spans.end(), [](const Span &a, const Span &b) { return a.from < b.from; });
+    uintptr_t any = 0, out = 0;      // where those so far end
+    for (const Span &s : spans) {
+        if (s.from < out || (s.out && s.from < any)) refuse("muon_step: a weight or a momentum lies over another tensor of the call");
+        any = std::max(any, s.to);
+        if (s.out) out = std::max(out, s.to);
+    }
+}
+
 // muon_step([W ...], [G ...], [M ...], lr, momentum, weight decay, nesterov, steps, a, b, c, eps, stream); W and M in place
 PyObject *muon_step(PyObject *, PyObject *const *args, Py_ssize_t nargs)
 {
@@ -607,6 +636,7 @@ PyObject *muon_step(PyObject *, PyObject *const *args, Py_ssize_t nargs)
                 at::assert_no_internal_overlap(w[i]);       // (copies back to such tensors would be refused after the step)
                 at::assert_no_internal_overlap(m[i]);
             }
+            check_apart(w, g, m);
             const c10::DeviceGuard guard(w[0].device());
             std::vector<OrthJob> jobs;
             for (size_t i = 0; i < w.size(); ++i) {

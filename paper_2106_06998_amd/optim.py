@@ -36,7 +36,8 @@ def orthogonalize(G, steps=5, coefficients=COEFFICIENTS, eps=1e-7):
 
 def muon_step(weights, grads, momenta, lr, momentum=0.95, weight_decay=0.0, nesterov=True, steps=5, coefficients=COEFFICIENTS, eps=1e-7):
     """One step for every weight, in place: M <- M + (1 - momentum)(G - M), U = G + momentum (M - G) or M,
-    W <- (1 - lr weight_decay) W - lr sqrt(max(1, rows/cols)) orthogonalize(U).  Momenta are float32."""
+    W <- (1 - lr weight_decay) W - lr sqrt(max(1, rows/cols)) orthogonalize(U).  Momenta are float32.  Weights and
+    momenta share no memory with each other or with a gradient."""
     if not weights:
         if grads or momenta:
             raise ValueError("muon_step: as many gradients and momenta as weights are expected")

@@ -117,3 +117,23 @@ def test_an_expanded_momentum_or_weight_is_refused_before_anything_runs():
         assert untouched(small, copies, versions)
     optim.muon_step([w], [torch.ones(1, 20, device=DEV).expand(12, 20)], [m], 0.1)        # (a gradient may be)
     assert bool(w.any())
+
+
+def test_tensors_over_each_other_are_refused():
+    """The same weight twice, a momentum over another one's end, a momentum that is a gradient: two workgroups would race."""
+    (w, g, m), copies = some(40, 60, "f32")
+    versions = (w._version, m._version)
+    other, buf = torch.zeros(40, 60, device=DEV), torch.zeros(41, 60, device=DEV)
+    gaps = torch.zeros(40, 120, device=DEV)[:, ::2]
+    for call in (([w, w], [g, g], [m, other]), ([w, other], [g, g], [m, m]), ([w, other], [g, g], [buf[:40], buf[1:]]), ([w], [g], [g]),
+                 ([w, other], [g, m], [m, buf[1:]]), ([gaps, gaps], [g, g], [m, other])):
+        with pytest.raises(RuntimeError, match="lies over another tensor"):
+            optim.muon_step(*call, 0.1)
+    assert untouched((w, g, m), copies, versions) and not other.any() and not buf.any()
+    # neighbours in one buffer, one gradient for two weights and columns between each other are fine
+    pair = torch.zeros(2, 40, 60, device=DEV)
+    optim.muon_step([pair[0], pair[1]], [g, g], [m, other], 0.1)
+    cols = torch.zeros(40, 120, device=DEV)
+    optim.muon_step([cols[:, ::2], cols[:, 1::2]], [g, g], [buf[1:], torch.zeros(40, 60, device=DEV)], 0.1)
+    torch.cuda.synchronize()
+    assert bool(pair[0].any()) and bool(pair[1].any()) and torch.equal(cols[:, ::2], cols[:, 1::2])
