@@ -444,31 +444,35 @@ PyObject *norm_forward(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     return Py_BuildValue("NNN", wrap(y), wrap(mean), wrap(rstd));
 }
 
-// norm_backward(dy, x, mean, rstd, weight or None, axis, need_dx, need_dw, need_db, stream) -> (dx, dw, db), None where not asked for
+// norm_backward(dy, x, mean, rstd, weight or None, axis, need_dx, need_dw, need_db, dw and db in float32 or the type of x,
+// stream) -> (dx, dw, db), None where not asked for
 PyObject *norm_backward(PyObject *, PyObject *const *args, Py_ssize_t nargs)
 {
-    if (!ready(nargs, 10, "norm_backward")) return nullptr;
+    if (!ready(nargs, 11, "norm_backward")) return nullptr;
     const Tensor dy = tensor_arg(args[0]), x = tensor_arg(args[1]), mean = tensor_arg(args[2]), rstd = tensor_arg(args[3]), weight = tensor_arg(args[4]);
-    long long v[5];
-    if (!ints(args, 5, 5, v)) return nullptr;
+    long long v[6];
+    if (!ints(args, 5, 6, v)) return nullptr;
     Tensor dx, dw, db;
     if (!run([&] {
             const c10::DeviceGuard guard(x.device());
             NormView n = norm_view(x, weight, Tensor(), v[0], 0.0);
+            const at::ScalarType wt = v[4] ? at::kFloat : x.scalar_type();
+            if (weight.defined() && weight.scalar_type() != wt) refuse("layer_norm: the gradients of the parameters are of the weight's type");
+            n.d.w_dtype = dtype_code(wt);
             if (dy.sizes() != x.sizes() || dy.device() != x.device()) refuse("layer_norm: the gradient has another shape or device than the input");
             for (const Tensor *t : {&mean, &rstd})
                 if (t->scalar_type() != at::kFloat || t->device() != x.device() || t->numel() != n.d.outer * n.d.inner)
                     refuse("layer_norm: mean and rstd are those of the forward pass");
             const Tensor g = (dy.scalar_type() == x.scalar_type() ? dy : dy.to(x.scalar_type())).contiguous(n.format);
             const Tensor w = solid(weight), mu = mean.contiguous(), rs = rstd.contiguous();
-            const at::TensorOptions po = x.options().dtype(weight.defined() ? weight.scalar_type() : x.scalar_type());
+            const at::TensorOptions po = x.options().dtype(wt);
             if (v[1]) dx = at::empty(x.sizes(), x.options(), n.format);
             if (v[2]) dw = at::empty({n.d.C}, po);
             if (v[3]) db = at::empty({n.d.C}, po);
             Tensor ws;
             if (v[2] || v[3]) ws = bytes_on(L.layernorm_workspace_bytes(&n.d), x);
             check(L.layernorm_bwd(&n.d, ptr(g), ptr(n.x), ptr(mu) ? mu.data_ptr<float>() : nullptr, ptr(rs) ? rs.data_ptr<float>() : nullptr, ptr(w), ptr(dx),
-                                  ptr(dw), ptr(db), ptr(ws), ws.defined() ? (size_t)ws.numel() : 0, reinterpret_cast<void *>(v[4])),
+                                  ptr(dw), ptr(db), ptr(ws), ws.defined() ? (size_t)ws.numel() : 0, reinterpret_cast<void *>(v[5])),
                   "xconv_layernorm_bwd");
         }))
         return nullptr;

@@ -23,11 +23,15 @@ def layer_norm_forward(x, weight=None, bias=None, eps=1e-5, axis=-1):
     return _glue().norm_forward(x, weight, bias, eps, axis, _raw_stream(x))
 
 
-def layer_norm_backward(dy, x, mean, rstd, weight=None, axis=-1, need=(True, True, True)):
+def layer_norm_backward(dy, x, mean, rstd, weight=None, axis=-1, need=(True, True, True), param_dtype=None):
     """(dx, dweight, dbias) from the forward pass's input and statistics; `need` says which are wanted (None for the
-    others)."""
+    others).  dweight and dbias are of the weight's type; without a weight of `param_dtype`, float32 or the type of x (None)."""
     _check_input(x)
-    return _glue().norm_backward(dy, x, mean, rstd, weight, axis, need[0], need[1], need[2], _raw_stream(x))
+    if weight is not None or param_dtype is None:
+        param_dtype = x.dtype if weight is None else weight.dtype
+    if param_dtype not in (torch.float32, x.dtype):
+        raise RuntimeError("layer_norm: parameters are float32 or of the input's type, not %s" % param_dtype)
+    return _glue().norm_backward(dy, x, mean, rstd, weight, axis, need[0], need[1], need[2], param_dtype == torch.float32, _raw_stream(x))
 
 
 class _LayerNormFunction(torch.autograd.Function):
@@ -42,9 +46,7 @@ class _LayerNormFunction(torch.autograd.Function):
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
         x, mean, rstd, weight = ctx.saved_tensors
-        dx, dw, db = layer_norm_backward(dy, x, mean, rstd, weight, ctx.axis, ctx.needs_input_grad[:3])
-        if db is not None and db.dtype != ctx.bias_dtype:
-            db = db.to(ctx.bias_dtype)       # (a bias without a weight)
+        dx, dw, db = layer_norm_backward(dy, x, mean, rstd, weight, ctx.axis, ctx.needs_input_grad[:3], ctx.bias_dtype)
         return dx, dw, db, None, None
 
 
