@@ -434,6 +434,11 @@ typedef struct xconv_muon_args64 {      /* the same in 64 bits: 1 - 0.95 is 0.05
     int32_t nesterov;
 } xconv_muon_args64;
 size_t xconv_orth_workspace_bytes(const xconv_orth_item *items, int count, const xconv_orth_args *args);   /* reads rows and cols; 0: not valid */
+/* The way that matrix `index` of a call takes, for reports and tests (host only; reads rows and cols).  Fills out[0..15] with the kind
+ * (0 one workgroup, 1 steps one at a time, 2 steps in groups), the tiles' side and the runs of X X^T (out[1], out[4]) and of the other
+ * symmetric products (out[2], out[5]), the tiles' side of P X (out[3]), rows and columns of a workgroup that takes both products by A
+ * (out[6], out[7]; then out[2], out[3] and out[5] are 0), the number of groups (out[8]) and the steps of the first seven. */
+xconv_status xconv_orth_plan_info(const xconv_orth_item *items, int count, const xconv_orth_args *args, int index, int32_t *out);
 xconv_status xconv_orth(const xconv_orth_item *items, int count, const xconv_orth_args *args, void *ws_dev, size_t ws_bytes, void *stream);
 xconv_status xconv_muon_step(const xconv_orth_item *items, int count, const xconv_orth_args *args, const xconv_muon_args *muon, void *ws_dev,
                              size_t ws_bytes, void *stream);

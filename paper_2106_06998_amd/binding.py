@@ -169,6 +169,8 @@ def lib():
         L.xconv_layernorm_bwd.argtypes = [PN, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.xconv_orth_workspace_bytes.restype = sz
         L.xconv_orth_workspace_bytes.argtypes = [PI, i32, PA]
+        L.xconv_orth_plan_info.restype = i32
+        L.xconv_orth_plan_info.argtypes = [PI, i32, PA, i32, vp]
         L.xconv_orth.restype = i32
         L.xconv_orth.argtypes = [PI, i32, PA, vp, sz, vp]
         L.xconv_muon_step.restype = i32
@@ -527,6 +529,17 @@ def make_orth_args(g_dtype="f32", out_dtype="f32", steps=5, coefficients=(3.4445
 
 def xconv_orth_workspace_bytes(items, count, args):
     return int(lib().xconv_orth_workspace_bytes(items, int(count), ctypes.byref(args)))
+
+
+ORTH_PLAN_FIELDS = ("kind", "gram_tile", "square_tile", "apply_tile", "gram_runs", "square_runs", "merge_rows", "merge_cols")
+
+
+def xconv_orth_plan_info(items, count, args, index=0):
+    out = (ctypes.c_int32 * 16)()
+    _check(lib().xconv_orth_plan_info(items, int(count), ctypes.byref(args), int(index), ctypes.cast(out, ctypes.c_void_p)), "xconv_orth_plan_info")
+    plan = dict(zip(ORTH_PLAN_FIELDS, [int(v) for v in out]))
+    plan["groups"] = [int(v) for v in out[9:9 + min(out[8], 7)]]
+    return plan
 
 
 def xconv_orth(items, count, args, ws_dev, stream=None):

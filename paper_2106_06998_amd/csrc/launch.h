@@ -140,6 +140,7 @@ hipError_t launch_norm_bwd(const xconv_norm_desc *d, const void *dY, const void 
 
 // orth_kernels.hip: orthogonalisation of matrices (muon: of a momentum, with the update of the weights); ws: orth_ws_bytes
 size_t orth_ws_bytes(const xconv_orth_item *items, int count);
+void orth_plan_info(const xconv_orth_item *items, int count, const xconv_orth_args *args, int index, int32_t *out);
 hipError_t launch_orth(const xconv_orth_item *items, int count, const xconv_orth_args *args, const xconv_muon_args64 *muon, void *ws, hipStream_t st);
 
 // pixel_kernels.hip: Xbar[b, j] = sum_k X[b, k] Zimg[j, k] (forward product of the pixel x channel probes)

@@ -1598,6 +1598,34 @@ size_t orth_ws_bytes(const xconv_orth_item *items, int count)
     return std::max<size_t>(256, kind_ws(items, count, SINGLE) + kind_ws(items, count, GROUPED));
 }
 
+void orth_plan_info(const xconv_orth_item *items, int count, const xconv_orth_args *args, int index, int32_t *out)
+{
+    std::fill(out, out + 16, 0);
+    const xconv_orth_item *it = items + index;
+    const int kind = kind_of(*it);
+    out[0] = kind;
+    int sizes[64], groups = args->steps;
+    std::fill(sizes, sizes + groups, 1);
+    if (kind == GROUPED) groups = groups_of(args, sizes);
+    out[8] = groups;
+    for (int k = 0; k < std::min(groups, 7); ++k) out[9 + k] = sizes[k];
+    if (kind == NARROW) return;
+    wide_runs(items, count, kind, [&](const xconv_orth_item *const *list, int n) {
+        const int at = (int)(std::find(list, list + n, it) - list);
+        if (at == n) return true;
+        const OrthPlan P = plan_orth(list, n);
+        const OrthPlan::Mat &q = P.mat[at];
+        for (int k = 0; k < 3; ++k) out[1 + k] = k > 0 && q.merge ? 0 : q.big[k] ? 128 : 64;
+        out[4] = q.gsplits;
+        out[5] = q.merge ? 0 : q.psplits;
+        if (q.merge) {
+            out[6] = 32 * P.merge_mb;
+            out[7] = 32 * P.merge_cb;
+        }
+        return false;
+    });
+}
+
 hipError_t launch_orth(const xconv_orth_item *items, int count, const xconv_orth_args *args, const xconv_muon_args64 *muon, void *ws, hipStream_t st)
 {
     bool any[3] = {};

@@ -1435,6 +1435,15 @@ size_t xconv_orth_workspace_bytes(const xconv_orth_item *items, int count, const
     return check_orth(items, count, args, nullptr, false) == XCONV_OK ? orth_ws_bytes(items, count) : 0;
 }
 
+xconv_status xconv_orth_plan_info(const xconv_orth_item *items, int count, const xconv_orth_args *args, int index, int32_t *out)
+{
+    const xconv_status s = check_orth(items, count, args, nullptr, false);
+    if (s != XCONV_OK) return s;
+    if (!out || index < 0 || index >= count) return XCONV_EINVAL;
+    orth_plan_info(items, count, args, index, out);
+    return XCONV_OK;
+}
+
 xconv_status xconv_orth(const xconv_orth_item *items, int count, const xconv_orth_args *args, void *ws_dev, size_t ws_bytes, void *stream)
 {
     return run_orth(items, count, args, nullptr, ws_dev, ws_bytes, stream);

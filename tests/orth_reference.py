@@ -118,3 +118,27 @@ def excess(got, want, dtype, each):
     error of what was rounded, if it was rounded once."""
     got, want = got.double(), want.double()
     return float(((got - want).abs() - half_place(want.abs() + each, dtype)).max())
+
+
+# Calls, and the way that their first and last matrix takes (xconv_orth_plan_info): every kind of launch and every size of tile, where
+# the tests of accuracy and of equal bits go.  The host tests hold the library to this table, so that a threshold that moves shows.
+SINGLE, GROUPED = 1, 2
+WAYS = {
+    "one workgroup": ([(64, 576)], dict(kind=0)),
+    "one workgroup, largest": ([(768, 64)], dict(kind=0)),
+    "both products, 64 rows": ([(64, 769)], dict(kind=SINGLE, gram_tile=64, gram_runs=2, merge_rows=128, merge_cols=32)),
+    "both products, 128 rows": ([(100, 900)], dict(kind=SINGLE, gram_tile=64, gram_runs=2, merge_rows=128, merge_cols=32)),
+    "both products, 128 rows, 64 columns": ([(120, 2000)] * 20, dict(kind=SINGLE, gram_tile=64, gram_runs=5, merge_rows=128, merge_cols=64)),
+    "both products, 256 rows": ([(200, 147)], dict(kind=SINGLE, gram_tile=64, gram_runs=1, merge_rows=256, merge_cols=32)),
+    "both products, 256 rows, 64 columns": ([(250, 700)] * 20, dict(kind=SINGLE, gram_tile=64, gram_runs=1, merge_rows=256, merge_cols=64)),
+    "steps, tiles of 64": ([(320, 330)], dict(kind=SINGLE, gram_tile=64, square_tile=64, apply_tile=64, gram_runs=1, square_runs=1)),
+    "steps, tiles of 128": ([(700, 710)] * 24, dict(kind=SINGLE, gram_tile=128, square_tile=128, apply_tile=128, gram_runs=2, square_runs=1)),
+    "steps, split sums": ([(1600, 1700)], dict(kind=SINGLE, gram_tile=64, square_tile=64, apply_tile=64, gram_runs=2, square_runs=2)),
+    "groups, 256 rows": ([(256, 1152)], dict(kind=GROUPED, gram_tile=64, square_tile=64, apply_tile=64, gram_runs=3, square_runs=1)),
+    "groups, just wide enough": ([(362, 725)], dict(kind=GROUPED, gram_tile=64, square_tile=64, apply_tile=64, gram_runs=2, square_runs=1)),
+    "groups, tall": ([(1100, 260)], dict(kind=GROUPED, gram_tile=64, square_tile=64, apply_tile=64, gram_runs=3, square_runs=1)),
+    "groups, apply in tiles of 128": ([(300, 1300)] * 8, dict(kind=GROUPED, gram_tile=64, square_tile=64, apply_tile=128, gram_runs=3, square_runs=1)),
+    "groups, tiles of 128": ([(640, 1400)] * 24, dict(kind=GROUPED, gram_tile=128, square_tile=128, apply_tile=128, gram_runs=3, square_runs=1)),
+    "groups, split products of A": ([(1600, 3300)], dict(kind=GROUPED, gram_tile=128, square_tile=64, apply_tile=128, gram_runs=4, square_runs=2)),
+    "groups, split products of A in tiles of 128": ([(2048, 4096)], dict(kind=GROUPED, gram_tile=128, square_tile=128, apply_tile=128, gram_runs=3, square_runs=3)),
+}
