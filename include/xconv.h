@@ -404,10 +404,12 @@ xconv_status xconv_layernorm_bwd(const xconv_norm_desc *desc, const void *dY_dev
  * out_dev: O, or the weights W (updated in place), of out_dtype; M_dev: [rows, cols] floats, updated in place (not used by
  * xconv_orth).  Row-major, aligned to the element size; outputs of one call do not overlap anything else it is given.
  * Products run on the 16-bit matrix cores with every float as the sum of two fp16 numbers (22 bits; three products, fp32
- * sums).  Matrices of at least 128 rows and 2^18 values that are at least twice as wide take up to three steps on A alone.  Results are
- * as far from 64 bits as those of fp32 products, with such steps up to four times as far (a few 1e-6 of O).  O and W are
- * rounded once, from fp32 sums.  A zero matrix gives zeros; a matrix with an infinity
- * or a NaN gives NaN (its momentum keeps the value).  Deterministic.
+ * sums).  Matrices of at least 128 rows and 2^18 values that are at least twice as wide take up to three steps on A alone.  O and W are
+ * rounded once, from fp32 sums.  Seen, not limits: gradients end 5e-7 to 5e-6 of O from 64 bits, as with fp32 products.  A step multiplies
+ * the error of a small singular value as it does the value, so it is up to 1.3e-5 for singular values down to 1e-4 and for half of the rank
+ * (fp32 products 4e-6 to 8e-6).  Steps on A alone multiply errors of A besides: most matrices show none of it, one with a large singular
+ * value above equal ones reaches 2.3e-5 (fp32 products 9e-6), one with a dominant column 6e-6 (1e-6).
+ * A zero matrix gives zeros; a matrix with an infinity or a NaN gives NaN (its momentum keeps the value).  Deterministic.
  * The work of a call is ordered on `stream`.  Where it has matrices that take different kernels, two streams of the library's own work
  * beside it: they start after what `stream` holds, and it goes on after them (while it is captured, all launches are on it).
  * ws_dev: xconv_orth_workspace_bytes() bytes, 256-byte aligned.

@@ -1225,7 +1225,8 @@ constexpr int kMergeM = 256;        // most rows of a matrix that takes both pro
 // P' P by X: three products of m x m matrices take the place of X X^T and P X.  That is less work where n > m, but more launches: a
 // matrix alone gains from about 700000 values on (five steps, one at a time against groups: 512 x 4608 238 and 210 us, 512 x 1024 176
 // and 187, 256 x 2304 137 and 147), several at once earlier (8 of 512 x 4608 820 and 530, 8 of 512 x 1024 335 and 313, 6 of 256 x 2304
-// 209 and 181, 16 of 256 x 1152 293 and 193, 4 of 700 x 1100 358 and 350).
+// 209 and 181, 16 of 256 x 1152 293 and 193).  Less wide matrices gain too little (4 of 700 x 1100 358 and 350).  The rule cannot look at the
+// rest of a call, which would change a result's bits: a single matrix between the two sizes pays for it.
 bool grouped(const xconv_orth_item &it)
 {
     const int m = std::min(it.rows, it.cols), n = std::max(it.rows, it.cols);
@@ -1235,7 +1236,8 @@ bool grouped(const xconv_orth_item &it)
 // of A, q the polynomial), 11.9 with a = 3.44, where it would fade with a new X X^T; at the start A is small.  Products of P are kept as
 // a sixteenth of themselves, below 16.  Five steps with a = 3.44, simulated: gradients of 200 to 800 rows 2.2e-6 to 3.2e-6 in groups of
 // three and two, 1.3e-6 to 2.3e-6 one at a time and with fp32 products; matrices of equal singular values 2.7e-6 to 7.4e-6 against
-// 1.5e-6 to 2.1e-6; below 128 rows up to 1e-5 against 1.3e-6.
+// 1.5e-6 to 2.1e-6; one large singular value above equal ones 2.3e-5 against 9e-6, a dominant column 6e-6 against 8e-7, 384 x 900; below
+// 128 rows up to 1e-5 against 1.3e-6.
 int groups_of(const xconv_orth_args *args, int (&sizes)[64])
 {
     int groups = 0;
