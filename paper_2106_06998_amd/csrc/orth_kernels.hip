@@ -27,7 +27,7 @@
 #include <algorithm>
 #include <cmath>
 #include <mutex>
-#include <vector>
+#include <new>
 
 #include "common.h"
 #include "launch.h"
@@ -1552,46 +1552,43 @@ struct Sides {
     int device;
     hipStream_t stream[2];
     hipEvent_t start, done[2];
+    Sides *next;
 };
 std::mutex g_sides_mu;
-std::vector<Sides> &free_sides()
-{
-    static std::vector<Sides> *sides = new std::vector<Sides>;       // (never destroyed: the runtime may be gone by then)
-    return *sides;
-}
-bool take_sides(Sides &out)
+Sides *g_sides = nullptr;       // those that no call has; a list that takes no memory to put one back (never destroyed: the runtime may be gone by then)
+// null: none to be had
+Sides *take_sides()
 {
     int device = 0;
-    if (hipGetDevice(&device) != hipSuccess) return false;
+    if (hipGetDevice(&device) != hipSuccess) return nullptr;
     {
         std::lock_guard<std::mutex> lk(g_sides_mu);
-        std::vector<Sides> &f = free_sides();
-        for (size_t i = 0; i < f.size(); ++i)
-            if (f[i].device == device) {
-                out = f[i];
-                f.erase(f.begin() + i);
-                return true;
+        for (Sides **p = &g_sides; *p; p = &(*p)->next)
+            if ((*p)->device == device) {
+                Sides *s = *p;
+                *p = s->next;
+                return s;
             }
     }
-    Sides s{device, {nullptr, nullptr}, nullptr, {nullptr, nullptr}};
-    bool ok = hipEventCreateWithFlags(&s.start, hipEventDisableTiming) == hipSuccess;
+    Sides *s = new (std::nothrow) Sides{device, {nullptr, nullptr}, nullptr, {nullptr, nullptr}, nullptr};
+    if (!s) return nullptr;
+    bool ok = hipEventCreateWithFlags(&s->start, hipEventDisableTiming) == hipSuccess;
     for (int i = 0; i < 2; ++i)
-        ok = ok && hipStreamCreateWithFlags(&s.stream[i], hipStreamNonBlocking) == hipSuccess && hipEventCreateWithFlags(&s.done[i], hipEventDisableTiming) == hipSuccess;
-    if (ok) {
-        out = s;
-        return true;
-    }
+        ok = ok && hipStreamCreateWithFlags(&s->stream[i], hipStreamNonBlocking) == hipSuccess && hipEventCreateWithFlags(&s->done[i], hipEventDisableTiming) == hipSuccess;
+    if (ok) return s;
     for (int i = 0; i < 2; ++i) {
-        if (s.done[i]) (void)hipEventDestroy(s.done[i]);
-        if (s.stream[i]) (void)hipStreamDestroy(s.stream[i]);
+        if (s->done[i]) (void)hipEventDestroy(s->done[i]);
+        if (s->stream[i]) (void)hipStreamDestroy(s->stream[i]);
     }
-    if (s.start) (void)hipEventDestroy(s.start);
-    return false;
+    if (s->start) (void)hipEventDestroy(s->start);
+    delete s;
+    return nullptr;
 }
-void give_sides(const Sides &s)
+void give_sides(Sides *s)
 {
     std::lock_guard<std::mutex> lk(g_sides_mu);
-    free_sides().push_back(s);
+    s->next = g_sides;
+    g_sides = s;
 }
 }  // namespace
 
@@ -1641,14 +1638,13 @@ hipError_t launch_orth(const xconv_orth_item *items, int count, const xconv_orth
     };
     // (not while the caller's stream is captured: streams of a capture are not to be used by other calls until its end)
     hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
-    Sides sides;
-    bool beside = false;
+    Sides *sides = nullptr;
     if (any[NARROW] + any[SINGLE] + any[GROUPED] > 1) {
-        beside = hipStreamIsCapturing(st, &capture) == hipSuccess && capture == hipStreamCaptureStatusNone && take_sides(sides);
-        if (!beside) (void)hipGetLastError();
+        if (hipStreamIsCapturing(st, &capture) == hipSuccess && capture == hipStreamCaptureStatusNone) sides = take_sides();
+        if (!sides) (void)hipGetLastError();
     }
     hipError_t e = hipSuccess;
-    if (!beside) {
+    if (!sides) {
         for (int kind : {NARROW, GROUPED, SINGLE})
             if (any[kind] && e == hipSuccess) e = run(kind, st);
         return e;
@@ -1656,13 +1652,13 @@ hipError_t launch_orth(const xconv_orth_item *items, int count, const xconv_orth
     // the longest chain stays on the caller's stream
     const int own = any[GROUPED] ? GROUPED : SINGLE;
     int used = 0;
-    e = hipEventRecord(sides.start, st);
+    e = hipEventRecord(sides->start, st);
     for (int kind : {NARROW, GROUPED, SINGLE}) {
         if (!any[kind] || e != hipSuccess) continue;
         hipStream_t on = st;
         if (kind != own) {
-            on = sides.stream[used];
-            e = hipStreamWaitEvent(on, sides.start, 0);
+            on = sides->stream[used];
+            e = hipStreamWaitEvent(on, sides->start, 0);
             if (e != hipSuccess) break;
             ++used;
         }
@@ -1670,9 +1666,9 @@ hipError_t launch_orth(const xconv_orth_item *items, int count, const xconv_orth
     }
     // also after an error: what was launched ends before the caller's stream goes on
     for (int i = 0; i < used; ++i) {
-        hipError_t j = hipEventRecord(sides.done[i], sides.stream[i]);
-        if (j == hipSuccess) j = hipStreamWaitEvent(st, sides.done[i], 0);
-        if (j != hipSuccess) (void)hipStreamSynchronize(sides.stream[i]);
+        hipError_t j = hipEventRecord(sides->done[i], sides->stream[i]);
+        if (j == hipSuccess) j = hipStreamWaitEvent(st, sides->done[i], 0);
+        if (j != hipSuccess) (void)hipStreamSynchronize(sides->stream[i]);
         if (e == hipSuccess) e = j;
     }
     give_sides(sides);
