@@ -376,8 +376,8 @@ xconv_status xconv_relu_bwd(int dtype, const void *dY_dev, const void *mask_dev,
  * means ones, beta_dev NULL zeros.  mean_dev, rstd_dev: [outer * inner] floats, written by the forward pass (NULL: not
  * wanted), read by the backward pass.  dX_dev, dgamma_dev, dbeta_dev NULL: not wanted.  Sums are fp32, the variance of
  * the centred values, each output rounded once (nearest even) and overwritten; deterministic.  Y_dev may be X_dev, dX_dev may be dY_dev or X_dev.  Pointers aligned to the element
- * size.  ws_dev (4-byte aligned): xconv_layernorm_workspace_bytes() bytes, for the backward pass with dgamma or dbeta;
- * else it may be NULL.  outer == 0 is a no-op of the forward pass and gives zero dgamma and dbeta.
+ * size.  ws_dev (4-byte aligned): xconv_layernorm_workspace_bytes() bytes (8 C a workgroup, up to 1024 of them: more than the tensors
+ * for few long rows), for the backward pass with dgamma or dbeta; else it may be NULL.  outer == 0 is a no-op of the forward pass and gives zero dgamma and dbeta.
  * XCONV_EINVAL: null desc or pointer, C or inner < 1, outer < 0, bad enum, eps negative or not finite;
  * XCONV_EUNSUPPORTED: C above 2^24, inner above 2^30, outer * inner above 2^40. */
 typedef struct xconv_norm_desc {
@@ -412,7 +412,9 @@ xconv_status xconv_layernorm_bwd(const xconv_norm_desc *desc, const void *dY_dev
  * A zero matrix gives zeros; a matrix with an infinity or a NaN gives NaN (its momentum keeps the value).  Deterministic.
  * The work of a call is ordered on `stream`.  Where it has matrices that take different kernels, two streams of the library's own work
  * beside it: they start after what `stream` holds, and it goes on after them (while it is captured, all launches are on it).
- * ws_dev: xconv_orth_workspace_bytes() bytes, 256-byte aligned.
+ * ws_dev: xconv_orth_workspace_bytes() bytes, 256-byte aligned: of up to 24 matrices at once, 12 bytes a value each and 4 to 16 a value of
+ * its square matrices, extents padded to 64 or 128 (a matrix of few rows takes those of 64; 24 of 2048 x 4096 4.7 GB).  Long lists
+ * of large matrices are better given in shorter ones where that is too much.
  * XCONV_EINVAL: a null pointer, count < 0, rows or cols < 1, bad enum, steps < 0, eps, lr, momentum, weight_decay or a
  * coefficient not a finite float, eps < 0; XCONV_EUNSUPPORTED: min(rows, cols) above 32768, an extent above 2^24, rows * cols above
  * 2^31, steps above 64, and coefficients with which a singular value s that starts in [0, 1] passes 3.5 before the last step

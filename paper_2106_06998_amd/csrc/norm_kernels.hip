@@ -19,6 +19,10 @@
 // 2049 rows of 5001 fp16, 13.6 us = 3.0 TB/s (a workgroup a row, two sums through LDS; unmasked whole rows would be the same);
 // backward, 131072 rows of 64 fp32, 18.5 us = 5.4 TB/s and 3.8 us for the join; 256 x 256 x 28 x 28 fp16 planes, 76 us = 4.0 TB/s
 // and 5 us (the plane of 1568 bytes is no whole lines: lines at the tiles' edges are fetched by two workgroups).
+// Further from a copy's rate: backward over few long rows, where the partial sums of up to 1024 workgroups are 8 C bytes each, written and
+// read again (4096 x 4096 bf16 54 us, 34 MB of them beside 100 MB of tensors; 2048 x 8192 97 us, 67 MB); and the shapes whose backward
+// pass keeps registers in scratch: planes of 513 to 1024 channels (33 of a thread's in fp32, 96 to 98 in 16 bits: 64 x 1024 x 28 x 28 fp16
+// 202 us = 1.5 TB/s), 16-bit rows of 16385 to 24576 channels (63), and four of them in 16-bit planes of 65 to 512 channels.
 #include <algorithm>
 
 #include "common.h"

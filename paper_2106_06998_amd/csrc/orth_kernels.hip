@@ -1546,7 +1546,7 @@ hipError_t launch_wide(const xconv_orth_item *const *items, int count, const xco
 
 namespace {
 // Streams beside the caller's for the kinds of matrices of a call: each kind is a chain of launches that leave most of the chip idle
-// (18 layers of three kinds: 379 us one kind after the other, 215 us beside each other; 64 x 576 and 128 x 1152: 146 and 111).  They start after what the caller's stream holds
+// (18 layers of three kinds: 379 us one kind after the other, 215 us beside each other, with 11 bits in the last product; 64 x 576 and 128 x 1152: 146 and 111).  They start after what the caller's stream holds
 // and it goes on after them, so a call looks as if all of it ran there.  Kept for later calls; one call at a time has them.
 struct Sides {
     int device;
