@@ -391,6 +391,78 @@ xconv_status xconv_layernorm_fwd(const xconv_norm_desc *desc, const void *X_dev,
 xconv_status xconv_layernorm_bwd(const xconv_norm_desc *desc, const void *dY_dev, const void *X_dev, const float *mean_dev, const float *rstd_dev,
                                  const void *gamma_dev, void *dX_dev, void *dgamma_dev, void *dbeta_dev, void *ws_dev, size_t ws_bytes, void *stream);
 
+/* ---- dropout without a stored mask -------------------------------------------------
+ * Forward and backward pass are the same call: every value of the mask is drawn from the seed where it is applied.
+ *
+ *   forward   Y[i] = kept[i] X[i] 65536 / (65536 - drop_q16);   backward  dX[i] = kept[i] dY[i] 65536 / (65536 - drop_q16)
+ *   kept[i]   bits 16 (i%4) .. 16 (i%4) + 15 of word i/4 of the SplitMix64 stream of (seed + *step_dev) xor 0x3C6EF372FE94F82B
+ *             are not below drop_q16
+ *
+ * A value is dropped with probability drop_q16 / 65536 (0: a copy, 65536: zeros); a dropped one is zero also where it was an infinity or a
+ * NaN.  step_dev: one 64-bit number on the device that is added to the seed when the kernel runs, or NULL for 0: a captured graph that
+ * advances it draws other masks on every replay (without one, the same).  It must hold the same number in both passes.
+ * n values of `dtype` in memory order, products fp32, rounded once; Y_dev may be X_dev, anything else of it must not overlap X.  Pointers
+ * aligned to the element size, step_dev to 8 bytes.  n == 0 is a no-op; XCONV_EINVAL: a null (but step_dev) or misaligned pointer, bad
+ * dtype, n < 0, drop_q16 outside 0..65536, overlap; XCONV_EUNSUPPORTED: n above 2^40.
+ * xconv_dropout_mask: kept[first .. first + n - 1] as bytes 0 and 1, on the host (step_dev must be NULL). */
+typedef struct xconv_drop {
+    uint64_t seed;
+    const int64_t *step_dev;
+    int32_t drop_q16;
+} xconv_drop;
+xconv_status xconv_dropout(int dtype, const void *X_dev, void *Y_dev, long long n, const xconv_drop *drop, void *stream);
+xconv_status xconv_dropout_mask(const xconv_drop *drop, long long first, long long n, uint8_t *mask_host);
+
+/* ---- root-mean-square norm over channels -------------------------------------------
+ * With the addition of a residual and the dropout in front of it: the end of a residual branch and the start of the next one.
+ *
+ *   forward   H = R + drop(X);  rstd = 1/sqrt((1/C) sum_c H[o,c,i]^2 + eps);  Y[o,c,i] = H[o,c,i] rstd gamma[c]
+ *   8 bits    H = R + X;  scale = max(max_c |Y[o,c,i]|, 2^-100) / top;  Q[o,c,i] = Y[o,c,i] / scale, rounded to nearest even
+ *             (XCONV_E4M3: top 448; XCONV_INT8: top 127)
+ *   backward  g = dY gamma;  xh = H rstd;  dZ = rstd (g - xh (1/C) sum_c (g xh)) + dH
+ *             dR = dZ;  dX = drop(dZ);  dgamma[c] = sum_{o,i} dY xh
+ *
+ * Extents, types, gamma and the dropout's places (memory order) as for layer normalisation and dropout above; desc->eps is not read by the
+ * backward pass.  R_dev NULL: no residual.  drop NULL or drop_q16 0: no dropout.  H_dev (forward) NULL: not wanted.  rstd_dev, scale_dev: [outer * inner]
+ * floats; rstd_dev NULL in the forward pass: not wanted.  dH_dev NULL: zeros.  dX_dev, dR_dev, dgamma_dev NULL: not wanted.  Statistics and Y are of the fp32
+ * sum R + drop(X), H is that sum rounded once; the backward pass goes by the rounded H.  Sums are fp32 (squares above 3e38
+ * overflow).  A position with a NaN or an infinity gives NaN, its scale too.  Every output is overwritten, rounded once; deterministic.  An output may be one of
+ * the inputs of its own type (the same address and extent); otherwise nothing overlaps an output.  Pointers aligned to the element size.
+ * ws_dev (4-byte aligned): xconv_rmsnorm_workspace_bytes() bytes, for dgamma; else it may be NULL.  outer == 0 is a no-op of the forward pass and gives zero dgamma.
+ * Statuses as for layer normalisation; XCONV_EINVAL also for a bad `drop` or q_type and for overlap. */
+typedef enum { XCONV_E4M3 = 0, XCONV_INT8 = 1 } xconv_8bit;
+size_t xconv_rmsnorm_workspace_bytes(const xconv_norm_desc *desc);
+xconv_status xconv_rmsnorm_fwd(const xconv_norm_desc *desc, const void *X_dev, const void *R_dev, const void *gamma_dev, void *Y_dev, void *H_dev,
+                               float *rstd_dev, const xconv_drop *drop, void *stream);
+xconv_status xconv_rmsnorm_fwd_8bit(const xconv_norm_desc *desc, int q_type, const void *X_dev, const void *R_dev, const void *gamma_dev, void *Q_dev,
+                                    float *scale_dev, void *H_dev, void *stream);
+xconv_status xconv_rmsnorm_bwd(const xconv_norm_desc *desc, const void *dY_dev, const void *H_dev, const float *rstd_dev, const void *gamma_dev,
+                               const void *dH_dev, void *dX_dev, void *dR_dev, void *dgamma_dev, void *ws_dev, size_t ws_bytes, const xconv_drop *drop,
+                               void *stream);
+
+/* ---- embeddings ----------------------------------------------------------------------
+ * Rows of a table by index (class labels, code maps, tokens), as channels-last activations, and the table's gradient:
+ *
+ *   forward   Y[i,:] = scale W[t_i,:]
+ *   backward  dW[v,:] = scale sum_{i: t_i = v} dY[i,:], zeros for a row that no index names and for v = padding_idx
+ *
+ * idx_dev: [n] integers of 32 bits, or 64 with index64 != 0; an index outside 0..rows-1 gives a row of NaN and belongs to no row's gradient.
+ * W is [rows, C], Y and dY [n, C] of `dtype`, dW [rows, C] of dw_dtype (XCONV_F32 or `dtype`), overwritten.  Products and sums fp32, rounded once; the sums of a row
+ * are in an order that depends on the indices alone: deterministic.  padding_idx: -1 for none.
+ * Pointers aligned to the element size; ws_dev (256-byte aligned): xconv_embed_workspace_bytes() bytes (about 16 an index, 8 a row, and 8 C
+ * floats for 8 to 64 indices).  Outputs overlap nothing.  n == 0: a no-op of the forward pass, a zero dW.
+ * XCONV_EINVAL: null desc or pointer, n < 0, rows or C < 1, bad enum, scale not finite, padding_idx outside -1..rows-1;
+ * XCONV_EUNSUPPORTED: n above 2^27, rows above 2^31 - 1 (backward: 2^22), C above 2^24; xconv_embed_workspace_bytes() is 0 then. */
+typedef struct xconv_embed_desc {
+    int64_t n, rows;
+    int32_t C, dtype, index64, padding_idx;
+    float scale;
+} xconv_embed_desc;
+size_t xconv_embed_workspace_bytes(const xconv_embed_desc *desc);
+xconv_status xconv_embed_fwd(const xconv_embed_desc *desc, const void *idx_dev, const void *W_dev, void *Y_dev, void *stream);
+xconv_status xconv_embed_bwd(const xconv_embed_desc *desc, const void *idx_dev, const void *dY_dev, void *dW_dev, int dw_dtype, void *ws_dev,
+                             size_t ws_bytes, void *stream);
+
 /* ---- orthogonalised weight updates ---------------------------------------------------
  * What a weight gradient (of xconv_dw_estimate, say) can be used for: `steps` Newton-Schulz products bring the singular
  * values of a matrix near one.  A convolution's weights [C_out, C_in, kH, kW] count as [C_out, C_in*kH*kW].

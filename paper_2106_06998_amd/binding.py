@@ -40,6 +40,15 @@ class xconv_norm_desc(ctypes.Structure):
                 ("w_dtype", ctypes.c_int32), ("eps", ctypes.c_float)]
 
 
+class xconv_drop(ctypes.Structure):
+    _fields_ = [("seed", ctypes.c_uint64), ("step_dev", ctypes.c_void_p), ("drop_q16", ctypes.c_int32)]
+
+
+class xconv_embed_desc(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int64), ("rows", ctypes.c_int64), ("C", ctypes.c_int32), ("dtype", ctypes.c_int32), ("index64", ctypes.c_int32),
+                ("padding_idx", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
 class xconv_orth_item(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int32), ("cols", ctypes.c_int32), ("G_dev", ctypes.c_void_p), ("out_dev", ctypes.c_void_p),
                 ("M_dev", ctypes.c_void_p)]
@@ -167,6 +176,25 @@ def lib():
         L.xconv_layernorm_fwd.argtypes = [PN, vp, vp, vp, vp, vp, vp, vp]
         L.xconv_layernorm_bwd.restype = i32
         L.xconv_layernorm_bwd.argtypes = [PN, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        PD, PE = ctypes.POINTER(xconv_drop), ctypes.POINTER(xconv_embed_desc)
+        L.xconv_dropout.restype = i32
+        L.xconv_dropout.argtypes = [i32, vp, vp, ctypes.c_longlong, PD, vp]
+        L.xconv_dropout_mask.restype = i32
+        L.xconv_dropout_mask.argtypes = [PD, ctypes.c_longlong, ctypes.c_longlong, vp]
+        L.xconv_rmsnorm_workspace_bytes.restype = sz
+        L.xconv_rmsnorm_workspace_bytes.argtypes = [PN]
+        L.xconv_rmsnorm_fwd.restype = i32
+        L.xconv_rmsnorm_fwd.argtypes = [PN, vp, vp, vp, vp, vp, vp, PD, vp]
+        L.xconv_rmsnorm_fwd_8bit.restype = i32
+        L.xconv_rmsnorm_fwd_8bit.argtypes = [PN, i32, vp, vp, vp, vp, vp, vp, vp]
+        L.xconv_rmsnorm_bwd.restype = i32
+        L.xconv_rmsnorm_bwd.argtypes = [PN, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, PD, vp]
+        L.xconv_embed_workspace_bytes.restype = sz
+        L.xconv_embed_workspace_bytes.argtypes = [PE]
+        L.xconv_embed_fwd.restype = i32
+        L.xconv_embed_fwd.argtypes = [PE, vp, vp, vp, vp]
+        L.xconv_embed_bwd.restype = i32
+        L.xconv_embed_bwd.argtypes = [PE, vp, vp, vp, i32, vp, sz, vp]
         L.xconv_orth_workspace_bytes.restype = sz
         L.xconv_orth_workspace_bytes.argtypes = [PI, i32, PA]
         L.xconv_orth_plan_info.restype = i32
@@ -512,6 +540,68 @@ def xconv_layernorm_bwd(desc, dY_dev, X_dev, mean_dev, rstd_dev, gamma_dev, dX_d
     _check(lib().xconv_layernorm_bwd(ctypes.byref(desc), _ptr(dY_dev), _ptr(X_dev), _ptr(mean_dev), _ptr(rstd_dev), _ptr(gamma_dev),
                                      _ptr(dX_dev), _ptr(dgamma_dev), _ptr(dbeta_dev), _ptr(ws_dev), _nbytes(ws_dev), _stream(stream)),
            "xconv_layernorm_bwd")
+
+
+# ---- dropout without a stored mask ------------------------------------------------------
+def make_drop(seed, drop_q16, step_dev=None):
+    return xconv_drop(seed, None if step_dev is None else step_dev.data_ptr(), drop_q16)
+
+
+def xconv_dropout(dtype, X_dev, Y_dev, n, drop, stream=None):
+    _check(lib().xconv_dropout(DTYPES[dtype] if isinstance(dtype, str) else dtype, _ptr(X_dev), _ptr(Y_dev), int(n), ctypes.byref(drop), _stream(stream)),
+           "xconv_dropout")
+
+
+def xconv_dropout_mask(drop, first, n):
+    """kept[first .. first + n - 1] as a numpy array of truth values."""
+    mask = np.empty(max(0, int(n)), dtype=np.uint8)
+    _check(lib().xconv_dropout_mask(ctypes.byref(drop), int(first), int(n), mask.ctypes.data_as(ctypes.c_void_p)), "xconv_dropout_mask")
+    return mask.astype(bool)
+
+
+# ---- root-mean-square norm over channels ------------------------------------------------
+XCONV_E4M3, XCONV_INT8 = 0, 1
+
+
+def _ref(struct):
+    return None if struct is None else ctypes.byref(struct)
+
+
+def xconv_rmsnorm_workspace_bytes(desc):
+    return int(lib().xconv_rmsnorm_workspace_bytes(ctypes.byref(desc)))
+
+
+def xconv_rmsnorm_fwd(desc, X_dev, R_dev, gamma_dev, Y_dev, H_dev=None, rstd_dev=None, drop=None, stream=None):
+    _check(lib().xconv_rmsnorm_fwd(ctypes.byref(desc), _ptr(X_dev), _ptr(R_dev), _ptr(gamma_dev), _ptr(Y_dev), _ptr(H_dev), _ptr(rstd_dev), _ref(drop),
+                                   _stream(stream)), "xconv_rmsnorm_fwd")
+
+
+def xconv_rmsnorm_fwd_8bit(desc, q_type, X_dev, R_dev, gamma_dev, Q_dev, scale_dev, H_dev=None, stream=None):
+    _check(lib().xconv_rmsnorm_fwd_8bit(ctypes.byref(desc), int(q_type), _ptr(X_dev), _ptr(R_dev), _ptr(gamma_dev), _ptr(Q_dev), _ptr(scale_dev), _ptr(H_dev),
+                                        _stream(stream)), "xconv_rmsnorm_fwd_8bit")
+
+
+def xconv_rmsnorm_bwd(desc, dY_dev, H_dev, rstd_dev, gamma_dev, dH_dev, dX_dev, dR_dev, dgamma_dev, ws_dev, drop=None, stream=None):
+    _check(lib().xconv_rmsnorm_bwd(ctypes.byref(desc), _ptr(dY_dev), _ptr(H_dev), _ptr(rstd_dev), _ptr(gamma_dev), _ptr(dH_dev), _ptr(dX_dev), _ptr(dR_dev),
+                                   _ptr(dgamma_dev), _ptr(ws_dev), _nbytes(ws_dev), _ref(drop), _stream(stream)), "xconv_rmsnorm_bwd")
+
+
+# ---- embeddings -------------------------------------------------------------------------
+def make_embed_desc(n, rows, C, dtype="f32", index64=True, padding_idx=-1, scale=1.0):
+    return xconv_embed_desc(n, rows, C, DTYPES[dtype] if isinstance(dtype, str) else dtype, int(index64), padding_idx, scale)
+
+
+def xconv_embed_workspace_bytes(desc):
+    return int(lib().xconv_embed_workspace_bytes(ctypes.byref(desc)))
+
+
+def xconv_embed_fwd(desc, idx_dev, W_dev, Y_dev, stream=None):
+    _check(lib().xconv_embed_fwd(ctypes.byref(desc), _ptr(idx_dev), _ptr(W_dev), _ptr(Y_dev), _stream(stream)), "xconv_embed_fwd")
+
+
+def xconv_embed_bwd(desc, idx_dev, dY_dev, dW_dev, dw_dtype, ws_dev, stream=None):
+    _check(lib().xconv_embed_bwd(ctypes.byref(desc), _ptr(idx_dev), _ptr(dY_dev), _ptr(dW_dev), DTYPES[dw_dtype] if isinstance(dw_dtype, str) else dw_dtype,
+                                 _ptr(ws_dev), _nbytes(ws_dev), _stream(stream)), "xconv_embed_bwd")
 
 
 # ---- orthogonalised weight updates ------------------------------------------------------

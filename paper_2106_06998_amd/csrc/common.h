@@ -37,7 +37,10 @@ enum KernelId {
     K_BIAS = 18,
     K_NORM = 19,
     K_ORTH = 20,
-    K_COUNT = 21
+    K_DROP = 21,
+    K_RMS = 22,
+    K_EMBED = 23,
+    K_COUNT = 24
 };
 
 // Where the probe output of a voxel goes in Xt.  sd == 0: plain order, pixel `first` of the

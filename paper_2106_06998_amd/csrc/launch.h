@@ -138,6 +138,23 @@ hipError_t launch_norm_fwd(const xconv_norm_desc *d, const void *X, const void *
 hipError_t launch_norm_bwd(const xconv_norm_desc *d, const void *dY, const void *X, const float *mean, const float *rstd, const void *gamma, void *dX,
                            void *dgamma, void *dbeta, float *part, hipStream_t st);
 
+// dropout_kernels.hip: masks drawn from a seed; Y may be X
+void host_dropout_mask(const xconv_drop *drop, long long first, long long n, uint8_t *mask);
+hipError_t launch_dropout(int dtype, const void *X, void *Y, long long n, const xconv_drop *drop, hipStream_t st);
+
+// rms_kernels.hip: root-mean-square norm; residual, gamma, H, rstd, drop, dH, dX, dR, dgamma may be null; part: rms_ws_bytes(d) bytes, for dgamma
+size_t rms_ws_bytes(const xconv_norm_desc *d);
+hipError_t launch_rms_fwd(const xconv_norm_desc *d, const void *X, const void *residual, const void *gamma, void *Y, void *H, float *rstd, const xconv_drop *drop,
+                          hipStream_t st);
+hipError_t launch_rms_fwd8(const xconv_norm_desc *d, bool int8, const void *X, const void *residual, const void *gamma, void *Q, float *scale, void *H, hipStream_t st);
+hipError_t launch_rms_bwd(const xconv_norm_desc *d, const void *dY, const void *H, const float *rstd, const void *gamma, const void *dH, void *dX, void *dR,
+                          void *dgamma, float *part, const xconv_drop *drop, hipStream_t st);
+
+// embed_kernels.hip: rows of a table by index and the table's gradient; ws: embed_ws_bytes(d) bytes
+size_t embed_ws_bytes(const xconv_embed_desc *d);
+hipError_t launch_embed_fwd(const xconv_embed_desc *d, const void *idx, const void *W, void *Y, hipStream_t st);
+hipError_t launch_embed_bwd(const xconv_embed_desc *d, const void *idx, const void *dY, void *dW, int dw_dtype, void *ws, hipStream_t st);
+
 // orth_kernels.hip: orthogonalisation of matrices (muon: of a momentum, with the update of the weights); ws: orth_ws_bytes
 size_t orth_ws_bytes(const xconv_orth_item *items, int count);
 void orth_plan_info(const xconv_orth_item *items, int count, const xconv_orth_args *args, int index, int32_t *out);

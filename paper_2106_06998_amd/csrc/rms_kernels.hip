@@ -1,0 +1,821 @@
+// Root-mean-square norm over the channels of every position, with the addition of a residual and the dropout in front of it.
+//     forward   h = residual + drop(x), rstd = 1 / sqrt(sum_c h^2 / C + eps), y = h rstd gamma
+//     8 bits    the same (no dropout), scale = max(max_c |y|, 2^-100) / top, q = y / scale rounded (top: 448 for e4m3, 127 for int8)
+//     backward  g = dy gamma, xh = h rstd, dz = rstd (g - xh sum_c (g xh) / C) + dh, dresidual = dz, dx = drop(dz),
+//               dgamma = sum over positions of dy xh
+// Tensors are [outer, C, inner] as for layer normalisation (norm_core.h), which the division of the work follows too.  Bound by HBM:
+// every tensor is read once; h stays in registers as floats, so that statistics and y are those of the unrounded sum, while the stored h
+// is rounded once.  The mask of dropout is drawn in registers, in both passes.
+//
+// Backward: a workgroup walks positions and adds dgamma up in registers; the workgroups' sums are added in order by a second launch.
+#include "drop.h"
+#include "launch.h"
+#include "norm_core.h"
+
+namespace xc {
+
+namespace {
+
+struct RmsArgs : NormGeom {
+    const void *x, *res, *gamma;  // forward: input and residual (or null); backward: x is the stored h
+    const void *dy, *dh;          // backward; dh may be null
+    void *y, *h;                  // forward: y or q, and h (null: not stored); backward: dresidual and dx (either may be null)
+    float *rstd, *scale;          // rstd: written (forward, may be null) or read (backward); scale: of the 8-bit output
+    float *part;                  // backward: [workgroups][C] partial sums of dgamma, null when it is not wanted
+    DropArgs drop;
+    float top;
+    int w32, int8, fours;         // gamma in fp32; q is int8; dropout's places are multiples of 4
+};
+
+template <int DT, int V> __device__ inline void load_gamma(const RmsArgs &a, const Part &p, float (&g)[V])
+{
+    if (DT == XCONV_F32 || a.w32) load_params<XCONV_F32, V>(a.gamma, p, 1.f, g);
+    else load_params<DT, V>(a.gamma, p, 1.f, g);
+}
+template <int DT> __device__ inline float load_gamma1(const RmsArgs &a, int c)
+{
+    if (DT == XCONV_F32 || a.w32) return load_param<XCONV_F32>(a.gamma, c, 1.f);
+    else return load_param<DT>(a.gamma, c, 1.f);
+}
+
+// ---- 8 bits --------------------------------------------------------------------------------------------------------
+// The magnitude that a position's scale goes by; compared as bits, where a NaN is above everything and makes the scale a NaN
+constexpr float kLeast8 = 0x1p-100f;
+__device__ inline uint32_t magnitude(float y) { return __float_as_uint(y) & 0x7fffffffu; }
+
+__device__ inline uint32_t four8(float a, float b, float c, float d, int int8)
+{
+    if (int8) {
+        auto one = [](float v) { return (uint32_t)(int)fminf(fmaxf(rintf(v), -127.f), 127.f) & 0xffu; };
+        // (a NaN would become -127 by fmaxf; it is 0, and the scale says NaN)
+        auto safe = [&](float v) { return v == v ? one(v) : 0u; };
+        return safe(a) | safe(b) << 8 | safe(c) << 16 | safe(d) << 24;
+    }
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);        // round to nearest even
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+    return (uint32_t)w;
+}
+template <int V> struct __attribute__((packed, aligned(1))) Loose8 { uint32_t w[V / 4]; };
+// V values y times inv from p.at on of the run
+template <int V> __device__ inline void store8(uint8_t *run, const Part &p, const float (&y)[V], float inv, int int8)
+{
+    Loose8<V> o;
+#pragma unroll
+    for (int j = 0; j < V / 4; ++j) o.w[j] = four8(y[4 * j] * inv, y[4 * j + 1] * inv, y[4 * j + 2] * inv, y[4 * j + 3] * inv, int8);
+    if (p.hi == V) {
+        *reinterpret_cast<Loose8<V> *>(run + p.at) = o;
+    } else {
+#pragma unroll
+        for (int i = 0; i < V - 1; ++i)
+            if (i < p.hi) run[p.at + i] = (uint8_t)(o.w[i / 4] >> (8 * (i % 4)));
+    }
+}
+
+// largest of R values over a group of G lanes, as group_sum
+template <int G, int R> __device__ inline void group_max(uint32_t (&s)[R], float *red, int &turn)
+{
+#pragma unroll
+    for (int o = (G < 64 ? G : 64) / 2; o >= 1; o >>= 1)
+#pragma unroll
+        for (int r = 0; r < R; ++r) s[r] = max(s[r], (uint32_t)__shfl_xor((int)s[r], o));
+    if constexpr (G > 64) {
+        constexpr int W = G / 64;
+        uint32_t *slot = reinterpret_cast<uint32_t *>(red) + turn * W * R;
+        turn ^= 1;
+        if ((threadIdx.x & 63) == 0)
+#pragma unroll
+            for (int r = 0; r < R; ++r) slot[(threadIdx.x >> 6) * R + r] = s[r];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < W; ++i)
+#pragma unroll
+            for (int r = 0; r < R; ++r) s[r] = max(s[r], slot[i * R + r]);
+    }
+}
+
+// ---- rows ----------------------------------------------------------------------------------------------------------
+// G lanes a row, K vectors a lane, R rows at once; K == 0: a row is read again for every pass over it.  OUT8: q and scale instead of y
+template <int DT, bool OUT8, int G, int K, int R>
+__global__ __launch_bounds__(row_threads<G>) void rms_rows_fwd_kernel(RmsArgs a)
+{
+    typedef typename NormElem<DT>::t elem_t;
+    constexpr int V = NormElem<DT>::V, RP = row_threads<G> / G, KR = K > 0 ? K : 1;
+    __shared__ float red[G > 64 ? 2 * R * (G / 64) : 1];
+    int turn = 0;
+    const int lane = threadIdx.x % G, grp = threadIdx.x / G;
+    const int nv = (a.C + V - 1) / V;
+    const elem_t *X = static_cast<const elem_t *>(a.x), *RES = static_cast<const elem_t *>(a.res);
+    const uint64_t key = a.drop.q16 ? drop_key(a.drop) : 0;
+    auto rounds = [&](auto &&body) {
+        if constexpr (K > 0) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) body(k, lane + k * G);
+        } else {
+            for (int v = lane; v < nv; v += G) body(0, v);
+        }
+    };
+    for (long long r0 = (long long)blockIdx.x * (RP * R); r0 < a.outer; r0 += (long long)gridDim.x * (RP * R)) {   // (the same count for all threads)
+        float h[R][KR][V];
+        uint4 rx[R][KR], rr[R][KR];
+        size_t at[R];
+        bool on[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const long long row = r0 + r * RP + grp;
+            on[r] = row < a.outer;
+            at[r] = (size_t)(on[r] ? row : 0) * a.C;
+        }
+        auto get = [&](const elem_t *x, int r, int v, const Part &p) { return v < nv ? load_part<DT>(x + at[r], p) : uint4{0, 0, 0, 0}; };
+        auto make = [&](int r, int k, int v, const Part &p) {
+            unpack<DT>(rx[r][k], h[r][k]);
+            if (a.drop.q16) drop_values<V>(a.drop, key, at[r] + p.at, a.fours, h[r][k]);
+            if (RES) {
+                float t[V];
+                unpack<DT>(rr[r][k], t);
+#pragma unroll
+                for (int i = 0; i < V; ++i) h[r][k][i] += t[i];
+            }
+        };
+        if constexpr (K > 0) {
+            rounds([&](int k, int v) {
+                const Part p = part_of<V>(v, a.C, a.exact);
+#pragma unroll
+                for (int r = 0; r < R; ++r) rx[r][k] = get(X, r, v, p);
+            });
+            if (RES)
+                rounds([&](int k, int v) {
+                    const Part p = part_of<V>(v, a.C, a.exact);
+#pragma unroll
+                    for (int r = 0; r < R; ++r) rr[r][k] = get(RES, r, v, p);
+                });
+        }
+        // h of a round: in registers, or read again
+        auto value = [&](int r, int k, int v, const Part &p) {
+            if constexpr (K == 0) {
+                rx[r][0] = get(X, r, v, p);
+                if (RES) rr[r][0] = get(RES, r, v, p);
+                make(r, 0, v, p);
+            }
+        };
+        float s[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) s[r] = 0.f;
+        rounds([&](int k, int v) {
+            const Part p = part_of<V>(v, a.C, a.exact);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                if constexpr (K > 0) make(r, k, v, p);
+                else value(r, k, v, p);
+                if (K > 0 ? !masked<G>(a, k, nv) : !a.ragged) {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) s[r] += h[r][k][i] * h[r][k][i];       // (zeros past the last vector)
+                } else {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) s[r] += v < nv && own(p, i) ? h[r][k][i] * h[r][k][i] : 0.f;
+                }
+            }
+        });
+        group_sum<G>(s, red, turn);
+        float rstd[R], inv[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) rstd[r] = rstd_of(s[r], a);
+        if constexpr (OUT8) {
+            uint32_t m[R];
+#pragma unroll
+            for (int r = 0; r < R; ++r) m[r] = __float_as_uint(kLeast8);
+            rounds([&](int k, int v) {
+                if (v >= nv) return;
+                const Part p = part_of<V>(v, a.C, a.exact);
+                float g[V];
+                load_gamma<DT, V>(a, p, g);
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    value(r, k, v, p);
+#pragma unroll
+                    for (int i = 0; i < V; ++i)
+                        if (i < p.hi) m[r] = max(m[r], magnitude(h[r][k][i] * rstd[r] * g[i]));
+                }
+            });
+            group_max<G>(m, red, turn);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const float most = __uint_as_float(m[r]);
+                inv[r] = a.top / most;
+                if (lane == 0 && on[r]) a.scale[r0 + r * RP + grp] = most / a.top;
+            }
+        }
+        rounds([&](int k, int v) {
+            if (v >= nv) return;
+            const Part p = part_of<V>(v, a.C, a.exact);
+            float g[V];
+            load_gamma<DT, V>(a, p, g);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                if (!on[r]) continue;
+                value(r, k, v, p);
+                if (a.h) store_part<DT>(static_cast<elem_t *>(a.h) + at[r], pack<DT>(h[r][k]), p);
+                float t[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) t[i] = h[r][k][i] * rstd[r] * g[i];
+                if constexpr (OUT8) store8<V>(static_cast<uint8_t *>(a.y) + at[r], p, t, inv[r], a.int8);
+                else store_part<DT>(static_cast<elem_t *>(a.y) + at[r], pack<DT>(t), p);
+            }
+        });
+        if (!OUT8 && lane == 0 && a.rstd) {
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                if (on[r]) a.rstd[r0 + r * RP + grp] = rstd[r];
+        }
+    }
+}
+
+// T threads, so T / G rows at once; every lane adds up dgamma of its own columns.  K == 0: one row a workgroup at a time, dgamma in the
+// workgroup's own slots of `part`.
+template <int DT, int G, int K, int R, int T>
+__global__ __launch_bounds__(T) void rms_rows_bwd_kernel(RmsArgs a)
+{
+    typedef typename NormElem<DT>::t elem_t;
+    constexpr int V = NormElem<DT>::V, RP = T / G, KR = K > 0 ? K : 1;
+    __shared__ float red[G > 64 ? 2 * R * (T / 64) : 1];
+    int turn = 0;
+    const int lane = threadIdx.x % G, grp = threadIdx.x / G;
+    const elem_t *H = static_cast<const elem_t *>(a.x), *DY = static_cast<const elem_t *>(a.dy), *DH = static_cast<const elem_t *>(a.dh);
+    elem_t *DR = static_cast<elem_t *>(a.y), *DX = static_cast<elem_t *>(a.h);
+    const int nv = (a.C + V - 1) / V;
+    const uint64_t key = a.drop.q16 ? drop_key(a.drop) : 0;
+    float *part = a.part ? a.part + (size_t)blockIdx.x * a.C : nullptr;
+    auto rounds = [&](auto &&body) {
+        if constexpr (K > 0) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) body(k, lane + k * G);
+        } else {
+            for (int v = lane; v < nv; v += G) body(0, v);
+        }
+    };
+    float ag[KR][V];
+#pragma unroll
+    for (int k = 0; k < KR; ++k)
+#pragma unroll
+        for (int i = 0; i < V; ++i) ag[k][i] = 0.f;
+    bool first = true;
+    for (long long r0 = (long long)blockIdx.x * (RP * R); r0 < a.outer; r0 += (long long)gridDim.x * (RP * R), first = false) {   // (the same count for all threads)
+        uint4 rx[R][KR], rd[R][KR], rh[R][KR];
+        float rstd[R], c[R];
+        size_t at[R];
+        bool on[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const long long row = r0 + r * RP + grp;
+            on[r] = row < a.outer;
+            at[r] = (size_t)(on[r] ? row : 0) * a.C;
+            rstd[r] = on[r] ? a.rstd[row] : 0.f;
+            c[r] = 0.f;
+        }
+        auto get = [&](const elem_t *x, int r, int v, const Part &p) { return on[r] && v < nv ? load_part<DT>(x + at[r], p) : uint4{0, 0, 0, 0}; };
+        if constexpr (K > 0) {
+            rounds([&](int k, int v) {
+                const Part p = part_of<V>(v, a.C, a.exact);
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    rx[r][k] = get(H, r, v, p);
+                    rd[r][k] = get(DY, r, v, p);
+                }
+            });
+            if (DH)
+                rounds([&](int k, int v) {
+                    const Part p = part_of<V>(v, a.C, a.exact);
+#pragma unroll
+                    for (int r = 0; r < R; ++r) rh[r][k] = get(DH, r, v, p);
+                });
+        }
+        rounds([&](int k, int v) {
+            const Part p = part_of<V>(v, a.C, a.exact);
+            float g[V];
+            if (v < nv) {
+                load_gamma<DT, V>(a, p, g);
+            } else {
+#pragma unroll
+                for (int i = 0; i < V; ++i) g[i] = 0.f;
+            }
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                if constexpr (K == 0) {
+                    rx[r][0] = get(H, r, v, p);
+                    rd[r][0] = get(DY, r, v, p);
+                }
+                float x[V], d[V];
+                unpack<DT>(rx[r][k], x);
+                unpack<DT>(rd[r][k], d);
+                if (K > 0 ? masked<G>(a, k, nv) : a.ragged) {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        const bool mine = on[r] && v < nv && own(p, i);
+                        x[i] = mine ? x[i] : 0.f;
+                        d[i] = mine ? d[i] : 0.f;
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const float t = d[i] * (x[i] * rstd[r]);
+                    c[r] += t * g[i];
+                    if constexpr (K > 0) {
+                        ag[k][i] += t;
+                    } else if (part && (!a.ragged || own(p, i))) {
+                        float *q = part + p.at + i;
+                        *q = (first ? 0.f : *q) + t;
+                    }
+                }
+            }
+        });
+        if (!DR && !DX) continue;
+        group_sum<G, R, T>(c, red, turn);
+        rounds([&](int k, int v) {
+            if (v >= nv) return;
+            const Part p = part_of<V>(v, a.C, a.exact);
+            float g[V];
+            load_gamma<DT, V>(a, p, g);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                if (!on[r]) continue;
+                if constexpr (K == 0) {
+                    rx[r][0] = get(H, r, v, p);
+                    rd[r][0] = get(DY, r, v, p);
+                    if (DH) rh[r][0] = get(DH, r, v, p);
+                }
+                const float c1 = c[r] * a.inv_c;
+                float x[V], d[V];
+                unpack<DT>(rx[r][k], x);
+                unpack<DT>(rd[r][k], d);
+#pragma unroll
+                for (int i = 0; i < V; ++i) x[i] = rstd[r] * (d[i] * g[i] - (x[i] * rstd[r]) * c1);
+                if (DH) {
+                    unpack<DT>(rh[r][k], d);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) x[i] += d[i];
+                }
+                if (DR) store_part<DT>(DR + at[r], pack<DT>(x), p);
+                if (DX) {
+                    if (a.drop.q16) drop_values<V>(a.drop, key, at[r] + p.at, a.fours, x);
+                    store_part<DT>(DX + at[r], pack<DT>(x), p);
+                }
+            }
+        });
+    }
+    if (K == 0 || !part) return;
+    // groups of one workgroup hold the same columns: added up in order of the groups
+    if constexpr (RP > 1) {
+        constexpr int W = G * V;
+        __shared__ float cols[RP * W];
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            if (k > 0) __syncthreads();
+#pragma unroll
+            for (int i = 0; i < V; ++i) cols[grp * W + lane * V + i] = ag[k][i];
+            __syncthreads();
+            for (int q = threadIdx.x; q < W; q += T) {
+                const int v = k * G + q / V;
+                if (v >= nv) continue;
+                const Part p = part_of<V>(v, a.C, a.exact);
+                if (!own(p, q % V)) continue;
+                float s = 0.f;
+                for (int r = 0; r < RP; ++r) s += cols[r * W + q];
+                part[p.at + q % V] = s;
+            }
+        }
+    } else {
+        rounds([&](int k, int v) {
+            if (v >= nv) return;
+            const Part p = part_of<V>(v, a.C, a.exact);
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (own(p, i)) part[p.at + i] = ag[k][i];
+        });
+    }
+}
+
+// ---- planes --------------------------------------------------------------------------------------------------------
+// largest over the threads along the channels of V columns, as column_sum
+template <int N, int NW> __device__ inline void column_max(uint32_t (&s)[N], float *red)
+{
+#pragma unroll
+    for (int o = kNormTX; o < 64; o <<= 1)
+#pragma unroll
+        for (int i = 0; i < N; ++i) s[i] = max(s[i], (uint32_t)__shfl_xor((int)s[i], o));
+    const int tx = threadIdx.x % kNormTX;
+    uint32_t *m = reinterpret_cast<uint32_t *>(red);
+    __syncthreads();                     // whoever still reads the last sum
+    if ((threadIdx.x & 63) < kNormTX)
+#pragma unroll
+        for (int i = 0; i < N; ++i) m[((threadIdx.x >> 6) * kNormTX + tx) * N + i] = s[i];
+    __syncthreads();
+#pragma unroll 2
+    for (int w = 0; w < NW; ++w)
+#pragma unroll
+        for (int i = 0; i < N; ++i) s[i] = max(s[i], m[(w * kNormTX + tx) * N + i]);
+}
+
+// WHOLE: planes of at least one vector whose last vectors overlap, the ordinary case
+template <int DT, bool OUT8, int NW, int K, bool WHOLE>
+__global__ __launch_bounds__(NW * 64) void rms_planes_fwd_kernel(RmsArgs a)
+{
+    typedef typename NormElem<DT>::t elem_t;
+    constexpr int V = NormElem<DT>::V, TY = NW * kNormTYW, KR = K > 0 ? K : 1;
+    __shared__ float red[NW * kNormTX * V];
+    const int ty = threadIdx.x / kNormTX;
+    const uint64_t key = a.drop.q16 ? drop_key(a.drop) : 0;
+    const TileRun run = tiles_of(a);
+    auto rounds = [&](auto &&body) {
+        if constexpr (K > 0) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) body(k, ty + k * TY);
+        } else {
+            for (int c = ty; c < a.C; c += TY) body(0, c);
+        }
+    };
+    for (long long tile = run.from; tile < run.to; tile += run.step) {
+        const PlaneAt at = plane_at<V>(a, tile);
+        const elem_t *x = static_cast<const elem_t *>(a.x) + at.base;
+        const elem_t *res = a.res ? static_cast<const elem_t *>(a.res) + at.base : nullptr;
+        float h[KR][V];
+        uint4 rx[KR], rr[KR];
+        auto make = [&](int k, int c) {
+            unpack<DT>(rx[k], h[k]);
+            if (a.drop.q16) drop_values<V>(a.drop, key, at.base + (size_t)c * a.inner + at.p.at, a.fours, h[k]);
+            if (res) {
+                float t[V];
+                unpack<DT>(rr[k], t);
+#pragma unroll
+                for (int i = 0; i < V; ++i) h[k][i] += t[i];
+            }
+        };
+        if constexpr (K > 0) {
+            rounds([&](int k, int c) { rx[k] = plane_get<DT, WHOLE>(a, x, at, c); });
+            if (res) rounds([&](int k, int c) { rr[k] = plane_get<DT, WHOLE>(a, res, at, c); });
+            rounds(make);
+        }
+        auto value = [&](int k, int c) {
+            if constexpr (K == 0) {
+                rx[0] = plane_get<DT, WHOLE>(a, x, at, c);
+                if (res) rr[0] = plane_get<DT, WHOLE>(a, res, at, c);
+                make(0, c);
+            }
+        };
+        float s[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) s[i] = 0.f;
+        rounds([&](int k, int c) {
+            value(k, c);
+#pragma unroll
+            for (int i = 0; i < V; ++i) s[i] += h[k][i] * h[k][i];      // (channels that do not exist are zeros)
+        });
+        column_sum<V, NW>(s, red);
+        float rstd[V], inv[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) rstd[i] = rstd_of(s[i], a);
+        if constexpr (OUT8) {
+            uint32_t m[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) m[i] = __float_as_uint(kLeast8);
+            rounds([&](int k, int c) {
+                if (c >= a.C) return;
+                value(k, c);
+                const float g = load_gamma1<DT>(a, c);
+#pragma unroll
+                for (int i = 0; i < V; ++i) m[i] = max(m[i], magnitude(h[k][i] * rstd[i] * g));
+            });
+            column_max<V, NW>(m, red);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float most = __uint_as_float(m[i]);
+                inv[i] = a.top / most;
+                if (ty == 0 && at.on && own(at.p, i)) a.scale[at.pos + i] = most / a.top;
+            }
+        }
+        if (!at.on) continue;
+        rounds([&](int k, int c) {
+            if (c >= a.C) return;
+            value(k, c);
+            const float g = load_gamma1<DT>(a, c);
+            if (a.h) plane_put<DT, WHOLE>(a, static_cast<elem_t *>(a.h) + at.base, at, c, pack<DT>(h[k]));
+            float t[V];
+            if constexpr (OUT8) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) t[i] = h[k][i] * rstd[i] * g * inv[i];
+                store8<V>(static_cast<uint8_t *>(a.y) + at.base + (size_t)c * a.inner, at.p, t, 1.f, a.int8);
+            } else {
+#pragma unroll
+                for (int i = 0; i < V; ++i) t[i] = h[k][i] * rstd[i] * g;
+                plane_put<DT, WHOLE>(a, static_cast<elem_t *>(a.y) + at.base, at, c, pack<DT>(t));
+            }
+        });
+        if (!OUT8 && ty == 0 && a.rstd) {
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (own(at.p, i)) a.rstd[at.pos + i] = rstd[i];
+        }
+    }
+}
+
+template <int DT, int NW, int K, bool WHOLE>
+__global__ __launch_bounds__(NW * 64, 4) void rms_planes_bwd_kernel(RmsArgs a)
+{
+    typedef typename NormElem<DT>::t elem_t;
+    constexpr int V = NormElem<DT>::V, TY = NW * kNormTYW, KR = K > 0 ? K : 1;
+    __shared__ float red[NW * kNormTX * V];
+    const int ty = threadIdx.x / kNormTX, tx = threadIdx.x % kNormTX;
+    const elem_t *H = static_cast<const elem_t *>(a.x), *DY = static_cast<const elem_t *>(a.dy), *DH = static_cast<const elem_t *>(a.dh);
+    elem_t *DR = static_cast<elem_t *>(a.y), *DX = static_cast<elem_t *>(a.h);
+    const uint64_t key = a.drop.q16 ? drop_key(a.drop) : 0;
+    float *part = a.part ? a.part + (size_t)blockIdx.x * a.C : nullptr;
+    float ag[KR], gk[KR];
+#pragma unroll
+    for (int k = 0; k < KR; ++k) {
+        ag[k] = 0.f;
+        gk[k] = load_gamma1<DT>(a, min(ty + k * TY, a.C - 1));
+    }
+    auto rounds = [&](auto &&body) {
+        if constexpr (K > 0) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) body(k, ty + k * TY);
+        } else {
+            for (int c = ty; c < a.C; c += TY) body(0, c);
+        }
+    };
+    bool first = true;
+    const TileRun run = tiles_of(a);
+    if (K == 0 && part && run.from >= run.to)
+        for (int c = threadIdx.x; c < a.C; c += NW * 64) part[c] = 0.f;
+    for (long long tile = run.from; tile < run.to; tile += run.step, first = false) {
+        const PlaneAt at = plane_at<V>(a, tile);
+        uint4 rx[KR], rd[KR];
+        auto get = [&](int k, int c) {
+            rx[k] = plane_get<DT, WHOLE>(a, H + at.base, at, c);
+            rd[k] = plane_get<DT, WHOLE>(a, DY + at.base, at, c);
+        };
+        if constexpr (K > 0) rounds(get);
+        float rstd[V], c1[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            rstd[i] = at.on && i < at.p.hi ? a.rstd[at.pos + i] : 0.f;
+            c1[i] = 0.f;
+        }
+        rounds([&](int k, int c) {
+            if constexpr (K == 0) get(0, c);
+            float x[V], d[V], sg = 0.f;
+            unpack<DT>(rx[k], x);
+            unpack<DT>(rd[k], d);
+            const float g = K > 0 ? gk[k] : load_gamma1<DT>(a, c);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float t = d[i] * (x[i] * rstd[i]);
+                c1[i] += t * g;
+                sg += i >= at.p.lo ? t : 0.f;
+            }
+            if constexpr (K > 0) {
+                ag[k] += sg;
+            } else if (part) {
+#pragma unroll
+                for (int o = kNormTX / 2; o >= 1; o >>= 1) sg += __shfl_xor(sg, o);
+                if (tx == 0) part[c] = (first ? 0.f : part[c]) + sg;
+            }
+        });
+        if (!DR && !DX) continue;
+        column_sum<V, NW>(c1, red);
+        if (!at.on) continue;
+#pragma unroll
+        for (int i = 0; i < V; ++i) c1[i] *= a.inv_c;
+        rounds([&](int k, int c) {
+            if (c >= a.C) return;
+            if constexpr (K == 0) get(0, c);
+            uint4 rh{0, 0, 0, 0};
+            if (DH) rh = plane_get<DT, WHOLE>(a, DH + at.base, at, c);
+            float x[V], d[V];
+            unpack<DT>(rx[k], x);
+            unpack<DT>(rd[k], d);
+            const float g = K > 0 ? gk[k] : load_gamma1<DT>(a, c);
+#pragma unroll
+            for (int i = 0; i < V; ++i) x[i] = rstd[i] * (d[i] * g - (x[i] * rstd[i]) * c1[i]);
+            if (DH) {
+                unpack<DT>(rh, d);
+#pragma unroll
+                for (int i = 0; i < V; ++i) x[i] += d[i];
+            }
+            if (DR) plane_put<DT, WHOLE>(a, DR + at.base, at, c, pack<DT>(x));
+            if (DX) {
+                if (a.drop.q16) drop_values<V>(a.drop, key, at.base + (size_t)c * a.inner + at.p.at, a.fours, x);
+                plane_put<DT, WHOLE>(a, DX + at.base, at, c, pack<DT>(x));
+            }
+        });
+    }
+    if (K == 0 || !part) return;
+    rounds([&](int k, int c) {
+        float sg = ag[k];
+#pragma unroll
+        for (int o = kNormTX / 2; o >= 1; o >>= 1) sg += __shfl_xor(sg, o);
+        if (tx == 0 && c < a.C) part[c] = sg;
+    });
+}
+
+// dgamma[c] = sum over the n workgroups' partial sums, in order: a workgroup takes 32 columns, its 32 rows of threads share the sums
+constexpr int kRmsJoinCols = 32, kRmsJoinThreads = 1024;
+template <int WT> __global__ __launch_bounds__(kRmsJoinThreads) void rms_join_kernel(const float *part, int n, int C, void *dgamma)
+{
+    constexpr int RW = kRmsJoinThreads / kRmsJoinCols;
+    __shared__ float red[kRmsJoinThreads / 64][kRmsJoinCols];
+    const int col = threadIdx.x % kRmsJoinCols, w = threadIdx.x / kRmsJoinCols;
+    const int c = blockIdx.x * kRmsJoinCols + col;
+    float s = 0.f;
+    if (c < C) {
+#pragma unroll 8
+        for (int b = w; b < n; b += RW) s += part[(size_t)b * C + c];
+    }
+    s += __shfl_xor(s, 32);
+    if ((threadIdx.x & 63) < kRmsJoinCols) red[threadIdx.x >> 6][col] = s;
+    __syncthreads();
+    if (threadIdx.x >= kRmsJoinCols || c >= C) return;
+    float t = 0.f;
+#pragma unroll
+    for (int i = 0; i < kRmsJoinThreads / 64; ++i) t += red[i][col];
+    static_cast<typename NormElem<WT>::t *>(dgamma)[c] = norm_round<WT>(t);
+}
+
+// ---- launches ------------------------------------------------------------------------------------------------------
+struct RmsShape {
+    int G, K, R, T;   // rows: lanes a row, vectors a lane (0: read again), rows at once, threads a workgroup
+    int NW;           // planes: waves a workgroup
+    int V;
+};
+
+// The smallest group that holds a row with one vector a lane; past a wave, two and four vectors a lane, then groups of several waves
+RmsShape rms_rows_shape(int dtype, int C, bool backward)
+{
+    const int V = dtype == XCONV_F32 ? 4 : 8, nv = ceil_div(C, V);
+    const int T = backward ? 512 : 256;
+    for (int G : {4, 8, 16, 32, 64})
+        if (nv <= G) return {G, 1, 2, T, 0, V};
+    if (nv <= 128) return {64, 2, 1, T, 0, V};
+    if (nv <= 256) return {64, 4, 1, T, 0, V};
+    for (int G : {256, 1024})
+        for (int K : {2, 4})
+            if (nv <= K * G) return {G, K, 1, backward ? std::max(512, G) : G, 0, V};
+    return {1024, 0, 1, 1024, 0, V};
+}
+// 8 channels a wave and round: enough waves for 4 rounds, 8 with 16 waves
+RmsShape rms_planes_shape(int dtype, int C)
+{
+    const int V = dtype == XCONV_F32 ? 4 : 8;
+    for (int NW : {4, 8, 16})
+        for (int K : {1, 2, 4})
+            if (C <= kNormTYW * NW * K) return {0, K, 1, 0, NW, V};
+    if (C <= kNormTYW * 16 * 8) return {0, 8, 1, 0, 16, V};
+    return {0, 0, 1, 0, 16, V};
+}
+
+constexpr int kRmsBlocks = 512;            // most workgroups that leave partial sums
+constexpr long long kRmsGrid = 1 << 20;    // most workgroups of the forward pass
+
+int rms_blocks(const xconv_norm_desc *d, const RmsShape &s, bool bwd)
+{
+    if (d->inner > 1) {
+        const long long want = plane_tiles(d, s.V);
+        return (int)std::min<long long>(want > 8 ? (want + 7) / 8 * 8 : want, bwd ? 2 * kRmsBlocks : kRmsGrid);
+    }
+    const int rows = s.T / s.G * s.R;
+    return (int)std::min<long long>((d->outer + rows - 1) / rows, bwd ? kRmsBlocks : kRmsGrid);
+}
+
+enum RmsPass { kRmsForward, kRmsForward8, kRmsBackward };
+
+template <int DT, int G, int K, int R> hipError_t go_rms_rows(const RmsArgs &a, RmsPass pass, int blocks, hipStream_t st)
+{
+    const dim3 grid((unsigned)blocks);
+    if (pass == kRmsForward) {
+        hipLaunchKernelGGL((rms_rows_fwd_kernel<DT, false, G, K, R>), grid, dim3(row_threads<G>), 0, st, a);
+    } else if (pass == kRmsForward8) {
+        hipLaunchKernelGGL((rms_rows_fwd_kernel<DT, true, G, K, R>), grid, dim3(row_threads<G>), 0, st, a);
+    } else {
+        constexpr int T = G > 512 ? G : 512;
+        hipLaunchKernelGGL((rms_rows_bwd_kernel<DT, G, K, R, T>), grid, dim3(T), 0, st, a);
+    }
+    return hipGetLastError();
+}
+template <int DT> hipError_t go_rms_rows_shape(const RmsArgs &a, const RmsShape &s, RmsPass pass, int blocks, hipStream_t st)
+{
+    switch (s.G * 8 + s.K) {
+    case 4 * 8 + 1: return go_rms_rows<DT, 4, 1, 2>(a, pass, blocks, st);
+    case 8 * 8 + 1: return go_rms_rows<DT, 8, 1, 2>(a, pass, blocks, st);
+    case 16 * 8 + 1: return go_rms_rows<DT, 16, 1, 2>(a, pass, blocks, st);
+    case 32 * 8 + 1: return go_rms_rows<DT, 32, 1, 2>(a, pass, blocks, st);
+    case 64 * 8 + 1: return go_rms_rows<DT, 64, 1, 2>(a, pass, blocks, st);
+    case 64 * 8 + 2: return go_rms_rows<DT, 64, 2, 1>(a, pass, blocks, st);
+    case 64 * 8 + 4: return go_rms_rows<DT, 64, 4, 1>(a, pass, blocks, st);
+    case 256 * 8 + 2: return go_rms_rows<DT, 256, 2, 1>(a, pass, blocks, st);
+    case 256 * 8 + 4: return go_rms_rows<DT, 256, 4, 1>(a, pass, blocks, st);
+    case 1024 * 8 + 2: return go_rms_rows<DT, 1024, 2, 1>(a, pass, blocks, st);
+    case 1024 * 8 + 4: return go_rms_rows<DT, 1024, 4, 1>(a, pass, blocks, st);
+    default: return go_rms_rows<DT, 1024, 0, 1>(a, pass, blocks, st);
+    }
+}
+template <int DT, int NW, int K, bool WHOLE> hipError_t go_rms_planes(const RmsArgs &a, RmsPass pass, int blocks, hipStream_t st)
+{
+    const dim3 grid((unsigned)blocks), block(NW * 64);
+    if (pass == kRmsForward) hipLaunchKernelGGL((rms_planes_fwd_kernel<DT, false, NW, K, WHOLE>), grid, block, 0, st, a);
+    else if (pass == kRmsForward8) hipLaunchKernelGGL((rms_planes_fwd_kernel<DT, true, NW, K, WHOLE>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((rms_planes_bwd_kernel<DT, NW, K, WHOLE>), grid, block, 0, st, a);
+    return hipGetLastError();
+}
+template <int DT, bool WHOLE> hipError_t go_rms_planes_shape(const RmsArgs &a, const RmsShape &s, RmsPass pass, int blocks, hipStream_t st)
+{
+    switch (s.NW * 32 + s.K) {
+    case 4 * 32 + 1: return go_rms_planes<DT, 4, 1, WHOLE>(a, pass, blocks, st);
+    case 4 * 32 + 2: return go_rms_planes<DT, 4, 2, WHOLE>(a, pass, blocks, st);
+    case 4 * 32 + 4: return go_rms_planes<DT, 4, 4, WHOLE>(a, pass, blocks, st);
+    case 8 * 32 + 4: return go_rms_planes<DT, 8, 4, WHOLE>(a, pass, blocks, st);
+    case 16 * 32 + 4: return go_rms_planes<DT, 16, 4, WHOLE>(a, pass, blocks, st);
+    case 16 * 32 + 8: return go_rms_planes<DT, 16, 8, WHOLE>(a, pass, blocks, st);
+    default: return go_rms_planes<DT, 16, 0, WHOLE>(a, pass, blocks, st);
+    }
+}
+
+template <int DT> hipError_t launch_rms_dt(const xconv_norm_desc *d, RmsArgs a, RmsPass pass, void *dgamma, hipStream_t st)
+{
+    const bool planes = d->inner > 1, bwd = pass == kRmsBackward;
+    constexpr int V = NormElem<DT>::V;
+    // outputs over inputs: the overlapping part of a plane may be another workgroup's, that of a row read again another lane's
+    const size_t bytes = (size_t)d->outer * d->C * d->inner * (DT == XCONV_F32 ? 4 : 2);
+    bool over = false;
+    for (const void *out : {pass == kRmsForward8 ? nullptr : a.y, a.h})
+        for (const void *in : {a.x, a.res, a.dy, a.dh}) over = over || overlap(out, in, bytes);
+    const RmsShape s = planes ? rms_planes_shape(DT, d->C) : rms_rows_shape(DT, d->C, bwd);
+    a.ragged = (planes ? d->inner : (int64_t)d->C) % V != 0;
+    a.exact = planes ? over || d->inner < V : d->C < V || (s.K == 0 && over);
+    a.outer = d->outer;
+    a.C = d->C;
+    a.inner = (int)d->inner;
+    a.eps = d->eps;
+    a.count = (float)d->C;
+    a.inv_c = 1.0f / a.count;
+    a.nvi = ceil_div((int)d->inner, s.V);
+    a.tiles = plane_tiles(d, s.V);
+    a.w32 = d->w_dtype == XCONV_F32;
+    a.fours = (planes ? d->inner : (int64_t)d->C) % 4 == 0;
+    const int blocks = rms_blocks(d, s, bwd);
+    hipError_t e = hipSuccess;
+    if (d->outer > 0) {
+        if (!planes) e = go_rms_rows_shape<DT>(a, s, pass, blocks, st);
+        else if (a.exact) e = go_rms_planes_shape<DT, false>(a, s, pass, blocks, st);
+        else e = go_rms_planes_shape<DT, true>(a, s, pass, blocks, st);
+    }
+    if (e != hipSuccess || !dgamma) return e;
+    const dim3 grid((unsigned)ceil_div(d->C, kRmsJoinCols));
+    if (a.w32) hipLaunchKernelGGL(rms_join_kernel<XCONV_F32>, grid, dim3(kRmsJoinThreads), 0, st, a.part, blocks, d->C, dgamma);
+    else hipLaunchKernelGGL(rms_join_kernel<DT>, grid, dim3(kRmsJoinThreads), 0, st, a.part, blocks, d->C, dgamma);
+    return hipGetLastError();
+}
+
+hipError_t launch_rms(const xconv_norm_desc *d, const RmsArgs &a, RmsPass pass, void *dgamma, hipStream_t st)
+{
+    if (d->dtype == XCONV_F32) return launch_rms_dt<XCONV_F32>(d, a, pass, dgamma, st);
+    if (d->dtype == XCONV_BF16) return launch_rms_dt<XCONV_BF16>(d, a, pass, dgamma, st);
+    return launch_rms_dt<XCONV_F16>(d, a, pass, dgamma, st);
+}
+
+}  // namespace
+
+size_t rms_ws_bytes(const xconv_norm_desc *d)
+{
+    const RmsShape s = d->inner > 1 ? rms_planes_shape(d->dtype, d->C) : rms_rows_shape(d->dtype, d->C, true);
+    return (size_t)rms_blocks(d, s, true) * d->C * sizeof(float);
+}
+
+hipError_t launch_rms_fwd(const xconv_norm_desc *d, const void *X, const void *residual, const void *gamma, void *Y, void *H, float *rstd, const xconv_drop *drop,
+                          hipStream_t st)
+{
+    RmsArgs a{};
+    a.x = X; a.res = residual; a.gamma = gamma; a.y = Y; a.h = H; a.rstd = rstd;
+    a.drop = drop_args(drop);
+    return launch_rms(d, a, kRmsForward, nullptr, st);
+}
+
+hipError_t launch_rms_fwd8(const xconv_norm_desc *d, bool int8, const void *X, const void *residual, const void *gamma, void *Q, float *scale, void *H, hipStream_t st)
+{
+    RmsArgs a{};
+    a.x = X; a.res = residual; a.gamma = gamma; a.y = Q; a.h = H; a.scale = scale;
+    a.int8 = int8;
+    a.top = int8 ? 127.f : 448.f;
+    a.drop = drop_args(nullptr);
+    return launch_rms(d, a, kRmsForward8, nullptr, st);
+}
+
+hipError_t launch_rms_bwd(const xconv_norm_desc *d, const void *dY, const void *H, const float *rstd, const void *gamma, const void *dH, void *dX, void *dR,
+                          void *dgamma, float *part, const xconv_drop *drop, hipStream_t st)
+{
+    RmsArgs a{};
+    a.x = H; a.dy = dY; a.dh = dH; a.gamma = gamma; a.y = dR; a.h = dX;
+    a.rstd = const_cast<float *>(rstd);
+    a.part = dgamma ? part : nullptr;
+    a.drop = drop_args(drop);
+    return launch_rms(d, a, kRmsBackward, dgamma, st);
+}
+
+}  // namespace xc

@@ -48,6 +48,14 @@ struct Lib {
     decltype(&xconv_layernorm_workspace_bytes) layernorm_workspace_bytes;
     decltype(&xconv_layernorm_fwd) layernorm_fwd;
     decltype(&xconv_layernorm_bwd) layernorm_bwd;
+    decltype(&xconv_dropout) dropout;
+    decltype(&xconv_rmsnorm_workspace_bytes) rmsnorm_workspace_bytes;
+    decltype(&xconv_rmsnorm_fwd) rmsnorm_fwd;
+    decltype(&xconv_rmsnorm_fwd_8bit) rmsnorm_fwd_8bit;
+    decltype(&xconv_rmsnorm_bwd) rmsnorm_bwd;
+    decltype(&xconv_embed_workspace_bytes) embed_workspace_bytes;
+    decltype(&xconv_embed_fwd) embed_fwd;
+    decltype(&xconv_embed_bwd) embed_bwd;
     decltype(&xconv_orth_workspace_bytes) orth_workspace_bytes;
     decltype(&xconv_orth) orth;
     decltype(&xconv_muon_step64) muon_step;
@@ -378,25 +386,25 @@ struct NormView {
     at::MemoryFormat format;
     std::vector<int64_t> stats;
 };
-NormView norm_view(const Tensor &x, const Tensor &weight, const Tensor &bias, int64_t axis, double eps)
+NormView norm_view(const Tensor &x, const Tensor &weight, const Tensor &bias, int64_t axis, double eps, const std::string &who = "layer_norm")
 {
-    if (!x.is_cuda()) refuse("layer_norm: runs on the GPU only (input on " + x.device().str() + ")");
-    if (!storage_type(x)) refuse(std::string("layer_norm: storage type ") + at::toString(x.scalar_type()) + " is not supported (float32, bfloat16, float16)");
+    if (!x.is_cuda()) refuse(who + ": runs on the GPU only (input on " + x.device().str() + ")");
+    if (!storage_type(x)) refuse(who + ": storage type " + at::toString(x.scalar_type()) + " is not supported (float32, bfloat16, float16)");
     const int64_t dim = x.dim();
     if (axis < 0) axis += dim;
-    if (dim < 1 || (axis != dim - 1 && (axis != 1 || dim < 2))) refuse("layer_norm: the channels are the last axis or axis 1 of the input");
+    if (dim < 1 || (axis != dim - 1 && (axis != 1 || dim < 2))) refuse(who + ": the channels are the last axis or axis 1 of the input");
     NormView v;
     v.format = at::MemoryFormat::Contiguous;
     const int64_t C = x.size(axis);
-    if (C < 1 || C > INT32_MAX) refuse("layer_norm: no channels");
+    if (C < 1 || C > INT32_MAX) refuse(who + ": no channels");
     int wt = -1;
     for (const Tensor *p : {&weight, &bias}) {
         if (!p->defined()) continue;
-        if (p->device() != x.device() || p->dim() != 1 || p->size(0) != C) refuse("layer_norm: expected parameters of " + std::to_string(C) + " channels on the input's device");
+        if (p->device() != x.device() || p->dim() != 1 || p->size(0) != C) refuse(who + ": expected parameters of " + std::to_string(C) + " channels on the input's device");
         if (!storage_type(*p) || (p->scalar_type() != at::kFloat && p->scalar_type() != x.scalar_type()))
-            refuse("layer_norm: parameters are float32 or of the input's type");
+            refuse(who + ": parameters are float32 or of the input's type");
         const int t = dtype_code(p->scalar_type());
-        if (wt >= 0 && wt != t) refuse("layer_norm: weight and bias are of one type");
+        if (wt >= 0 && wt != t) refuse(who + ": weight and bias are of one type");
         wt = t;
     }
     int64_t inner = 1;
@@ -477,6 +485,223 @@ PyObject *norm_backward(PyObject *, PyObject *const *args, Py_ssize_t nargs)
         }))
         return nullptr;
     return Py_BuildValue("NNN", wrap(dx), wrap(dw), wrap(db));
+}
+
+// ---- dropout without a stored mask ----
+// one 64-bit number that is added to the seed, or none
+xconv_drop drop_of(long long q16, long long seed, const Tensor &step, const Tensor &like, const char *who)
+{
+    if (step.defined() && (step.scalar_type() != at::kLong || step.numel() != 1 || step.device() != like.device()))
+        refuse(std::string(who) + ": step is one int64 value on the input's device");
+    return xconv_drop{(uint64_t)seed, static_cast<const int64_t *>(ptr(step)), (int32_t)q16};
+}
+void check_storage(const Tensor &x, const char *who)
+{
+    if (!x.defined()) refuse(std::string(who) + ": a tensor is expected");
+    if (!x.is_cuda()) refuse(std::string(who) + ": runs on the GPU only (input on " + x.device().str() + ")");
+    if (!storage_type(x)) refuse(std::string(who) + ": storage type " + at::toString(x.scalar_type()) + " is not supported (float32, bfloat16, float16)");
+}
+
+// dropout(x, q16, seed, step or None, like: (shape, strides, dtype code) or None, stream) -> y in the memory order of x (or of `like`)
+PyObject *dropout(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    if (!ready(nargs, 6, "dropout")) return nullptr;
+    const Tensor x = tensor_arg(args[0]), step = tensor_arg(args[3]);
+    long long v[2], s, code = -1;
+    if (!ints(args, 1, 2, v) || !ints(args, 5, 1, &s)) return nullptr;
+    std::vector<int64_t> dims[2];
+    if (args[4] != Py_None) {
+        for (int k = 0; k < 2; ++k) {
+            PyObject *t = PyTuple_GetItem(args[4], k);
+            for (Py_ssize_t i = 0; t && i < PyTuple_Size(t); ++i) dims[k].push_back(PyLong_AsLongLong(PyTuple_GetItem(t, i)));
+        }
+        if (!PyErr_Occurred()) code = PyLong_AsLongLong(PyTuple_GetItem(args[4], 2));
+        if (PyErr_Occurred()) return nullptr;
+    }
+    Tensor y;
+    if (!run([&] {
+            check_storage(x, "dropout");
+            const c10::DeviceGuard guard(x.device());
+            const xconv_drop d = drop_of(v[0], v[1], step, x, "dropout");
+            Tensor src = x;
+            if (code >= 0) {
+                const at::ScalarType t = code == XCONV_F32 ? at::kFloat : code == XCONV_BF16 ? at::kBFloat16 : at::kHalf;
+                y = at::empty_strided(dims[0], dims[1], x.options().dtype(t));
+                if (x.sizes() != y.sizes()) refuse("dropout: the gradient has another shape than the output");
+                if (x.scalar_type() != t || x.strides() != y.strides()) {
+                    y.copy_(x);
+                    src = y;
+                }
+            } else {
+                if (!x.is_non_overlapping_and_dense()) src = x.contiguous();
+                y = at::empty_strided(src.sizes(), src.strides(), src.options());
+            }
+            check(L.dropout(dtype_code(src.scalar_type()), ptr(src), ptr(y), src.numel(), &d, reinterpret_cast<void *>(s)), "xconv_dropout");
+        }))
+        return nullptr;
+    return wrap(y);
+}
+
+// ---- root-mean-square norm over channels ----
+// t in the memory order of the view, for the kernels
+Tensor beside(const Tensor &t, const Tensor &x, const NormView &n, const char *what, bool convert)
+{
+    if (!t.defined()) return t;
+    if (t.sizes() != x.sizes() || t.device() != x.device()) refuse(std::string("rms_norm: ") + what + " has another shape or device than the input");
+    if (t.scalar_type() != x.scalar_type()) {
+        if (!convert) refuse(std::string("rms_norm: ") + what + " is of the input's type");
+        return t.to(x.scalar_type()).contiguous(n.format);
+    }
+    return t.contiguous(n.format);
+}
+
+// rms_forward(x, weight or None, residual or None, eps, axis, q16, seed, step or None, stream) -> (y, h or None where it is x, rstd)
+PyObject *rms_forward(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    if (!ready(nargs, 9, "rms_forward")) return nullptr;
+    const Tensor x = tensor_arg(args[0]), weight = tensor_arg(args[1]), residual = tensor_arg(args[2]), step = tensor_arg(args[7]);
+    const double eps = PyFloat_AsDouble(args[3]);
+    if (eps == -1.0 && PyErr_Occurred()) return nullptr;
+    long long v[3], s;
+    if (!ints(args, 4, 3, v) || !ints(args, 8, 1, &s)) return nullptr;
+    Tensor y, h, rstd;
+    if (!run([&] {
+            check_storage(x, "rms_norm");
+            const c10::DeviceGuard guard(x.device());
+            const NormView n = norm_view(x, weight, Tensor(), v[0], eps, "rms_norm");
+            const Tensor w = solid(weight), r = beside(residual, x, n, "the residual", false);
+            const xconv_drop d = drop_of(v[1], v[2], step, x, "rms_norm");
+            y = at::empty(x.sizes(), x.options(), n.format);
+            if (r.defined() || d.drop_q16 != 0) h = at::empty(x.sizes(), x.options(), n.format);
+            rstd = at::empty(n.stats, x.options().dtype(at::kFloat));
+            check(L.rmsnorm_fwd(&n.d, ptr(n.x), ptr(r), ptr(w), ptr(y), ptr(h), rstd.data_ptr<float>(), &d, reinterpret_cast<void *>(s)), "xconv_rmsnorm_fwd");
+        }))
+        return nullptr;
+    return Py_BuildValue("NNN", wrap(y), wrap(h), wrap(rstd));
+}
+
+// rms_forward_8bit(x, weight or None, residual or None, eps, axis, int8, stream) -> (q, scale, h or None where it is x)
+PyObject *rms_forward_8bit(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    if (!ready(nargs, 7, "rms_forward_8bit")) return nullptr;
+    const Tensor x = tensor_arg(args[0]), weight = tensor_arg(args[1]), residual = tensor_arg(args[2]);
+    const double eps = PyFloat_AsDouble(args[3]);
+    if (eps == -1.0 && PyErr_Occurred()) return nullptr;
+    long long v[3];
+    if (!ints(args, 4, 3, v)) return nullptr;
+    Tensor q, scale, h;
+    if (!run([&] {
+            check_storage(x, "rms_norm_8bit");
+            const c10::DeviceGuard guard(x.device());
+            const NormView n = norm_view(x, weight, Tensor(), v[0], eps, "rms_norm_8bit");
+            const Tensor w = solid(weight), r = beside(residual, x, n, "the residual", false);
+            q = at::empty(x.sizes(), x.options().dtype(v[1] ? at::kChar : at::kFloat8_e4m3fn), n.format);
+            scale = at::empty(n.stats, x.options().dtype(at::kFloat));
+            if (r.defined()) h = at::empty(x.sizes(), x.options(), n.format);
+            check(L.rmsnorm_fwd_8bit(&n.d, v[1] ? XCONV_INT8 : XCONV_E4M3, ptr(n.x), ptr(r), ptr(w), ptr(q), scale.data_ptr<float>(), ptr(h), reinterpret_cast<void *>(v[2])),
+                  "xconv_rmsnorm_fwd_8bit");
+        }))
+        return nullptr;
+    return Py_BuildValue("NNN", wrap(q), wrap(scale), wrap(h));
+}
+
+// rms_backward(dy, h, rstd, weight or None, dh or None, axis, q16, seed, need_dx, need_dresidual, need_dw, dw in float32 or the type of h,
+// step or None, stream) -> (dx, dresidual, dw), None where not asked for; without dropout dx and dresidual are one tensor
+PyObject *rms_backward(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    if (!ready(nargs, 14, "rms_backward")) return nullptr;
+    const Tensor dy = tensor_arg(args[0]), h = tensor_arg(args[1]), rstd = tensor_arg(args[2]), weight = tensor_arg(args[3]), dh = tensor_arg(args[4]),
+                 step = tensor_arg(args[12]);
+    long long v[7], s;
+    if (!ints(args, 5, 7, v) || !ints(args, 13, 1, &s)) return nullptr;
+    Tensor dx, dr, dw;
+    if (!run([&] {
+            check_storage(h, "rms_norm");
+            if (!dy.defined() || !rstd.defined()) refuse("rms_norm: a gradient and the forward pass's rstd are expected");
+            const c10::DeviceGuard guard(h.device());
+            NormView n = norm_view(h, weight, Tensor(), v[0], 0.0, "rms_norm");
+            const at::ScalarType wt = v[6] ? at::kFloat : h.scalar_type();
+            if (weight.defined() && weight.scalar_type() != wt) refuse("rms_norm: the gradient of the weight is of its type");
+            n.d.w_dtype = dtype_code(wt);
+            const Tensor g = beside(dy, h, n, "the gradient", true), gh = beside(dh, h, n, "the gradient of h", true);
+            if (rstd.scalar_type() != at::kFloat || rstd.device() != h.device() || rstd.numel() != n.d.outer * n.d.inner)
+                refuse("rms_norm: rstd is that of the forward pass");
+            const xconv_drop d = drop_of(v[1], v[2], step, h, "rms_norm");
+            const Tensor w = solid(weight), rs = rstd.contiguous();
+            const bool drops = d.drop_q16 != 0;
+            // without dropout dX is dR
+            if (v[4] || (v[3] && !drops)) dr = at::empty(h.sizes(), h.options(), n.format);
+            if (v[3] && drops) dx = at::empty(h.sizes(), h.options(), n.format);
+            if (v[5]) dw = at::empty({n.d.C}, h.options().dtype(wt));
+            Tensor ws;
+            if (v[5]) ws = bytes_on(L.rmsnorm_workspace_bytes(&n.d), h);
+            check(L.rmsnorm_bwd(&n.d, ptr(g), ptr(n.x), static_cast<const float *>(ptr(rs)), ptr(w), ptr(gh), ptr(dx), ptr(dr), ptr(dw), ptr(ws),
+                                ws.defined() ? (size_t)ws.numel() : 0, &d, reinterpret_cast<void *>(s)),
+                  "xconv_rmsnorm_bwd");
+            if (v[3] && !drops) dx = dr;
+            if (!v[4]) dr = Tensor();
+        }))
+        return nullptr;
+    return Py_BuildValue("NNN", wrap(dx), wrap(dr), wrap(dw));
+}
+
+// ---- embeddings ----
+Tensor check_indices(const Tensor &idx, const Tensor &like)
+{
+    if (!idx.defined() || (idx.scalar_type() != at::kLong && idx.scalar_type() != at::kInt)) refuse("embedding: indices are int64 or int32");
+    if (idx.device() != like.device()) refuse("embedding: indices and values are on one device");
+    return idx.contiguous();
+}
+// embed_forward(indices, weight, scale, stream) -> [indices' shape, C]
+PyObject *embed_forward(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    if (!ready(nargs, 4, "embed_forward")) return nullptr;
+    const Tensor idx = tensor_arg(args[0]), weight = tensor_arg(args[1]);
+    const double scale = PyFloat_AsDouble(args[2]);
+    long long s;
+    if ((scale == -1.0 && PyErr_Occurred()) || !ints(args, 3, 1, &s)) return nullptr;
+    Tensor y;
+    if (!run([&] {
+            check_storage(weight, "embedding");
+            if (weight.dim() != 2 || weight.size(0) < 1 || weight.size(1) < 1 || weight.size(1) > INT32_MAX) refuse("embedding: the table is a matrix with at least one row and column");
+            const c10::DeviceGuard guard(weight.device());
+            const Tensor i = check_indices(idx, weight), w = weight.contiguous();
+            std::vector<int64_t> shape = idx.sizes().vec();
+            shape.push_back(w.size(1));
+            y = at::empty(shape, w.options());
+            const xconv_embed_desc d{i.numel(), w.size(0), (int32_t)w.size(1), dtype_code(w.scalar_type()), i.scalar_type() == at::kLong, -1, (float)scale};
+            check(L.embed_fwd(&d, ptr(i), ptr(w), ptr(y), reinterpret_cast<void *>(s)), "xconv_embed_fwd");
+        }))
+        return nullptr;
+    return wrap(y);
+}
+// embed_backward(dy, indices, rows, scale, padding index or -1, dw in float32 or the type of dy, stream) -> dw [rows, C]
+PyObject *embed_backward(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    if (!ready(nargs, 7, "embed_backward")) return nullptr;
+    const Tensor dy = tensor_arg(args[0]), idx = tensor_arg(args[1]);
+    const double scale = PyFloat_AsDouble(args[3]);
+    long long rows, v[3];
+    if ((scale == -1.0 && PyErr_Occurred()) || !ints(args, 2, 1, &rows) || !ints(args, 4, 3, v)) return nullptr;
+    Tensor dw;
+    if (!run([&] {
+            check_storage(dy, "embedding");
+            const c10::DeviceGuard guard(dy.device());
+            const Tensor i = check_indices(idx, dy);
+            if (dy.dim() != idx.dim() + 1 || dy.size(-1) < 1 || dy.size(-1) > INT32_MAX || dy.numel() != idx.numel() * dy.size(-1)) refuse("embedding: the gradient is of the indices' shape and the channels");
+            if (rows < 1 || v[0] < -1 || v[0] >= rows || v[0] > INT32_MAX) refuse("embedding: expected a positive number of rows and a padding index among them");
+            const Tensor g = dy.contiguous();
+            const at::ScalarType wt = v[1] ? at::kFloat : dy.scalar_type();
+            const xconv_embed_desc d{i.numel(), rows, (int32_t)dy.size(-1), dtype_code(dy.scalar_type()), i.scalar_type() == at::kLong, (int32_t)v[0], (float)scale};
+            const size_t need = L.embed_workspace_bytes(&d);
+            if (need == 0 && i.numel() > 0)     // (refused before anything is launched, with the reason)
+                check(L.embed_bwd(&d, ptr(i), ptr(g), ptr(g), dtype_code(wt), nullptr, 0, reinterpret_cast<void *>(v[2])), "xconv_embed_bwd");
+            const Tensor ws = bytes_on(need, dy);
+            dw = at::empty({rows, dy.size(-1)}, dy.options().dtype(wt));
+            check(L.embed_bwd(&d, ptr(i), ptr(g), ptr(dw), dtype_code(wt), ptr(ws), (size_t)ws.numel(), reinterpret_cast<void *>(v[2])), "xconv_embed_bwd");
+        }))
+        return nullptr;
+    return wrap(dw);
 }
 
 // ---- orthogonalised weight updates ----
@@ -723,6 +948,14 @@ PyObject *glue_init(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     get(L.layernorm_workspace_bytes, "xconv_layernorm_workspace_bytes");
     get(L.layernorm_fwd, "xconv_layernorm_fwd");
     get(L.layernorm_bwd, "xconv_layernorm_bwd");
+    get(L.dropout, "xconv_dropout");
+    get(L.rmsnorm_workspace_bytes, "xconv_rmsnorm_workspace_bytes");
+    get(L.rmsnorm_fwd, "xconv_rmsnorm_fwd");
+    get(L.rmsnorm_fwd_8bit, "xconv_rmsnorm_fwd_8bit");
+    get(L.rmsnorm_bwd, "xconv_rmsnorm_bwd");
+    get(L.embed_workspace_bytes, "xconv_embed_workspace_bytes");
+    get(L.embed_fwd, "xconv_embed_fwd");
+    get(L.embed_bwd, "xconv_embed_bwd");
     get(L.orth_workspace_bytes, "xconv_orth_workspace_bytes");
     get(L.orth, "xconv_orth");
     get(L.muon_step, "xconv_muon_step64");
@@ -747,6 +980,12 @@ PyMethodDef g_methods[] = {
     XC_METHOD("relu_backward", relu_backward),
     XC_METHOD("norm_forward", norm_forward),
     XC_METHOD("norm_backward", norm_backward),
+    XC_METHOD("dropout", dropout),
+    XC_METHOD("rms_forward", rms_forward),
+    XC_METHOD("rms_forward_8bit", rms_forward_8bit),
+    XC_METHOD("rms_backward", rms_backward),
+    XC_METHOD("embed_forward", embed_forward),
+    XC_METHOD("embed_backward", embed_backward),
     XC_METHOD("orthogonalize", orthogonalize),
     XC_METHOD("muon_step", muon_step),
     {nullptr, nullptr, 0, nullptr},

@@ -5,6 +5,7 @@
 #include <cmath>
 #include <cstdlib>
 #include <cstring>
+#include <initializer_list>
 #include <mutex>
 #include <vector>
 
@@ -1382,6 +1383,196 @@ xconv_status xconv_layernorm_bwd(const xconv_norm_desc *desc, const void *dY_dev
     return XCONV_OK;
 }
 
+// ---- dropout, root-mean-square norm, embeddings ----------------------------------------
+namespace {
+// outputs may be inputs (the same address) where `same`; nothing else of an output lies over anything
+struct Span {
+    const void *p;
+    size_t bytes;
+};
+bool apart(const Span &a, const Span &b, bool same)
+{
+    if (!a.p || !b.p || a.bytes == 0 || b.bytes == 0) return true;
+    if (same && a.p == b.p && a.bytes == b.bytes) return true;
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+    return x + a.bytes <= y || y + b.bytes <= x;
+}
+bool drop_ok(const xconv_drop *d)
+{
+    return d->drop_q16 >= 0 && d->drop_q16 <= 65536 && aligned_to(d->step_dev, 8);
+}
+// inputs: `like` of the outputs' own type, which an output may be, and others
+bool outputs_apart(std::initializer_list<Span> outputs, std::initializer_list<Span> like, std::initializer_list<Span> others)
+{
+    for (const Span *o = outputs.begin(); o != outputs.end(); ++o) {
+        for (const Span *q = outputs.begin(); q != o; ++q)
+            if (!apart(*o, *q, false)) return false;
+        for (const Span &i : like)
+            if (!apart(*o, i, true)) return false;
+        for (const Span &i : others)
+            if (!apart(*o, i, false)) return false;
+    }
+    return true;
+}
+}  // namespace
+
+xconv_status xconv_dropout(int dtype, const void *X_dev, void *Y_dev, long long n, const xconv_drop *drop, void *stream)
+{
+    if (dtype < XCONV_F32 || dtype > XCONV_F16 || n < 0 || !drop || !drop_ok(drop)) return XCONV_EINVAL;
+    if (n == 0) return XCONV_OK;
+    if (!X_dev || !Y_dev || !aligned_to(X_dev, elem_bytes(dtype)) || !aligned_to(Y_dev, elem_bytes(dtype))) return XCONV_EINVAL;
+    if (n > (1LL << 40)) return XCONV_EUNSUPPORTED;
+    const size_t bytes = (size_t)n * elem_bytes(dtype);
+    if (!outputs_apart({{Y_dev, bytes}}, {{X_dev, bytes}}, {{drop->step_dev, 8}})) return XCONV_EINVAL;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    XC_LAUNCH(K_DROP, st, launch_dropout(dtype, X_dev, Y_dev, n, drop, st));
+    return XCONV_OK;
+}
+
+xconv_status xconv_dropout_mask(const xconv_drop *drop, long long first, long long n, uint8_t *mask_host)
+{
+    if (!drop || drop->step_dev || !drop_ok(drop) || first < 0 || n < 0 || (n > 0 && !mask_host)) return XCONV_EINVAL;
+    host_dropout_mask(drop, first, n, mask_host);
+    return XCONV_OK;
+}
+
+namespace {
+// as for layer normalisation; the sizes in bytes that overlap is judged by fit 64 bits
+xconv_status check_rms(const xconv_norm_desc *d)
+{
+    const xconv_status s = check_norm(d);
+    return s == XCONV_OK && d->outer * d->inner > (1LL << 48) / d->C ? XCONV_EUNSUPPORTED : s;
+}
+}  // namespace
+
+size_t xconv_rmsnorm_workspace_bytes(const xconv_norm_desc *desc)
+{
+    return check_rms(desc) == XCONV_OK && desc->outer > 0 ? rms_ws_bytes(desc) : 0;
+}
+
+namespace {
+struct NormSizes {
+    size_t e, w, bytes, pos, params;
+};
+NormSizes norm_sizes(const xconv_norm_desc *d)
+{
+    const size_t e = elem_bytes(d->dtype), w = elem_bytes(d->w_dtype), pos = (size_t)d->outer * (size_t)d->inner;
+    return {e, w, pos * (size_t)d->C * e, pos * 4, (size_t)d->C * w};
+}
+}  // namespace
+
+xconv_status xconv_rmsnorm_fwd(const xconv_norm_desc *desc, const void *X_dev, const void *R_dev, const void *gamma_dev, void *Y_dev, void *H_dev,
+                               float *rstd_dev, const xconv_drop *drop, void *stream)
+{
+    const xconv_status s = check_rms(desc);
+    if (s != XCONV_OK) return s;
+    if (drop && !drop_ok(drop)) return XCONV_EINVAL;
+    if (desc->outer == 0) return XCONV_OK;
+    if (!X_dev || !Y_dev) return XCONV_EINVAL;
+    const NormSizes n = norm_sizes(desc);
+    for (const void *p : {X_dev, R_dev, (const void *)Y_dev, (const void *)H_dev})
+        if (!aligned_to(p, n.e)) return XCONV_EINVAL;
+    if (!aligned_to(gamma_dev, n.w) || !aligned_to(rstd_dev, 4)) return XCONV_EINVAL;
+    const Span g{gamma_dev, n.params}, st8{drop ? drop->step_dev : nullptr, 8}, r{rstd_dev, n.pos};
+    if (!outputs_apart({{Y_dev, n.bytes}, {H_dev, n.bytes}}, {{X_dev, n.bytes}, {R_dev, n.bytes}}, {g, st8, r}) ||
+        !outputs_apart({r}, {}, {{X_dev, n.bytes}, {R_dev, n.bytes}, g, st8}))
+        return XCONV_EINVAL;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    XC_LAUNCH(K_RMS, st, launch_rms_fwd(desc, X_dev, R_dev, gamma_dev, Y_dev, H_dev, rstd_dev, drop, st));
+    return XCONV_OK;
+}
+
+xconv_status xconv_rmsnorm_fwd_8bit(const xconv_norm_desc *desc, int q_type, const void *X_dev, const void *R_dev, const void *gamma_dev, void *Q_dev,
+                                    float *scale_dev, void *H_dev, void *stream)
+{
+    const xconv_status s = check_rms(desc);
+    if (s != XCONV_OK) return s;
+    if (q_type != XCONV_E4M3 && q_type != XCONV_INT8) return XCONV_EINVAL;
+    if (desc->outer == 0) return XCONV_OK;
+    if (!X_dev || !Q_dev || !scale_dev) return XCONV_EINVAL;
+    const NormSizes n = norm_sizes(desc);
+    for (const void *p : {X_dev, R_dev, (const void *)H_dev})
+        if (!aligned_to(p, n.e)) return XCONV_EINVAL;
+    if (!aligned_to(gamma_dev, n.w) || !aligned_to(scale_dev, 4)) return XCONV_EINVAL;
+    const Span g{gamma_dev, n.params}, x{X_dev, n.bytes}, r{R_dev, n.bytes}, q{Q_dev, n.bytes / n.e}, sc{scale_dev, n.pos};
+    if (!outputs_apart({{H_dev, n.bytes}}, {x, r}, {g}) || !outputs_apart({q, sc, {H_dev, n.bytes}}, {}, {g}) || !outputs_apart({q, sc}, {}, {x, r})) return XCONV_EINVAL;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    XC_LAUNCH(K_RMS, st, launch_rms_fwd8(desc, q_type == XCONV_INT8, X_dev, R_dev, gamma_dev, Q_dev, scale_dev, H_dev, st));
+    return XCONV_OK;
+}
+
+xconv_status xconv_rmsnorm_bwd(const xconv_norm_desc *desc, const void *dY_dev, const void *H_dev, const float *rstd_dev, const void *gamma_dev,
+                               const void *dH_dev, void *dX_dev, void *dR_dev, void *dgamma_dev, void *ws_dev, size_t ws_bytes, const xconv_drop *drop,
+                               void *stream)
+{
+    const xconv_status s = check_rms(desc);
+    if (s != XCONV_OK) return s;
+    if (drop && !drop_ok(drop)) return XCONV_EINVAL;
+    if (!dgamma_dev && ((!dX_dev && !dR_dev) || desc->outer == 0)) return XCONV_OK;
+    const NormSizes n = norm_sizes(desc);
+    for (const void *p : {dY_dev, H_dev, dH_dev, (const void *)dX_dev, (const void *)dR_dev})
+        if (!aligned_to(p, n.e)) return XCONV_EINVAL;
+    if (!aligned_to(gamma_dev, n.w) || !aligned_to(dgamma_dev, n.w) || !aligned_to(rstd_dev, 4) || !aligned_to(ws_dev, 4)) return XCONV_EINVAL;
+    if (desc->outer > 0) {
+        if (!dY_dev || !H_dev || !rstd_dev || (dgamma_dev && !ws_dev)) return XCONV_EINVAL;
+        if (dgamma_dev && ws_bytes < rms_ws_bytes(desc)) return XCONV_EWORKSPACE;
+    }
+    const Span g{gamma_dev, n.params}, dg{dgamma_dev, n.params}, st8{drop ? drop->step_dev : nullptr, 8}, r{rstd_dev, n.pos}, ws{dgamma_dev ? ws_dev : nullptr, desc->outer > 0 ? rms_ws_bytes(desc) : 0};
+    const Span dy{dY_dev, n.bytes}, h{H_dev, n.bytes}, dh{dH_dev, n.bytes}, dx{dX_dev, n.bytes}, dr{dR_dev, n.bytes};
+    if (!outputs_apart({dx, dr}, {dy, h, dh}, {g, dg, st8, r, ws}) || !outputs_apart({dg, ws}, {}, {dy, h, dh, g, st8, r})) return XCONV_EINVAL;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    XC_LAUNCH(K_RMS, st, launch_rms_bwd(desc, dY_dev, H_dev, rstd_dev, gamma_dev, dH_dev, dX_dev, dR_dev, dgamma_dev, static_cast<float *>(ws_dev), drop, st));
+    return XCONV_OK;
+}
+
+namespace {
+xconv_status check_embed(const xconv_embed_desc *d, bool backward)
+{
+    if (!d || d->n < 0 || d->rows < 1 || d->C < 1 || d->dtype < XCONV_F32 || d->dtype > XCONV_F16 || !std::isfinite(d->scale)) return XCONV_EINVAL;
+    if (d->padding_idx < -1 || d->padding_idx >= d->rows) return XCONV_EINVAL;
+    if (d->n > (1LL << 27) || d->rows > (backward ? 1LL << 22 : 0x7fffffffLL) || d->C > (1 << 24)) return XCONV_EUNSUPPORTED;
+    return XCONV_OK;
+}
+}  // namespace
+
+size_t xconv_embed_workspace_bytes(const xconv_embed_desc *desc)
+{
+    return check_embed(desc, true) == XCONV_OK && desc->n > 0 ? embed_ws_bytes(desc) : 0;
+}
+
+xconv_status xconv_embed_fwd(const xconv_embed_desc *desc, const void *idx_dev, const void *W_dev, void *Y_dev, void *stream)
+{
+    const xconv_status s = check_embed(desc, false);
+    if (s != XCONV_OK) return s;
+    if (desc->n == 0) return XCONV_OK;
+    const size_t e = elem_bytes(desc->dtype), i = desc->index64 ? 8 : 4;
+    if (!idx_dev || !W_dev || !Y_dev || !aligned_to(idx_dev, i) || !aligned_to(W_dev, e) || !aligned_to(Y_dev, e)) return XCONV_EINVAL;
+    if (!outputs_apart({{Y_dev, (size_t)desc->n * desc->C * e}}, {}, {{idx_dev, (size_t)desc->n * i}, {W_dev, (size_t)desc->rows * desc->C * e}})) return XCONV_EINVAL;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    XC_LAUNCH(K_EMBED, st, launch_embed_fwd(desc, idx_dev, W_dev, Y_dev, st));
+    return XCONV_OK;
+}
+
+xconv_status xconv_embed_bwd(const xconv_embed_desc *desc, const void *idx_dev, const void *dY_dev, void *dW_dev, int dw_dtype, void *ws_dev,
+                             size_t ws_bytes, void *stream)
+{
+    const xconv_status s = check_embed(desc, true);
+    if (s != XCONV_OK) return s;
+    if (dw_dtype != XCONV_F32 && dw_dtype != desc->dtype) return XCONV_EINVAL;
+    const size_t e = elem_bytes(desc->dtype), i = desc->index64 ? 8 : 4, w = elem_bytes(dw_dtype);
+    if (!dW_dev || !aligned_to(dW_dev, w)) return XCONV_EINVAL;
+    if (desc->n > 0) {
+        if (!idx_dev || !dY_dev || !ws_dev || !aligned_to(idx_dev, i) || !aligned_to(dY_dev, e) || !aligned_to(ws_dev, 256)) return XCONV_EINVAL;
+        const size_t need = embed_ws_bytes(desc);
+        if (ws_bytes < need) return XCONV_EWORKSPACE;
+        if (!outputs_apart({{dW_dev, (size_t)desc->rows * desc->C * w}, {ws_dev, need}}, {}, {{idx_dev, (size_t)desc->n * i}, {dY_dev, (size_t)desc->n * desc->C * e}}))
+            return XCONV_EINVAL;
+    }
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    XC_LAUNCH(K_EMBED, st, launch_embed_bwd(desc, idx_dev, dY_dev, dW_dev, dw_dtype, ws_dev, st));
+    return XCONV_OK;
+}
+
 // ---- orthogonalised weight updates ------------------------------------------------------
 namespace {
 // pointers: also those of the matrices
@@ -1522,6 +1713,9 @@ const char *xconv_prof_kernel_name(int id)
     case K_PIXEL_FWD: return "pixel_fwd_kernel";
     case K_NORM: return "norm_kernel";
     case K_ORTH: return "orth_kernel";
+    case K_DROP: return "dropout_kernel";
+    case K_RMS: return "rms_kernel";
+    case K_EMBED: return "embed_kernel";
     case K_RELU: return "relu_sign_kernel";
     default: return "unknown";
     }

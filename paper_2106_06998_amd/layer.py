@@ -259,12 +259,14 @@ class XConv3d(torch.nn.Conv3d):
         return super().extra_repr() + ", r=%d, probe=%s" % (self.r, self.probe)
 
 
-def convert_net(model, r=16, probe="rademacher", mode="channel", min_in_channels=None, relu=False, engine="library"):
+def convert_net(model, r=16, probe="rademacher", mode="channel", min_in_channels=None, relu=False, engine="library", dropout=False):
     """Replaces, in place, every torch.nn.Conv2d (and, in mode "channel", torch.nn.Conv3d) of `model` that the layer supports (dilation 1,
     groups 1, zero padding, and at least `min_in_channels` input channels; default: more than r in
     mode "channel", where fewer channels than probing vectors save nothing) by an XConv2d that
     shares its parameters.  relu=True also replaces every torch.nn.ReLU by a SignReLU, which keeps one bit per
-    element instead of its output.  Returns the model and the number of convolutions replaced."""
+    element instead of its output; dropout=True every torch.nn.Dropout by an XDropout (dropout.py), which keeps a seed
+    instead of its mask.  Returns the model and the number of convolutions replaced."""
+    from .dropout import XDropout
     if min_in_channels is None:
         min_in_channels = r + 1 if mode == "channel" else 1
     n = 0
@@ -272,6 +274,9 @@ def convert_net(model, r=16, probe="rademacher", mode="channel", min_in_channels
         for name, child in list(parent.named_children()):
             if relu and type(child) is torch.nn.ReLU:
                 setattr(parent, name, SignReLU())
+                continue
+            if dropout and type(child) is torch.nn.Dropout:
+                setattr(parent, name, XDropout(child.p).train(child.training))
                 continue
             if type(child) is torch.nn.Conv3d and mode == "channel":
                 kD, pd = child.kernel_size[0], child.padding[0] if not isinstance(child.padding, str) else -1
