@@ -33,28 +33,36 @@ __device__ inline long long index_at(const void *idx, int wide, long long i)
 }
 
 // G lanes a place; an index outside the table gives a row of NaN
-template <int DT, int G>
+template <int DT, int G, int R>
 __global__ __launch_bounds__(kThreads) void embed_lookup_kernel(LookupArgs a)
 {
     typedef typename NormElem<DT>::t elem_t;
     constexpr int V = NormElem<DT>::V;
     const int lane = threadIdx.x % G, nv = (a.C + V - 1) / V, exact = a.C < V;
-    for (long long i = (long long)blockIdx.x * (kThreads / G) + threadIdx.x / G; i < a.n; i += (long long)gridDim.x * (kThreads / G)) {
-        const long long t = index_at(a.idx, a.wide, i);
-        const bool there = t >= 0 && t < a.rows;
-        const elem_t *w = static_cast<const elem_t *>(a.w) + (size_t)(there ? t : 0) * a.C;
-        elem_t *y = static_cast<elem_t *>(a.y) + (size_t)i * a.C;
+    constexpr int RP = kThreads / G;     // places of a workgroup, R times
+    for (long long i0 = (long long)blockIdx.x * (RP * R) + threadIdx.x / G; i0 < a.n; i0 += (long long)gridDim.x * (RP * R)) {
+        long long t[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) t[r] = i0 + r * RP < a.n ? index_at(a.idx, a.wide, i0 + r * RP) : -1;
         for (int v = blockIdx.y * G + lane; v < nv; v += gridDim.y * G) {
             const Part p = part_of<V>(v, a.C, exact);
-            float x[V];
-            unpack<DT>(there ? load_part<DT>(w, p) : uint4{0, 0, 0, 0}, x);
+            uint4 raw[R];
 #pragma unroll
-            for (int k = 0; k < V; ++k) {
-                x[k] = there ? x[k] * a.scale : __builtin_nanf("");
-                // (an fp32 product that is then rounded, in every type; left alone, products become fp16 numbers in one instruction)
-                if constexpr (DT == XCONV_F16) asm("" : "+v"(x[k]));
+            for (int r = 0; r < R; ++r)
+                raw[r] = t[r] >= 0 && t[r] < a.rows ? load_part<DT>(static_cast<const elem_t *>(a.w) + (size_t)t[r] * a.C, p) : uint4{0, 0, 0, 0};
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                if (i0 + r * RP >= a.n) break;
+                float x[V];
+                unpack<DT>(raw[r], x);
+#pragma unroll
+                for (int k = 0; k < V; ++k) {
+                    x[k] = t[r] >= 0 && t[r] < a.rows ? x[k] * a.scale : __builtin_nanf("");
+                    // (an fp32 product that is then rounded, in every type; left alone, products become fp16 numbers in one instruction)
+                    if constexpr (DT == XCONV_F16) asm("" : "+v"(x[k]));
+                }
+                store_part<DT>(static_cast<elem_t *>(a.y) + (size_t)(i0 + r * RP) * a.C, pack<DT>(x), p);
             }
-            store_part<DT>(y, pack<DT>(x), p);
         }
     }
 }
@@ -340,10 +348,11 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(SumArgs a)
 }
 
 // the runs that cross chunks, a workgroup each: 64 lanes along 256 columns, the waves share the chunks
+constexpr int kJoinWaves = 4;
 template <int WT>
-__global__ __launch_bounds__(kSortThreads) void embed_join_kernel(SumArgs a)
+__global__ __launch_bounds__(kJoinWaves * 64) void embed_join_kernel(SumArgs a)
 {
-    __shared__ float4 red[kSortWaves][64];
+    __shared__ float4 red[kJoinWaves][64];
     const int chunk = blockIdx.x, total = *a.total;
     const long long end = ((long long)chunk + 1) * a.chunk;
     if (end >= total) return;
@@ -356,8 +365,8 @@ __global__ __launch_bounds__(kSortThreads) void embed_join_kernel(SumArgs a)
     const float *part = a.part + (size_t)chunk * 2 * a.pitch;
     float4 s{0.f, 0.f, 0.f, 0.f};
     if (c < a.C) {
-#pragma unroll 8
-        for (int k = wave; k < n; k += kSortWaves) {
+#pragma unroll 16
+        for (int k = wave; k < n; k += kJoinWaves) {
             const float4 q = *reinterpret_cast<const float4 *>(part + ((size_t)k * 2 + (k == 0 ? 1 : 0)) * a.pitch + c);
             s.x += q.x; s.y += q.y; s.z += q.z; s.w += q.w;
         }
@@ -365,7 +374,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_join_kernel(SumArgs a)
     red[wave][lane] = s;
     __syncthreads();
     if (wave != 0 || c >= a.C) return;
-    for (int w = 1; w < min(n, kSortWaves); ++w) {
+    for (int w = 1; w < min(n, kJoinWaves); ++w) {
         const float4 q = red[w][lane];
         s.x += q.x; s.y += q.y; s.z += q.z; s.w += q.w;
     }
@@ -382,7 +391,7 @@ __global__ __launch_bounds__(kThreads) void embed_zero_kernel(uint8_t *p, size_t
 }
 
 // ---- launches ------------------------------------------------------------------------------------------------------
-constexpr int kShortList = 1 << 16;
+constexpr int kShortList = 1 << 14;
 
 struct EmbedPlan {
     int nb, shift, keys;
@@ -409,7 +418,7 @@ EmbedPlan embed_plan(const xconv_embed_desc *d)
     p.tiles = ceil_div(nv, p.G);
     // a few thousand waves where there is work for them; chunks long enough that few runs cross them
     p.chunk = 8;
-    while (p.chunk < 64 && d->n / p.chunk * p.tiles * p.G / 64 > 4096) p.chunk *= 2;
+    while (p.chunk < 256 && d->n / p.chunk * p.tiles * p.G / 64 > 2048) p.chunk *= 2;
     p.chunks = (int)((d->n + p.chunk - 1) / p.chunk);
     p.pitch = round_up(d->C, 4);
     size_t at = 0;
@@ -445,14 +454,17 @@ template <int DT, int WT> hipError_t go_sum(const SumArgs &a, const EmbedPlan &p
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.chunks < 2) return e;
-    hipLaunchKernelGGL(embed_join_kernel<WT>, dim3((unsigned)(p.chunks - 1), (unsigned)ceil_div(a.C, 256)), dim3(kSortThreads), 0, st, s);
+    hipLaunchKernelGGL(embed_join_kernel<WT>, dim3((unsigned)(p.chunks - 1), (unsigned)ceil_div(a.C, 256)), dim3(kJoinWaves * 64), 0, st, s);
     return hipGetLastError();
 }
 
 template <int DT, int G> void go_lookup(const LookupArgs &a, int tiles, hipStream_t st)
 {
-    const long long blocks = std::min<long long>((a.n + kThreads / G - 1) / (kThreads / G), 1 << 20);
-    hipLaunchKernelGGL((embed_lookup_kernel<DT, G>), dim3((unsigned)blocks, (unsigned)tiles), dim3(kThreads), 0, st, a);
+    // four places a group where that leaves enough workgroups
+    constexpr int RP = kThreads / G;
+    const long long one = (a.n + RP - 1) / RP, four = (a.n + 4 * RP - 1) / (4 * RP);
+    if (four * tiles >= 2048) hipLaunchKernelGGL((embed_lookup_kernel<DT, G, 4>), dim3((unsigned)std::min<long long>(four, 1 << 20), (unsigned)tiles), dim3(kThreads), 0, st, a);
+    else hipLaunchKernelGGL((embed_lookup_kernel<DT, G, 1>), dim3((unsigned)std::min<long long>(one, 1 << 20), (unsigned)tiles), dim3(kThreads), 0, st, a);
 }
 template <int DT> hipError_t launch_lookup_dt(const LookupArgs &a, hipStream_t st)
 {

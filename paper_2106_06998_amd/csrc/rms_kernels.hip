@@ -27,10 +27,29 @@ struct RmsArgs : NormGeom {
     int w32, int8, fours;         // gamma in fp32; q is int8; dropout's places are multiples of 4
 };
 
-template <int DT, int V> __device__ inline void load_gamma(const RmsArgs &a, const Part &p, float (&g)[V])
+// SHORT: vectors may be shorter than V (rows shorter than a vector, and rows that are read again)
+template <int DT, bool SHORT> __device__ inline uint4 get_part(const typename NormElem<DT>::t *run, const Part &p)
 {
-    if (DT == XCONV_F32 || a.w32) load_params<XCONV_F32, V>(a.gamma, p, 1.f, g);
-    else load_params<DT, V>(a.gamma, p, 1.f, g);
+    if constexpr (SHORT) return load_part<DT>(run, p);
+    else return load_loose<DT>(run + p.at);
+}
+template <int DT, bool SHORT> __device__ inline void put_part(typename NormElem<DT>::t *run, const uint4 &v, const Part &p)
+{
+    if constexpr (SHORT) store_part<DT>(run, v, p);
+    else store_loose<DT>(run + p.at, v);
+}
+// gamma's address anew: its values are loaded where they are used, not kept for the rows to come
+__device__ inline const void *gamma_of(const RmsArgs &a)
+{
+    const void *p = a.gamma;
+    asm volatile("" : "+s"(p));
+    return p;
+}
+template <int DT, int V, bool SHORT> __device__ inline void load_gamma(const RmsArgs &a, const void *gamma, Part p, float (&g)[V])
+{
+    if constexpr (!SHORT) p.hi = V;
+    if (DT == XCONV_F32 || a.w32) load_params<XCONV_F32, V>(gamma, p, 1.f, g);
+    else load_params<DT, V>(gamma, p, 1.f, g);
 }
 template <int DT> __device__ inline float load_gamma1(const RmsArgs &a, int c)
 {
@@ -57,12 +76,12 @@ __device__ inline uint32_t four8(float a, float b, float c, float d, int int8)
 }
 template <int V> struct __attribute__((packed, aligned(1))) Loose8 { uint32_t w[V / 4]; };
 // V values y times inv from p.at on of the run
-template <int V> __device__ inline void store8(uint8_t *run, const Part &p, const float (&y)[V], float inv, int int8)
+template <int V, bool SHORT> __device__ inline void store8(uint8_t *run, const Part &p, const float (&y)[V], float inv, int int8)
 {
     Loose8<V> o;
 #pragma unroll
     for (int j = 0; j < V / 4; ++j) o.w[j] = four8(y[4 * j] * inv, y[4 * j + 1] * inv, y[4 * j + 2] * inv, y[4 * j + 3] * inv, int8);
-    if (p.hi == V) {
+    if (!SHORT || p.hi == V) {
         *reinterpret_cast<Loose8<V> *>(run + p.at) = o;
     } else {
 #pragma unroll
@@ -72,7 +91,7 @@ template <int V> __device__ inline void store8(uint8_t *run, const Part &p, cons
 }
 
 // largest of R values over a group of G lanes, as group_sum
-template <int G, int R> __device__ inline void group_max(uint32_t (&s)[R], float *red, int &turn)
+template <int G, int R, int T> __device__ inline void group_max(uint32_t (&s)[R], float *red, int &turn)
 {
 #pragma unroll
     for (int o = (G < 64 ? G : 64) / 2; o >= 1; o >>= 1)
@@ -80,12 +99,13 @@ template <int G, int R> __device__ inline void group_max(uint32_t (&s)[R], float
         for (int r = 0; r < R; ++r) s[r] = max(s[r], (uint32_t)__shfl_xor((int)s[r], o));
     if constexpr (G > 64) {
         constexpr int W = G / 64;
-        uint32_t *slot = reinterpret_cast<uint32_t *>(red) + turn * W * R;
+        uint32_t *slot = reinterpret_cast<uint32_t *>(red) + turn * (T / 64) * R;
         turn ^= 1;
         if ((threadIdx.x & 63) == 0)
 #pragma unroll
             for (int r = 0; r < R; ++r) slot[(threadIdx.x >> 6) * R + r] = s[r];
         __syncthreads();
+        if constexpr (T > G) slot += threadIdx.x / G * W * R;
 #pragma unroll
         for (int i = 0; i < W; ++i)
 #pragma unroll
@@ -94,13 +114,17 @@ template <int G, int R> __device__ inline void group_max(uint32_t (&s)[R], float
 }
 
 // ---- rows ----------------------------------------------------------------------------------------------------------
+// waves a SIMD that the forward pass leaves registers for
+template <int K, int R> constexpr int rms_waves = K * R >= 4 ? 4 : K * R == 3 ? 5 : 6;
+
 // G lanes a row, K vectors a lane, R rows at once; K == 0: a row is read again for every pass over it.  OUT8: q and scale instead of y
 template <int DT, bool OUT8, int G, int K, int R>
-__global__ __launch_bounds__(row_threads<G>) void rms_rows_fwd_kernel(RmsArgs a)
+__global__ __launch_bounds__(row_threads<G>, (rms_waves<K, R>)) void rms_rows_fwd_kernel(RmsArgs a)
 {
     typedef typename NormElem<DT>::t elem_t;
-    constexpr int V = NormElem<DT>::V, RP = row_threads<G> / G, KR = K > 0 ? K : 1;
-    __shared__ float red[G > 64 ? 2 * R * (G / 64) : 1];
+    constexpr int V = NormElem<DT>::V, T = row_threads<G>, RP = T / G, KR = K > 0 ? K : 1;
+    constexpr bool SHORT = G == 4 || K == 0;
+    __shared__ float red[G > 64 ? 2 * R * (T / 64) : 1];
     int turn = 0;
     const int lane = threadIdx.x % G, grp = threadIdx.x / G;
     const int nv = (a.C + V - 1) / V;
@@ -115,6 +139,7 @@ __global__ __launch_bounds__(row_threads<G>) void rms_rows_fwd_kernel(RmsArgs a)
         }
     };
     for (long long r0 = (long long)blockIdx.x * (RP * R); r0 < a.outer; r0 += (long long)gridDim.x * (RP * R)) {   // (the same count for all threads)
+        const void *gamma = gamma_of(a);
         float h[R][KR][V];
         uint4 rx[R][KR], rr[R][KR];
         size_t at[R];
@@ -125,7 +150,7 @@ __global__ __launch_bounds__(row_threads<G>) void rms_rows_fwd_kernel(RmsArgs a)
             on[r] = row < a.outer;
             at[r] = (size_t)(on[r] ? row : 0) * a.C;
         }
-        auto get = [&](const elem_t *x, int r, int v, const Part &p) { return v < nv ? load_part<DT>(x + at[r], p) : uint4{0, 0, 0, 0}; };
+        auto get = [&](const elem_t *x, int r, int v, const Part &p) { return v < nv ? get_part<DT, SHORT>(x + at[r], p) : uint4{0, 0, 0, 0}; };
         auto make = [&](int r, int k, int v, const Part &p) {
             unpack<DT>(rx[r][k], h[r][k]);
             if (a.drop.q16) drop_values<V>(a.drop, key, at[r] + p.at, a.fours, h[r][k]);
@@ -138,13 +163,13 @@ __global__ __launch_bounds__(row_threads<G>) void rms_rows_fwd_kernel(RmsArgs a)
         };
         if constexpr (K > 0) {
             rounds([&](int k, int v) {
-                const Part p = part_of<V>(v, a.C, a.exact);
+                const Part p = part_of<V>(v, a.C, SHORT ? a.exact : 0);
 #pragma unroll
                 for (int r = 0; r < R; ++r) rx[r][k] = get(X, r, v, p);
             });
             if (RES)
                 rounds([&](int k, int v) {
-                    const Part p = part_of<V>(v, a.C, a.exact);
+                    const Part p = part_of<V>(v, a.C, SHORT ? a.exact : 0);
 #pragma unroll
                     for (int r = 0; r < R; ++r) rr[r][k] = get(RES, r, v, p);
                 });
@@ -161,7 +186,7 @@ __global__ __launch_bounds__(row_threads<G>) void rms_rows_fwd_kernel(RmsArgs a)
 #pragma unroll
         for (int r = 0; r < R; ++r) s[r] = 0.f;
         rounds([&](int k, int v) {
-            const Part p = part_of<V>(v, a.C, a.exact);
+            const Part p = part_of<V>(v, a.C, SHORT ? a.exact : 0);
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 if constexpr (K > 0) make(r, k, v, p);
@@ -175,52 +200,77 @@ __global__ __launch_bounds__(row_threads<G>) void rms_rows_fwd_kernel(RmsArgs a)
                 }
             }
         });
-        group_sum<G>(s, red, turn);
-        float rstd[R], inv[R];
+        group_sum<G, R, T>(s, red, turn);
+        float rstd[R];
 #pragma unroll
         for (int r = 0; r < R; ++r) rstd[r] = rstd_of(s[r], a);
+        auto keep_h = [&](int r, int k, const Part &p) {
+            if (a.h && on[r]) put_part<DT, SHORT>(static_cast<elem_t *>(a.h) + at[r], pack<DT>(h[r][k]), p);
+        };
+        // h becomes y
+        auto scale = [&](int r, int k, const float (&g)[V]) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) h[r][k][i] = h[r][k][i] * rstd[r] * g[i];
+        };
         if constexpr (OUT8) {
             uint32_t m[R];
 #pragma unroll
             for (int r = 0; r < R; ++r) m[r] = __float_as_uint(kLeast8);
             rounds([&](int k, int v) {
                 if (v >= nv) return;
-                const Part p = part_of<V>(v, a.C, a.exact);
+                const Part p = part_of<V>(v, a.C, SHORT ? a.exact : 0);
                 float g[V];
-                load_gamma<DT, V>(a, p, g);
+                load_gamma<DT, V, SHORT>(a, gamma, p, g);
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
                     value(r, k, v, p);
+                    if (K > 0) keep_h(r, k, p);
+                    scale(r, k, g);
+                    // (values past a short vector are zeros, or NaN where the position has one)
 #pragma unroll
-                    for (int i = 0; i < V; ++i)
-                        if (i < p.hi) m[r] = max(m[r], magnitude(h[r][k][i] * rstd[r] * g[i]));
+                    for (int i = 0; i < V; ++i) m[r] = max(m[r], magnitude(h[r][k][i]));
                 }
             });
-            group_max<G>(m, red, turn);
+            group_max<G, R, T>(m, red, turn);
+            float inv[R];
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 const float most = __uint_as_float(m[r]);
                 inv[r] = a.top / most;
                 if (lane == 0 && on[r]) a.scale[r0 + r * RP + grp] = most / a.top;
             }
+            rounds([&](int k, int v) {
+                if (v >= nv) return;
+                const Part p = part_of<V>(v, a.C, SHORT ? a.exact : 0);
+                float g[V];
+                if (K == 0) load_gamma<DT, V, SHORT>(a, gamma, p, g);
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    if (!on[r]) continue;
+                    if constexpr (K == 0) {
+                        value(r, k, v, p);
+                        keep_h(r, k, p);
+                        scale(r, k, g);
+                    }
+                    store8<V, SHORT>(static_cast<uint8_t *>(a.y) + at[r], p, h[r][k], inv[r], a.int8);
+                }
+            });
+        } else {
+            rounds([&](int k, int v) {
+                if (v >= nv) return;
+                const Part p = part_of<V>(v, a.C, SHORT ? a.exact : 0);
+                float g[V];
+                load_gamma<DT, V, SHORT>(a, gamma, p, g);
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    if (!on[r]) continue;
+                    value(r, k, v, p);
+                    keep_h(r, k, p);
+                    scale(r, k, g);
+                    put_part<DT, SHORT>(static_cast<elem_t *>(a.y) + at[r], pack<DT>(h[r][k]), p);
+                }
+            });
         }
-        rounds([&](int k, int v) {
-            if (v >= nv) return;
-            const Part p = part_of<V>(v, a.C, a.exact);
-            float g[V];
-            load_gamma<DT, V>(a, p, g);
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                if (!on[r]) continue;
-                value(r, k, v, p);
-                if (a.h) store_part<DT>(static_cast<elem_t *>(a.h) + at[r], pack<DT>(h[r][k]), p);
-                float t[V];
-#pragma unroll
-                for (int i = 0; i < V; ++i) t[i] = h[r][k][i] * rstd[r] * g[i];
-                if constexpr (OUT8) store8<V>(static_cast<uint8_t *>(a.y) + at[r], p, t, inv[r], a.int8);
-                else store_part<DT>(static_cast<elem_t *>(a.y) + at[r], pack<DT>(t), p);
-            }
-        });
         if (!OUT8 && lane == 0 && a.rstd) {
 #pragma unroll
             for (int r = 0; r < R; ++r)
@@ -232,10 +282,11 @@ __global__ __launch_bounds__(row_threads<G>) void rms_rows_fwd_kernel(RmsArgs a)
 // T threads, so T / G rows at once; every lane adds up dgamma of its own columns.  K == 0: one row a workgroup at a time, dgamma in the
 // workgroup's own slots of `part`.
 template <int DT, int G, int K, int R, int T>
-__global__ __launch_bounds__(T) void rms_rows_bwd_kernel(RmsArgs a)
+__global__ __launch_bounds__(T, 4) void rms_rows_bwd_kernel(RmsArgs a)
 {
     typedef typename NormElem<DT>::t elem_t;
     constexpr int V = NormElem<DT>::V, RP = T / G, KR = K > 0 ? K : 1;
+    constexpr bool SHORT = G == 4 || K == 0;
     __shared__ float red[G > 64 ? 2 * R * (T / 64) : 1];
     int turn = 0;
     const int lane = threadIdx.x % G, grp = threadIdx.x / G;
@@ -259,6 +310,7 @@ __global__ __launch_bounds__(T) void rms_rows_bwd_kernel(RmsArgs a)
         for (int i = 0; i < V; ++i) ag[k][i] = 0.f;
     bool first = true;
     for (long long r0 = (long long)blockIdx.x * (RP * R); r0 < a.outer; r0 += (long long)gridDim.x * (RP * R), first = false) {   // (the same count for all threads)
+        const void *gamma = K > 2 ? gamma_of(a) : a.gamma;
         uint4 rx[R][KR], rd[R][KR], rh[R][KR];
         float rstd[R], c[R];
         size_t at[R];
@@ -271,10 +323,10 @@ __global__ __launch_bounds__(T) void rms_rows_bwd_kernel(RmsArgs a)
             rstd[r] = on[r] ? a.rstd[row] : 0.f;
             c[r] = 0.f;
         }
-        auto get = [&](const elem_t *x, int r, int v, const Part &p) { return on[r] && v < nv ? load_part<DT>(x + at[r], p) : uint4{0, 0, 0, 0}; };
+        auto get = [&](const elem_t *x, int r, int v, const Part &p) { return on[r] && v < nv ? get_part<DT, SHORT>(x + at[r], p) : uint4{0, 0, 0, 0}; };
         if constexpr (K > 0) {
             rounds([&](int k, int v) {
-                const Part p = part_of<V>(v, a.C, a.exact);
+                const Part p = part_of<V>(v, a.C, SHORT ? a.exact : 0);
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
                     rx[r][k] = get(H, r, v, p);
@@ -283,16 +335,16 @@ __global__ __launch_bounds__(T) void rms_rows_bwd_kernel(RmsArgs a)
             });
             if (DH)
                 rounds([&](int k, int v) {
-                    const Part p = part_of<V>(v, a.C, a.exact);
+                    const Part p = part_of<V>(v, a.C, SHORT ? a.exact : 0);
 #pragma unroll
                     for (int r = 0; r < R; ++r) rh[r][k] = get(DH, r, v, p);
                 });
         }
         rounds([&](int k, int v) {
-            const Part p = part_of<V>(v, a.C, a.exact);
+            const Part p = part_of<V>(v, a.C, SHORT ? a.exact : 0);
             float g[V];
             if (v < nv) {
-                load_gamma<DT, V>(a, p, g);
+                load_gamma<DT, V, SHORT>(a, gamma, p, g);
             } else {
 #pragma unroll
                 for (int i = 0; i < V; ++i) g[i] = 0.f;
@@ -325,15 +377,19 @@ __global__ __launch_bounds__(T) void rms_rows_bwd_kernel(RmsArgs a)
                         *q = (first ? 0.f : *q) + t;
                     }
                 }
+                if constexpr (K > 0) {
+                    keep_packed(rx[r][k], ag[k]);
+                    keep_packed(rd[r][k], ag[k]);
+                }
             }
         });
         if (!DR && !DX) continue;
         group_sum<G, R, T>(c, red, turn);
         rounds([&](int k, int v) {
             if (v >= nv) return;
-            const Part p = part_of<V>(v, a.C, a.exact);
+            const Part p = part_of<V>(v, a.C, SHORT ? a.exact : 0);
             float g[V];
-            load_gamma<DT, V>(a, p, g);
+            load_gamma<DT, V, SHORT>(a, gamma, p, g);
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 if (!on[r]) continue;
@@ -353,10 +409,10 @@ __global__ __launch_bounds__(T) void rms_rows_bwd_kernel(RmsArgs a)
 #pragma unroll
                     for (int i = 0; i < V; ++i) x[i] += d[i];
                 }
-                if (DR) store_part<DT>(DR + at[r], pack<DT>(x), p);
+                if (DR) put_part<DT, SHORT>(DR + at[r], pack<DT>(x), p);
                 if (DX) {
                     if (a.drop.q16) drop_values<V>(a.drop, key, at[r] + p.at, a.fours, x);
-                    store_part<DT>(DX + at[r], pack<DT>(x), p);
+                    put_part<DT, SHORT>(DX + at[r], pack<DT>(x), p);
                 }
             }
         });
@@ -375,7 +431,7 @@ __global__ __launch_bounds__(T) void rms_rows_bwd_kernel(RmsArgs a)
             for (int q = threadIdx.x; q < W; q += T) {
                 const int v = k * G + q / V;
                 if (v >= nv) continue;
-                const Part p = part_of<V>(v, a.C, a.exact);
+                const Part p = part_of<V>(v, a.C, SHORT ? a.exact : 0);
                 if (!own(p, q % V)) continue;
                 float s = 0.f;
                 for (int r = 0; r < RP; ++r) s += cols[r * W + q];
@@ -385,7 +441,7 @@ __global__ __launch_bounds__(T) void rms_rows_bwd_kernel(RmsArgs a)
     } else {
         rounds([&](int k, int v) {
             if (v >= nv) return;
-            const Part p = part_of<V>(v, a.C, a.exact);
+            const Part p = part_of<V>(v, a.C, SHORT ? a.exact : 0);
 #pragma unroll
             for (int i = 0; i < V; ++i)
                 if (own(p, i)) part[p.at + i] = ag[k][i];
@@ -414,6 +470,14 @@ template <int N, int NW> __device__ inline void column_max(uint32_t (&s)[N], flo
         for (int i = 0; i < N; ++i) s[i] = max(s[i], m[(w * kNormTX + tx) * N + i]);
 }
 
+// The thread's first channel anew: offsets of its channels are computed where they are used, not kept (for every channel two registers,
+// which the loop over the tiles would carry along)
+__device__ inline int again(int ty)
+{
+    asm volatile("" : "+v"(ty));
+    return ty;
+}
+
 // WHOLE: planes of at least one vector whose last vectors overlap, the ordinary case
 template <int DT, bool OUT8, int NW, int K, bool WHOLE>
 __global__ __launch_bounds__(NW * 64) void rms_planes_fwd_kernel(RmsArgs a)
@@ -426,8 +490,9 @@ __global__ __launch_bounds__(NW * 64) void rms_planes_fwd_kernel(RmsArgs a)
     const TileRun run = tiles_of(a);
     auto rounds = [&](auto &&body) {
         if constexpr (K > 0) {
+            const int t = again(ty);
 #pragma unroll
-            for (int k = 0; k < K; ++k) body(k, ty + k * TY);
+            for (int k = 0; k < K; ++k) body(k, t + k * TY);
         } else {
             for (int c = ty; c < a.C; c += TY) body(0, c);
         }
@@ -449,9 +514,19 @@ __global__ __launch_bounds__(NW * 64) void rms_planes_fwd_kernel(RmsArgs a)
             }
         };
         if constexpr (K > 0) {
-            rounds([&](int k, int c) { rx[k] = plane_get<DT, WHOLE>(a, x, at, c); });
-            if (res) rounds([&](int k, int c) { rr[k] = plane_get<DT, WHOLE>(a, res, at, c); });
-            rounds(make);
+            // four channels at a time: more would be under way than registers hold
+#pragma unroll
+            for (int k0 = 0; k0 < K; k0 += 4) {
+                const int t = again(ty);
+#pragma unroll
+                for (int k = k0; k < min(K, k0 + 4); ++k) rx[k] = plane_get<DT, WHOLE>(a, x, at, t + k * TY);
+                if (res)
+#pragma unroll
+                    for (int k = k0; k < min(K, k0 + 4); ++k) rr[k] = plane_get<DT, WHOLE>(a, res, at, t + k * TY);
+#pragma unroll
+                for (int k = k0; k < min(K, k0 + 4); ++k) make(k, t + k * TY);
+                if constexpr (K > 4) __builtin_amdgcn_sched_barrier(0);
+            }
         }
         auto value = [&](int k, int c) {
             if constexpr (K == 0) {
@@ -469,9 +544,18 @@ __global__ __launch_bounds__(NW * 64) void rms_planes_fwd_kernel(RmsArgs a)
             for (int i = 0; i < V; ++i) s[i] += h[k][i] * h[k][i];      // (channels that do not exist are zeros)
         });
         column_sum<V, NW>(s, red);
-        float rstd[V], inv[V];
+        float rstd[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) rstd[i] = rstd_of(s[i], a);
+        auto keep_h = [&](int k, int c) {
+            if (a.h && at.on) plane_put<DT, WHOLE>(a, static_cast<elem_t *>(a.h) + at.base, at, c, pack<DT>(h[k]));
+        };
+        // h becomes y
+        auto scale = [&](int k, int c) {
+            const float g = load_gamma1<DT>(a, c);
+#pragma unroll
+            for (int i = 0; i < V; ++i) h[k][i] = h[k][i] * rstd[i] * g;
+        };
         if constexpr (OUT8) {
             uint32_t m[V];
 #pragma unroll
@@ -479,35 +563,41 @@ __global__ __launch_bounds__(NW * 64) void rms_planes_fwd_kernel(RmsArgs a)
             rounds([&](int k, int c) {
                 if (c >= a.C) return;
                 value(k, c);
-                const float g = load_gamma1<DT>(a, c);
+                if (K > 0) keep_h(k, c);
+                scale(k, c);
 #pragma unroll
-                for (int i = 0; i < V; ++i) m[i] = max(m[i], magnitude(h[k][i] * rstd[i] * g));
+                for (int i = 0; i < V; ++i) m[i] = max(m[i], magnitude(h[k][i]));
             });
             column_max<V, NW>(m, red);
+            if (!at.on) continue;
+            float inv[V];
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const float most = __uint_as_float(m[i]);
                 inv[i] = a.top / most;
-                if (ty == 0 && at.on && own(at.p, i)) a.scale[at.pos + i] = most / a.top;
+                if (ty == 0 && own(at.p, i)) a.scale[at.pos + i] = most / a.top;
             }
+            rounds([&](int k, int c) {
+                if (c >= a.C) return;
+                if constexpr (K == 0) {
+                    value(k, c);
+                    keep_h(k, c);
+                    scale(k, c);
+                }
+#pragma unroll
+                for (int i = 0; i < V; ++i) h[k][i] *= inv[i];
+                store8<V, !WHOLE>(static_cast<uint8_t *>(a.y) + at.base + (size_t)c * a.inner, at.p, h[k], 1.f, a.int8);
+            });
+        } else {
+            if (!at.on) continue;
+            rounds([&](int k, int c) {
+                if (c >= a.C) return;
+                value(k, c);
+                keep_h(k, c);
+                scale(k, c);
+                plane_put<DT, WHOLE>(a, static_cast<elem_t *>(a.y) + at.base, at, c, pack<DT>(h[k]));
+            });
         }
-        if (!at.on) continue;
-        rounds([&](int k, int c) {
-            if (c >= a.C) return;
-            value(k, c);
-            const float g = load_gamma1<DT>(a, c);
-            if (a.h) plane_put<DT, WHOLE>(a, static_cast<elem_t *>(a.h) + at.base, at, c, pack<DT>(h[k]));
-            float t[V];
-            if constexpr (OUT8) {
-#pragma unroll
-                for (int i = 0; i < V; ++i) t[i] = h[k][i] * rstd[i] * g * inv[i];
-                store8<V>(static_cast<uint8_t *>(a.y) + at.base + (size_t)c * a.inner, at.p, t, 1.f, a.int8);
-            } else {
-#pragma unroll
-                for (int i = 0; i < V; ++i) t[i] = h[k][i] * rstd[i] * g;
-                plane_put<DT, WHOLE>(a, static_cast<elem_t *>(a.y) + at.base, at, c, pack<DT>(t));
-            }
-        });
         if (!OUT8 && ty == 0 && a.rstd) {
 #pragma unroll
             for (int i = 0; i < V; ++i)
@@ -531,12 +621,13 @@ __global__ __launch_bounds__(NW * 64, 4) void rms_planes_bwd_kernel(RmsArgs a)
 #pragma unroll
     for (int k = 0; k < KR; ++k) {
         ag[k] = 0.f;
-        gk[k] = load_gamma1<DT>(a, min(ty + k * TY, a.C - 1));
+        gk[k] = K <= 4 ? load_gamma1<DT>(a, min(ty + k * TY, a.C - 1)) : 0.f;
     }
     auto rounds = [&](auto &&body) {
         if constexpr (K > 0) {
+            const int t = again(ty);
 #pragma unroll
-            for (int k = 0; k < K; ++k) body(k, ty + k * TY);
+            for (int k = 0; k < K; ++k) body(k, t + k * TY);
         } else {
             for (int c = ty; c < a.C; c += TY) body(0, c);
         }
@@ -547,24 +638,33 @@ __global__ __launch_bounds__(NW * 64, 4) void rms_planes_bwd_kernel(RmsArgs a)
         for (int c = threadIdx.x; c < a.C; c += NW * 64) part[c] = 0.f;
     for (long long tile = run.from; tile < run.to; tile += run.step, first = false) {
         const PlaneAt at = plane_at<V>(a, tile);
-        uint4 rx[KR], rd[KR];
+        uint4 rx[KR], rd[KR], rh[KR];
         auto get = [&](int k, int c) {
             rx[k] = plane_get<DT, WHOLE>(a, H + at.base, at, c);
             rd[k] = plane_get<DT, WHOLE>(a, DY + at.base, at, c);
         };
-        if constexpr (K > 0) rounds(get);
-        float rstd[V], c1[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            rstd[i] = at.on && i < at.p.hi ? a.rstd[at.pos + i] : 0.f;
-            c1[i] = 0.f;
+        auto get_h = [&](int k, int c) { rh[k] = plane_get<DT, WHOLE>(a, DH + at.base, at, c); };
+        if constexpr (K > 0) {
+            rounds(get);
+            if (DH && K <= 4) rounds(get_h);
         }
+        float rstd[V], c1[V];
+        if constexpr (WHOLE) {
+            load_params<XCONV_F32, V>(a.rstd, Part{0, 0, V}, 0.f, rstd, at.pos);
+#pragma unroll
+            for (int i = 0; i < V; ++i) rstd[i] = at.on ? rstd[i] : 0.f;
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i) rstd[i] = at.on && i < at.p.hi ? a.rstd[at.pos + i] : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < V; ++i) c1[i] = 0.f;
         rounds([&](int k, int c) {
             if constexpr (K == 0) get(0, c);
             float x[V], d[V], sg = 0.f;
             unpack<DT>(rx[k], x);
             unpack<DT>(rd[k], d);
-            const float g = K > 0 ? gk[k] : load_gamma1<DT>(a, c);
+            const float g = K > 0 && K <= 4 ? gk[k] : load_gamma1<DT>(a, min(c, a.C - 1));
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const float t = d[i] * (x[i] * rstd[i]);
@@ -573,6 +673,9 @@ __global__ __launch_bounds__(NW * 64, 4) void rms_planes_bwd_kernel(RmsArgs a)
             }
             if constexpr (K > 0) {
                 ag[k] += sg;
+                keep_packed(rx[k], c1);
+                keep_packed(rd[k], c1);
+                if constexpr (K > 4) __builtin_amdgcn_sched_barrier(0);
             } else if (part) {
 #pragma unroll
                 for (int o = kNormTX / 2; o >= 1; o >>= 1) sg += __shfl_xor(sg, o);
@@ -587,16 +690,15 @@ __global__ __launch_bounds__(NW * 64, 4) void rms_planes_bwd_kernel(RmsArgs a)
         rounds([&](int k, int c) {
             if (c >= a.C) return;
             if constexpr (K == 0) get(0, c);
-            uint4 rh{0, 0, 0, 0};
-            if (DH) rh = plane_get<DT, WHOLE>(a, DH + at.base, at, c);
+            if (DH && (K == 0 || K > 4)) get_h(k, c);
             float x[V], d[V];
             unpack<DT>(rx[k], x);
             unpack<DT>(rd[k], d);
-            const float g = K > 0 ? gk[k] : load_gamma1<DT>(a, c);
+            const float g = K > 0 && K <= 4 ? gk[k] : load_gamma1<DT>(a, min(c, a.C - 1));
 #pragma unroll
             for (int i = 0; i < V; ++i) x[i] = rstd[i] * (d[i] * g - (x[i] * rstd[i]) * c1[i]);
             if (DH) {
-                unpack<DT>(rh, d);
+                unpack<DT>(rh[k], d);
 #pragma unroll
                 for (int i = 0; i < V; ++i) x[i] += d[i];
             }
@@ -605,6 +707,7 @@ __global__ __launch_bounds__(NW * 64, 4) void rms_planes_bwd_kernel(RmsArgs a)
                 if (a.drop.q16) drop_values<V>(a.drop, key, at.base + (size_t)c * a.inner + at.p.at, a.fours, x);
                 plane_put<DT, WHOLE>(a, DX + at.base, at, c, pack<DT>(x));
             }
+            __builtin_amdgcn_sched_barrier(0);      // (rounds beside each other would hold more values than there are registers)
         });
     }
     if (K == 0 || !part) return;
@@ -646,7 +749,8 @@ struct RmsShape {
     int V;
 };
 
-// The smallest group that holds a row with one vector a lane; past a wave, two and four vectors a lane, then groups of several waves
+// The smallest group that holds a row with one vector a lane; past a wave, two to four vectors a lane, then groups of several waves with
+// three or four (groups of 256 with two or four left up to half of the lanes without work)
 RmsShape rms_rows_shape(int dtype, int C, bool backward)
 {
     const int V = dtype == XCONV_F32 ? 4 : 8, nv = ceil_div(C, V);
@@ -654,10 +758,15 @@ RmsShape rms_rows_shape(int dtype, int C, bool backward)
     for (int G : {4, 8, 16, 32, 64})
         if (nv <= G) return {G, 1, 2, T, 0, V};
     if (nv <= 128) return {64, 2, 1, T, 0, V};
-    if (nv <= 256) return {64, 4, 1, T, 0, V};
-    for (int G : {256, 1024})
-        for (int K : {2, 4})
-            if (nv <= K * G) return {G, K, 1, backward ? std::max(512, G) : G, 0, V};
+    if (backward) {
+        for (int G : {128, 256, 512, 1024})
+            if (nv <= 2 * G) return {G, 2, 1, std::max(T, G), 0, V};
+        if (nv <= 3 * 1024) return {1024, 3, 1, 1024, 0, V};
+    } else {
+        for (int G : {64, 128, 256, 512, 1024})
+            for (int K : {3, 4})
+                if (nv <= K * G) return {G, K, 1, std::max(T, G), 0, V};
+    }
     return {1024, 0, 1, 1024, 0, V};
 }
 // 8 channels a wave and round: enough waves for 4 rounds, 8 with 16 waves
@@ -686,16 +795,18 @@ int rms_blocks(const xconv_norm_desc *d, const RmsShape &s, bool bwd)
 
 enum RmsPass { kRmsForward, kRmsForward8, kRmsBackward };
 
+// (of the shapes with several vectors a lane, the forward passes take three and four past a wave, the backward pass two, and three of 1024 lanes)
 template <int DT, int G, int K, int R> hipError_t go_rms_rows(const RmsArgs &a, RmsPass pass, int blocks, hipStream_t st)
 {
     const dim3 grid((unsigned)blocks);
-    if (pass == kRmsForward) {
-        hipLaunchKernelGGL((rms_rows_fwd_kernel<DT, false, G, K, R>), grid, dim3(row_threads<G>), 0, st, a);
-    } else if (pass == kRmsForward8) {
-        hipLaunchKernelGGL((rms_rows_fwd_kernel<DT, true, G, K, R>), grid, dim3(row_threads<G>), 0, st, a);
+    if (pass != kRmsBackward) {
+        if constexpr (K != 2 || G == 64) {
+            if (pass == kRmsForward) hipLaunchKernelGGL((rms_rows_fwd_kernel<DT, false, G, K, R>), grid, dim3(row_threads<G>), 0, st, a);
+            else hipLaunchKernelGGL((rms_rows_fwd_kernel<DT, true, G, K, R>), grid, dim3(row_threads<G>), 0, st, a);
+        }
     } else {
         constexpr int T = G > 512 ? G : 512;
-        hipLaunchKernelGGL((rms_rows_bwd_kernel<DT, G, K, R, T>), grid, dim3(T), 0, st, a);
+        if constexpr (K < 3 || (G == 1024 && K == 3)) hipLaunchKernelGGL((rms_rows_bwd_kernel<DT, G, K, R, T>), grid, dim3(T), 0, st, a);
     }
     return hipGetLastError();
 }
@@ -708,10 +819,19 @@ template <int DT> hipError_t go_rms_rows_shape(const RmsArgs &a, const RmsShape 
     case 32 * 8 + 1: return go_rms_rows<DT, 32, 1, 2>(a, pass, blocks, st);
     case 64 * 8 + 1: return go_rms_rows<DT, 64, 1, 2>(a, pass, blocks, st);
     case 64 * 8 + 2: return go_rms_rows<DT, 64, 2, 1>(a, pass, blocks, st);
+    case 64 * 8 + 3: return go_rms_rows<DT, 64, 3, 1>(a, pass, blocks, st);
     case 64 * 8 + 4: return go_rms_rows<DT, 64, 4, 1>(a, pass, blocks, st);
+    case 128 * 8 + 2: return go_rms_rows<DT, 128, 2, 1>(a, pass, blocks, st);
+    case 128 * 8 + 3: return go_rms_rows<DT, 128, 3, 1>(a, pass, blocks, st);
+    case 128 * 8 + 4: return go_rms_rows<DT, 128, 4, 1>(a, pass, blocks, st);
     case 256 * 8 + 2: return go_rms_rows<DT, 256, 2, 1>(a, pass, blocks, st);
+    case 256 * 8 + 3: return go_rms_rows<DT, 256, 3, 1>(a, pass, blocks, st);
     case 256 * 8 + 4: return go_rms_rows<DT, 256, 4, 1>(a, pass, blocks, st);
+    case 512 * 8 + 2: return go_rms_rows<DT, 512, 2, 1>(a, pass, blocks, st);
+    case 512 * 8 + 3: return go_rms_rows<DT, 512, 3, 1>(a, pass, blocks, st);
+    case 512 * 8 + 4: return go_rms_rows<DT, 512, 4, 1>(a, pass, blocks, st);
     case 1024 * 8 + 2: return go_rms_rows<DT, 1024, 2, 1>(a, pass, blocks, st);
+    case 1024 * 8 + 3: return go_rms_rows<DT, 1024, 3, 1>(a, pass, blocks, st);
     case 1024 * 8 + 4: return go_rms_rows<DT, 1024, 4, 1>(a, pass, blocks, st);
     default: return go_rms_rows<DT, 1024, 0, 1>(a, pass, blocks, st);
     }
