@@ -25,6 +25,7 @@ struct RmsArgs : NormGeom {
     DropArgs drop;
     float top;
     int w32, int8, fours;         // gamma in fp32; q is int8; dropout's places are multiples of 4
+    int over;                     // an output lies over an input
 };
 
 // SHORT: vectors may be shorter than V (rows shorter than a vector, and rows that are read again)
@@ -75,12 +76,12 @@ __device__ inline uint32_t four8(float a, float b, float c, float d, int int8)
     return (uint32_t)w;
 }
 template <int V> struct __attribute__((packed, aligned(1))) Loose8 { uint32_t w[V / 4]; };
-// V values y times inv from p.at on of the run
-template <int V, bool SHORT> __device__ inline void store8(uint8_t *run, const Part &p, const float (&y)[V], float inv, int int8)
+// V values from p.at on of the run
+template <int V, bool SHORT> __device__ inline void store8(uint8_t *run, const Part &p, const float (&y)[V], int int8)
 {
     Loose8<V> o;
 #pragma unroll
-    for (int j = 0; j < V / 4; ++j) o.w[j] = four8(y[4 * j] * inv, y[4 * j + 1] * inv, y[4 * j + 2] * inv, y[4 * j + 3] * inv, int8);
+    for (int j = 0; j < V / 4; ++j) o.w[j] = four8(y[4 * j], y[4 * j + 1], y[4 * j + 2], y[4 * j + 3], int8);
     if (!SHORT || p.hi == V) {
         *reinterpret_cast<Loose8<V> *>(run + p.at) = o;
     } else {
@@ -90,50 +91,66 @@ template <int V, bool SHORT> __device__ inline void store8(uint8_t *run, const P
     }
 }
 
-// largest of R values over a group of G lanes, as group_sum
-template <int G, int R, int T> __device__ inline void group_max(uint32_t (&s)[R], float *red, int &turn)
+// Largest of R values over a group of G lanes; for groups of several waves in two parts with a barrier of the caller's (group_sum's) between
+// them: what a wave has, into `slot` of `red`, and what all have
+template <int G, int R, int T> __device__ inline void group_max(uint32_t (&s)[R], uint32_t *red, int slot)
 {
 #pragma unroll
     for (int o = (G < 64 ? G : 64) / 2; o >= 1; o >>= 1)
 #pragma unroll
         for (int r = 0; r < R; ++r) s[r] = max(s[r], (uint32_t)__shfl_xor((int)s[r], o));
+    if (G > 64 && (threadIdx.x & 63) == 0)
+#pragma unroll
+        for (int r = 0; r < R; ++r) red[(slot * (T / 64) + (threadIdx.x >> 6)) * R + r] = s[r];
+}
+template <int G, int R, int T> __device__ inline void group_max_join(uint32_t (&s)[R], const uint32_t *red, int slot)
+{
     if constexpr (G > 64) {
-        constexpr int W = G / 64;
-        uint32_t *slot = reinterpret_cast<uint32_t *>(red) + turn * (T / 64) * R;
-        turn ^= 1;
-        if ((threadIdx.x & 63) == 0)
+        const uint32_t *q = red + (slot * (T / 64) + (T > G ? threadIdx.x / G * (G / 64) : 0)) * R;
 #pragma unroll
-            for (int r = 0; r < R; ++r) slot[(threadIdx.x >> 6) * R + r] = s[r];
-        __syncthreads();
-        if constexpr (T > G) slot += threadIdx.x / G * W * R;
+        for (int i = 0; i < G / 64; ++i)
 #pragma unroll
-        for (int i = 0; i < W; ++i)
-#pragma unroll
-            for (int r = 0; r < R; ++r) s[r] = max(s[r], slot[i * R + r]);
+            for (int r = 0; r < R; ++r) s[r] = max(s[r], q[i * R + r]);
     }
 }
 
-// ---- rows ----------------------------------------------------------------------------------------------------------
-// waves a SIMD that the forward pass leaves registers for
-template <int K, int R> constexpr int rms_waves = K * R >= 4 ? 4 : K * R == 3 ? 5 : 6;
+// A thread's first vector (channel) anew: offsets and masks of its vectors are computed where they are used, not kept: the loop over the rows
+// (tiles) would carry them along, for every vector more registers than its values take
+__device__ inline int again(int first)
+{
+    asm volatile("" : "+v"(first));
+    return first;
+}
 
-// G lanes a row, K vectors a lane, R rows at once; K == 0: a row is read again for every pass over it.  OUT8: q and scale instead of y
+// ---- rows ----------------------------------------------------------------------------------------------------------
+// Threads of a workgroup.  Groups of a wave and less wait for nobody; those of several waves are a workgroup of their own in the forward
+// pass, so that a barrier holds up one row.
+template <int G> constexpr int rms_fwd_threads = G > 64 ? G : 256;
+// waves a SIMD that the forward pass leaves registers for: 8 registers a vector and lane hold h
+template <int G, int K, int R> constexpr int rms_fwd_waves = K > 4 && G < 1024 ? 3 : K * R >= 4 ? 4 : K * R == 3 ? 5 : 6;
+
+// G lanes a row, K vectors a lane, R rows at once; K == 0: a row is read again for its second pass.  OUT8: q and scale instead of y.
+// One reduction a row: in the 8-bit form h becomes h gamma as soon as its square is in the sum, and the largest |h gamma| goes along (two
+// reductions: 8192 x 8192 fp16 66 us, 47 so).
 template <int DT, bool OUT8, int G, int K, int R>
-__global__ __launch_bounds__(row_threads<G>, (rms_waves<K, R>)) void rms_rows_fwd_kernel(RmsArgs a)
+__global__ __launch_bounds__(rms_fwd_threads<G>, (rms_fwd_waves<G, K, R>)) void rms_rows_fwd_kernel(RmsArgs a)
 {
     typedef typename NormElem<DT>::t elem_t;
-    constexpr int V = NormElem<DT>::V, T = row_threads<G>, RP = T / G, KR = K > 0 ? K : 1;
-    constexpr bool SHORT = G == 4 || K == 0;
+    constexpr int V = NormElem<DT>::V, T = rms_fwd_threads<G>, RP = T / G, KR = K > 0 ? K : 1;
+    constexpr bool SHORT = G == 4 || K == 0, EARLY = OUT8;
     __shared__ float red[G > 64 ? 2 * R * (T / 64) : 1];
+    __shared__ uint32_t redm[G > 64 && OUT8 ? 2 * R * (T / 64) : 1];
     int turn = 0;
     const int lane = threadIdx.x % G, grp = threadIdx.x / G;
     const int nv = (a.C + V - 1) / V;
     const elem_t *X = static_cast<const elem_t *>(a.x), *RES = static_cast<const elem_t *>(a.res);
-    const uint64_t key = a.drop.q16 ? drop_key(a.drop) : 0;
+    const bool drops = !OUT8 && a.drop.q16;
+    const uint64_t key = drops ? drop_key(a.drop) : 0;
     auto rounds = [&](auto &&body) {
         if constexpr (K > 0) {
+            const int l = again(lane);
 #pragma unroll
-            for (int k = 0; k < K; ++k) body(k, lane + k * G);
+            for (int k = 0; k < K; ++k) body(k, l + k * G);
         } else {
             for (int v = lane; v < nv; v += G) body(0, v);
         }
@@ -151,9 +168,9 @@ __global__ __launch_bounds__(row_threads<G>, (rms_waves<K, R>)) void rms_rows_fw
             at[r] = (size_t)(on[r] ? row : 0) * a.C;
         }
         auto get = [&](const elem_t *x, int r, int v, const Part &p) { return v < nv ? get_part<DT, SHORT>(x + at[r], p) : uint4{0, 0, 0, 0}; };
-        auto make = [&](int r, int k, int v, const Part &p) {
+        auto make = [&](int r, int k, const Part &p) {
             unpack<DT>(rx[r][k], h[r][k]);
-            if (a.drop.q16) drop_values<V>(a.drop, key, at[r] + p.at, a.fours, h[r][k]);
+            if (drops) drop_values<V>(a.drop, key, at[r] + p.at, a.fours, h[r][k]);
             if (RES) {
                 float t[V];
                 unpack<DT>(rr[r][k], t);
@@ -173,24 +190,34 @@ __global__ __launch_bounds__(row_threads<G>, (rms_waves<K, R>)) void rms_rows_fw
 #pragma unroll
                     for (int r = 0; r < R; ++r) rr[r][k] = get(RES, r, v, p);
                 });
-        }
-        // h of a round: in registers, or read again
-        auto value = [&](int r, int k, int v, const Part &p) {
-            if constexpr (K == 0) {
-                rx[r][0] = get(X, r, v, p);
-                if (RES) rr[r][0] = get(RES, r, v, p);
-                make(r, 0, v, p);
+            // h may lie over what another lane's overlapping vector still reads
+            if (a.over) {
+                __builtin_amdgcn_s_waitcnt(0);
+                if constexpr (G > 64) __syncthreads();
             }
-        };
+        }
         float s[R];
+        uint32_t m[R];
 #pragma unroll
-        for (int r = 0; r < R; ++r) s[r] = 0.f;
+        for (int r = 0; r < R; ++r) s[r] = 0.f, m[r] = 0;
         rounds([&](int k, int v) {
             const Part p = part_of<V>(v, a.C, SHORT ? a.exact : 0);
+            float g[V];
+            if (EARLY) {
+                if (v < nv) {
+                    load_gamma<DT, V, SHORT>(a, gamma, p, g);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) g[i] = 0.f;
+                }
+            }
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                if constexpr (K > 0) make(r, k, v, p);
-                else value(r, k, v, p);
+                if constexpr (K == 0) {
+                    rx[r][0] = get(X, r, v, p);
+                    if (RES) rr[r][0] = get(RES, r, v, p);
+                }
+                make(r, k, p);
                 if (K > 0 ? !masked<G>(a, k, nv) : !a.ragged) {
 #pragma unroll
                     for (int i = 0; i < V; ++i) s[r] += h[r][k][i] * h[r][k][i];       // (zeros past the last vector)
@@ -198,79 +225,53 @@ __global__ __launch_bounds__(row_threads<G>, (rms_waves<K, R>)) void rms_rows_fw
 #pragma unroll
                     for (int i = 0; i < V; ++i) s[r] += v < nv && own(p, i) ? h[r][k][i] * h[r][k][i] : 0.f;
                 }
-            }
-        });
-        group_sum<G, R, T>(s, red, turn);
-        float rstd[R];
+                if (K > 0 && a.h && on[r] && v < nv) put_part<DT, SHORT>(static_cast<elem_t *>(a.h) + at[r], pack<DT>(h[r][k]), p);
+                if constexpr (EARLY) {
 #pragma unroll
-        for (int r = 0; r < R; ++r) rstd[r] = rstd_of(s[r], a);
-        auto keep_h = [&](int r, int k, const Part &p) {
-            if (a.h && on[r]) put_part<DT, SHORT>(static_cast<elem_t *>(a.h) + at[r], pack<DT>(h[r][k]), p);
-        };
-        // h becomes y
-        auto scale = [&](int r, int k, const float (&g)[V]) {
-#pragma unroll
-            for (int i = 0; i < V; ++i) h[r][k][i] = h[r][k][i] * rstd[r] * g[i];
-        };
-        if constexpr (OUT8) {
-            uint32_t m[R];
-#pragma unroll
-            for (int r = 0; r < R; ++r) m[r] = __float_as_uint(kLeast8);
-            rounds([&](int k, int v) {
-                if (v >= nv) return;
-                const Part p = part_of<V>(v, a.C, SHORT ? a.exact : 0);
-                float g[V];
-                load_gamma<DT, V, SHORT>(a, gamma, p, g);
-#pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    value(r, k, v, p);
-                    if (K > 0) keep_h(r, k, p);
-                    scale(r, k, g);
-                    // (values past a short vector are zeros, or NaN where the position has one)
+                    for (int i = 0; i < V; ++i) h[r][k][i] *= g[i];
 #pragma unroll
                     for (int i = 0; i < V; ++i) m[r] = max(m[r], magnitude(h[r][k][i]));
                 }
-            });
-            group_max<G, R, T>(m, red, turn);
-            float inv[R];
+            }
+        });
+        const int slot = turn;
+        if constexpr (OUT8) group_max<G, R, T>(m, redm, slot);
+        group_sum<G, R, T>(s, red, turn);
+        float rstd[R], f[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            rstd[r] = rstd_of(s[r], a);
+            f[r] = rstd[r];
+        }
+        if constexpr (OUT8) {
+            group_max_join<G, R, T>(m, redm, slot);
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                const float most = __uint_as_float(m[r]);
-                inv[r] = a.top / most;
+                const float most = __uint_as_float(max(magnitude(__uint_as_float(m[r]) * rstd[r]), __float_as_uint(kLeast8)));
+                f[r] = rstd[r] * (a.top / most);
                 if (lane == 0 && on[r]) a.scale[r0 + r * RP + grp] = most / a.top;
             }
-            rounds([&](int k, int v) {
-                if (v >= nv) return;
-                const Part p = part_of<V>(v, a.C, SHORT ? a.exact : 0);
-                float g[V];
-                if (K == 0) load_gamma<DT, V, SHORT>(a, gamma, p, g);
-#pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    if (!on[r]) continue;
-                    if constexpr (K == 0) {
-                        value(r, k, v, p);
-                        keep_h(r, k, p);
-                        scale(r, k, g);
-                    }
-                    store8<V, SHORT>(static_cast<uint8_t *>(a.y) + at[r], p, h[r][k], inv[r], a.int8);
-                }
-            });
-        } else {
-            rounds([&](int k, int v) {
-                if (v >= nv) return;
-                const Part p = part_of<V>(v, a.C, SHORT ? a.exact : 0);
-                float g[V];
-                load_gamma<DT, V, SHORT>(a, gamma, p, g);
-#pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    if (!on[r]) continue;
-                    value(r, k, v, p);
-                    keep_h(r, k, p);
-                    scale(r, k, g);
-                    put_part<DT, SHORT>(static_cast<elem_t *>(a.y) + at[r], pack<DT>(h[r][k]), p);
-                }
-            });
         }
+        rounds([&](int k, int v) {
+            if (v >= nv) return;
+            const Part p = part_of<V>(v, a.C, SHORT ? a.exact : 0);
+            float g[V];
+            if (K == 0 || !EARLY) load_gamma<DT, V, SHORT>(a, gamma, p, g);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                if (!on[r]) continue;
+                if constexpr (K == 0) {
+                    rx[r][0] = get(X, r, v, p);
+                    if (RES) rr[r][0] = get(RES, r, v, p);
+                    make(r, 0, p);
+                    if (a.h) put_part<DT, SHORT>(static_cast<elem_t *>(a.h) + at[r], pack<DT>(h[r][k]), p);
+                }
+#pragma unroll
+                for (int i = 0; i < V; ++i) h[r][k][i] *= K == 0 || !EARLY ? f[r] * g[i] : f[r];
+                if constexpr (OUT8) store8<V, SHORT>(static_cast<uint8_t *>(a.y) + at[r], p, h[r][k], a.int8);
+                else put_part<DT, SHORT>(static_cast<elem_t *>(a.y) + at[r], pack<DT>(h[r][k]), p);
+            }
+        });
         if (!OUT8 && lane == 0 && a.rstd) {
 #pragma unroll
             for (int r = 0; r < R; ++r)
@@ -297,8 +298,9 @@ __global__ __launch_bounds__(T, 4) void rms_rows_bwd_kernel(RmsArgs a)
     float *part = a.part ? a.part + (size_t)blockIdx.x * a.C : nullptr;
     auto rounds = [&](auto &&body) {
         if constexpr (K > 0) {
+            const int l = again(lane);
 #pragma unroll
-            for (int k = 0; k < K; ++k) body(k, lane + k * G);
+            for (int k = 0; k < K; ++k) body(k, l + k * G);
         } else {
             for (int v = lane; v < nv; v += G) body(0, v);
         }
@@ -309,9 +311,41 @@ __global__ __launch_bounds__(T, 4) void rms_rows_bwd_kernel(RmsArgs a)
 #pragma unroll
         for (int i = 0; i < V; ++i) ag[k][i] = 0.f;
     bool first = true;
-    for (long long r0 = (long long)blockIdx.x * (RP * R); r0 < a.outer; r0 += (long long)gridDim.x * (RP * R), first = false) {   // (the same count for all threads)
-        const void *gamma = K > 2 ? gamma_of(a) : a.gamma;
-        uint4 rx[R][KR], rd[R][KR], rh[R][KR];
+    // what is read of R rows
+    struct Rows {
+        uint4 x[R][KR], d[R][KR], h[R][KR];
+        float rstd[R];
+    };
+    auto fetch = [&](long long r0, Rows &f) {
+        size_t at[R];
+        bool on[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const long long row = r0 + r * RP + grp;
+            on[r] = row < a.outer;
+            at[r] = (size_t)(on[r] ? row : 0) * a.C;
+            f.rstd[r] = on[r] ? a.rstd[row] : 0.f;
+        }
+        rounds([&](int k, int v) {
+            const Part p = part_of<V>(v, a.C, SHORT ? a.exact : 0);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                f.x[r][k] = on[r] && v < nv ? get_part<DT, SHORT>(H + at[r], p) : uint4{0, 0, 0, 0};
+                f.d[r][k] = on[r] && v < nv ? get_part<DT, SHORT>(DY + at[r], p) : uint4{0, 0, 0, 0};
+            }
+        });
+        if (DH)
+            rounds([&](int k, int v) {
+                const Part p = part_of<V>(v, a.C, SHORT ? a.exact : 0);
+#pragma unroll
+                for (int r = 0; r < R; ++r) f.h[r][k] = on[r] && v < nv ? get_part<DT, SHORT>(DH + at[r], p) : uint4{0, 0, 0, 0};
+            });
+    };
+    const long long step = (long long)gridDim.x * (RP * R);
+    Rows next;
+    if constexpr (K > 0) fetch((long long)blockIdx.x * (RP * R), next);
+    for (long long r0 = (long long)blockIdx.x * (RP * R); r0 < a.outer; r0 += step, first = false) {   // (the same count for all threads)
+        Rows now;
         float rstd[R], c[R];
         size_t at[R];
         bool on[R];
@@ -320,26 +354,23 @@ __global__ __launch_bounds__(T, 4) void rms_rows_bwd_kernel(RmsArgs a)
             const long long row = r0 + r * RP + grp;
             on[r] = row < a.outer;
             at[r] = (size_t)(on[r] ? row : 0) * a.C;
-            rstd[r] = on[r] ? a.rstd[row] : 0.f;
             c[r] = 0.f;
         }
-        auto get = [&](const elem_t *x, int r, int v, const Part &p) { return on[r] && v < nv ? get_part<DT, SHORT>(x + at[r], p) : uint4{0, 0, 0, 0}; };
         if constexpr (K > 0) {
-            rounds([&](int k, int v) {
-                const Part p = part_of<V>(v, a.C, SHORT ? a.exact : 0);
+            // the rows to come are under way while these are worked on
+            now = next;
+            if (r0 + step < a.outer) fetch(r0 + step, next);
 #pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    rx[r][k] = get(H, r, v, p);
-                    rd[r][k] = get(DY, r, v, p);
-                }
-            });
-            if (DH)
-                rounds([&](int k, int v) {
-                    const Part p = part_of<V>(v, a.C, SHORT ? a.exact : 0);
+            for (int r = 0; r < R; ++r) rstd[r] = now.rstd[r];
+        } else {
 #pragma unroll
-                    for (int r = 0; r < R; ++r) rh[r][k] = get(DH, r, v, p);
-                });
+            for (int r = 0; r < R; ++r) rstd[r] = on[r] ? a.rstd[r0 + r * RP + grp] : 0.f;
         }
+        auto &rx = now.x;
+        auto &rd = now.d;
+        auto &rh = now.h;
+        const void *gamma = a.gamma;
+        auto get = [&](const elem_t *x, int r, int v, const Part &p) { return on[r] && v < nv ? get_part<DT, SHORT>(x + at[r], p) : uint4{0, 0, 0, 0}; };
         rounds([&](int k, int v) {
             const Part p = part_of<V>(v, a.C, SHORT ? a.exact : 0);
             float g[V];
@@ -450,32 +481,24 @@ __global__ __launch_bounds__(T, 4) void rms_rows_bwd_kernel(RmsArgs a)
 }
 
 // ---- planes --------------------------------------------------------------------------------------------------------
-// largest over the threads along the channels of V columns, as column_sum
-template <int N, int NW> __device__ inline void column_max(uint32_t (&s)[N], float *red)
+// largest over the threads along the channels of N columns, along with column_sum's sums: what a wave has in front of it, what all have
+// behind it (its barriers serve both)
+template <int N> __device__ inline void column_max(uint32_t (&s)[N], uint32_t *red)
 {
 #pragma unroll
     for (int o = kNormTX; o < 64; o <<= 1)
 #pragma unroll
         for (int i = 0; i < N; ++i) s[i] = max(s[i], (uint32_t)__shfl_xor((int)s[i], o));
-    const int tx = threadIdx.x % kNormTX;
-    uint32_t *m = reinterpret_cast<uint32_t *>(red);
-    __syncthreads();                     // whoever still reads the last sum
     if ((threadIdx.x & 63) < kNormTX)
 #pragma unroll
-        for (int i = 0; i < N; ++i) m[((threadIdx.x >> 6) * kNormTX + tx) * N + i] = s[i];
-    __syncthreads();
+        for (int i = 0; i < N; ++i) red[((threadIdx.x >> 6) * kNormTX + threadIdx.x % kNormTX) * N + i] = s[i];
+}
+template <int N, int NW> __device__ inline void column_max_join(uint32_t (&s)[N], const uint32_t *red)
+{
 #pragma unroll 2
     for (int w = 0; w < NW; ++w)
 #pragma unroll
-        for (int i = 0; i < N; ++i) s[i] = max(s[i], m[(w * kNormTX + tx) * N + i]);
-}
-
-// The thread's first channel anew: offsets of its channels are computed where they are used, not kept (for every channel two registers,
-// which the loop over the tiles would carry along)
-__device__ inline int again(int ty)
-{
-    asm volatile("" : "+v"(ty));
-    return ty;
+        for (int i = 0; i < N; ++i) s[i] = max(s[i], red[(w * kNormTX + threadIdx.x % kNormTX) * N + i]);
 }
 
 // WHOLE: planes of at least one vector whose last vectors overlap, the ordinary case
@@ -485,8 +508,11 @@ __global__ __launch_bounds__(NW * 64) void rms_planes_fwd_kernel(RmsArgs a)
     typedef typename NormElem<DT>::t elem_t;
     constexpr int V = NormElem<DT>::V, TY = NW * kNormTYW, KR = K > 0 ? K : 1;
     __shared__ float red[NW * kNormTX * V];
+    __shared__ uint32_t redm[OUT8 ? 2 * NW * kNormTX * V : 1];       // (two, taken in turn: no barrier stands behind the reading of one)
+    int turn = 0;
     const int ty = threadIdx.x / kNormTX;
-    const uint64_t key = a.drop.q16 ? drop_key(a.drop) : 0;
+    const bool drops = !OUT8 && a.drop.q16;
+    const uint64_t key = drops ? drop_key(a.drop) : 0;
     const TileRun run = tiles_of(a);
     auto rounds = [&](auto &&body) {
         if constexpr (K > 0) {
@@ -505,7 +531,7 @@ __global__ __launch_bounds__(NW * 64) void rms_planes_fwd_kernel(RmsArgs a)
         uint4 rx[KR], rr[KR];
         auto make = [&](int k, int c) {
             unpack<DT>(rx[k], h[k]);
-            if (a.drop.q16) drop_values<V>(a.drop, key, at.base + (size_t)c * a.inner + at.p.at, a.fours, h[k]);
+            if (drops) drop_values<V>(a.drop, key, at.base + (size_t)c * a.inner + at.p.at, a.fours, h[k]);
             if (res) {
                 float t[V];
                 unpack<DT>(rr[k], t);
@@ -536,68 +562,60 @@ __global__ __launch_bounds__(NW * 64) void rms_planes_fwd_kernel(RmsArgs a)
             }
         };
         float s[V];
+        uint32_t m[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) s[i] = 0.f;
+        for (int i = 0; i < V; ++i) s[i] = 0.f, m[i] = 0;
         rounds([&](int k, int c) {
             value(k, c);
 #pragma unroll
             for (int i = 0; i < V; ++i) s[i] += h[k][i] * h[k][i];      // (channels that do not exist are zeros)
-        });
-        column_sum<V, NW>(s, red);
-        float rstd[V];
+            if (K > 0 && a.h && at.on && c < a.C) plane_put<DT, WHOLE>(a, static_cast<elem_t *>(a.h) + at.base, at, c, pack<DT>(h[k]));
+            if constexpr (K > 0 || OUT8) {
+                const float g = load_gamma1<DT>(a, min(c, a.C - 1));
 #pragma unroll
-        for (int i = 0; i < V; ++i) rstd[i] = rstd_of(s[i], a);
-        auto keep_h = [&](int k, int c) {
-            if (a.h && at.on) plane_put<DT, WHOLE>(a, static_cast<elem_t *>(a.h) + at.base, at, c, pack<DT>(h[k]));
-        };
-        // h becomes y
-        auto scale = [&](int k, int c) {
-            const float g = load_gamma1<DT>(a, c);
-#pragma unroll
-            for (int i = 0; i < V; ++i) h[k][i] = h[k][i] * rstd[i] * g;
-        };
-        if constexpr (OUT8) {
-            uint32_t m[V];
-#pragma unroll
-            for (int i = 0; i < V; ++i) m[i] = __float_as_uint(kLeast8);
-            rounds([&](int k, int c) {
-                if (c >= a.C) return;
-                value(k, c);
-                if (K > 0) keep_h(k, c);
-                scale(k, c);
+                for (int i = 0; i < V; ++i) h[k][i] *= g;
+            }
+            if constexpr (OUT8) {
 #pragma unroll
                 for (int i = 0; i < V; ++i) m[i] = max(m[i], magnitude(h[k][i]));
-            });
-            column_max<V, NW>(m, red);
-            if (!at.on) continue;
-            float inv[V];
+            }
+        });
+        uint32_t *mine = redm + turn * (NW * kNormTX * V);
+        if constexpr (OUT8) {
+            turn ^= 1;
+            column_max<V>(m, mine);
+        }
+        column_sum<V, NW>(s, red);
+        float rstd[V], f[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            rstd[i] = rstd_of(s[i], a);
+            f[i] = rstd[i];
+        }
+        if constexpr (OUT8) {
+            column_max_join<V, NW>(m, mine);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const float most = __uint_as_float(m[i]);
-                inv[i] = a.top / most;
-                if (ty == 0 && own(at.p, i)) a.scale[at.pos + i] = most / a.top;
+                const float most = __uint_as_float(max(magnitude(__uint_as_float(m[i]) * rstd[i]), __float_as_uint(kLeast8)));
+                f[i] = rstd[i] * (a.top / most);
+                if (ty == 0 && at.on && own(at.p, i)) a.scale[at.pos + i] = most / a.top;
             }
-            rounds([&](int k, int c) {
-                if (c >= a.C) return;
-                if constexpr (K == 0) {
-                    value(k, c);
-                    keep_h(k, c);
-                    scale(k, c);
-                }
-#pragma unroll
-                for (int i = 0; i < V; ++i) h[k][i] *= inv[i];
-                store8<V, !WHOLE>(static_cast<uint8_t *>(a.y) + at.base + (size_t)c * a.inner, at.p, h[k], 1.f, a.int8);
-            });
-        } else {
-            if (!at.on) continue;
-            rounds([&](int k, int c) {
-                if (c >= a.C) return;
-                value(k, c);
-                keep_h(k, c);
-                scale(k, c);
-                plane_put<DT, WHOLE>(a, static_cast<elem_t *>(a.y) + at.base, at, c, pack<DT>(h[k]));
-            });
         }
+        if (!at.on) continue;
+        rounds([&](int k, int c) {
+            if (c >= a.C) return;
+            if constexpr (K == 0) {
+                value(k, c);
+                if (a.h) plane_put<DT, WHOLE>(a, static_cast<elem_t *>(a.h) + at.base, at, c, pack<DT>(h[k]));
+                const float g = load_gamma1<DT>(a, c);
+#pragma unroll
+                for (int i = 0; i < V; ++i) h[k][i] *= g;
+            }
+#pragma unroll
+            for (int i = 0; i < V; ++i) h[k][i] *= f[i];
+            if constexpr (OUT8) store8<V, !WHOLE>(static_cast<uint8_t *>(a.y) + at.base + (size_t)c * a.inner, at.p, h[k], a.int8);
+            else plane_put<DT, WHOLE>(a, static_cast<elem_t *>(a.y) + at.base, at, c, pack<DT>(h[k]));
+        });
         if (!OUT8 && ty == 0 && a.rstd) {
 #pragma unroll
             for (int i = 0; i < V; ++i)
@@ -669,7 +687,7 @@ __global__ __launch_bounds__(NW * 64, 4) void rms_planes_bwd_kernel(RmsArgs a)
             for (int i = 0; i < V; ++i) {
                 const float t = d[i] * (x[i] * rstd[i]);
                 c1[i] += t * g;
-                sg += i >= at.p.lo ? t : 0.f;
+                sg += !a.ragged || i >= at.p.lo ? t : 0.f;
             }
             if constexpr (K > 0) {
                 ag[k] += sg;
@@ -729,7 +747,7 @@ template <int WT> __global__ __launch_bounds__(kRmsJoinThreads) void rms_join_ke
     const int c = blockIdx.x * kRmsJoinCols + col;
     float s = 0.f;
     if (c < C) {
-#pragma unroll 8
+#pragma unroll 16
         for (int b = w; b < n; b += RW) s += part[(size_t)b * C + c];
     }
     s += __shfl_xor(s, 32);
@@ -749,23 +767,37 @@ struct RmsShape {
     int V;
 };
 
-// The smallest group that holds a row with one vector a lane; past a wave, two to four vectors a lane, then groups of several waves with
-// three or four (groups of 256 with two or four left up to half of the lanes without work)
-RmsShape rms_rows_shape(int dtype, int C, bool backward)
+// The smallest group that holds a row with one vector a lane; past a wave up to eight vectors a lane, then groups of several waves with
+// five to eight.  A wave to a row waits for no other: 8192 rows of 5000 fp16 in 8 bits take @ us with two waves of five vectors a lane, 40 with
+// four of three; backward @ us, 82 with eight waves of two.
+enum RmsPass { kRmsForward, kRmsForward8, kRmsBackward };
+// the shapes that a pass has: up to eight vectors a lane forward; up to six in 8 bits, whose gamma takes registers beside h; two backward,
+// where every vector takes 32 registers (sums of dgamma, three tensors, those of the rows to come)
+constexpr bool rms_has(RmsPass pass, int G, int K)
 {
+    if (K < 2) return true;
+    if (pass == kRmsBackward) return K == 2;
+    if (G == 64) return K != 8 || pass == kRmsForward;
+    if (pass == kRmsForward) return G < 1024 && (K == 5 || K == 6 || K == 8);
+    return G < 1024 ? K >= 4 && K <= 6 : K == 4;
+}
+
+RmsShape rms_rows_shape(int dtype, int C, RmsPass pass)
+{
+    const bool backward = pass == kRmsBackward;
     const int V = dtype == XCONV_F32 ? 4 : 8, nv = ceil_div(C, V);
-    const int T = backward ? 512 : 256;
+    auto threads = [&](int G) { return backward ? std::max(512, G) : G > 64 ? G : 256; };
     for (int G : {4, 8, 16, 32, 64})
-        if (nv <= G) return {G, 1, 2, T, 0, V};
-    if (nv <= 128) return {64, 2, 1, T, 0, V};
+        if (nv <= G) return {G, 1, 2, threads(G), 0, V};
     if (backward) {
-        for (int G : {128, 256, 512, 1024})
-            if (nv <= 2 * G) return {G, 2, 1, std::max(T, G), 0, V};
-        if (nv <= 3 * 1024) return {1024, 3, 1, 1024, 0, V};
-    } else {
         for (int G : {64, 128, 256, 512, 1024})
-            for (int K : {3, 4})
-                if (nv <= K * G) return {G, K, 1, std::max(T, G), 0, V};
+            if (nv <= 2 * G) return {G, 2, 1, threads(G), 0, V};
+    } else {
+        for (int K : {2, 3, 4})
+            if (nv <= K * 64) return {64, K, 1, threads(64), 0, V};
+        for (int G : {64, 128, 256, 512, 1024})
+            for (int K : {4, 5, 6, 8})
+                if (nv <= K * G && rms_has(pass, G, K)) return {G, K, 1, threads(G), 0, V};
     }
     return {1024, 0, 1, 1024, 0, V};
 }
@@ -780,7 +812,7 @@ RmsShape rms_planes_shape(int dtype, int C)
     return {0, 0, 1, 0, 16, V};
 }
 
-constexpr int kRmsBlocks = 512;            // most workgroups that leave partial sums
+constexpr int kRmsBlocks = 512;            // most workgroups that leave partial sums (planes: twice as many)
 constexpr long long kRmsGrid = 1 << 20;    // most workgroups of the forward pass
 
 int rms_blocks(const xconv_norm_desc *d, const RmsShape &s, bool bwd)
@@ -793,46 +825,49 @@ int rms_blocks(const xconv_norm_desc *d, const RmsShape &s, bool bwd)
     return (int)std::min<long long>((d->outer + rows - 1) / rows, bwd ? kRmsBlocks : kRmsGrid);
 }
 
-enum RmsPass { kRmsForward, kRmsForward8, kRmsBackward };
-
-// (of the shapes with several vectors a lane, the forward passes take three and four past a wave, the backward pass two, and three of 1024 lanes)
 template <int DT, int G, int K, int R> hipError_t go_rms_rows(const RmsArgs &a, RmsPass pass, int blocks, hipStream_t st)
 {
     const dim3 grid((unsigned)blocks);
-    if (pass != kRmsBackward) {
-        if constexpr (K != 2 || G == 64) {
-            if (pass == kRmsForward) hipLaunchKernelGGL((rms_rows_fwd_kernel<DT, false, G, K, R>), grid, dim3(row_threads<G>), 0, st, a);
-            else hipLaunchKernelGGL((rms_rows_fwd_kernel<DT, true, G, K, R>), grid, dim3(row_threads<G>), 0, st, a);
-        }
-    } else {
-        constexpr int T = G > 512 ? G : 512;
-        if constexpr (K < 3 || (G == 1024 && K == 3)) hipLaunchKernelGGL((rms_rows_bwd_kernel<DT, G, K, R, T>), grid, dim3(T), 0, st, a);
-    }
+    constexpr int TF = rms_fwd_threads<G>, TB = G > 512 ? G : 512;
+    if constexpr (rms_has(kRmsForward, G, K))
+        if (pass == kRmsForward) hipLaunchKernelGGL((rms_rows_fwd_kernel<DT, false, G, K, R>), grid, dim3(TF), 0, st, a);
+    if constexpr (rms_has(kRmsForward8, G, K))
+        if (pass == kRmsForward8) hipLaunchKernelGGL((rms_rows_fwd_kernel<DT, true, G, K, R>), grid, dim3(TF), 0, st, a);
+    if constexpr (rms_has(kRmsBackward, G, K))
+        if (pass == kRmsBackward) hipLaunchKernelGGL((rms_rows_bwd_kernel<DT, G, K, R, TB>), grid, dim3(TB), 0, st, a);
     return hipGetLastError();
 }
 template <int DT> hipError_t go_rms_rows_shape(const RmsArgs &a, const RmsShape &s, RmsPass pass, int blocks, hipStream_t st)
 {
-    switch (s.G * 8 + s.K) {
-    case 4 * 8 + 1: return go_rms_rows<DT, 4, 1, 2>(a, pass, blocks, st);
-    case 8 * 8 + 1: return go_rms_rows<DT, 8, 1, 2>(a, pass, blocks, st);
-    case 16 * 8 + 1: return go_rms_rows<DT, 16, 1, 2>(a, pass, blocks, st);
-    case 32 * 8 + 1: return go_rms_rows<DT, 32, 1, 2>(a, pass, blocks, st);
-    case 64 * 8 + 1: return go_rms_rows<DT, 64, 1, 2>(a, pass, blocks, st);
-    case 64 * 8 + 2: return go_rms_rows<DT, 64, 2, 1>(a, pass, blocks, st);
-    case 64 * 8 + 3: return go_rms_rows<DT, 64, 3, 1>(a, pass, blocks, st);
-    case 64 * 8 + 4: return go_rms_rows<DT, 64, 4, 1>(a, pass, blocks, st);
-    case 128 * 8 + 2: return go_rms_rows<DT, 128, 2, 1>(a, pass, blocks, st);
-    case 128 * 8 + 3: return go_rms_rows<DT, 128, 3, 1>(a, pass, blocks, st);
-    case 128 * 8 + 4: return go_rms_rows<DT, 128, 4, 1>(a, pass, blocks, st);
-    case 256 * 8 + 2: return go_rms_rows<DT, 256, 2, 1>(a, pass, blocks, st);
-    case 256 * 8 + 3: return go_rms_rows<DT, 256, 3, 1>(a, pass, blocks, st);
-    case 256 * 8 + 4: return go_rms_rows<DT, 256, 4, 1>(a, pass, blocks, st);
-    case 512 * 8 + 2: return go_rms_rows<DT, 512, 2, 1>(a, pass, blocks, st);
-    case 512 * 8 + 3: return go_rms_rows<DT, 512, 3, 1>(a, pass, blocks, st);
-    case 512 * 8 + 4: return go_rms_rows<DT, 512, 4, 1>(a, pass, blocks, st);
-    case 1024 * 8 + 2: return go_rms_rows<DT, 1024, 2, 1>(a, pass, blocks, st);
-    case 1024 * 8 + 3: return go_rms_rows<DT, 1024, 3, 1>(a, pass, blocks, st);
-    case 1024 * 8 + 4: return go_rms_rows<DT, 1024, 4, 1>(a, pass, blocks, st);
+    switch (s.G * 16 + s.K) {
+    case 4 * 16 + 1: return go_rms_rows<DT, 4, 1, 2>(a, pass, blocks, st);
+    case 8 * 16 + 1: return go_rms_rows<DT, 8, 1, 2>(a, pass, blocks, st);
+    case 16 * 16 + 1: return go_rms_rows<DT, 16, 1, 2>(a, pass, blocks, st);
+    case 32 * 16 + 1: return go_rms_rows<DT, 32, 1, 2>(a, pass, blocks, st);
+    case 64 * 16 + 1: return go_rms_rows<DT, 64, 1, 2>(a, pass, blocks, st);
+    case 64 * 16 + 2: return go_rms_rows<DT, 64, 2, 1>(a, pass, blocks, st);
+    case 64 * 16 + 3: return go_rms_rows<DT, 64, 3, 1>(a, pass, blocks, st);
+    case 64 * 16 + 4: return go_rms_rows<DT, 64, 4, 1>(a, pass, blocks, st);
+    case 64 * 16 + 5: return go_rms_rows<DT, 64, 5, 1>(a, pass, blocks, st);
+    case 64 * 16 + 6: return go_rms_rows<DT, 64, 6, 1>(a, pass, blocks, st);
+    case 64 * 16 + 8: return go_rms_rows<DT, 64, 8, 1>(a, pass, blocks, st);
+    case 128 * 16 + 2: return go_rms_rows<DT, 128, 2, 1>(a, pass, blocks, st);
+    case 128 * 16 + 4: return go_rms_rows<DT, 128, 4, 1>(a, pass, blocks, st);
+    case 128 * 16 + 5: return go_rms_rows<DT, 128, 5, 1>(a, pass, blocks, st);
+    case 128 * 16 + 6: return go_rms_rows<DT, 128, 6, 1>(a, pass, blocks, st);
+    case 128 * 16 + 8: return go_rms_rows<DT, 128, 8, 1>(a, pass, blocks, st);
+    case 256 * 16 + 2: return go_rms_rows<DT, 256, 2, 1>(a, pass, blocks, st);
+    case 256 * 16 + 4: return go_rms_rows<DT, 256, 4, 1>(a, pass, blocks, st);
+    case 256 * 16 + 5: return go_rms_rows<DT, 256, 5, 1>(a, pass, blocks, st);
+    case 256 * 16 + 6: return go_rms_rows<DT, 256, 6, 1>(a, pass, blocks, st);
+    case 256 * 16 + 8: return go_rms_rows<DT, 256, 8, 1>(a, pass, blocks, st);
+    case 512 * 16 + 2: return go_rms_rows<DT, 512, 2, 1>(a, pass, blocks, st);
+    case 512 * 16 + 4: return go_rms_rows<DT, 512, 4, 1>(a, pass, blocks, st);
+    case 512 * 16 + 5: return go_rms_rows<DT, 512, 5, 1>(a, pass, blocks, st);
+    case 512 * 16 + 6: return go_rms_rows<DT, 512, 6, 1>(a, pass, blocks, st);
+    case 512 * 16 + 8: return go_rms_rows<DT, 512, 8, 1>(a, pass, blocks, st);
+    case 1024 * 16 + 2: return go_rms_rows<DT, 1024, 2, 1>(a, pass, blocks, st);
+    case 1024 * 16 + 4: return go_rms_rows<DT, 1024, 4, 1>(a, pass, blocks, st);
     default: return go_rms_rows<DT, 1024, 0, 1>(a, pass, blocks, st);
     }
 }
@@ -866,7 +901,8 @@ template <int DT> hipError_t launch_rms_dt(const xconv_norm_desc *d, RmsArgs a, 
     bool over = false;
     for (const void *out : {pass == kRmsForward8 ? nullptr : a.y, a.h})
         for (const void *in : {a.x, a.res, a.dy, a.dh}) over = over || overlap(out, in, bytes);
-    const RmsShape s = planes ? rms_planes_shape(DT, d->C) : rms_rows_shape(DT, d->C, bwd);
+    const RmsShape s = planes ? rms_planes_shape(DT, d->C) : rms_rows_shape(DT, d->C, pass);
+    a.over = over;
     a.ragged = (planes ? d->inner : (int64_t)d->C) % V != 0;
     a.exact = planes ? over || d->inner < V : d->C < V || (s.K == 0 && over);
     a.outer = d->outer;
@@ -904,7 +940,7 @@ hipError_t launch_rms(const xconv_norm_desc *d, const RmsArgs &a, RmsPass pass, 
 
 size_t rms_ws_bytes(const xconv_norm_desc *d)
 {
-    const RmsShape s = d->inner > 1 ? rms_planes_shape(d->dtype, d->C) : rms_rows_shape(d->dtype, d->C, true);
+    const RmsShape s = d->inner > 1 ? rms_planes_shape(d->dtype, d->C) : rms_rows_shape(d->dtype, d->C, kRmsBackward);
     return (size_t)rms_blocks(d, s, true) * d->C * sizeof(float);
 }
 
