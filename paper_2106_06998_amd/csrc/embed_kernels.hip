@@ -88,8 +88,8 @@ struct SortArgs {
     int *total;               // places that count
 };
 
-// kShort: one bucket of the whole list; kSplit: one slice, keys are the buckets; kBucket: one bucket of a list that is split
-enum SortMode { kShort, kSplitList, kBucket };
+// kSplitList: one slice, keys are the buckets; kBucket: one bucket of a list that is split
+enum SortMode { kSplitList, kBucket };
 
 // index of place i, -1 where it does not count
 __device__ inline int index_of(const SortArgs &a, int i, int end)
@@ -134,6 +134,98 @@ __global__ __launch_bounds__(kSortThreads) void embed_count_kernel(SortArgs a)
     for (int b = threadIdx.x; b < a.nb; b += kSortThreads) a.hist[(size_t)blockIdx.x * a.nb + b] = counts[b];
 }
 
+// lanes whose key is the same, for keys of so many bits; none for a key below zero
+__device__ inline uint64_t same_keys(int key, int bits)
+{
+    const uint64_t all = __ballot(key >= 0);
+    uint32_t lo = (uint32_t)all, hi = (uint32_t)(all >> 32);
+    for (int b = 0; b < bits; ++b) {
+        const uint32_t bit = (uint32_t)key >> b & 1u;
+        const uint64_t v = __ballot(bit);
+        lo &= (uint32_t)v ^ (bit - 1u);
+        hi &= (uint32_t)(v >> 32) ^ (bit - 1u);
+    }
+    return key < 0 ? 0 : (uint64_t)hi << 32 | lo;
+}
+__device__ inline int lanes_below(uint64_t lanes)
+{
+    return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(lanes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)lanes, 0));
+}
+
+// `start`: where key k begins (of all waves); every wave's counter of it becomes the place of its first entry
+__device__ inline void wave_starts(int *counters, int waves, int pitch, int k, int start)
+{
+    int at = start;
+    for (int w = 0; w < waves; ++w) {
+        const int c = counters[w * pitch + k];
+        counters[w * pitch + k] = at;
+        at += c;
+    }
+}
+
+// Lists of up to 1024 U places, a bucket a workgroup: every workgroup reads the whole list once and keeps the keys of its own bucket in
+// registers, U a lane.  64k places: @ us (three launches over a split list @)
+template <int U>
+__global__ __launch_bounds__(kSortThreads) void embed_short_kernel(SortArgs a)
+{
+    extern __shared__ int counters[];    // [waves][keys], then the waves' sums
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63, me = blockIdx.x;
+    int *sums = counters + kSortWaves * a.keys, *mine = counters + wave * a.keys;
+    const int lo = wave * (64 * U), keys = (a.rows - me + a.nb - 1) >> a.shift;
+    for (int k = threadIdx.x; k < kSortWaves * a.keys; k += kSortThreads) counters[k] = 0;
+    __syncthreads();
+    uint32_t held[U / 2];                // keys and one, in pairs; 0: another bucket's
+    int below = 0;                       // places of the buckets in front of this one
+    constexpr int B = U < 16 ? U : 16;
+#pragma unroll
+    for (int u0 = 0; u0 < U; u0 += B) {
+        int t[B];
+#pragma unroll
+        for (int u = 0; u < B; ++u) t[u] = index_of(a, lo + 64 * (u0 + u) + lane, a.n);
+#pragma unroll
+        for (int u = 0; u < B; ++u) {
+            const int bucket = t[u] & (a.nb - 1);
+            below += t[u] >= 0 && bucket < me ? 1 : 0;
+            const int key = t[u] >= 0 && bucket == me ? t[u] >> a.shift : -1;
+            if (key >= 0) atomicAdd(&mine[key], 1);
+            held[(u0 + u) / 2] = u % 2 ? held[(u0 + u) / 2] | (uint32_t)(key + 1) << 16 : (uint32_t)(key + 1);
+        }
+        __builtin_amdgcn_sched_barrier(0);           // (more loads at once would not fit the registers)
+    }
+    int base;
+    (void)scan_exclusive(below, sums, base);         // (its barrier stands behind the counting too)
+    for (int k0 = 0; k0 < keys; k0 += kSortThreads) {
+        const int k = k0 + (int)threadIdx.x;
+        int n = 0, all;
+        if (k < keys)
+            for (int w = 0; w < kSortWaves; ++w) n += counters[w * a.keys + k];
+        const int start = base + scan_exclusive(n, sums, all);
+        base += all;
+        if (k < keys) {
+            wave_starts(counters, kSortWaves, a.keys, k, start);
+            a.run[me + (k << a.shift)] = int2{start, n};
+        }
+    }
+    if (threadIdx.x == 0 && me == (int)gridDim.x - 1) *a.total = base;
+    __syncthreads();
+    // place the entries in order of the places: few of a round are this bucket's, or many of one key.  (A wave's counters are its own: its
+    // reads and writes of them are in order, and `volatile` keeps every one of them.)
+    volatile int *next = mine;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int key = (int)(u % 2 ? held[u / 2] >> 16 : held[u / 2] & 0xffffu) - 1;
+        uint64_t left = __ballot(key >= 0);
+        while (left) {
+            const int k = __builtin_amdgcn_readlane(key, __builtin_ctzll(left));
+            const uint64_t same = __ballot(key == k);
+            const int at = next[k];
+            if (key == k) a.sorted[at + lanes_below(same)] = int2{me + (k << a.shift), lo + 64 * u + lane};
+            if (lane == 0) next[k] = at + __popcll(same);
+            left &= ~same;
+        }
+    }
+}
+
 template <int MODE>
 __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(SortArgs a)
 {
@@ -142,15 +234,16 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(SortArgs a)
     int *sums = counters + waves * a.keys, *mine = counters + wave * a.keys;
     const int me = blockIdx.x;           // bucket or slice
     // the list: places from .. to - 1, or entries of `split`
-    int from = 0, to = a.n;
+    int from, to;
     if constexpr (MODE == kSplitList) {
         from = me * a.slice;
         to = min(a.n, from + a.slice);
-    } else if constexpr (MODE == kBucket) {
+    } else {
         from = a.first[me];
         to = a.first[me + 1];
     }
     const int keys = MODE == kSplitList ? a.nb : (a.rows - me + a.nb - 1) >> a.shift;
+    const int bits = 32 - __builtin_clz(max(keys - 1, 1));
     for (int k = threadIdx.x; k < waves * a.keys; k += blockDim.x) counters[k] = 0;
     __syncthreads();
     // each wave a part of the list, whole rounds of 64
@@ -166,27 +259,27 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(SortArgs a)
             place = i;
         }
     };
-    auto key_of = [&](int t) { return MODE == kSplitList ? t & (a.nb - 1) : t >> a.shift; };
-    auto counts = [&](int t) { return t >= 0 && (MODE != kShort || (t & (a.nb - 1)) == me); };
+    auto key_of = [&](int t) { return t < 0 ? -1 : MODE == kSplitList ? t & (a.nb - 1) : t >> a.shift; };
 
-    int below = 0;                       // places of the buckets in front of this one (kShort)
-    for (int i0 = lo; i0 < hi; i0 += 256) {
-        int t[4], place;
+    for (int i0 = lo; i0 < hi; i0 += 512) {
+        int t[8], place;
 #pragma unroll
-        for (int u = 0; u < 4; ++u) entry(i0 + 64 * u + lane, t[u], place);
+        for (int u = 0; u < 8; ++u) entry(i0 + 64 * u + lane, t[u], place);
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            if (MODE == kShort) below += t[u] >= 0 && (t[u] & (a.nb - 1)) < me ? 1 : 0;
-            if (counts(t[u])) atomicAdd(&mine[key_of(t[u])], 1);
+        for (int u = 0; u < 8; ++u) {
+            if constexpr (MODE == kSplitList) {
+                if (t[u] >= 0) atomicAdd(&mine[key_of(t[u])], 1);
+            } else {
+                // (in a bucket many lanes may have one key, whose additions would wait for each other)
+                if (i0 + 64 * u >= hi) break;
+                const uint64_t same = same_keys(key_of(t[u]), bits);
+                if ((same >> lane) == 1) mine[key_of(t[u])] += __popcll(same);
+            }
         }
     }
     __syncthreads();
     // where the keys begin, and every wave's part of them
     int base = MODE == kBucket ? from : 0, all;
-    if constexpr (MODE == kShort) {
-        (void)scan_exclusive(below, sums, all);
-        base = all;
-    }
     for (int k0 = 0; k0 < keys; k0 += blockDim.x) {
         const int k = k0 + (int)threadIdx.x;
         int n = 0, before = 0;           // of the whole workgroup; split lists: of all slices, and of those in front of this one
@@ -207,12 +300,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(SortArgs a)
         const int start = base + scan_exclusive(n, sums, all);
         base += all;
         if (k < keys) {
-            int at = start + before;
-            for (int w = 0; w < waves; ++w) {
-                const int c = counters[w * a.keys + k];
-                counters[w * a.keys + k] = at;
-                at += c;
-            }
+            wave_starts(counters, waves, a.keys, k, start + before);
             if constexpr (MODE == kSplitList) {
                 if (me == 0) a.first[k] = start;
                 if (me == 0 && a.rows <= a.nb && k < a.rows) a.run[k] = int2{start, n};
@@ -221,31 +309,25 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(SortArgs a)
             }
         }
     }
-    if (threadIdx.x == 0 && (MODE == kSplitList ? me == 0 : MODE == kShort && me == (int)gridDim.x - 1)) {
-        *a.total = base;
-        if (MODE == kSplitList) a.first[a.nb] = base;
-    }
+    if (MODE == kSplitList && threadIdx.x == 0 && me == 0) *a.total = a.first[a.nb] = base;
     __syncthreads();
-    // place the entries: those of a round that have one key in order of the lanes (a wave's counters are its own: its reads and writes of
-    // them are in order, and `volatile` keeps every one of them)
+    // place the entries in order of the list.  (A wave's counters are its own: its reads and writes of them are in order, and `volatile`
+    // keeps every one of them.)
     volatile int *next = mine;
     int2 *out = MODE == kSplitList && a.rows > a.nb ? a.split : a.sorted;
-    for (int i0 = lo; i0 < hi; i0 += 256) {
-        int t[4], place[4];
+    for (int i0 = lo; i0 < hi; i0 += 512) {
+        int t[8], place[8];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) entry(i0 + 64 * u + lane, t[u], place[u]);
+        for (int u = 0; u < 8; ++u) entry(i0 + 64 * u + lane, t[u], place[u]);
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const bool has = counts(t[u]);
-            const int key = has ? key_of(t[u]) : -1;
-            uint64_t left = __ballot(has);
-            while (left) {
-                const int k = __builtin_amdgcn_readlane(key, __builtin_ctzll(left));
-                const uint64_t same = __ballot(key == k);
-                const int at = next[k];
-                if (key == k) out[at + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(same >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)same, 0))] = int2{t[u], place[u]};
-                if (lane == 0) next[k] = at + __popcll(same);
-                left &= ~same;
+        for (int u = 0; u < 8; ++u) {
+            if (i0 + 64 * u >= hi) break;
+            const int key = key_of(t[u]);
+            const uint64_t same = same_keys(key, bits);
+            if (key >= 0) {
+                const int at = next[key];
+                out[at + lanes_below(same)] = int2{t[u], place[u]};
+                if ((same >> lane) == 1) next[key] = at + __popcll(same);       // the last of them
             }
         }
     }
@@ -259,11 +341,12 @@ struct SumArgs {
     const int *total;
     float *part;          // [chunks][2][pitch]: the end of a run from earlier chunks (or one that fills the chunk), a run that goes on
     int C, pitch, chunk;  // chunk: places of a chunk, a multiple of 8
+    int n;                // places in all (of which *total count)
     int rows;
-    int blocks;           // of the sums; those behind them write the rows of zeros
+    int blocks, tiles;    // workgroups of the sums along the places and along the columns; those behind them write the rows of zeros
     float scale;
 };
-constexpr int kZeroRows = 16;       // rows of a workgroup that writes zeros
+constexpr int kZeroVectors = 4 * kThreads;      // of a workgroup that writes zeros
 
 template <int DT, int WT> __device__ inline void store_row(const SumArgs &a, int row, const Part &p, const float (&s)[NormElem<DT>::V])
 {
@@ -287,30 +370,36 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(SumArgs a)
     typedef typename NormElem<DT>::t elem_t;
     constexpr int V = NormElem<DT>::V, RP = kThreads / G, U = 8;
     const int nv = (a.C + V - 1) / V, exact = a.C < V;
-    if ((int)blockIdx.x >= a.blocks) {
-        if (blockIdx.y) return;
-        const int r0 = ((int)blockIdx.x - a.blocks) * kZeroRows;
+    if ((int)blockIdx.x >= a.blocks * a.tiles) {
         float zero[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) zero[i] = 0.f;
-        for (int r = r0 + (int)(threadIdx.x >> 6); r < min(a.rows, r0 + kZeroRows); r += kThreads / 64) {
-            if (a.run[r].y != 0) continue;
-            for (int v = threadIdx.x & 63; v < nv; v += 64) store_row<DT, WT>(a, r, part_of<V>(v, a.C, exact), zero);
-        }
+        const long long first = (long long)((int)blockIdx.x - a.blocks * a.tiles) * kZeroVectors + threadIdx.x, all = (long long)a.rows * nv;
+        for (long long v0 = first; v0 < all; v0 += (long long)((int)gridDim.x - a.blocks * a.tiles) * kZeroVectors)
+#pragma unroll
+            for (int u = 0; u < kZeroVectors / kThreads; ++u) {
+                const long long q = v0 + u * kThreads;
+                const int row = (int)(all < (1LL << 31) ? (uint32_t)q / (uint32_t)nv : q / nv);
+                if (row < a.rows && a.run[row].y == 0) store_row<DT, WT>(a, row, part_of<V>((int)(q - (long long)row * nv), a.C, exact), zero);
+            }
         return;
     }
-    const int chunk = blockIdx.x * RP + threadIdx.x / G, v = blockIdx.y * G + threadIdx.x % G;
-    const int total = *a.total;
+    const int tile = (int)blockIdx.x % a.tiles, chunk = (int)blockIdx.x / a.tiles * RP + threadIdx.x / G, v = tile * G + threadIdx.x % G;
     const long long from = (long long)chunk * a.chunk;
-    if (from >= total || v >= nv) return;
-    const int lo = (int)from, hi = (int)min((long long)total, from + a.chunk);
+    if (from >= a.n || v >= nv) return;
+    // (entries past the total are not written, and count for nothing)
+    const int lo = (int)from, total = *a.total, hi = (int)min((long long)total, from + a.chunk);
+    int2 e[U], before = a.sorted[max(lo - 1, 0)];
+#pragma unroll
+    for (int u = 0; u < U; ++u) e[u] = a.sorted[min(lo + u, a.n - 1)];
+    if (lo >= total) return;
     const Part p = part_of<V>(v, a.C, exact);
     const elem_t *DY = static_cast<const elem_t *>(a.dy);
     float s[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) s[i] = 0.f;
-    int cur = a.sorted[lo].x;
-    bool open = lo > 0 && a.sorted[lo - 1].x == cur;        // the run began in an earlier chunk
+    int cur = e[0].x;
+    bool open = lo > 0 && before.x == cur;                   // the run began in an earlier chunk
     auto leave = [&](bool goes_on) {
         if (!open && !goes_on) {
             store_row<DT, WT>(a, cur, p, s);
@@ -322,12 +411,12 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(SumArgs a)
         }
     };
     for (int e0 = lo; e0 < hi; e0 += U) {
-        int2 e[U];
         uint4 raw[U];
+        int2 ahead[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) e[u] = a.sorted[min(e0 + u, hi - 1)];
+        for (int u = 0; u < U; ++u) raw[u] = e0 + u < hi ? load_part<DT>(DY + (size_t)e[u].y * a.C, p) : uint4{0, 0, 0, 0};
 #pragma unroll
-        for (int u = 0; u < U; ++u) raw[u] = load_part<DT>(DY + (size_t)e[u].y * a.C, p);
+        for (int u = 0; u < U; ++u) ahead[u] = a.sorted[min(e0 + U + u, a.n - 1)];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (e0 + u >= hi) break;
@@ -343,6 +432,8 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(SumArgs a)
 #pragma unroll
             for (int i = 0; i < V; ++i) s[i] += t[i];
         }
+#pragma unroll
+        for (int u = 0; u < U; ++u) e[u] = ahead[u];
     }
     leave(hi < total && a.sorted[hi].x == cur);
 }
@@ -353,11 +444,10 @@ template <int WT>
 __global__ __launch_bounds__(kJoinWaves * 64) void embed_join_kernel(SumArgs a)
 {
     __shared__ float4 red[kJoinWaves][64];
-    const int chunk = blockIdx.x, total = *a.total;
-    const long long end = ((long long)chunk + 1) * a.chunk;
-    if (end >= total) return;
-    const int t = a.sorted[end - 1].x;
-    if (a.sorted[end].x != t) return;
+    const int chunk = blockIdx.x;
+    const long long end = ((long long)chunk + 1) * a.chunk;      // (below n: the last chunk has no workgroup)
+    const int total = *a.total, t = a.sorted[end - 1].x, behind = a.sorted[end].x;
+    if (end >= total || behind != t) return;
     const int2 run = a.run[t];
     if (run.x < (long long)chunk * a.chunk) return;          // it began in an earlier chunk, whose workgroup joins it
     const int n = (run.x + run.y - 1) / a.chunk - chunk + 1; // chunks
@@ -391,7 +481,7 @@ __global__ __launch_bounds__(kThreads) void embed_zero_kernel(uint8_t *p, size_t
 }
 
 // ---- launches ------------------------------------------------------------------------------------------------------
-constexpr int kShortList = 1 << 14;
+constexpr int kShortList = 16 * kSortThreads;
 
 struct EmbedPlan {
     int nb, shift, keys;
@@ -416,9 +506,9 @@ EmbedPlan embed_plan(const xconv_embed_desc *d)
     const int V = d->dtype == XCONV_F32 ? 4 : 8, nv = ceil_div(d->C, V);
     p.G = column_lanes(nv);
     p.tiles = ceil_div(nv, p.G);
-    // a few thousand waves where there is work for them; chunks long enough that few runs cross them
+    // a few thousand waves where there is work for them; chunks long enough that few runs cross them and few partial sums make up a long run
     p.chunk = 8;
-    while (p.chunk < 256 && d->n / p.chunk * p.tiles * p.G / 64 > 2048) p.chunk *= 2;
+    while (p.chunk < 256 && (d->n / p.chunk > 16384 || d->n / p.chunk * p.tiles * p.G / 64 > 2048)) p.chunk *= 2;
     p.chunks = (int)((d->n + p.chunk - 1) / p.chunk);
     p.pitch = round_up(d->C, 4);
     size_t at = 0;
@@ -445,7 +535,10 @@ template <int DT, int WT> hipError_t go_sum(const SumArgs &a, const EmbedPlan &p
     SumArgs s = a;
     const int rp = kThreads / p.G;
     s.blocks = ceil_div(p.chunks, rp);
-    const dim3 grid((unsigned)(s.blocks + ceil_div(a.rows, kZeroRows)), (unsigned)p.tiles), block(kThreads);
+    constexpr int V = NormElem<DT>::V;
+    const long long zeros = std::min<long long>(((long long)a.rows * ceil_div(a.C, V) + kZeroVectors - 1) / kZeroVectors, 1 << 20);
+    s.tiles = p.tiles;
+    const dim3 grid((unsigned)((long long)s.blocks * s.tiles + zeros)), block(kThreads);
     switch (p.G) {
     case 8: hipLaunchKernelGGL((embed_sum_kernel<DT, WT, 8>), grid, block, 0, st, s); break;
     case 16: hipLaunchKernelGGL((embed_sum_kernel<DT, WT, 16>), grid, block, 0, st, s); break;
@@ -512,7 +605,10 @@ hipError_t launch_embed_bwd(const xconv_embed_desc *d, const void *idx, const vo
     s.total = reinterpret_cast<int *>(base + p.total);
     auto lds = [](int waves, int keys) { return (size_t)(waves * keys + waves) * 4; };
     if (p.small) {
-        hipLaunchKernelGGL(embed_sort_kernel<kShort>, dim3((unsigned)std::min<long long>(p.nb, d->rows)), dim3(kSortThreads), lds(kSortWaves, p.keys), st, s);
+        const dim3 grid((unsigned)std::min<long long>(p.nb, d->rows)), block(kSortThreads);
+        const size_t l = lds(kSortWaves, p.keys);
+        if (d->n <= 4 * kSortThreads) hipLaunchKernelGGL(embed_short_kernel<4>, grid, block, l, st, s);
+        else hipLaunchKernelGGL(embed_short_kernel<16>, grid, block, l, st, s);
     } else {
         s.split = reinterpret_cast<int2 *>(base + p.split);
         s.hist = reinterpret_cast<int *>(base + p.hist);
@@ -535,6 +631,7 @@ hipError_t launch_embed_bwd(const xconv_embed_desc *d, const void *idx, const vo
     a.run = s.run;
     a.total = s.total;
     a.part = reinterpret_cast<float *>(base + p.part);
+    a.n = (int)d->n;
     a.C = d->C;
     a.pitch = p.pitch;
     a.chunk = p.chunk;
