@@ -42,7 +42,7 @@ struct NormGeom {
     int C, inner;
     float eps, inv_c, count;   // count = C, inv_c = 1 / C
     int nvi;              // vectors a plane
-    long long tiles;      // tiles of kNormTX vectors of positions (planes)
+    long long tiles;      // tiles of kNormTX vectors of positions, or what the kernel takes (planes)
     int ragged;           // rows (planes) are no whole number of vectors: values that are not a vector's own are masked
     int exact;            // last vectors do not overlap (shorter than a vector; outputs over inputs that are read again)
 };
@@ -200,25 +200,26 @@ template <int G> constexpr int row_threads = G > 256 ? G : 256;
 constexpr int kNormTX = 8;               // lanes along the positions
 constexpr int kNormTYW = 64 / kNormTX;   // channels of a wave
 
-// sums over the threads along the channels of N columns of V positions each; `red` [NW][kNormTX][N * V]
-template <int N, int NW> __device__ inline void column_sum(float (&s)[N], float *red)
+// sums over the threads along the channels of N columns of V positions each, TX lanes lie along the positions; `red` [NW][TX][N * V].
+// FRESH: nobody still reads `red` (the caller takes two in turn)
+template <int N, int NW, int TX = kNormTX, bool FRESH = false> __device__ inline void column_sum(float (&s)[N], float *red)
 {
 #pragma unroll
-    for (int o = kNormTX; o < 64; o <<= 1)
+    for (int o = TX; o < 64; o <<= 1)
 #pragma unroll
         for (int i = 0; i < N; ++i) s[i] += __shfl_xor(s[i], o);
-    const int tx = threadIdx.x % kNormTX;
-    __syncthreads();                     // whoever still reads the last sum
-    if ((threadIdx.x & 63) < kNormTX)
+    const int tx = threadIdx.x % TX;
+    if constexpr (!FRESH) __syncthreads();   // whoever still reads the last sum
+    if ((threadIdx.x & 63) < TX)
 #pragma unroll
-        for (int i = 0; i < N; ++i) red[((threadIdx.x >> 6) * kNormTX + tx) * N + i] = s[i];
+        for (int i = 0; i < N; ++i) red[((threadIdx.x >> 6) * TX + tx) * N + i] = s[i];
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < N; ++i) s[i] = 0.f;
 #pragma unroll 2
     for (int w = 0; w < NW; ++w)
 #pragma unroll
-        for (int i = 0; i < N; ++i) s[i] += red[(w * kNormTX + tx) * N + i];
+        for (int i = 0; i < N; ++i) s[i] += red[(w * TX + tx) * N + i];
 }
 
 // where the thread's vector of positions lies: first value of channel 0 of the image, its first position, the vector's part
@@ -228,10 +229,10 @@ struct PlaneAt {
     Part p;
     bool on;
 };
-template <int V> __device__ inline PlaneAt plane_at(const NormGeom &a, long long tile)
+template <int V, int TX = kNormTX> __device__ inline PlaneAt plane_at(const NormGeom &a, long long tile)
 {
-    const long long q = tile * kNormTX + threadIdx.x % kNormTX;
-    const long long img = a.tiles * kNormTX < (1LL << 31) ? (long long)((uint32_t)q / (uint32_t)a.nvi) : q / a.nvi;
+    const long long q = tile * TX + threadIdx.x % TX;
+    const long long img = a.tiles * TX < (1LL << 31) ? (long long)((uint32_t)q / (uint32_t)a.nvi) : q / a.nvi;
     if (img >= a.outer) return {0, 0, {0, 0, V}, false};
     const Part p = part_of<V>((int)(q - img * a.nvi), a.inner, a.exact);
     return {(size_t)img * a.C * a.inner, img * a.inner + p.at, p, true};
@@ -268,7 +269,7 @@ __device__ inline TileRun tiles_of(const NormGeom &a)
 }
 
 // ---- host ----------------------------------------------------------------------------------------------------------
-inline long long plane_tiles(const xconv_norm_desc *d, int V) { return (d->outer * ceil_div((int)d->inner, V) + kNormTX - 1) / kNormTX; }
+inline long long plane_tiles(const xconv_norm_desc *d, int V, int TX = kNormTX) { return (d->outer * ceil_div((int)d->inner, V) + TX - 1) / TX; }
 
 inline bool overlap(const void *a, const void *b, size_t bytes)
 {

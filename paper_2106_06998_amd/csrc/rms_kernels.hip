@@ -483,34 +483,34 @@ __global__ __launch_bounds__(T, 4) void rms_rows_bwd_kernel(RmsArgs a)
 // ---- planes --------------------------------------------------------------------------------------------------------
 // largest over the threads along the channels of N columns, along with column_sum's sums: what a wave has in front of it, what all have
 // behind it (its barriers serve both)
-template <int N> __device__ inline void column_max(uint32_t (&s)[N], uint32_t *red)
+template <int N, int TX> __device__ inline void column_max(uint32_t (&s)[N], uint32_t *red)
 {
 #pragma unroll
-    for (int o = kNormTX; o < 64; o <<= 1)
+    for (int o = TX; o < 64; o <<= 1)
 #pragma unroll
         for (int i = 0; i < N; ++i) s[i] = max(s[i], (uint32_t)__shfl_xor((int)s[i], o));
-    if ((threadIdx.x & 63) < kNormTX)
+    if ((threadIdx.x & 63) < TX)
 #pragma unroll
-        for (int i = 0; i < N; ++i) red[((threadIdx.x >> 6) * kNormTX + threadIdx.x % kNormTX) * N + i] = s[i];
+        for (int i = 0; i < N; ++i) red[((threadIdx.x >> 6) * TX + threadIdx.x % TX) * N + i] = s[i];
 }
-template <int N, int NW> __device__ inline void column_max_join(uint32_t (&s)[N], const uint32_t *red)
+template <int N, int NW, int TX> __device__ inline void column_max_join(uint32_t (&s)[N], const uint32_t *red)
 {
 #pragma unroll 2
     for (int w = 0; w < NW; ++w)
 #pragma unroll
-        for (int i = 0; i < N; ++i) s[i] = max(s[i], red[(w * kNormTX + threadIdx.x % kNormTX) * N + i]);
+        for (int i = 0; i < N; ++i) s[i] = max(s[i], red[(w * TX + threadIdx.x % TX) * N + i]);
 }
 
 // WHOLE: planes of at least one vector whose last vectors overlap, the ordinary case
-template <int DT, bool OUT8, int NW, int K, bool WHOLE>
+template <int DT, bool OUT8, int NW, int K, int TX, bool WHOLE>
 __global__ __launch_bounds__(NW * 64) void rms_planes_fwd_kernel(RmsArgs a)
 {
     typedef typename NormElem<DT>::t elem_t;
-    constexpr int V = NormElem<DT>::V, TY = NW * kNormTYW, KR = K > 0 ? K : 1;
-    __shared__ float red[NW * kNormTX * V];
-    __shared__ uint32_t redm[OUT8 ? 2 * NW * kNormTX * V : 1];       // (two, taken in turn: no barrier stands behind the reading of one)
+    constexpr int V = NormElem<DT>::V, TY = NW * (64 / TX), KR = K > 0 ? K : 1;
+    __shared__ float red[2 * NW * TX * V];       // (two, taken in turn: no barrier stands behind the reading of one)
+    __shared__ uint32_t redm[OUT8 ? 2 * NW * TX * V : 1];
     int turn = 0;
-    const int ty = threadIdx.x / kNormTX;
+    const int ty = threadIdx.x / TX;
     const bool drops = !OUT8 && a.drop.q16;
     const uint64_t key = drops ? drop_key(a.drop) : 0;
     const TileRun run = tiles_of(a);
@@ -524,7 +524,7 @@ __global__ __launch_bounds__(NW * 64) void rms_planes_fwd_kernel(RmsArgs a)
         }
     };
     for (long long tile = run.from; tile < run.to; tile += run.step) {
-        const PlaneAt at = plane_at<V>(a, tile);
+        const PlaneAt at = plane_at<V, TX>(a, tile);
         const elem_t *x = static_cast<const elem_t *>(a.x) + at.base;
         const elem_t *res = a.res ? static_cast<const elem_t *>(a.res) + at.base : nullptr;
         float h[KR][V];
@@ -580,12 +580,10 @@ __global__ __launch_bounds__(NW * 64) void rms_planes_fwd_kernel(RmsArgs a)
                 for (int i = 0; i < V; ++i) m[i] = max(m[i], magnitude(h[k][i]));
             }
         });
-        uint32_t *mine = redm + turn * (NW * kNormTX * V);
-        if constexpr (OUT8) {
-            turn ^= 1;
-            column_max<V>(m, mine);
-        }
-        column_sum<V, NW>(s, red);
+        const int slot = turn * (NW * TX * V);
+        turn ^= 1;
+        if constexpr (OUT8) column_max<V, TX>(m, redm + slot);
+        column_sum<V, NW, TX, true>(s, red + slot);
         float rstd[V], f[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
@@ -593,7 +591,7 @@ __global__ __launch_bounds__(NW * 64) void rms_planes_fwd_kernel(RmsArgs a)
             f[i] = rstd[i];
         }
         if constexpr (OUT8) {
-            column_max_join<V, NW>(m, mine);
+            column_max_join<V, NW, TX>(m, redm + slot);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const float most = __uint_as_float(max(magnitude(__uint_as_float(m[i]) * rstd[i]), __float_as_uint(kLeast8)));
@@ -624,13 +622,14 @@ __global__ __launch_bounds__(NW * 64) void rms_planes_fwd_kernel(RmsArgs a)
     }
 }
 
-template <int DT, int NW, int K, bool WHOLE>
+template <int DT, int NW, int K, int TX, bool WHOLE>
 __global__ __launch_bounds__(NW * 64, 4) void rms_planes_bwd_kernel(RmsArgs a)
 {
     typedef typename NormElem<DT>::t elem_t;
-    constexpr int V = NormElem<DT>::V, TY = NW * kNormTYW, KR = K > 0 ? K : 1;
-    __shared__ float red[NW * kNormTX * V];
-    const int ty = threadIdx.x / kNormTX, tx = threadIdx.x % kNormTX;
+    constexpr int V = NormElem<DT>::V, TY = NW * (64 / TX), KR = K > 0 ? K : 1;
+    __shared__ float red[2 * NW * TX * V];       // (two, taken in turn)
+    int turn = 0;
+    const int ty = threadIdx.x / TX, tx = threadIdx.x % TX;
     const elem_t *H = static_cast<const elem_t *>(a.x), *DY = static_cast<const elem_t *>(a.dy), *DH = static_cast<const elem_t *>(a.dh);
     elem_t *DR = static_cast<elem_t *>(a.y), *DX = static_cast<elem_t *>(a.h);
     const uint64_t key = a.drop.q16 ? drop_key(a.drop) : 0;
@@ -655,7 +654,7 @@ __global__ __launch_bounds__(NW * 64, 4) void rms_planes_bwd_kernel(RmsArgs a)
     if (K == 0 && part && run.from >= run.to)
         for (int c = threadIdx.x; c < a.C; c += NW * 64) part[c] = 0.f;
     for (long long tile = run.from; tile < run.to; tile += run.step, first = false) {
-        const PlaneAt at = plane_at<V>(a, tile);
+        const PlaneAt at = plane_at<V, TX>(a, tile);
         uint4 rx[KR], rd[KR], rh[KR];
         auto get = [&](int k, int c) {
             rx[k] = plane_get<DT, WHOLE>(a, H + at.base, at, c);
@@ -696,12 +695,13 @@ __global__ __launch_bounds__(NW * 64, 4) void rms_planes_bwd_kernel(RmsArgs a)
                 if constexpr (K > 4) __builtin_amdgcn_sched_barrier(0);
             } else if (part) {
 #pragma unroll
-                for (int o = kNormTX / 2; o >= 1; o >>= 1) sg += __shfl_xor(sg, o);
+                for (int o = TX / 2; o >= 1; o >>= 1) sg += __shfl_xor(sg, o);
                 if (tx == 0) part[c] = (first ? 0.f : part[c]) + sg;
             }
         });
         if (!DR && !DX) continue;
-        column_sum<V, NW>(c1, red);
+        column_sum<V, NW, TX, true>(c1, red + turn * (NW * TX * V));
+        turn ^= 1;
         if (!at.on) continue;
 #pragma unroll
         for (int i = 0; i < V; ++i) c1[i] *= a.inv_c;
@@ -732,7 +732,7 @@ __global__ __launch_bounds__(NW * 64, 4) void rms_planes_bwd_kernel(RmsArgs a)
     rounds([&](int k, int c) {
         float sg = ag[k];
 #pragma unroll
-        for (int o = kNormTX / 2; o >= 1; o >>= 1) sg += __shfl_xor(sg, o);
+        for (int o = TX / 2; o >= 1; o >>= 1) sg += __shfl_xor(sg, o);
         if (tx == 0 && c < a.C) part[c] = sg;
     });
 }
@@ -765,6 +765,7 @@ struct RmsShape {
     int G, K, R, T;   // rows: lanes a row, vectors a lane (0: read again), rows at once, threads a workgroup
     int NW;           // planes: waves a workgroup
     int V;
+    int TX;           // planes: lanes along the positions
 };
 
 // The smallest group that holds a row with one vector a lane; past a wave up to eight vectors a lane, then groups of several waves with
@@ -788,38 +789,39 @@ RmsShape rms_rows_shape(int dtype, int C, RmsPass pass)
     const int V = dtype == XCONV_F32 ? 4 : 8, nv = ceil_div(C, V);
     auto threads = [&](int G) { return backward ? std::max(512, G) : G > 64 ? G : 256; };
     for (int G : {4, 8, 16, 32, 64})
-        if (nv <= G) return {G, 1, 2, threads(G), 0, V};
+        if (nv <= G) return {G, 1, 2, threads(G), 0, V, kNormTX};
     if (backward) {
         for (int G : {64, 128, 256, 512, 1024})
-            if (nv <= 2 * G) return {G, 2, 1, threads(G), 0, V};
+            if (nv <= 2 * G) return {G, 2, 1, threads(G), 0, V, kNormTX};
     } else {
         for (int K : {2, 3, 4})
-            if (nv <= K * 64) return {64, K, 1, threads(64), 0, V};
+            if (nv <= K * 64) return {64, K, 1, threads(64), 0, V, kNormTX};
         for (int G : {64, 128, 256, 512, 1024})
             for (int K : {4, 5, 6, 8})
-                if (nv <= K * G && rms_has(pass, G, K)) return {G, K, 1, threads(G), 0, V};
+                if (nv <= K * G && rms_has(pass, G, K)) return {G, K, 1, threads(G), 0, V, kNormTX};
     }
-    return {1024, 0, 1, 1024, 0, V};
+    return {1024, 0, 1, 1024, 0, V, kNormTX};
 }
 // 8 channels a wave and round: enough waves for 4 rounds, 8 with 16 waves
 RmsShape rms_planes_shape(int dtype, int C)
 {
     const int V = dtype == XCONV_F32 ? 4 : 8;
-    for (int NW : {4, 8, 16})
-        for (int K : {1, 2, 4})
-            if (C <= kNormTYW * NW * K) return {0, K, 1, 0, NW, V};
-    if (C <= kNormTYW * 16 * 8) return {0, 8, 1, 0, 16, V};
-    return {0, 0, 1, 0, 16, V};
+    for (int K : {1, 2, 4})
+        if (C <= 32 * K) return {0, K, 1, 0, 4, V, 8};
+    if (C <= 256) return {0, 4, 1, 0, 8, V, 8};
+    for (int NW : {8, 16})
+        if (C <= 64 * NW) return {0, 4, 1, 0, NW, V, 4};
+    return {0, 0, 1, 0, 16, V, 8};
 }
 
-constexpr int kRmsBlocks = 512;            // most workgroups that leave partial sums (planes: twice as many)
+constexpr int kRmsBlocks = 512;            // most workgroups that leave partial sums, of 8 waves
 constexpr long long kRmsGrid = 1 << 20;    // most workgroups of the forward pass
 
 int rms_blocks(const xconv_norm_desc *d, const RmsShape &s, bool bwd)
 {
     if (d->inner > 1) {
-        const long long want = plane_tiles(d, s.V);
-        return (int)std::min<long long>(want > 8 ? (want + 7) / 8 * 8 : want, bwd ? 2 * kRmsBlocks : kRmsGrid);
+        const long long want = plane_tiles(d, s.V, s.TX);
+        return (int)std::min<long long>(want > 8 ? (want + 7) / 8 * 8 : want, bwd ? 8 * kRmsBlocks / s.NW : kRmsGrid);     // (what the chip holds at once)
     }
     const int rows = s.T / s.G * s.R;
     return (int)std::min<long long>((d->outer + rows - 1) / rows, bwd ? kRmsBlocks : kRmsGrid);
@@ -871,24 +873,24 @@ template <int DT> hipError_t go_rms_rows_shape(const RmsArgs &a, const RmsShape 
     default: return go_rms_rows<DT, 1024, 0, 1>(a, pass, blocks, st);
     }
 }
-template <int DT, int NW, int K, bool WHOLE> hipError_t go_rms_planes(const RmsArgs &a, RmsPass pass, int blocks, hipStream_t st)
+template <int DT, int NW, int K, int TX, bool WHOLE> hipError_t go_rms_planes(const RmsArgs &a, RmsPass pass, int blocks, hipStream_t st)
 {
     const dim3 grid((unsigned)blocks), block(NW * 64);
-    if (pass == kRmsForward) hipLaunchKernelGGL((rms_planes_fwd_kernel<DT, false, NW, K, WHOLE>), grid, block, 0, st, a);
-    else if (pass == kRmsForward8) hipLaunchKernelGGL((rms_planes_fwd_kernel<DT, true, NW, K, WHOLE>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((rms_planes_bwd_kernel<DT, NW, K, WHOLE>), grid, block, 0, st, a);
+    if (pass == kRmsForward) hipLaunchKernelGGL((rms_planes_fwd_kernel<DT, false, NW, K, TX, WHOLE>), grid, block, 0, st, a);
+    else if (pass == kRmsForward8) hipLaunchKernelGGL((rms_planes_fwd_kernel<DT, true, NW, K, TX, WHOLE>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((rms_planes_bwd_kernel<DT, NW, K, TX, WHOLE>), grid, block, 0, st, a);
     return hipGetLastError();
 }
 template <int DT, bool WHOLE> hipError_t go_rms_planes_shape(const RmsArgs &a, const RmsShape &s, RmsPass pass, int blocks, hipStream_t st)
 {
-    switch (s.NW * 32 + s.K) {
-    case 4 * 32 + 1: return go_rms_planes<DT, 4, 1, WHOLE>(a, pass, blocks, st);
-    case 4 * 32 + 2: return go_rms_planes<DT, 4, 2, WHOLE>(a, pass, blocks, st);
-    case 4 * 32 + 4: return go_rms_planes<DT, 4, 4, WHOLE>(a, pass, blocks, st);
-    case 8 * 32 + 4: return go_rms_planes<DT, 8, 4, WHOLE>(a, pass, blocks, st);
-    case 16 * 32 + 4: return go_rms_planes<DT, 16, 4, WHOLE>(a, pass, blocks, st);
-    case 16 * 32 + 8: return go_rms_planes<DT, 16, 8, WHOLE>(a, pass, blocks, st);
-    default: return go_rms_planes<DT, 16, 0, WHOLE>(a, pass, blocks, st);
+    switch ((s.NW * 8 + s.K) * 8 + s.TX % 8) {
+    case (4 * 8 + 1) * 8 + 0: return go_rms_planes<DT, 4, 1, 8, WHOLE>(a, pass, blocks, st);
+    case (4 * 8 + 2) * 8 + 0: return go_rms_planes<DT, 4, 2, 8, WHOLE>(a, pass, blocks, st);
+    case (4 * 8 + 4) * 8 + 0: return go_rms_planes<DT, 4, 4, 8, WHOLE>(a, pass, blocks, st);
+    case (8 * 8 + 4) * 8 + 0: return go_rms_planes<DT, 8, 4, 8, WHOLE>(a, pass, blocks, st);
+    case (8 * 8 + 4) * 8 + 4: return go_rms_planes<DT, 8, 4, 4, WHOLE>(a, pass, blocks, st);
+    case (16 * 8 + 4) * 8 + 4: return go_rms_planes<DT, 16, 4, 4, WHOLE>(a, pass, blocks, st);
+    default: return go_rms_planes<DT, 16, 0, 8, WHOLE>(a, pass, blocks, st);
     }
 }
 
@@ -912,7 +914,7 @@ template <int DT> hipError_t launch_rms_dt(const xconv_norm_desc *d, RmsArgs a, 
     a.count = (float)d->C;
     a.inv_c = 1.0f / a.count;
     a.nvi = ceil_div((int)d->inner, s.V);
-    a.tiles = plane_tiles(d, s.V);
+    a.tiles = plane_tiles(d, s.V, s.TX);
     a.w32 = d->w_dtype == XCONV_F32;
     a.fours = (planes ? d->inner : (int64_t)d->C) % 4 == 0;
     const int blocks = rms_blocks(d, s, bwd);
