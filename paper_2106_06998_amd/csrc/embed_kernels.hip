@@ -164,7 +164,8 @@ __device__ inline void wave_starts(int *counters, int waves, int pitch, int k, i
 }
 
 // Lists of up to 1024 U places, a bucket a workgroup: every workgroup reads the whole list once and keeps the keys of its own bucket in
-// registers, U a lane.  64k places: @ us (three launches over a split list @)
+// registers, U a lane.  16384 places take 13 us so and 15 over a split list, whose launches are three; 65536 take 96 (every workgroup reads
+// half a megabyte) and 21.
 template <int U>
 __global__ __launch_bounds__(kSortThreads) void embed_short_kernel(SortArgs a)
 {
@@ -508,7 +509,7 @@ EmbedPlan embed_plan(const xconv_embed_desc *d)
     p.tiles = ceil_div(nv, p.G);
     // a few thousand waves where there is work for them; chunks long enough that few runs cross them and few partial sums make up a long run
     p.chunk = 8;
-    while (p.chunk < 256 && (d->n / p.chunk > 16384 || d->n / p.chunk * p.tiles * p.G / 64 > 2048)) p.chunk *= 2;
+    while (p.chunk < 256 && (d->n / p.chunk > 8192 || d->n / p.chunk * p.tiles * p.G / 64 > 2048)) p.chunk *= 2;
     p.chunks = (int)((d->n + p.chunk - 1) / p.chunk);
     p.pitch = round_up(d->C, 4);
     size_t at = 0;

@@ -386,25 +386,25 @@ struct NormView {
     at::MemoryFormat format;
     std::vector<int64_t> stats;
 };
-NormView norm_view(const Tensor &x, const Tensor &weight, const Tensor &bias, int64_t axis, double eps, const std::string &who = "layer_norm")
+NormView norm_view(const Tensor &x, const Tensor &weight, const Tensor &bias, int64_t axis, double eps, const char *who = "layer_norm")
 {
-    if (!x.is_cuda()) refuse(who + ": runs on the GPU only (input on " + x.device().str() + ")");
-    if (!storage_type(x)) refuse(who + ": storage type " + at::toString(x.scalar_type()) + " is not supported (float32, bfloat16, float16)");
+    if (!x.is_cuda()) refuse(std::string(who) + ": runs on the GPU only (input on " + x.device().str() + ")");
+    if (!storage_type(x)) refuse(std::string(who) + ": storage type " + at::toString(x.scalar_type()) + " is not supported (float32, bfloat16, float16)");
     const int64_t dim = x.dim();
     if (axis < 0) axis += dim;
-    if (dim < 1 || (axis != dim - 1 && (axis != 1 || dim < 2))) refuse(who + ": the channels are the last axis or axis 1 of the input");
+    if (dim < 1 || (axis != dim - 1 && (axis != 1 || dim < 2))) refuse(std::string(who) + ": the channels are the last axis or axis 1 of the input");
     NormView v;
     v.format = at::MemoryFormat::Contiguous;
     const int64_t C = x.size(axis);
-    if (C < 1 || C > INT32_MAX) refuse(who + ": no channels");
+    if (C < 1 || C > INT32_MAX) refuse(std::string(who) + ": no channels");
     int wt = -1;
     for (const Tensor *p : {&weight, &bias}) {
         if (!p->defined()) continue;
-        if (p->device() != x.device() || p->dim() != 1 || p->size(0) != C) refuse(who + ": expected parameters of " + std::to_string(C) + " channels on the input's device");
+        if (p->device() != x.device() || p->dim() != 1 || p->size(0) != C) refuse(std::string(who) + ": expected parameters of " + std::to_string(C) + " channels on the input's device");
         if (!storage_type(*p) || (p->scalar_type() != at::kFloat && p->scalar_type() != x.scalar_type()))
-            refuse(who + ": parameters are float32 or of the input's type");
+            refuse(std::string(who) + ": parameters are float32 or of the input's type");
         const int t = dtype_code(p->scalar_type());
-        if (wt >= 0 && wt != t) refuse(who + ": weight and bias are of one type");
+        if (wt >= 0 && wt != t) refuse(std::string(who) + ": weight and bias are of one type");
         wt = t;
     }
     int64_t inner = 1;

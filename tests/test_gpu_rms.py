@@ -20,7 +20,8 @@ def _normal(shape, dtype, seed, scale=1.0):
 
 # every group of lanes, vectors a lane, and the rows that are read again; whole and ragged lengths
 ROWS = [(1, 1), (3, 2), (5, 3), (7, 7), (9, 8), (130, 32), (131, 33), (64, 64), (33, 100), (50, 127), (17, 256), (19, 300), (9, 512), (5, 1000), (6, 1024), (3, 2001), (4, 2048),
-        (3, 4096), (2, 5001), (3, 8191), (2, 8192), (2, 12000), (1, 16385), (2, 20000), (1, 33000), (2, 40003), (700, 48), (1500, 20)]
+        (3, 4096), (2, 5001), (3, 8191), (2, 8192), (2, 12000), (1, 16385), (2, 20000), (1, 33000), (2, 40003), (700, 48), (1500, 20),
+        (3, 1500), (3, 2500), (2, 3000), (2, 6001), (2, 10000), (2, 14002), (1, 24000), (1, 32000)]
 PLANES = [(1, 1, 1, 2), (2, 3, 1, 3), (2, 5, 2, 2), (3, 8, 4, 4), (2, 17, 5, 7), (1, 32, 3, 3), (2, 33, 8, 8), (2, 64, 6, 5), (1, 100, 7, 9), (2, 128, 4, 4), (1, 200, 5, 5), (1, 256, 7, 7),
           (1, 300, 3, 11), (1, 512, 4, 5), (1, 700, 3, 5), (1, 1024, 5, 5), (1, 1500, 3, 7), (40, 16, 12, 10)]
 
@@ -153,6 +154,7 @@ def test_empty():
 @pytest.mark.parametrize("out", [torch.float8_e4m3fn, torch.int8])
 @pytest.mark.parametrize("dtype", sorted(TYPES))
 @pytest.mark.parametrize("shape,axis", [((1, 1), -1), ((3, 5), -1), ((5, 64), -1), ((9, 300), -1), ((1, 4096), -1), ((4, 5001), -1), ((2, 9000), -1), ((2, 40001), -1),
+                                        ((2, 1500), -1), ((2, 2500), -1), ((2, 2999), -1), ((2, 6000), -1), ((2, 12000), -1), ((2, 17000), -1), ((2, 21000), -1), ((2, 32000), -1),
                                         ((2, 3, 1, 2), 1), ((2, 20, 5, 7), 1), ((1, 130, 4, 6), 1), ((1, 700, 3, 5), 1), ((1, 1100, 2, 5), 1)])
 def test_8_bits(shape, axis, dtype, out):
     dt = TYPES[dtype]
@@ -270,7 +272,7 @@ def test_deterministic():
         assert all(torch.equal(a, b) for a, b in zip(first, again))
 
 
-@pytest.mark.parametrize("shape,axis", [((33, 100), -1), ((3, 40003), -1), ((3, 20, 5, 7), 1), ((2, 1100, 3, 5), 1)])
+@pytest.mark.parametrize("shape,axis", [((33, 100), -1), ((600, 1001), -1), ((700, 5001), -1), ((3, 40003), -1), ((3, 20, 5, 7), 1), ((2, 1100, 3, 5), 1)])
 def test_in_place_through_the_abi(shape, axis):
     """outputs may be inputs of their type; what is too close is refused"""
     n = shape[axis]
