@@ -65,7 +65,8 @@ def dropout(x, p, seed, step=None):
 
 class _Draws:
     """The seeds of a module: another one for every forward pass.  A captured graph keeps the seed that it was captured with, so
-    there a `step` is expected, which the program advances between replays."""
+    there a `step` is expected, which the program advances between replays.  (As with any module, a backward pass is captured while
+    no eager graph of the same parameters is kept: torch's engine ends the process otherwise.)"""
 
     def _next_seed(self, x):
         if self.step is None and x.is_cuda and torch.cuda.is_current_stream_capturing():

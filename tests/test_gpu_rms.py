@@ -209,6 +209,7 @@ def test_autograd(dtype, p, residual):
     want = N.rms_norm_backward(a, hs, rstd, w.detach(), b if residual else None, 1, p, 7)
     for g, v in zip((x.grad, r.grad if residual else None, w.grad), want):
         assert g is None or torch.equal(g, v)
+    assert not residual or x.grad.data_ptr() != r.grad.data_ptr()         # (one tensor came back for both without dropout)
     if residual:
         # h alone, y alone, with broadcast gradients and of another type
         for outputs in ("h", "y"):

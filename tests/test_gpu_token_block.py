@@ -82,3 +82,67 @@ def test_captured_training_steps():
         torch.cuda.synchronize()
         assert torch.equal(table, t0) and torch.equal(w, w0) and int(step) == k + 1
     assert bool(torch.isfinite(table).all())
+
+
+def test_captured_autograd_step():
+    """forward and backward through the modules as one graph, with every eager graph of the parameters gone, against the functions"""
+    from paper_2106_06998_amd.embedding import embedding_backward, embedding_forward
+    step = torch.zeros(1, dtype=torch.int64, device=DEV)
+    embed, drop, norm = XEmbedding(40, 32, scale=2.0).to(DEV), XDropout(0.2, step=step), N.XRMSNorm(32, p=0.3, step=step).to(DEV)
+    idx = torch.randint(0, 40, (6, 21), generator=torch.Generator().manual_seed(1)).to(DEV)
+    r, a, b = (torch.randn(6, 21, 32, generator=torch.Generator().manual_seed(k)).to(DEV) for k in (2, 3, 4))
+
+    def loss():
+        y, h = norm(drop(embed(idx)), r)
+        return (y * a).sum() + (h * b).sum()
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(2):
+            embed.weight.grad = norm.weight.grad = None
+            loss().backward()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    embed.weight.grad = norm.weight.grad = None
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        loss().backward()
+    seeds = drop.last_seed, norm.last_seed
+    for k in range(4):
+        step.fill_(5 - 2 * k)
+        idx.copy_(torch.randint(0, 40, (6, 21), generator=torch.Generator().manual_seed(10 + k)))
+        graph.replay()
+        torch.cuda.synchronize()
+        x = dropout_forward(embedding_forward(idx, embed.weight.detach(), 2.0), 0.2, seeds[0], step)
+        _, h, rstd = N.rms_norm_forward(x, norm.weight.detach(), r, 1e-6, -1, 0.3, seeds[1], step)
+        dx, _, dw = N.rms_norm_backward(a, h, rstd, norm.weight.detach(), b, -1, 0.3, seeds[1], step)
+        dt = embedding_backward(dropout_forward(dx, 0.2, seeds[0], step), idx, 40, 2.0)
+        torch.cuda.synchronize()
+        assert torch.equal(norm.weight.grad, dw) and torch.equal(embed.weight.grad, dt)
+
+
+def test_two_threads_on_two_streams():
+    from concurrent.futures import ThreadPoolExecutor
+    from paper_2106_06998_amd.embedding import embedding_backward
+    made = []
+    for k in range(2):
+        g = torch.Generator().manual_seed(k)
+        idx = torch.randint(0, 500 + 3000 * k, (1500 + 60000 * k,), generator=g).to(DEV)
+        dy = torch.randn(idx.numel(), 24, generator=g).to(DEV)
+        made.append((dy, idx, 500 + 3000 * k))
+
+    def run(k, stream):
+        dy, idx, rows = made[k]
+        with torch.cuda.stream(stream):
+            dw = embedding_backward(dy, idx, rows)
+            y, h, rstd = N.rms_norm_forward(dy, None, dy, 1e-6, -1, 0.25, k)
+            return dw, y, rstd, N.rms_norm_backward(y, h, rstd, None, dy, -1, 0.25, k)[2]
+
+    want = [run(k, torch.cuda.current_stream()) for k in range(2)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    with ThreadPoolExecutor(2) as ex:
+        for got in [list(ex.map(lambda k: run(k, streams[k]), (0, 1))) for _ in range(5)]:
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for g, w in zip(got, want) for a, b in zip(g, w))
