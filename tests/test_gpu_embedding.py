@@ -214,3 +214,40 @@ def test_refusals():
         E.embedding(idx, w, axis=0)
     with pytest.raises(ValueError):
         E.embedding(idx[0], w, axis=1)
+
+
+def test_places_beyond_32_bits():
+    """a table, results, gradients and a gradient's source of more than 2^32 values each; only a few places are not zero"""
+    rows, c = 2 ** 31 - 1, 3
+    w = torch.zeros(rows, c, dtype=torch.float16, device=DEV)
+    w[-4:] = _normal((4, c), torch.float16, 1)
+    for idx in (torch.tensor([rows - 1, 0, rows - 4, rows - 2], dtype=t, device=DEV) for t in (torch.int32, torch.int64)):
+        assert torch.equal(E.embedding_forward(idx, w), w[idx.long()])
+    del w
+    n, c = 2 ** 22 + 9, 1032
+    w, idx = _normal((50, c), torch.bfloat16, 2), _indices(n, 50, "uniform")
+    y = E.embedding_forward(idx, w, 0.5)
+    assert torch.equal(y[-20:], w[idx[-20:]] * 0.5) and torch.equal(y[:20], w[idx[:20]] * 0.5)
+    y[:-20] = 0
+    assert torch.equal(E.embedding_backward(y, idx, 50, 0.25), E.embedding_backward(y[-20:].clone(), idx[-20:].clone(), 50, 0.25))
+    del y
+    rows = 2 ** 22
+    dy, idx = _normal((20000, c), torch.bfloat16, 3), rows - 1 - 7 * _indices(20000, 30, "uniform")
+    got = E.embedding_backward(dy, idx, rows, 1.0)
+    small, where = E.embedding_backward(dy, (rows - 1 - idx) // 7, 30, 1.0), rows - 1 - 7 * torch.arange(30, device=DEV)
+    assert torch.equal(got[where], small)
+    got[where] = 0
+    assert all(not bool(t.any()) for t in got.split(2 ** 19))
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+def test_widest(dtype):
+    """2^24 columns, the most that are taken"""
+    c = 2 ** 24
+    dy, idx = _normal((20, c), TYPES[dtype], 4), _indices(20, 3, "uniform")
+    got = E.embedding_backward(dy, idx, 3, 0.5)
+    for at in (0, c // 2 - 3, c - 40):
+        part = slice(at, at + 40)
+        want, off = ref.embedding_gradient(dy[:, part].contiguous(), idx, 3, 0.5)
+        ref.close(got[:, part], want, off)
+    assert torch.equal(E.embedding_forward(idx, dy[:3], 2.0), dy[:3][idx] * 2)

@@ -346,6 +346,29 @@ def test_places_beyond_32_bits():
     assert torch.equal(dr[-3:], small) and torch.equal(dx[-3:].cpu() == 0, (~keep) | (small.cpu() == 0))
 
 
+def test_planes_beyond_32_bits():
+    """maps whose values lie past 2^32; the last image against the same image alone, whose mask is moved to its place"""
+    n, c, h, w = 71000, 64, 31, 31
+    m = c * h * w
+    x = torch.zeros(n, c, h, w, dtype=torch.bfloat16, device=DEV)
+    x[-1] = _normal((c, h, w), torch.bfloat16, 1)
+    keep = torch.from_numpy(ref.kept(9, 32768, (n - 1) * m, m)).view(1, c, h, w).to(DEV)
+    alone = torch.where(keep, x[-1:] * 2, 0)
+    y, s, rstd = N.rms_norm_forward(x, None, None, EPS, 1, 0.5, 9)
+    wanted = N.rms_norm_forward(alone, None, None, EPS, 1)
+    assert torch.equal(s[-1:], alone) and torch.equal(y[-1:], wanted[0]) and torch.equal(rstd.view(n, h, w)[-1:], wanted[2].view(1, h, w))
+    assert not bool(y[:3].any())
+    del y, s
+    q, scale, _ = N.rms_norm_8bit(x, None, None, EPS, 1, torch.int8)
+    small = N.rms_norm_8bit(x[-1:].clone(), None, None, EPS, 1, torch.int8)
+    assert torch.equal(q[-1:], small[0]) and torch.equal(scale.view(n, h, w)[-1:], small[1].view(1, h, w))
+    del q
+    dx, dr, _ = N.rms_norm_backward(x, x, rstd, None, None, 1, 0.5, 9, need=(True, True, False))
+    hs, rs = x[-1:].clone(), rstd.view(n, h, w)[-1:].clone()
+    small = N.rms_norm_backward(hs, hs, rs, None, None, 1)[0]
+    assert torch.equal(dr[-1:], small) and torch.equal(dx[-1:] == 0, ~keep | (small == 0))
+
+
 def test_module():
     m = N.XRMSNorm(40, axis=1, p=0.25).to(DEV)
     x, r = _normal((2, 40, 3, 3), torch.float32, 1), _normal((2, 40, 3, 3), torch.float32, 2)
