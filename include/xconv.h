@@ -426,7 +426,7 @@ xconv_status xconv_dropout_mask(const xconv_drop *drop, long long first, long lo
  * backward pass.  R_dev NULL: no residual.  drop NULL or drop_q16 0: no dropout.  H_dev (forward) NULL: not wanted.  rstd_dev, scale_dev: [outer * inner]
  * floats; rstd_dev NULL in the forward pass: not wanted.  dH_dev NULL: zeros.  dX_dev, dR_dev, dgamma_dev NULL: not wanted.  Statistics and Y are of the fp32
  * sum R + drop(X), H is that sum rounded once; the backward pass goes by the rounded H.  Sums are fp32 (squares above 3e38
- * overflow).  A position with a NaN or an infinity gives NaN, its scale too.  Every output is overwritten, rounded once; deterministic.  An output may be one of
+ * overflow; in the 8-bit form products H gamma too).  A position with a NaN or an infinity gives NaN, its scale too.  Every output is overwritten, rounded once; deterministic.  An output may be one of
  * the inputs of its own type (the same address and extent); otherwise nothing overlaps an output.  Pointers aligned to the element size.
  * ws_dev (4-byte aligned): xconv_rmsnorm_workspace_bytes() bytes, for dgamma; else it may be NULL.  outer == 0 is a no-op of the forward pass and gives zero dgamma.
  * Statuses as for layer normalisation; XCONV_EINVAL also for a bad `drop` or q_type and for overlap. */

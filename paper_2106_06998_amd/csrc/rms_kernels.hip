@@ -81,6 +81,16 @@ __device__ inline uint32_t four8(float a, float b, float c, float d, int int8)
     w = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
     return (uint32_t)w;
 }
+// What h gamma is multiplied by: rstd ratio, ratio = top / max |y|.  Under a tiny eps that passes fp32 where y is zero or tiny (the least
+// magnitude gives a ratio of 5.7e32, rstd may be 1e6 and more), and a zero would become a NaN: then (true) h gamma takes rstd first and f is
+// the ratio, neither of which overflows.  One factor otherwise, at no cost: 8192 x 5001 fp16 36.4 us with and without the test.
+__device__ inline bool factor8(float rstd, float ratio, float &f)
+{
+    f = rstd * ratio;
+    const bool two = f == __builtin_inff() && rstd < __builtin_inff();
+    f = two ? ratio : f;
+    return two;
+}
 template <int V> struct __attribute__((packed, aligned(1))) Loose8 { uint32_t w[V / 4]; };
 // V values from p.at on of the run
 template <int V, bool SHORT> __device__ inline void store8(uint8_t *run, const Part &p, const float (&y)[V], int int8)
@@ -244,18 +254,25 @@ __global__ __launch_bounds__(rms_fwd_threads<G>, (rms_fwd_waves<G, K, R>)) void 
         if constexpr (OUT8) group_max<G, R, T>(m, redm, slot);
         group_sum<G, R, T>(s, red, turn);
         float rstd[R], f[R];
+        bool two[R];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             rstd[r] = rstd_of(s[r], a);
             f[r] = rstd[r];
+            two[r] = false;
         }
         if constexpr (OUT8) {
             group_max_join<G, R, T>(m, redm, slot);
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 const float most = __uint_as_float(max(magnitude(__uint_as_float(m[r]) * rstd[r]), __float_as_uint(kLeast8)));
-                f[r] = rstd[r] * (a.top / most);
+                two[r] = factor8(rstd[r], a.top / most, f[r]);
                 if (lane == 0 && on[r]) a.scale[r0 + r * RP + grp] = most / a.top;
+                if (K > 0 && two[r])
+#pragma unroll
+                    for (int k = 0; k < KR; ++k)
+#pragma unroll
+                        for (int i = 0; i < V; ++i) h[r][k][i] *= rstd[r];
             }
         }
         rounds([&](int k, int v) {
@@ -272,8 +289,13 @@ __global__ __launch_bounds__(rms_fwd_threads<G>, (rms_fwd_waves<G, K, R>)) void 
                     make(r, 0, p);
                     if (a.h) put_part<DT, SHORT>(static_cast<elem_t *>(a.h) + at[r], pack<DT>(h[r][k]), p);
                 }
+                if constexpr (K == 0 && OUT8) {
 #pragma unroll
-                for (int i = 0; i < V; ++i) h[r][k][i] *= K == 0 || !EARLY ? f[r] * g[i] : f[r];
+                    for (int i = 0; i < V; ++i) h[r][k][i] = h[r][k][i] * g[i] * (two[r] ? rstd[r] : 1.f) * f[r];
+                } else {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) h[r][k][i] *= EARLY ? f[r] : f[r] * g[i];
+                }
                 if constexpr (OUT8) store8<V, SHORT>(static_cast<uint8_t *>(a.y) + at[r], p, h[r][k], a.int8);
                 else put_part<DT, SHORT>(static_cast<elem_t *>(a.y) + at[r], pack<DT>(h[r][k]), p);
             }
@@ -593,19 +615,27 @@ __global__ __launch_bounds__(NW * 64) void rms_planes_fwd_kernel(RmsArgs a)
         if constexpr (OUT8) column_max<V, TX>(m, redm + slot);
         column_sum<V, NW, TX, true>(s, red + slot);
         float rstd[V], f[V];
+        bool two[V], any = false;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             rstd[i] = rstd_of(s[i], a);
             f[i] = rstd[i];
+            two[i] = false;
         }
         if constexpr (OUT8) {
             column_max_join<V, NW, TX>(m, redm + slot);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const float most = __uint_as_float(max(magnitude(__uint_as_float(m[i]) * rstd[i]), __float_as_uint(kLeast8)));
-                f[i] = rstd[i] * (a.top / most);
+                two[i] = factor8(rstd[i], a.top / most, f[i]);
+                any |= two[i];
                 if (ty == 0 && at.on && own(at.p, i)) a.scale[at.pos + i] = most / a.top;
             }
+            if (K > 0 && any)
+#pragma unroll
+                for (int k = 0; k < KR; ++k)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) h[k][i] *= two[i] ? rstd[i] : 1.f;
         }
         if (!at.on) continue;
         rounds([&](int k, int c) {
@@ -615,7 +645,7 @@ __global__ __launch_bounds__(NW * 64) void rms_planes_fwd_kernel(RmsArgs a)
                 if (a.h) plane_put<DT, WHOLE>(a, static_cast<elem_t *>(a.h) + at.base, at, c, pack<DT>(h[k]));
                 const float g = load_gamma1<DT>(a, c);
 #pragma unroll
-                for (int i = 0; i < V; ++i) h[k][i] *= g;
+                for (int i = 0; i < V; ++i) h[k][i] = h[k][i] * g * (OUT8 && two[i] ? rstd[i] : 1.f);
             }
 #pragma unroll
             for (int i = 0; i < V; ++i) h[k][i] *= f[i];
