@@ -400,7 +400,8 @@ xconv_status xconv_layernorm_bwd(const xconv_norm_desc *desc, const void *dY_dev
  *
  * A value is dropped with probability drop_q16 / 65536 (0: a copy, 65536: zeros); a dropped one is zero also where it was an infinity or a
  * NaN.  step_dev: one 64-bit number on the device that is added to the seed when the kernel runs, or NULL for 0: a captured graph that
- * advances it draws other masks on every replay (without one, the same).  It must hold the same number in both passes.
+ * advances it draws other masks on every replay (without one, the same).  It must hold the same number in both passes.  The mask goes by the
+ * sum alone: calls that share a step need seeds further apart than the step goes (random ones), or one has the other's mask a step later.
  * n values of `dtype` in memory order, products fp32, rounded once; Y_dev may be X_dev, anything else of it must not overlap X.  Pointers
  * aligned to the element size, step_dev to 8 bytes.  n == 0 is a no-op; XCONV_EINVAL: a null (but step_dev) or misaligned pointer, bad
  * dtype, n < 0, drop_q16 outside 0..65536, overlap; XCONV_EUNSUPPORTED: n above 2^40.

@@ -31,7 +31,8 @@ def _check_input(x):
 
 def dropout_forward(x, p, seed, step=None):
     """`x` with the mask of `seed` applied, in the memory order of x (that of a contiguous copy where x has gaps).  step: an int64
-    tensor of one value on the device that is added to the seed when the kernel runs."""
+    tensor of one value on the device that is added to the seed when the kernel runs; calls that share one take seeds that are further
+    apart than it goes (random ones), as the mask goes by the sum."""
     _check_input(x)
     return _glue().dropout(x, _rate(p), _seed(seed), step, None, _raw_stream(x))
 
@@ -63,6 +64,15 @@ def dropout(x, p, seed, step=None):
     return _DropoutFunction.apply(x, p, seed, step)
 
 
+def _far_apart(n):
+    """SplitMix64's last step, one to one: 64 bits that are far from those of n + 1.  Masks go by seed + step, so layers that share a
+    step must not have seeds next to each other: one's mask would be the other's a step later."""
+    n &= 0xFFFFFFFFFFFFFFFF
+    n = ((n ^ (n >> 30)) * 0xBF58476D1CE4E5B9) & 0xFFFFFFFFFFFFFFFF
+    n = ((n ^ (n >> 27)) * 0x94D049BB133111EB) & 0xFFFFFFFFFFFFFFFF
+    return n ^ (n >> 31)
+
+
 class _Draws:
     """The seeds of a module: another one for every forward pass.  A captured graph keeps the seed that it was captured with, so
     there a `step` is expected, which the program advances between replays.  (As with any module, a backward pass is captured while
@@ -71,7 +81,7 @@ class _Draws:
     def _next_seed(self, x):
         if self.step is None and x.is_cuda and torch.cuda.is_current_stream_capturing():
             raise RuntimeError("%s: a captured graph would apply one mask on every replay; give the module a step tensor and advance it" % type(self).__name__)
-        self.last_seed = (self.base_seed * 0x9E3779B1 + next(_calls)) & 0x7FFFFFFFFFFFFFFF
+        self.last_seed = _far_apart(self.base_seed * 0x9E3779B1 + next(_calls)) >> 1
         return self.last_seed
 
 
