@@ -6,6 +6,7 @@
 #include <dlfcn.h>
 
 #include <ATen/ATen.h>
+#include <ATen/CPUGeneratorImpl.h>
 #include <ATen/MemoryOverlap.h>
 #include <c10/core/DeviceGuard.h>
 #include <torch/csrc/Exceptions.h>
@@ -14,6 +15,7 @@
 #include <algorithm>
 #include <cmath>
 #include <exception>
+#include <mutex>
 #include <string>
 #include <vector>
 
@@ -502,6 +504,26 @@ void check_storage(const Tensor &x, const char *who)
     if (!storage_type(x)) refuse(std::string(who) + ": storage type " + at::toString(x.scalar_type()) + " is not supported (float32, bfloat16, float16)");
 }
 
+// dropout_seed(base seed) -> 63 bits drawn from torch's default CPU generator.  Masks go by seed + step, so layers that share a step must not
+// have seeds next to each other (one's mask would be the other's a step later): the sum with the base seed goes through SplitMix64's last step.
+PyObject *dropout_seed(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    if (!ready(nargs, 1, "dropout_seed")) return nullptr;
+    long long base;
+    if (!ints(args, 0, 1, &base)) return nullptr;
+    uint64_t n = 0;
+    if (!run([&] {
+            auto *gen = at::get_generator_or_default<at::CPUGeneratorImpl>(std::nullopt, at::detail::getDefaultCPUGenerator());
+            const std::lock_guard<std::mutex> lock(gen->mutex_);
+            n = gen->random64();
+        }))
+        return nullptr;
+    n += (uint64_t)base * 0x9E3779B97F4A7C15ull;
+    n = (n ^ (n >> 30)) * 0xBF58476D1CE4E5B9ull;
+    n = (n ^ (n >> 27)) * 0x94D049BB133111EBull;
+    return PyLong_FromLongLong((long long)((n ^ (n >> 31)) >> 1));
+}
+
 // dropout(x, q16, seed, step or None, like: (shape, strides, dtype code) or None, stream) -> y in the memory order of x (or of `like`)
 PyObject *dropout(PyObject *, PyObject *const *args, Py_ssize_t nargs)
 {
@@ -981,6 +1003,7 @@ PyMethodDef g_methods[] = {
     XC_METHOD("norm_forward", norm_forward),
     XC_METHOD("norm_backward", norm_backward),
     XC_METHOD("dropout", dropout),
+    XC_METHOD("dropout_seed", dropout_seed),
     XC_METHOD("rms_forward", rms_forward),
     XC_METHOD("rms_forward_8bit", rms_forward_8bit),
     XC_METHOD("rms_backward", rms_backward),

@@ -6,7 +6,7 @@ is left; places count in memory order.  A dropped value is zero also where it wa
 import torch
 
 from . import binding as xb
-from .layer import _DTYPE, _calls, _glue, _raw_stream
+from .layer import _DTYPE, _glue, _raw_stream
 
 
 def _rate(p, who="dropout"):
@@ -64,31 +64,24 @@ def dropout(x, p, seed, step=None):
     return _DropoutFunction.apply(x, p, seed, step)
 
 
-def _far_apart(n):
-    """SplitMix64's last step, one to one: 64 bits that are far from those of n + 1.  Masks go by seed + step, so layers that share a
-    step must not have seeds next to each other: one's mask would be the other's a step later."""
-    n &= 0xFFFFFFFFFFFFFFFF
-    n = ((n ^ (n >> 30)) * 0xBF58476D1CE4E5B9) & 0xFFFFFFFFFFFFFFFF
-    n = ((n ^ (n >> 27)) * 0x94D049BB133111EB) & 0xFFFFFFFFFFFFFFFF
-    return n ^ (n >> 31)
-
-
 class _Draws:
-    """The seeds of a module: another one for every forward pass.  A captured graph keeps the seed that it was captured with, so
-    there a `step` is expected, which the program advances between replays.  (As with any module, a backward pass is captured while
-    no eager graph of the same parameters is kept: torch's engine ends the process otherwise.)"""
+    """The seeds of a module: another one for every forward pass, drawn from torch's default CPU generator (and `base_seed`).  So they follow
+    torch.manual_seed and a saved state of the generator, torch.utils.checkpoint draws the same ones for the pass that it runs again, and
+    the masks of processes are unlike where their generators (or base seeds) are.  A captured graph keeps the seed that it was captured
+    with, so there a `step` is expected, which the program advances between replays.  (As with any module, a backward pass is captured
+    while no eager graph of the same parameters is kept: torch's engine ends the process otherwise.)"""
 
     def _next_seed(self, x):
         if self.step is None and x.is_cuda and torch.cuda.is_current_stream_capturing():
             raise RuntimeError("%s: a captured graph would apply one mask on every replay; give the module a step tensor and advance it" % type(self).__name__)
-        self.last_seed = _far_apart(self.base_seed * 0x9E3779B1 + next(_calls)) >> 1
+        self.last_seed = _glue().dropout_seed(_seed(self.base_seed))
         return self.last_seed
 
 
 class XDropout(torch.nn.Module, _Draws):
-    """torch.nn.Dropout that keeps a seed in place of its mask.  `last_seed` is the seed of the latest training forward call;
-    step: an int64 tensor of one value on the device, added to the seed (for captured graphs; it must not change between the
-    forward and the backward pass)."""
+    """torch.nn.Dropout that keeps a seed in place of its mask, drawn from torch's default CPU generator in every training forward call
+    (`last_seed` is the latest).  step: an int64 tensor of one value on the device, added to the seed (for captured graphs; it must not
+    change between the forward and the backward pass)."""
 
     def __init__(self, p=0.5, base_seed=0, step=None):
         super().__init__()

@@ -150,7 +150,7 @@ def rms_norm(x, weight=None, residual=None, eps=1e-6, axis=-1, p=0.0, seed=0, st
 class XRMSNorm(torch.nn.Module, _Draws):
     """Root-mean-square norm over `channels` channels at `axis` (-1 or 1 as of XLayerNorm; parameters as torch.nn.RMSNorm).  Called with a
     residual it returns (y, h): h = residual + x goes on as the residual stream, y into the next branch.  p: dropout of x in training,
-    drawn from a seed that changes with every forward call (`last_seed`; step and captured graphs: as of XDropout)."""
+    from a seed that every forward call draws (`last_seed`; generator, step and captured graphs: as of XDropout)."""
 
     def __init__(self, channels, eps=1e-6, axis=-1, elementwise_affine=True, p=0.0, base_seed=0, step=None, device=None, dtype=None):
         super().__init__()
