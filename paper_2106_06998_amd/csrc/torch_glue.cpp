@@ -504,11 +504,11 @@ void check_storage(const Tensor &x, const char *who)
     if (!storage_type(x)) refuse(std::string(who) + ": storage type " + at::toString(x.scalar_type()) + " is not supported (float32, bfloat16, float16)");
 }
 
-// dropout_seed(base seed) -> 63 bits drawn from torch's default CPU generator.  Masks go by seed + step, so layers that share a step must not
+// draw_seed(base seed) -> 63 bits drawn from torch's default CPU generator.  Masks go by seed + step, so layers that share a step must not
 // have seeds next to each other (one's mask would be the other's a step later): the sum with the base seed goes through SplitMix64's last step.
-PyObject *dropout_seed(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+PyObject *draw_seed(PyObject *, PyObject *const *args, Py_ssize_t nargs)
 {
-    if (!ready(nargs, 1, "dropout_seed")) return nullptr;
+    if (!ready(nargs, 1, "draw_seed")) return nullptr;
     long long base;
     if (!ints(args, 0, 1, &base)) return nullptr;
     uint64_t n = 0;
@@ -1003,7 +1003,7 @@ PyMethodDef g_methods[] = {
     XC_METHOD("norm_forward", norm_forward),
     XC_METHOD("norm_backward", norm_backward),
     XC_METHOD("dropout", dropout),
-    XC_METHOD("dropout_seed", dropout_seed),
+    XC_METHOD("draw_seed", draw_seed),
     XC_METHOD("rms_forward", rms_forward),
     XC_METHOD("rms_forward_8bit", rms_forward_8bit),
     XC_METHOD("rms_backward", rms_backward),

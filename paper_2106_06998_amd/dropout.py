@@ -74,7 +74,7 @@ class _Draws:
     def _next_seed(self, x):
         if self.step is None and x.is_cuda and torch.cuda.is_current_stream_capturing():
             raise RuntimeError("%s: a captured graph would apply one mask on every replay; give the module a step tensor and advance it" % type(self).__name__)
-        self.last_seed = _glue().dropout_seed(_seed(self.base_seed))
+        self.last_seed = _glue().draw_seed(_seed(self.base_seed))
         return self.last_seed
 
 

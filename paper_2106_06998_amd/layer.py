@@ -13,10 +13,9 @@ steps of a 2-D layer or a SignReLU are one native call each per pass (csrc/torch
 convolution and input gradient.
 
 Z is drawn from a seed that changes with every forward call (Algorithm 1: seed and probing matrix
-are redrawn for each layer and iteration); nothing but the seed is kept of it.
+are redrawn for each layer and iteration); nothing but the seed is kept of it.  Seeds come from torch's
+default CPU generator, as those of dropout do: torch.manual_seed and checkpoints govern them.
 """
-import itertools
-
 import torch
 import torch.nn.functional as F
 
@@ -25,7 +24,6 @@ from . import binding as xb
 MODES = ("channel", "multi", "independent")
 _MODE_CODE = {m: i for i, m in enumerate(MODES)}
 _DTYPE = {torch.float32: "f32", torch.bfloat16: "bf16", torch.float16: "f16"}
-_calls = itertools.count(1)
 
 
 def _pair(v):
@@ -57,6 +55,26 @@ def _glue():
         _torch_glue.init(xb.LIB_PATH, xb.XConvError)
         _glue_module = _torch_glue
     return _glue_module
+
+
+class _Seeds:
+    """A seed for every forward call of a layer, 63 bits from torch's default CPU generator.  torch.utils.checkpoint restores its state, so
+    the pass that is run again probes with the same Z: of the passes the state that is kept would be the second's, and the seed the first's."""
+
+    def __next__(self):
+        return _glue().draw_seed(0)
+
+
+_calls = _Seeds()
+
+
+def _draw(layer, x):
+    """the seed of a forward call, None where it is a plain convolution.  A call without gradients draws all the same: it may be the first
+    pass of a checkpoint, whose second pass, with them, has to find the generator where this one leaves it (for the masks behind it)."""
+    if not (layer.training and layer.weight.requires_grad and (x.is_cuda or torch.is_grad_enabled())):
+        return None
+    seed = (layer.base_seed * 0x9E3779B1 + next(_calls)) & 0x7FFFFFFFFFFFFFFF
+    return seed if torch.is_grad_enabled() else None
 
 
 def _raw_stream(t):
@@ -117,7 +135,7 @@ class XConv2d(torch.nn.Conv2d):
     and channels, Eq. (6), state B*r numbers) or "independent" (every input channel on its own).
     Supported: dilation 1, groups 1, zero padding given as numbers.  In eval mode, or when the
     weight needs no gradient, it is a plain convolution.  `last_seed` is the seed of the latest
-    training forward call.  engine: "library" runs the forward convolution and the exact input
+    training forward call; seeds are drawn from torch's default CPU generator.  engine: "library" runs the forward convolution and the exact input
     gradient on this library's kernels too, "framework" on torch's operators.
     """
 
@@ -136,9 +154,10 @@ class XConv2d(torch.nn.Conv2d):
         self.engine = engine
 
     def forward(self, x):
-        if not (self.training and torch.is_grad_enabled() and self.weight.requires_grad):
+        seed = _draw(self, x)
+        if seed is None:
             return super().forward(x)
-        self.last_seed = (self.base_seed * 0x9E3779B1 + next(_calls)) & 0x7FFFFFFFFFFFFFFF
+        self.last_seed = seed
         return _XConvFunction.apply(x, self.weight, self.bias, _pair(self.stride), _pair(self.padding), self.r, self.probe,
                                     self.mode, self.last_seed, self.engine)
 
@@ -249,9 +268,10 @@ class XConv3d(torch.nn.Conv3d):
         self.r, self.probe, self.base_seed, self.last_seed = int(r), probe, int(base_seed), None
 
     def forward(self, x):
-        if not (self.training and torch.is_grad_enabled() and self.weight.requires_grad):
+        seed = _draw(self, x)
+        if seed is None:
             return super().forward(x)
-        self.last_seed = (self.base_seed * 0x9E3779B1 + next(_calls)) & 0x7FFFFFFFFFFFFFFF
+        self.last_seed = seed
         return _XConv3dFunction.apply(x, self.weight, self.bias, _triple(self.stride), _triple(self.padding), self.r, self.probe,
                                       self.last_seed)
 

@@ -1,10 +1,11 @@
-"""Which seeds the modules with dropout draw, without a GPU: drawing is host code."""
+"""Which seeds the modules with dropout and the convolutions draw, without a GPU: drawing is host code."""
 import pytest
 import torch
 import torch.utils.checkpoint
 
 import token_reference as ref
 from paper_2106_06998_amd.dropout import XDropout
+from paper_2106_06998_amd.layer import _Seeds
 from paper_2106_06998_amd.norm import XRMSNorm
 
 X = torch.empty(0)
@@ -58,3 +59,11 @@ def test_a_checkpoint_draws_its_seeds_again(reentrant):
     x = torch.ones(4, requires_grad=True)
     torch.utils.checkpoint.checkpoint(part, torch.utils.checkpoint.checkpoint(part, x, use_reentrant=reentrant), use_reentrant=reentrant).sum().backward()
     assert len(drawn) == 4 and drawn[0] != drawn[1] and drawn[2:] == drawn[1::-1]
+
+
+def test_convolutions_draw_from_the_generator_too():
+    torch.manual_seed(5)
+    first = [next(_Seeds()) for _ in range(4)]
+    assert len(set(first)) == 4 and all(0 <= s < 2 ** 63 for s in first)
+    torch.manual_seed(5)
+    assert [next(_Seeds()) for _ in range(4)] == first
