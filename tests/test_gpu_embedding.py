@@ -176,7 +176,7 @@ def test_streams_and_graphs(n, rows):
         torch.cuda.synchronize()
 
 
-def test_places_beyond_32_bits():
+def test_long_runs_and_tables_beyond_32_bits():
     """a table and a gradient of more than 2^32 bytes, the last rows and places named"""
     rows, channels = 2 ** 20 + 3, 2 ** 12
     w = torch.zeros(rows, channels, dtype=torch.bfloat16, device=DEV)
