@@ -710,7 +710,8 @@ PyObject *embed_backward(PyObject *, PyObject *const *args, Py_ssize_t nargs)
             check_storage(dy, "embedding");
             const c10::DeviceGuard guard(dy.device());
             const Tensor i = check_indices(idx, dy);
-            if (dy.dim() != idx.dim() + 1 || dy.size(-1) < 1 || dy.size(-1) > INT32_MAX || dy.numel() != idx.numel() * dy.size(-1)) refuse("embedding: the gradient is of the indices' shape and the channels");
+            if (dy.dim() != idx.dim() + 1 || dy.size(-1) < 1 || dy.size(-1) > INT32_MAX || dy.sizes().slice(0, idx.dim()) != idx.sizes())
+                refuse("embedding: the gradient is of the indices' shape and the channels");
             if (rows < 1 || v[0] < -1 || v[0] >= rows || v[0] > INT32_MAX) refuse("embedding: expected a positive number of rows and a padding index among them");
             const Tensor g = dy.contiguous();
             const at::ScalarType wt = v[1] ? at::kFloat : dy.scalar_type();
