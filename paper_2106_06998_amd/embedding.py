@@ -23,11 +23,13 @@ def embedding_forward(indices, weight, scale=1.0):
 
 def embedding_backward(dy, indices, rows, scale=1.0, padding_idx=None, dtype=None):
     """The gradient [rows, C] of the table from that of the output; `dtype` float32 or the type of dy (None).  The row padding_idx
-    gets none, nor does an index outside the table give any."""
+    (a negative one counts from the end) gets none, nor does an index outside the table give any."""
     _check_values(dy)
     if dtype not in (None, torch.float32, dy.dtype):
         raise RuntimeError("embedding: the gradient of the table is float32 or of the output's type, not %s" % dtype)
-    return _glue().embed_backward(dy, indices, rows, scale, -1 if padding_idx is None else padding_idx, dtype == torch.float32, _raw_stream(dy))
+    # for the library -1 is none, and what is still below it is refused there
+    row = -1 if padding_idx is None else padding_idx if padding_idx >= 0 else padding_idx + rows if padding_idx >= -rows else -2
+    return _glue().embed_backward(dy, indices, rows, scale, row, dtype == torch.float32, _raw_stream(dy))
 
 
 class _EmbeddingFunction(torch.autograd.Function):

@@ -19,3 +19,18 @@ def test_gradients_of_another_shape_are_refused():
                 call(wrong)
     want, off = ref.embedding_gradient(dy, idx, 6, 1.0)
     ref.close(E.embedding_backward(dy, idx, 6), want, off)
+
+
+def test_padding_rows_count_from_the_end():
+    """as of embedding() and XEmbedding: -1 is the last row"""
+    idx = torch.arange(6, device=DEV).repeat(3)
+    dy = torch.randn(18, 4, device=DEV)
+    for row in range(-6, 6):
+        got = E.embedding_backward(dy, idx, 6, 1.0, row)
+        want, off = ref.embedding_gradient(dy, idx, 6, 1.0, row % 6)
+        ref.close(got, want, off)
+        assert bool((got[row] == 0).all()) and int((got == 0).all(1).sum()) == 1
+    assert not bool((E.embedding_backward(dy, idx, 6) == 0).any())
+    for row in (6, -7, 2 ** 40, -2 ** 40):
+        with pytest.raises(RuntimeError):
+            E.embedding_backward(dy, idx, 6, 1.0, row)
