@@ -265,6 +265,8 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(SortArgs a)
         }
     };
     auto key_of = [&](int t) { return t < 0 ? -1 : MODE == kSplitList ? t & (a.nb - 1) : t >> a.shift; };
+    // a wave's counters are its own: its lanes' reads and writes of them are in order, and `volatile` keeps every one of them
+    volatile int *next = mine;
 
     for (int i0 = lo; i0 < hi; i0 += 512) {
         int t[8], place;
@@ -278,7 +280,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(SortArgs a)
                 // (in a bucket many lanes may have one key, whose additions would wait for each other)
                 if (i0 + 64 * u >= hi) break;
                 const uint64_t same = same_keys(key_of(t[u]), bits);
-                if ((same >> lane) == 1) mine[key_of(t[u])] += __popcll(same);
+                if ((same >> lane) == 1) next[key_of(t[u])] = next[key_of(t[u])] + __popcll(same);
             }
         }
     }
@@ -316,9 +318,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(SortArgs a)
     }
     if (MODE == kSplitList && threadIdx.x == 0 && me == 0) *a.total = a.first[a.nb] = base;
     __syncthreads();
-    // place the entries in order of the list.  (A wave's counters are its own: its reads and writes of them are in order, and `volatile`
-    // keeps every one of them.)
-    volatile int *next = mine;
+    // place the entries in order of the list
     int2 *out = MODE == kSplitList && a.rows > a.nb ? a.split : a.sorted;
     for (int i0 = lo; i0 < hi; i0 += 512) {
         int t[8], place[8];
