@@ -450,8 +450,8 @@ xconv_status xconv_rmsnorm_bwd(const xconv_norm_desc *desc, const void *dY_dev, 
  * idx_dev: [n] integers of 32 bits, or 64 with index64 != 0; an index outside 0..rows-1 gives a row of NaN and belongs to no row's gradient.
  * W is [rows, C], Y and dY [n, C] of `dtype`, dW [rows, C] of dw_dtype (XCONV_F32 or `dtype`), overwritten.  Products and sums fp32, rounded once; the sums of a row
  * are in an order that depends on the indices alone: deterministic.  padding_idx: -1 for none.
- * Pointers aligned to the element size; ws_dev (256-byte aligned): xconv_embed_workspace_bytes() bytes (8 or 16 an index, 8 a row, and 8 C
- * for every 8 to 256 indices).  Outputs overlap nothing.  n == 0: a no-op of the forward pass, a zero dW.
+ * Pointers aligned to the element size; ws_dev (256-byte aligned): xconv_embed_workspace_bytes() bytes (8 or 16 an index, 8 a row, 8 C for
+ * every 8 to 256 indices, and up to 2.1 MB of counters for long lists and large tables).  Outputs overlap nothing.  n == 0: a no-op of the forward pass, a zero dW.
  * XCONV_EINVAL: null desc or pointer, n < 0, rows or C < 1, bad enum, scale not finite, padding_idx outside -1..rows-1;
  * XCONV_EUNSUPPORTED: n above 2^27, rows above 2^31 - 1 (backward: 2^22), C above 2^24; xconv_embed_workspace_bytes() is 0 then. */
 typedef struct xconv_embed_desc {
